@@ -291,6 +291,92 @@ st_status st_ring_bwd_last(const st_ring_desc* desc, const st_tensor* q, const s
                            int32_t kv_flags, void* const* dk_lowp, void* const* dv_lowp,
                            void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/* ---- attention with modified scores: capped by a tanh, biased by distance, masked by documents and prefixes ----
+ * One (Q shard, KV chunk) pair as in st_attn_block_fwd / st_attn_block_bwd, with scores
+ *   u = scale <q, k>,   y = softcap tanh(u / softcap),   s = y - slope_h |p_q - p_k|
+ * over the keys of the row's span.  The states fold with st_attn_merge and st_attn_combine, Delta comes from st_attn_delta.
+ *   softcap  0: scores are not capped; otherwise finite and positive
+ *   slopes   nullable; device fp32 [Hq], finite: what a unit of distance between the positions of query and key takes off the score
+ *   spans    nullable; device int64 [B,Sq,2], 16-byte aligned: query row i of batch entry b sees the keys at global positions
+ *            spans[b][i][0] <= p < spans[b][i][1] (and, with desc->causal, p <= its own); an empty span is legal (O = 0,
+ *            lse = -inf, no gradient).  st_mask_spans makes them; any other interval (a sliding window) is as good.
+ * Precision of ST_BF16: scores, softmax, sums in fp32 from the stored Q and K (Q is not scaled and rounded first, as the kernels
+ * of the plain scores do); P and the gradient of the scores are rounded to bf16 before the second contractions.
+ * Infinities and NaN in rows of Q, K, V, dO reach the results of the rows and keys that see them, and no others. */
+typedef struct {
+  float softcap;
+  const float* slopes;      /* device */
+  const int64_t* spans;     /* device */
+} st_score;
+
+/* Spans of a packed batch (host sizes, device tensors): documents lie one behind the other in every batch entry.
+ *   bounds  int64 [B,n_docs+1], rising (equal: an empty document): document d holds the positions bounds[d] <= p < bounds[d+1]
+ *   prefix  nullable, int64 [B,n_docs]: so many first tokens of document d are seen by all of its tokens, whatever `causal` says
+ *   spans   int64 [B,Sq,2] (out): a row sees its own document, with `causal` up to its own position or the prefix' end;
+ *           a row in no document gets an empty span.  Hand them on with desc->causal = 0: the causal order is in them.
+ * q_offset, q_seg, q_offset2 place the rows as in st_block_desc. */
+st_status st_mask_spans(int32_t B, int32_t Sq, int64_t q_offset, int32_t q_seg, int64_t q_offset2, int32_t causal,
+                        const int64_t* bounds, int32_t n_docs, const int64_t* prefix, int64_t* spans, void* hip_stream);
+
+/* Workspace of the two calls below, for these sizes (0: none is needed): device, 256-byte aligned; its contents mean nothing
+ * between calls, and calls that share one must be ordered on one stream.  Only whether desc and score have spans counts. */
+size_t st_attn_score_workspace_bytes(const st_block_desc* desc, const st_score* score, int32_t backward);
+
+/* score: nullable (plain scores).  o_part fp32 and / or o_lowp in desc->dtype, dense [B,Sq,Hq,D] (one may be NULL, overwritten);
+ * lse_part fp32 [B,Hq,Sq] (overwritten). */
+st_status st_attn_score_fwd(const st_block_desc* desc, const st_score* score, const st_tensor* q, const st_tensor* k,
+                            const st_tensor* v, float* o_part, float* lse_part, void* o_lowp, void* workspace,
+                            size_t workspace_bytes, void* hip_stream);
+
+/* Gradients of the pair from the FINAL lse and Delta: dense fp32 accumulators as in st_attn_block_bwd, ADDED to (flags = 0) or
+ * OVERWRITTEN (ST_GRAD_ASSIGN), and / or *_lowp, the same values rounded to desc->dtype, dense.  With ST_GRAD_ASSIGN one of
+ * accumulator and *_lowp may be NULL for each gradient; without it the accumulators are needed.  Every element has one writer and
+ * every sum a fixed order: results are bit-reproducible.  slopes have no gradient. */
+enum { ST_GRAD_ASSIGN = 1 };
+st_status st_attn_score_bwd(const st_block_desc* desc, const st_score* score, const st_tensor* q, const st_tensor* k,
+                            const st_tensor* v, const st_tensor* d_o, const float* lse_final, const float* delta,
+                            int32_t flags, float* dq_acc, float* dk_acc, float* dv_acc, void* dq_lowp, void* dk_lowp,
+                            void* dv_lowp, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* ---- norms of queries and keys for each head, and the rotation by their positions, in one pass ----
+ * For every token and head x[0 .. D):  n = x rsqrt(mean(x^2) + eps) weight (norm = 0: n = x), then the first `rot` values are
+ * rotated in pairs, (a, b) -> (a cos t - b sin t, a sin t + b cos t) with t = p f for the pair's axis position p and frequency f.
+ *   pairing     ST_ROPE_HALVES: pair j is (j, j + rot / 2); ST_ROPE_NEIGHBOURS: (2 j, 2 j + 1)
+ *   n_axes      1 .. ST_ROPE_MAX_AXES; the first axis_pairs[0] pairs turn by the positions of axis 0, the next axis_pairs[1] by
+ *               those of axis 1 (time, height, width of a video patch); they add up to rot / 2
+ *   positions   nullable; device int32 [n_axes,B,S].  NULL (one axis): the rows are those of a shard, at offset, and from row seg
+ *               on at offset2 (q_offset, q_seg, q_offset2 of st_block_desc)
+ *   freq        device fp64 [rot/2], radians per position (any: scaled ones too); angles are made in fp64, for far positions
+ *   q_weight, k_weight  nullable (ones); device fp32 [D], for norm = 1 only
+ * q, k: [B,S,Hq,D] and [B,S,Hkv,D] views (k is not read where Hkv = 0); arithmetic is fp32, rounded once.  q_out, k_out: views of
+ * the same type, which may be q and k themselves.  D <= 256, D % 8 == 0, rot even, 0 <= rot <= D. */
+enum { ST_ROPE_HALVES = 0, ST_ROPE_NEIGHBOURS = 1, ST_ROPE_MAX_AXES = 4 };
+typedef struct {
+  int32_t dtype, B, S, Hq, Hkv, D;
+  int32_t rot, pairing, norm;
+  float   eps;
+  int32_t n_axes;
+  int32_t axis_pairs[ST_ROPE_MAX_AXES];
+  int64_t offset;
+  int32_t seg;
+  int64_t offset2;
+} st_rope_desc;
+st_status st_qk_rope_fwd(const st_rope_desc* desc, const st_tensor* q, const st_tensor* k, const float* q_weight,
+                         const float* k_weight, const double* freq, const int32_t* positions, const st_tensor* q_out,
+                         const st_tensor* k_out, void* hip_stream);
+
+/* Gradients of the same pass.  q, k: its inputs (not read with norm = 0); d_q, d_k: gradients of its outputs, views in d_dtype
+ * (ST_F32, as the attention backward leaves them, or desc->dtype); dx_q, dx_k (out): gradients of q and k, views in desc->dtype
+ * (may be d_q, d_k where the types agree).  dw_q, dw_k: nullable fp32 [D], with norm = 1: gradients of the weights, added to, or
+ * overwritten with ST_GRAD_ASSIGN; sums have a fixed order.  workspace: st_qk_rope_bwd_workspace_bytes(desc) bytes, 256-byte
+ * aligned, needed with dw_q or dw_k only. */
+size_t st_qk_rope_bwd_workspace_bytes(const st_rope_desc* desc);
+st_status st_qk_rope_bwd(const st_rope_desc* desc, const st_tensor* q, const st_tensor* k, const st_tensor* d_q,
+                         const st_tensor* d_k, int32_t d_dtype, const float* q_weight, const float* k_weight,
+                         const double* freq, const int32_t* positions, int32_t flags, const st_tensor* dx_q,
+                         const st_tensor* dx_k, float* dw_q, float* dw_k, void* workspace, size_t workspace_bytes,
+                         void* hip_stream);
+
 /* ---- per-kernel timing for benchmarks (not part of the method) ----
  * Between st_profile_begin() and st_profile_end() the library records a HIP event on the launch
  * stream before and after every kernel it launches (this creates hipEvent_t objects; at most 4096

@@ -11,6 +11,7 @@ Without it, or with another torch or Python than it was built for, everything go
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 import sys
@@ -22,6 +23,8 @@ import torch
 ST_F32, ST_BF16 = 0, 1
 ST_RING_STEPWISE, ST_RING_FUSED = 0, 1
 ST_KV_ASSIGN = 1
+ST_GRAD_ASSIGN = 1
+ST_ROPE_HALVES, ST_ROPE_NEIGHBOURS, ST_ROPE_MAX_AXES = 0, 1, 4
 ST_MAX_CHUNKS = 256
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libstartrail.so")
@@ -53,6 +56,16 @@ class st_ring_desc(C.Structure):
                 ("k_offset", C.POINTER(C.c_int64)), ("q_seg", C.c_int32), ("q_offset2", C.c_int64)]
 
 
+class st_score(C.Structure):
+    _fields_ = [("softcap", C.c_float), ("slopes", C.c_void_p), ("spans", C.c_void_p)]
+
+
+class st_rope_desc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("B", C.c_int32), ("S", C.c_int32), ("Hq", C.c_int32), ("Hkv", C.c_int32), ("D", C.c_int32),
+                ("rot", C.c_int32), ("pairing", C.c_int32), ("norm", C.c_int32), ("eps", C.c_float), ("n_axes", C.c_int32),
+                ("axis_pairs", C.c_int32 * 4), ("offset", C.c_int64), ("seg", C.c_int32), ("offset2", C.c_int64)]
+
+
 class st_comm_report(C.Structure):
     _fields_ = [("ring_iterations", C.c_int32), ("startrail_iterations", C.c_int32),
                 ("ring_p2p_bytes_per_iter", C.c_int64), ("startrail_p2p_bytes_per_iter", C.c_int64),
@@ -81,6 +94,7 @@ def _load() -> C.CDLL:
                           "(there is no CPU fallback)")
     lib = C.CDLL(_LIB_PATH)
     T, D, R = C.POINTER(st_tensor), C.POINTER(st_block_desc), C.POINTER(st_ring_desc)
+    M, P = C.POINTER(st_score), C.POINTER(st_rope_desc)
     vp, f32p, i32p = C.c_void_p, C.c_void_p, C.POINTER(C.c_int32)
     sigs = {
         "st_attn_block_fwd": (C.c_int, [D, T, T, T, f32p, f32p, vp]),
@@ -105,6 +119,13 @@ def _load() -> C.CDLL:
         "st_ring_bwd_last": (C.c_int, [R, T, T, T, C.c_int32, f32p, i32p, C.c_int32, C.c_int32, f32p,
                                        C.POINTER(C.c_void_p), C.POINTER(C.c_void_p), C.c_int32,
                                        C.POINTER(C.c_void_p), C.POINTER(C.c_void_p), vp, C.c_size_t, vp]),
+        "st_mask_spans": (C.c_int, [C.c_int32, C.c_int32, C.c_int64, C.c_int32, C.c_int64, C.c_int32, vp, C.c_int32, vp, vp, vp]),
+        "st_attn_score_workspace_bytes": (C.c_size_t, [D, M, C.c_int32]),
+        "st_attn_score_fwd": (C.c_int, [D, M, T, T, T, f32p, f32p, vp, vp, C.c_size_t, vp]),
+        "st_attn_score_bwd": (C.c_int, [D, M, T, T, T, T, f32p, f32p, C.c_int32, f32p, f32p, f32p, vp, vp, vp, vp, C.c_size_t, vp]),
+        "st_qk_rope_fwd": (C.c_int, [P, T, T, f32p, f32p, vp, vp, T, T, vp]),
+        "st_qk_rope_bwd_workspace_bytes": (C.c_size_t, [P]),
+        "st_qk_rope_bwd": (C.c_int, [P, T, T, T, T, C.c_int32, f32p, f32p, vp, vp, C.c_int32, T, T, f32p, f32p, vp, C.c_size_t, vp]),
         "st_device_facts": (C.c_int, [C.POINTER(st_device_report)]),
         "st_mfma_probe": (C.c_int, [vp, C.c_int64, C.c_int32, C.c_int32, f32p, C.c_int64, C.POINTER(C.c_double), vp]),
         "st_mfma_probe_mixes": (C.c_int32, []),
@@ -151,7 +172,8 @@ def _native_half():
 _binding = _native_half()
 
 EXPORTS = ["st_attn_block_fwd", "st_attn_merge", "st_attn_combine", "st_attn_delta", "st_attn_block_bwd", "st_attn_block_bwd_workspace_bytes", "st_cast_from_f32",
-           "st_visit_order", "st_team_visit_order", "st_schedule_report", "st_ring_workspace_bytes", "st_ring_fwd", "st_ring_bwd", "st_ring_bwd_noalloc", "st_ring_bwd_noalloc_max_bytes", "st_ring_bwd_last", "st_device_facts", "st_mfma_probe", "st_mfma_probe_mixes", "st_mfma_probe_mix_name", "st_profile_begin",
+           "st_visit_order", "st_team_visit_order", "st_schedule_report", "st_ring_workspace_bytes", "st_ring_fwd", "st_ring_bwd", "st_ring_bwd_noalloc", "st_ring_bwd_noalloc_max_bytes", "st_ring_bwd_last", "st_mask_spans", "st_attn_score_workspace_bytes", "st_attn_score_fwd", "st_attn_score_bwd", "st_qk_rope_fwd",
+           "st_qk_rope_bwd_workspace_bytes", "st_qk_rope_bwd", "st_device_facts", "st_mfma_probe", "st_mfma_probe_mixes", "st_mfma_probe_mix_name", "st_profile_begin",
            "st_profile_end", "st_status_str",
            "st_last_error", "st_version"]
 
@@ -591,3 +613,227 @@ def st_ring_bwd_last(q, k_chunks, v_chunks, d_o, o, lse_final, q_offset: int, k_
 
 def _ptr_table(ts, n):
     return (C.c_void_p * n)(*[(t.data_ptr() if t is not None else None) for t in ts])
+
+
+# ---- attention with modified scores, norms and rotations of queries and keys
+
+@contextlib.contextmanager
+def _switched(device, stream):
+    """The tensors' device as the current one, and `stream` as torch's, so that what is allocated meanwhile belongs to it."""
+    with torch.cuda.device(device):
+        if stream is None:
+            yield
+        else:
+            with torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=device)):
+                yield
+
+
+_AS_IT_IS = contextlib.nullcontext()
+
+
+def _on_device(stream, *tensors):
+    """All tensors (None: left out) on one GPU; a context in which outputs and workspaces are allocated and the call is made."""
+    device = tensors[0].device
+    for t in tensors:
+        if t is not None and t.device != device:
+            raise ValueError(f"tensors on {device} and {t.device}")
+    if device.type != "cuda":
+        raise ValueError(f"expected tensors on a GPU, not on {device}")
+    return _AS_IT_IS if stream is None and device.index == torch._C._cuda_getDevice() else _switched(device, stream)
+
+
+def _dense(t, shape, dtype, name):
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}")
+    return t
+
+
+def _score_desc(q, k, v, q_offset, k_offset, causal, scale, softcap, slopes, spans):
+    if q.dim() != 4 or k.dim() != 4 or v.shape != k.shape or k.shape[0] != q.shape[0] or k.shape[3] != q.shape[3]:
+        raise ValueError("expected q [B,Sq,Hq,D] and k, v [B,Sk,Hkv,D]")
+    if k.dtype != q.dtype or v.dtype != q.dtype:
+        raise ValueError("q, k and v must have one dtype")
+    if slopes is not None:
+        _dense(slopes, (q.shape[2],), torch.float32, "slopes")
+    if spans is not None:
+        _dense(spans, (q.shape[0], q.shape[1], 2), torch.int64, "spans")
+    return _block_desc(q, k, q_offset, k_offset, causal, scale), \
+        st_score(float(softcap), slopes.data_ptr() if slopes is not None else None, spans.data_ptr() if spans is not None else None)
+
+
+def _score_workspace(d, m, backward: bool, workspace, device):
+    """(pointer, bytes, tensor that has to live until the call is made)"""
+    if workspace is None:
+        need = int(_lib.st_attn_score_workspace_bytes(C.byref(d), C.byref(m), 1 if backward else 0))
+        if need == 0:
+            return None, 0, None
+        workspace = torch.empty(need + 256, dtype=torch.uint8, device=device)
+    ptr, size = _aligned(workspace, 256)
+    return ptr, size, workspace
+
+
+def st_mask_spans(bounds, Sq: int, q_offset, causal: bool, prefix=None, spans=None, stream=None) -> torch.Tensor:
+    """Spans [B, Sq, 2] of the rows of packed documents: bounds int64 [B, n_docs + 1] (rising positions at which the documents
+    start, and the end of the last one), prefix int64 [B, n_docs] or None (first tokens that a whole document sees)."""
+    with _on_device(stream, bounds, prefix, spans):
+        if bounds.dim() != 2 or bounds.shape[1] < 1:
+            raise ValueError("bounds must be [B, n_docs + 1]")
+        B, n = bounds.shape[0], bounds.shape[1] - 1
+        _dense(bounds, (B, n + 1), torch.int64, "bounds")
+        if prefix is not None:
+            _dense(prefix, (B, n), torch.int64, "prefix")
+        spans = torch.empty((B, int(Sq), 2), dtype=torch.int64, device=bounds.device) if spans is None else \
+            _dense(spans, (B, int(Sq), 2), torch.int64, "spans")
+        off, seg, off2 = _q_runs(q_offset)
+        _check(_lib.st_mask_spans(B, int(Sq), off, seg, off2, 1 if causal else 0, _ptr(bounds), n, _ptr(prefix), _ptr(spans),
+                                  _stream(None)), "st_mask_spans")
+    return spans
+
+
+def st_attn_score_workspace_bytes(q, k, v, q_offset, k_offset: int, causal: bool, scale: float, softcap: float = 0.0, slopes=None,
+                                  spans=None, backward: bool = False) -> int:
+    d, m = _score_desc(q, k, v, q_offset, k_offset, causal, scale, softcap, slopes, spans)
+    return int(_lib.st_attn_score_workspace_bytes(C.byref(d), C.byref(m), 1 if backward else 0))
+
+
+def st_attn_score_fwd(q, k, v, q_offset, k_offset: int, causal: bool, scale: float, softcap: float = 0.0, slopes=None, spans=None,
+                      o_part=None, lse_part=None, o_lowp=None, lowp: bool = False, workspace=None, stream=None):
+    """(O, lse) of a query shard against one chunk.  O is the fp32 partial state, or with lowp=True alone O in the dtype of q; both
+    are written where both o_part and o_lowp are given (the fp32 one is returned)."""
+    with _on_device(stream, q, k, v, slopes, spans, o_part, lse_part, o_lowp, workspace):
+        d, m = _score_desc(q, k, v, q_offset, k_offset, causal, scale, softcap, slopes, spans)
+        B, Sq, Hq, D = q.shape
+        if o_lowp is None and lowp:
+            o_lowp = torch.empty((B, Sq, Hq, D), dtype=q.dtype, device=q.device)
+        elif o_lowp is not None:
+            _dense(o_lowp, (B, Sq, Hq, D), q.dtype, "o_lowp")
+        if o_part is None and o_lowp is None:
+            o_part = torch.empty((B, Sq, Hq, D), dtype=torch.float32, device=q.device)
+        elif o_part is not None:
+            _f32_dense(o_part, (B, Sq, Hq, D), "o_part")
+        lse_part = torch.empty((B, Hq, Sq), dtype=torch.float32, device=q.device) if lse_part is None else \
+            _f32_dense(lse_part, (B, Hq, Sq), "lse_part")
+        tq, tk, tv = _view(q), _view(k), _view(v)
+        ws, size, held = _score_workspace(d, m, False, workspace, q.device)
+        _check(_lib.st_attn_score_fwd(C.byref(d), C.byref(m), C.byref(tq), C.byref(tk), C.byref(tv), _ptr(o_part), _ptr(lse_part),
+                                      _ptr(o_lowp), C.c_void_p(ws), size, _stream(None)), "st_attn_score_fwd")
+    return (o_part if o_part is not None else o_lowp), lse_part
+
+
+def st_attn_score_bwd(q, k, v, d_o, lse_final, delta, q_offset, k_offset: int, causal: bool, scale: float, softcap: float = 0.0,
+                      slopes=None, spans=None, dq_acc=None, dk_acc=None, dv_acc=None, assign: bool = False, dq_lowp=None, dk_lowp=None,
+                      dv_lowp=None, workspace=None, stream=None):
+    """Gradients of the pair.  With accumulators (all three, fp32) they are added to, or overwritten with assign=True, and the
+    *_lowp given are their values in the dtype of q; without accumulators the gradients are written in the dtype of q, into the
+    *_lowp given or new tensors.  Returns (dq, dk, dv): the accumulators, or those."""
+    with _on_device(stream, q, k, v, d_o, lse_final, delta, slopes, spans, dq_acc, dk_acc, dv_acc, dq_lowp, dk_lowp, dv_lowp, workspace):
+        d, m = _score_desc(q, k, v, q_offset, k_offset, causal, scale, softcap, slopes, spans)
+        B, Sq, Hq, D = q.shape
+        if d_o.shape != q.shape or d_o.dtype != q.dtype:
+            raise ValueError("d_o must have the shape and dtype of q")
+        _f32_dense(lse_final, (B, Hq, Sq), "lse_final"); _f32_dense(delta, (B, Hq, Sq), "delta")
+        acc, low, shapes = [dq_acc, dk_acc, dv_acc], [dq_lowp, dk_lowp, dv_lowp], [tuple(q.shape), tuple(k.shape), tuple(k.shape)]
+        if any(a is not None for a in acc) and any(a is None for a in acc):
+            raise ValueError("dq_acc, dk_acc and dv_acc: all or none")
+        alone = acc[0] is None
+        for x, name in enumerate(("dq", "dk", "dv")):
+            if not alone:
+                _f32_dense(acc[x], shapes[x], name + "_acc")
+            if low[x] is not None:
+                _dense(low[x], shapes[x], q.dtype, name + "_lowp")
+            elif alone:
+                low[x] = torch.empty(shapes[x], dtype=q.dtype, device=q.device)
+        tq, tk, tv, td = _view(q), _view(k), _view(v), _view(d_o)
+        ws, size, held = _score_workspace(d, m, True, workspace, q.device)
+        _check(_lib.st_attn_score_bwd(C.byref(d), C.byref(m), C.byref(tq), C.byref(tk), C.byref(tv), C.byref(td), _ptr(lse_final),
+                                      _ptr(delta), ST_GRAD_ASSIGN if assign or alone else 0, *[_ptr(a) for a in acc],
+                                      *[_ptr(x) for x in low], C.c_void_p(ws), size, _stream(None)), "st_attn_score_bwd")
+    return tuple(low) if alone else tuple(acc)
+
+
+def _rope_desc(q, k, freq, offset, positions, axes, pairs, norm, eps, q_weight, k_weight):
+    B, S, Hq, D = q.shape
+    if k is not None and (k.dim() != 4 or k.shape[:2] != q.shape[:2] or k.shape[3] != D or k.dtype != q.dtype):
+        raise ValueError("expected q [B,S,Hq,D] and k [B,S,Hkv,D] of one dtype")
+    if pairs not in ("halves", "neighbours"):
+        raise ValueError(f"pairs must be 'halves' or 'neighbours', not {pairs!r}")
+    n = freq.numel()
+    _dense(freq, (n,), torch.float64, "freq")
+    axes = [n] if axes is None else [int(x) for x in axes]
+    if not 1 <= len(axes) <= ST_ROPE_MAX_AXES or sum(axes) != n:
+        raise ValueError(f"axes: up to {ST_ROPE_MAX_AXES} numbers of pairs that add up to the {n} frequencies")
+    if positions is not None:
+        _dense(positions, (len(axes), B, S), torch.int32, "positions")
+    for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        if w is not None:
+            _dense(w, (D,), torch.float32, name)
+    off, seg, off2 = _q_runs(offset)
+    return st_rope_desc(_dtype_code(q), B, S, Hq, k.shape[2] if k is not None else 0, D, 2 * n,
+                        ST_ROPE_NEIGHBOURS if pairs == "neighbours" else ST_ROPE_HALVES, 1 if norm else 0, float(eps), len(axes),
+                        (C.c_int32 * ST_ROPE_MAX_AXES)(*axes), off, seg, off2)
+
+
+def _like(t, ref, name):
+    if t.shape != ref.shape or t.dtype != ref.dtype:
+        raise ValueError(f"{name} must have the shape and dtype of its input")
+    return t
+
+
+def _maybe_view(t):
+    return _view(t) if t is not None else st_tensor(None, 0, 0, 0)
+
+
+def st_qk_rope_fwd(q, k, freq, offset=0, positions=None, axes=None, pairs: str = "halves", norm: bool = True, eps: float = 1e-6,
+                   q_weight=None, k_weight=None, q_out=None, k_out=None, stream=None):
+    """RMS norm of every head of q [B,S,Hq,D] and k [B,S,Hkv,D] (or None) over its D values, with fp32 weights [D] where given, and
+    the rotation of its first 2 len(freq) values: freq fp64 radians per position.  Positions are those of a shard's rows (offset: the
+    first one's, or (offset, rows of the first run, offset of the second)), or `positions` int32 [axes,B,S] with `axes` the numbers
+    of pairs that each axis turns.  Returns (q_out, k_out), new tensors unless given; they may be q and k."""
+    with _on_device(stream, q, k, freq, positions, q_weight, k_weight, q_out, k_out):
+        d = _rope_desc(q, k, freq, offset, positions, axes, pairs, norm, eps, q_weight, k_weight)
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else _like(q_out, q, "q_out")
+        if k is not None:
+            k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device) if k_out is None else _like(k_out, k, "k_out")
+        tq, tk, oq, ok = _view(q), _maybe_view(k), _view(q_out), _maybe_view(k_out if k is not None else None)
+        _check(_lib.st_qk_rope_fwd(C.byref(d), C.byref(tq), C.byref(tk), _ptr(q_weight), _ptr(k_weight), _ptr(freq), _ptr(positions),
+                                   C.byref(oq), C.byref(ok), _stream(None)), "st_qk_rope_fwd")
+    return q_out, k_out if k is not None else None
+
+
+def st_qk_rope_bwd(q, k, d_q, d_k, freq, offset=0, positions=None, axes=None, pairs: str = "halves", norm: bool = True,
+                   eps: float = 1e-6, q_weight=None, k_weight=None, dx_q=None, dx_k=None, dw_q=None, dw_k=None, assign: bool = False,
+                   workspace=None, stream=None):
+    """Gradients of st_qk_rope_fwd: d_q, d_k those of its outputs, fp32 or in the dtype of q.  Returns (dx_q, dx_k, dw_q, dw_k); the
+    weights' (None without weights) are added to the dw_q, dw_k given, or overwrite them with assign=True."""
+    with _on_device(stream, q, k, d_q, d_k, freq, positions, q_weight, k_weight, dx_q, dx_k, dw_q, dw_k, workspace):
+        d = _rope_desc(q, k, freq, offset, positions, axes, pairs, norm, eps, q_weight, k_weight)
+        if d_q.shape != q.shape or (k is not None and (d_k.shape != k.shape or d_k.dtype != d_q.dtype)):
+            raise ValueError("d_q and d_k must have the shapes of q and k, and one dtype")
+        D = q.shape[3]
+        dx_q = torch.empty(q.shape, dtype=q.dtype, device=q.device) if dx_q is None else _like(dx_q, q, "dx_q")
+        if k is not None:
+            dx_k = torch.empty(k.shape, dtype=k.dtype, device=k.device) if dx_k is None else _like(dx_k, k, "dx_k")
+        fresh = [(q_weight is not None and dw_q is None), (k is not None and k_weight is not None and dw_k is None)]
+        if (dw_q is not None or dw_k is not None) and any(fresh):
+            raise ValueError("dw_q and dw_k: both or neither, where both have weights")
+        if any(fresh):
+            assign = True
+            dw_q = torch.empty((D,), dtype=torch.float32, device=q.device) if fresh[0] else None
+            dw_k = torch.empty((D,), dtype=torch.float32, device=q.device) if fresh[1] else None
+        for w, name in ((dw_q, "dw_q"), (dw_k, "dw_k")):
+            if w is not None:
+                _f32_dense(w, (D,), name)
+        ptr, size = None, 0
+        if dw_q is not None or dw_k is not None:
+            if workspace is None:
+                workspace = torch.empty(int(_lib.st_qk_rope_bwd_workspace_bytes(C.byref(d))) + 256, dtype=torch.uint8, device=q.device)
+            ptr, size = _aligned(workspace, 256)
+        tq, tk, gq, gk, oq, ok = (_maybe_view(t) for t in (q, k, d_q, d_k if k is not None else None, dx_q, dx_k if k is not None else None))
+        _check(_lib.st_qk_rope_bwd(C.byref(d), C.byref(tq), C.byref(tk), C.byref(gq), C.byref(gk), _dtype_code(d_q), _ptr(q_weight),
+                                   _ptr(k_weight), _ptr(freq), _ptr(positions), ST_GRAD_ASSIGN if assign else 0, C.byref(oq),
+                                   C.byref(ok), _ptr(dw_q), _ptr(dw_k), C.c_void_p(ptr), size, _stream(None)), "st_qk_rope_bwd")
+    return dx_q, (dx_k if k is not None else None), dw_q, dw_k
+
+
+def st_qk_rope_bwd_workspace_bytes(q, k, freq, norm: bool = True) -> int:
+    return int(_lib.st_qk_rope_bwd_workspace_bytes(C.byref(_rope_desc(q, k, freq, 0, None, None, "halves", norm, 1e-6, None, None))))

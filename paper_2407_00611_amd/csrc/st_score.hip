@@ -1,0 +1,123 @@
+// Small passes beside the kernels of attention with modified scores: the row spans of documents and prefixes, what runs of 32 rows
+// see, and the sum of the shares of split gradients.
+#include "st_score.h"
+
+namespace st {
+namespace {
+
+// Row at position p of a packed batch entry: its document is the last one that starts at or before p (empty documents start where
+// the next one does, and are passed over).  bounds [B, n_docs + 1] rise; a row before the first or behind the last sees nothing.
+__global__ __launch_bounds__(256) void mask_spans_kernel(const Shape s, const int64_t* __restrict__ bounds, int32_t n_docs, const int64_t* __restrict__ prefix, int64_t* __restrict__ spans) {
+  const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (x >= (int64_t)s.B * s.Sq) return;
+  const int64_t b = x / s.Sq, p = q_pos(s, (int)(x - b * s.Sq));
+  const int64_t* e = bounds + b * (n_docs + 1);
+  int lo = 0, hi = n_docs + 1;                         // entries before lo are <= p, those from hi on are not
+  while (lo < hi) {
+    const int mid = (lo + hi) / 2;
+    if (e[mid] <= p) lo = mid + 1;
+    else hi = mid;
+  }
+  longlong2 w = make_longlong2(0, 0);
+  if (lo >= 1 && lo <= n_docs) {
+    w.x = e[lo - 1];
+    w.y = e[lo];
+    if (s.causal) {
+      const int64_t len = w.y - w.x, pre = prefix ? min(max(prefix[b * n_docs + lo - 1], (int64_t)0), len) : 0;
+      w.y = min(w.y, max(p + 1, w.x + pre));
+    }
+  }
+  *reinterpret_cast<longlong2*>(spans + 2 * x) = w;
+}
+
+// half a wavefront per run of 32 packed rows
+__global__ __launch_bounds__(256) void score_blocks_kernel(const ScoreArgs a, int32_t n_blk) {
+  const int64_t x = (int64_t)blockIdx.x * 8 + threadIdx.x / 32, n = (int64_t)a.s.B * n_blk;
+  const int r = threadIdx.x & 31, G = a.s.Hq / a.s.Hkv, M = a.s.Sq * G;
+  const int64_t at = min(x, n - 1);
+  const int b = (int)(at / n_blk), j = (int)(at - (int64_t)b * n_blk);
+  BlockSpan w = span_of(row_view(a, b, min(32 * j + r, M - 1) / G));
+#pragma unroll
+  for (int d = 1; d < 32; d *= 2)
+    w = span_join(w, BlockSpan{__shfl_xor(w.lo, d), __shfl_xor(w.hi, d), __shfl_xor(w.all_lo, d), __shfl_xor(w.all_hi, d)});
+  if (r == 0 && x < n) a.blocks[x] = make_int4(w.lo, w.hi, w.all_lo, w.all_hi);
+}
+
+struct PartSum {
+  const float* part;         // n sums of `floats` floats, one behind the other; null: nothing to add up
+  float* out;                // nullable; added to unless assign
+  void* low;                 // nullable
+  int32_t n;
+  int64_t floats;
+};
+struct PartSums {
+  PartSum x[3];
+  int32_t assign, bf16;
+};
+// four neighbouring floats a thread, in the order of the shares
+__global__ __launch_bounds__(256) void score_add_parts_kernel(const PartSums a) {
+  const PartSum& p = a.x[blockIdx.y];
+  for (int64_t e = 4 * ((int64_t)blockIdx.x * 256 + threadIdx.x); e < p.floats && p.part; e += (int64_t)gridDim.x * 1024) {
+    float4 y = *reinterpret_cast<const float4*>(p.part + e);
+    for (int k = 1; k < p.n; ++k) {
+      const float4 z = *reinterpret_cast<const float4*>(p.part + k * p.floats + e);
+      y.x += z.x; y.y += z.y; y.z += z.z; y.w += z.w;
+    }
+    if (!a.assign) {
+      const float4 z = *reinterpret_cast<const float4*>(p.out + e);
+      y.x += z.x; y.y += z.y; y.z += z.z; y.w += z.w;
+    }
+    if (p.out) *reinterpret_cast<float4*>(p.out + e) = y;
+    if (p.low && a.bf16) *reinterpret_cast<uint2*>((uint16_t*)p.low + e) = make_uint2(pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
+    else if (p.low) *reinterpret_cast<float4*>((float*)p.low + e) = y;
+  }
+}
+
+}  // namespace
+
+int score_split(int64_t jobs, int64_t slots, int64_t steps, int64_t least_steps, int most) {
+  if (jobs <= 0) return 1;
+  int64_t n = slots / jobs;
+  n = n > most ? most : n;
+  n = n > steps / least_steps ? steps / least_steps : n;
+  return n < 1 ? 1 : (int)n;
+}
+
+hipError_t launch_mask_spans(const Shape& s, const int64_t* bounds, int32_t n_docs, const int64_t* prefix, int64_t* spans, hipStream_t stream) {
+  const int64_t n = (int64_t)s.B * s.Sq;
+  if (n <= 0) return hipSuccess;
+  if ((n + 255) / 256 > kScoreGridMost) return hipErrorInvalidValue;
+  ProfScope prof("mask_spans", stream);
+  hipLaunchKernelGGL(mask_spans_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, stream, s, bounds, n_docs, prefix, spans);
+  return hipGetLastError();
+}
+
+hipError_t launch_score_blocks(const ScoreArgs& a, hipStream_t stream) {
+  const int64_t n_blk = ((int64_t)a.s.Sq * (a.s.Hq / a.s.Hkv) + 31) / 32, n = n_blk * a.s.B;
+  if (n <= 0) return hipSuccess;
+  if ((n + 7) / 8 > kScoreGridMost) return hipErrorInvalidValue;
+  ProfScope prof("score_blocks", stream);
+  hipLaunchKernelGGL(score_blocks_kernel, dim3((unsigned)((n + 7) / 8)), dim3(256), 0, stream, a, (int32_t)n_blk);
+  return hipGetLastError();
+}
+
+hipError_t launch_score_add_parts(const ScoreArgs& a, int bf16, hipStream_t stream) {
+  PartSums p{};
+  const int64_t n_q = (int64_t)a.s.B * a.s.Sq * a.s.Hq * a.s.D, n_kv = (int64_t)a.s.B * a.s.Sk * a.s.Hkv * a.s.D;
+  int64_t most = 0;
+  if (a.q_split > 1) p.x[0] = PartSum{a.part_dq, a.dq, a.dq_lowp, a.q_split, n_q}, most = n_q;
+  if (a.kv_split > 1) {
+    p.x[1] = PartSum{a.part_dk, a.dk, a.dk_lowp, a.kv_split, n_kv};
+    p.x[2] = PartSum{a.part_dv, a.dv, a.dv_lowp, a.kv_split, n_kv};
+    most = most > n_kv ? most : n_kv;
+  }
+  if (most == 0) return hipSuccess;
+  p.assign = a.assign;
+  p.bf16 = bf16;
+  const int64_t blocks = (most / 4 + 255) / 256;
+  ProfScope prof("score_add_parts", stream);
+  hipLaunchKernelGGL(score_add_parts_kernel, dim3((unsigned)(blocks < 4096 ? blocks : 4096), 3), dim3(256), 0, stream, p);
+  return hipGetLastError();
+}
+
+}  // namespace st

@@ -1,0 +1,179 @@
+"""Norms and rotations of queries and keys (st_qk_rope_fwd / _bwd) against the 64-bit oracle and its derivatives.
+
+Tolerances: arithmetic is fp32 (sums of up to 256 squares and some thousand products, 2^-24 each: 2e-6 in the norm), angles are off
+by 2e-7 at most, and a bf16 result is rounded once, by 2^-8 relative at most."""
+import math
+
+import pytest
+import torch
+
+import paper_2407_00611_amd as st
+from oracle import score as so
+
+pytestmark = pytest.mark.gpu
+
+
+def _near(x, ref, dtype, what):
+    x, ref = x.double(), ref.double()
+    assert x.shape == ref.shape and torch.isfinite(x).all(), what
+    if not ref.numel():
+        return
+    off, norm = float((x - ref).norm()), float(ref.norm())
+    assert off <= (2e-6 if dtype == torch.float32 else 2.0 ** -8) * norm + 1e-12, f"{what}: {off / max(norm, 1e-30):.3e} off"
+    rms = norm / math.sqrt(ref.numel())
+    worst = float(((x - ref).abs() / ref.abs().clamp(min=rms + 1e-30)).max())
+    assert worst <= (2e-5 if dtype == torch.float32 else 2.0 ** -8 + 2e-5), f"{what}: an element {worst:.3e} off"
+
+
+def _run(dtype, B, S, Hq, Hkv, D, rot, axes=None, pairs="halves", norm=True, weights=True, offset=0, layout="dense", d_low=False, seed=0):
+    g = torch.Generator().manual_seed(seed)
+    r = lambda *s: torch.randn(s, generator=g)
+    if layout == "packed":
+        x = r(B, S, Hq + 2 * Hkv, D).to(dtype).cuda()
+        q, k = x[:, :, :Hq], x[:, :, Hq:Hq + Hkv]
+    elif layout == "heads_first":
+        q, k = (r(B, h, S, D).to(dtype).cuda().transpose(1, 2) for h in (Hq, max(Hkv, 1)))
+    else:
+        q, k = (r(B, S, h, D).to(dtype).cuda() for h in (Hq, max(Hkv, 1)))
+    if not Hkv:
+        k = None
+    td = dtype if d_low else torch.float32
+    dq, dk = (r(B, S, h, D).to(td).cuda() for h in (Hq, max(Hkv, 1)))
+    n = rot // 2
+    freq = (10000.0 ** (-torch.arange(n, dtype=torch.float64) / max(n, 1))).cuda()
+    i = torch.arange(S)
+    if axes is None:
+        pos = torch.where(i < offset[1], offset[0] + i, offset[2] + i - offset[1]) if isinstance(offset, tuple) else offset + i
+        table, each = None, pos.expand(n, B, S).cuda()
+    else:
+        table = torch.randint(-50, 100000, (len(axes), B, S), generator=g, dtype=torch.int32).cuda()
+        each = table.long()[torch.repeat_interleave(torch.arange(len(axes)), torch.tensor(axes)).cuda()]
+    wq, wk = ((1 + 0.3 * r(D)).cuda() if norm and weights else None for _ in range(2))
+    print(f"[{dtype} B{B} S{S} {Hq}/{Hkv} D{D} rot {rot} {axes} {pairs} norm {norm} {layout} at {offset}]", flush=True)
+    how = dict(freq=freq, offset=offset, positions=table, axes=axes, pairs=pairs, norm=norm, q_weight=wq, k_weight=wk if Hkv else None)
+    got = st.st_qk_rope_fwd(q, k, **how)
+    grads = st.st_qk_rope_bwd(q, k, dq, dk, **how)
+    for x, w, d, y, dx, dw, name in ((q, wq, dq, got[0], grads[0], grads[2], "q"), (k, wk, dk, got[1], grads[1], grads[3], "k")):
+        if x is None:
+            assert y is None and dx is None and dw is None
+            continue
+        a = x.double().detach().requires_grad_()
+        b = w.double().requires_grad_() if w is not None else None
+        ref = so.rope(a, b, freq, each, pairs, norm)
+        (ref * d.double()).sum().backward()
+        _near(y, ref.detach(), dtype, name)
+        _near(dx, a.grad, dtype, "d" + name)
+        if w is None:
+            assert dw is None
+        else:
+            _near(dw, b.grad, torch.float32, "dw" + name)
+
+
+CASES = [
+    dict(B=1, S=1, Hq=1, Hkv=1, D=8, rot=8),
+    dict(B=2, S=1, Hq=32, Hkv=8, D=128, rot=128, offset=8191),
+    dict(B=1, S=7, Hq=3, Hkv=0, D=64, rot=64, offset=524287),
+    dict(B=2, S=33, Hq=5, Hkv=1, D=80, rot=40, pairs="neighbours", offset=(4, 20, 900000)),   # 20 pairs of 40, 20 that stay
+    dict(B=1, S=19, Hq=4, Hkv=2, D=72, rot=50),                                              # an odd number of pairs
+    dict(B=1, S=19, Hq=4, Hkv=2, D=256, rot=250, pairs="neighbours"),
+    dict(B=1, S=19, Hq=2, Hkv=2, D=256, rot=250),
+    dict(B=1, S=40, Hq=2, Hkv=1, D=96, rot=0),
+    dict(B=2, S=50, Hq=6, Hkv=2, D=64, rot=64, axes=[8, 12, 12]),
+    dict(B=1, S=21, Hq=2, Hkv=2, D=128, rot=120, axes=[3, 0, 50, 7], pairs="neighbours"),
+    dict(B=1, S=30, Hq=4, Hkv=4, D=64, rot=32, norm=False, axes=[9, 7]),
+    dict(B=2, S=30, Hq=4, Hkv=1, D=112, rot=112, weights=False),
+    dict(B=2, S=65, Hq=4, Hkv=2, D=128, rot=64, layout="packed"),
+    dict(B=2, S=65, Hq=4, Hkv=2, D=192, rot=96, layout="heads_first", d_low=True),
+    dict(B=1, S=1, Hq=70, Hkv=70, D=32, rot=16, offset=2 ** 31 - 1),
+    dict(B=3, S=1500, Hq=2, Hkv=1, D=64, rot=64, offset=1 << 20),                             # several tokens a workgroup
+]
+
+
+@pytest.mark.parametrize("case", CASES, ids=[str(i) for i in range(len(CASES))])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+def test_against_the_definition(dtype, case):
+    _run(dtype, seed=len(str(case)), **case)
+
+
+def test_many_tokens():
+    """More workgroups' sums than one per place of the chip, and a ragged end."""
+    _run(torch.bfloat16, 1, 9001, 3, 1, 64, 64, offset=7)
+    _run(torch.float32, 2, 8200, 1, 1, 32, 32, axes=[4, 12])
+
+
+@pytest.mark.parametrize("pairs", ["halves", "neighbours"])
+def test_in_place_and_added_gradients(pairs):
+    g = torch.Generator().manual_seed(3)
+    q, k = (torch.randn((2, 37, h, 64), generator=g).to(torch.bfloat16).cuda() for h in (4, 2))
+    w = torch.randn((2, 64), generator=g).cuda().unbind()
+    freq = (100.0 ** (-torch.arange(32, dtype=torch.float64) / 32)).cuda()
+    how = dict(freq=freq, offset=12, pairs=pairs, q_weight=w[0], k_weight=w[1])
+    a, b = st.st_qk_rope_fwd(q, k, **how)
+    q2, k2 = q.clone(), k.clone()
+    st.st_qk_rope_fwd(q2, k2, q_out=q2, k_out=k2, **how)
+    assert torch.equal(a, q2) and torch.equal(b, k2)
+    d = [torch.randn(t.shape, generator=g).to(torch.bfloat16).cuda() for t in (q, k)]
+    dx, dy, dwq, dwk = st.st_qk_rope_bwd(q, k, *d, **how)
+    d2 = [t.clone() for t in d]
+    twq, twk = torch.full((64,), 2.0).cuda(), torch.full((64,), -1.0).cuda()
+    st.st_qk_rope_bwd(q, k, *d2, dx_q=d2[0], dx_k=d2[1], dw_q=twq, dw_k=twk, **how)
+    assert torch.equal(d2[0], dx) and torch.equal(d2[1], dy)
+    assert torch.allclose(twq, dwq + 2, rtol=1e-6, atol=1e-5) and torch.allclose(twk, dwk - 1, rtol=1e-6, atol=1e-5)
+    st.st_qk_rope_bwd(q, k, *d, dw_q=twq, dw_k=twk, assign=True, **how)
+    assert torch.equal(twq, dwq) and torch.equal(twk, dwk)
+
+
+def test_captured_and_replayed():
+    g = torch.Generator().manual_seed(4)
+    q, k, dq, dk = (torch.randn((1, 300, h, 128), generator=g).to(torch.bfloat16).cuda() for h in (4, 2, 4, 2))
+    w = torch.ones((2, 128)).cuda().unbind()
+    freq = (10000.0 ** (-torch.arange(64, dtype=torch.float64) / 64)).cuda()
+    how = dict(freq=freq, offset=(5, 100, 2000), q_weight=w[0], k_weight=w[1])
+    outs = [torch.empty_like(t) for t in (q, k, q, k)] + [torch.empty((128,), device="cuda") for _ in range(2)]
+    ws = torch.empty(st.st_qk_rope_bwd_workspace_bytes(q, k, freq) + 256, dtype=torch.uint8, device="cuda")
+
+    def step():
+        st.st_qk_rope_fwd(q, k, q_out=outs[0], k_out=outs[1], **how)
+        st.st_qk_rope_bwd(q, k, dq, dk, dx_q=outs[2], dx_k=outs[3], dw_q=outs[4], dw_k=outs[5], assign=True, workspace=ws, **how)
+    step()
+    torch.cuda.synchronize()
+    eager = [t.clone() for t in outs]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(3):
+        for t in outs:
+            t.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, eager))
+        q.mul_(1.0)
+
+
+def test_a_layer_from_projections_to_their_gradients():
+    """Norms and rotations, attention with a cap and documents, and back: against differentiation of the whole in 64 bits."""
+    B, S, Hq, Hkv, D = 2, 150, 4, 2, 64
+    g = torch.Generator().manual_seed(8)
+    q, k, v, d_o = (torch.randn((B, S, h, D), generator=g).cuda() for h in (Hq, Hkv, Hkv, Hq))
+    wq, wk = ((1 + 0.2 * torch.randn((D,), generator=g)).cuda() for _ in range(2))
+    freq = (10000.0 ** (-torch.arange(32, dtype=torch.float64) / 32)).cuda()
+    bounds = torch.tensor([[0, 70, 150], [10, 90, 140]]).cuda()
+    rope = dict(freq=freq, q_weight=wq, k_weight=wk)
+    spans = st.st_mask_spans(bounds, S, 0, True)
+    mods = dict(softcap=5.0, spans=spans)
+    rq, rk = st.st_qk_rope_fwd(q, k, **rope)
+    o, lse = st.st_attn_score_fwd(rq, rk, v, 0, 0, False, 0.5, **mods)
+    gq, gk, gv = st.st_attn_score_bwd(rq, rk, v, d_o, lse, st.st_attn_delta(d_o, o), 0, 0, False, 0.5, **mods)
+    dq, dk, dwq, dwk = st.st_qk_rope_bwd(q, k, gq, gk, **rope)
+    leaves = [t.double().requires_grad_() for t in (q, k, v, wq, wk)]
+    pos = torch.arange(S, device="cuda")
+    each = pos.expand(32, B, S)
+    a, b = so.rope(leaves[0], leaves[3], freq, each, "halves", True), so.rope(leaves[1], leaves[4], freq, each, "halves", True)
+    ref, _ = so.forward(a, b, leaves[2], pos, pos, False, 0.5, cap=5.0, span=spans)
+    torch.nan_to_num(ref).mul(d_o.double()).sum().backward()
+    inside = spans[..., 1] > 0
+    for x, y, name in zip((dq, dk, gv, dwq, dwk), leaves, ("dq", "dk", "dv", "dwq", "dwk")):
+        # fp32 throughout: 1e-5 as the attention's gradients, four of its steps
+        y = torch.nan_to_num(y.grad)
+        assert float((x.double() - y).norm()) <= 4e-5 * float(y.norm()), name
+    assert float((o.double() - ref)[inside].norm()) <= 1e-5 * float(ref[inside].norm())
