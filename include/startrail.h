@@ -319,7 +319,7 @@ st_status st_mask_spans(int32_t B, int32_t Sq, int64_t q_offset, int32_t q_seg, 
                         const int64_t* bounds, int32_t n_docs, const int64_t* prefix, int64_t* spans, void* hip_stream);
 
 /* Workspace of the two calls below, for these sizes (0: none is needed): device, 256-byte aligned; its contents mean nothing
- * between calls, and calls that share one must be ordered on one stream.  Only whether desc and score have spans counts. */
+ * between calls, and calls that share one must be ordered on one stream.  What score holds does not count. */
 size_t st_attn_score_workspace_bytes(const st_block_desc* desc, const st_score* score, int32_t backward);
 
 /* score: nullable (plain scores).  o_part fp32 and / or o_lowp in desc->dtype, dense [B,Sq,Hq,D] (one may be NULL, overwritten);

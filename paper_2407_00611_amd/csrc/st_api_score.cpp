@@ -46,12 +46,12 @@ st::ScoreArgs score_args(const st_block_desc* d, const st_score* m) {
   return a;
 }
 
-// How the launches are split and where in the workspace their sums lie (byte offsets).  Places of the chip: two workgroups of the
-// query-stationary kernels on a compute unit, one of the bf16 dK / dV kernel, which takes more than half of the registers.
+// How the launches are split and where in the workspace their sums lie (byte offsets).  Places of the chip: two workgroups on each
+// of 256 compute units.
 constexpr int64_t kSplitBytesMost = (int64_t)256 << 20;
 struct ScorePlan {
   int n_split, q_split, kv_split;
-  size_t lse, dk, dv, blocks, bytes;
+  size_t lse, dk, dv, blocks, rows, bytes;
 };
 ScorePlan fwd_plan(const st::Shape& s, int dtype) {
   const int G = s.Hq / s.Hkv;
@@ -67,7 +67,7 @@ ScorePlan fwd_plan(const st::Shape& s, int dtype) {
   }
   return p;
 }
-ScorePlan bwd_plan(const st::Shape& s, int dtype, bool spans) {
+ScorePlan bwd_plan(const st::Shape& s, int dtype) {
   const int G = s.Hq / s.Hkv;
   const bool bf16 = dtype == ST_BF16;
   const int64_t rows = bf16 ? ((int64_t)s.Sq * G + st::kScoreRows - 1) / st::kScoreRows * s.Hkv * s.B : ((int64_t)s.Sq + 31) / 32 * s.Hq * s.B;
@@ -76,13 +76,15 @@ ScorePlan bwd_plan(const st::Shape& s, int dtype, bool spans) {
   ScorePlan p{};
   p.q_split = st::score_split(rows, 512, bf16 ? ((int64_t)s.Sk + 63) / 64 : ((int64_t)s.Sk + 255) / 256, bf16 ? 4 : 1, 16);
   while (p.q_split > 1 && p.q_split * n_q > kSplitBytesMost) --p.q_split;
-  p.kv_split = st::score_split(keys, bf16 ? 256 : 512, ((int64_t)s.Sq * G + 31) / 32, 8, 16);
+  p.kv_split = st::score_split(keys, 512, ((int64_t)s.Sq * G + 31) / 32, 8, 16);
   while (p.kv_split > 1 && p.kv_split * n_kv * 2 > kSplitBytesMost) --p.kv_split;
   p.dk = p.q_split > 1 ? align_up((size_t)(p.q_split * n_q), 256) : 0;
   const size_t kv = p.kv_split > 1 ? align_up((size_t)(p.kv_split * n_kv), 256) : 0;
   p.dv = p.dk + kv;
   p.blocks = p.dv + kv;
-  p.bytes = p.blocks + (bf16 && spans ? align_up((size_t)(((int64_t)s.Sq * G + 31) / 32 * s.B * 16), 256) : 0);
+  const int64_t blocks = ((int64_t)s.Sq * G + 31) / 32 * s.B;
+  p.rows = p.blocks + (bf16 ? align_up((size_t)blocks * sizeof(int4), 256) : 0);
+  p.bytes = p.rows + (bf16 ? (size_t)blocks * s.Hkv * st::kRowStats * 4 : 0);
   return p;
 }
 
@@ -166,7 +168,7 @@ st_status st_mask_spans(int32_t B, int32_t Sq, int64_t q_offset, int32_t q_seg, 
 size_t st_attn_score_workspace_bytes(const st_block_desc* d, const st_score* m, int32_t backward) {
   if (check_score(d, m) != ST_OK || (int64_t)d->B * d->Sq == 0) return 0;
   const st::Shape s = shape_of(d);
-  return backward ? bwd_plan(s, d->dtype, m && m->spans).bytes : fwd_plan(s, d->dtype).bytes;
+  return backward ? bwd_plan(s, d->dtype).bytes : fwd_plan(s, d->dtype).bytes;
 }
 
 st_status st_attn_score_fwd(const st_block_desc* d, const st_score* m, const st_tensor* q, const st_tensor* k, const st_tensor* v,
@@ -246,16 +248,17 @@ st_status st_attn_score_bwd(const st_block_desc* d, const st_score* m, const st_
   a.dq = dq_acc; a.dk = dk_acc; a.dv = dv_acc;
   a.dq_lowp = dq_lowp; a.dk_lowp = dk_lowp; a.dv_lowp = dv_lowp;
   if (n_q > 0) {
-    const ScorePlan p = bwd_plan(a.s, d->dtype, a.spans != nullptr);
+    const ScorePlan p = bwd_plan(a.s, d->dtype);
     ST_TRY(check_workspace(workspace, workspace_bytes, p.bytes, "score backward"));
     a.q_split = p.q_split;
     a.kv_split = p.kv_split;
     a.part_dq = (float*)workspace;
     a.part_dk = (float*)((char*)workspace + p.dk);
     a.part_dv = (float*)((char*)workspace + p.dv);
-    if (d->dtype == ST_BF16 && a.spans) {
+    if (d->dtype == ST_BF16) {
       a.blocks = (int4*)((char*)workspace + p.blocks);
-      ST_HIP(st::launch_score_blocks(a, (hipStream_t)hip_stream), "row spans launch");
+      a.rows = (float*)((char*)workspace + p.rows);
+      ST_HIP(st::launch_score_rows(a, (hipStream_t)hip_stream), "row statistics launch");
     }
   }
   ST_HIP(d->dtype == ST_BF16 ? st::launch_score_bwd_bf16(a, (hipStream_t)hip_stream) : st::launch_score_bwd_f32(a, (hipStream_t)hip_stream), "st_attn_score_bwd launch");

@@ -41,8 +41,15 @@ struct ScoreArgs {
   // (part_dk, part_dv + y B Sk Hkv D), and a last launch adds them up in order
   int32_t q_split, kv_split;
   float *part_dq, *part_dk, *part_dv;
-  int4* blocks;              // spans given: what every run of 32 rows sees (BlockSpan), [B, ceil(Sq G / 32)]
+  // bf16, made by launch_score_rows: what every run of 32 rows sees (BlockSpan), [B, ceil(Sq G / 32)], and the statistics of its
+  // rows, kRowStats floats, [B, Hkv, ceil(Sq G / 32)]
+  int4* blocks;
+  float* rows;
 };
+// of 32 rows: lse (log2 units, as if the nearest key had no bias; inf: a row without gradients), minus Delta, the keys it sees and
+// the nearest of them, slope (log2 units)
+constexpr int kRowStats = 8 * 32;
+enum { kRowLse = 0, kRowDelta = 1, kRowLo = 2, kRowHi = 3, kRowX = 4, kRowSlope = 5 };
 
 constexpr float kScoreLog2e = 1.4426950408889634f;
 constexpr float kScoreLn2 = 0.6931471805599453f;
@@ -50,7 +57,7 @@ constexpr float kScoreLn2 = 0.6931471805599453f;
 hipError_t launch_mask_spans(const Shape& s, const int64_t* bounds, int32_t n_docs, const int64_t* prefix, int64_t* spans, hipStream_t stream);
 hipError_t launch_score_fwd_bf16(const ScoreArgs& a, hipStream_t stream);
 hipError_t launch_score_fwd_f32(const ScoreArgs& a, hipStream_t stream);
-hipError_t launch_score_blocks(const ScoreArgs& a, hipStream_t stream);
+hipError_t launch_score_rows(const ScoreArgs& a, hipStream_t stream);
 hipError_t launch_score_bwd_bf16(const ScoreArgs& a, hipStream_t stream);
 hipError_t launch_score_bwd_f32(const ScoreArgs& a, hipStream_t stream);
 hipError_t launch_score_add_parts(const ScoreArgs& a, int bf16, hipStream_t stream);
@@ -133,6 +140,58 @@ __device__ __forceinline__ ScoreConst score_const(const ScoreArgs& a) {
 __device__ __forceinline__ float cap_r(float u, float c) {
   return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(u * c));
 }
+
+// A lane's operand reads from a swizzled LDS tile (swz of st_mfma.h): three addresses in registers, the rest of a fragment's place
+// is an exclusive or with a constant and the instruction's own offset.  (Left to the compiler, every fragment's address of a loop
+// has a register of its own, some sixty that the accumulators need.)
+template <int D>
+struct LaneReads {
+  uint32_t nat, lo, hi;
+  __device__ __forceinline__ explicit LaneReads(int lane) {
+    const int g = lane >> 5, r = lane & 31, s16 = lane & 15, half = (lane >> 4) & 1;
+    nat = (uint32_t)swz<D>(r, g);
+    const int row = 4 * g + (s16 >> 2);
+    lo = (uint32_t)(swz<D>(row, 2 * half + ((s16 & 3) >> 1)) + (s16 & 1) * 8);
+    hi = (lo + 8 * D * 2) ^ 32;                        // eight rows on: the swizzle flips the second chunk bit
+  }
+  // as lds_frag: row row0 + r, elements 16 ks + 8 g .. + 7
+  __device__ __forceinline__ bf16x8 frag(uint32_t tile, int row0, int ks) const {
+    return lds_read_b128((const ST_LDS char*)(uintptr_t)((tile + nat) ^ (uint32_t)(32 * ks)) + row0 * D * 2);
+  }
+  // as lds_frag_tr: column 32 db + r at rows row0 + 4 g .. + 3 and row0 + 8 + 4 g .. + 3
+  __device__ __forceinline__ bf16x8 frag_tr(uint32_t tile, int row0, int db) const {
+    const u32x2 x = lds_read_tr16((const ST_LDS char*)(uintptr_t)((tile + lo) ^ (uint32_t)(64 * db)) + row0 * D * 2);
+    const u32x2 y = lds_read_tr16((const ST_LDS char*)(uintptr_t)((tile + hi) ^ (uint32_t)(64 * db)) + row0 * D * 2);
+    return __builtin_bit_cast(bf16x8, u32x4{x[0], x[1], y[0], y[1]});
+  }
+};
+
+// What a lane holds of a row's scores against a block of keys until their exponentials are taken, so that each costs as few
+// instructions as can be: with a cap r of cap_r, which falls as the score rises; otherwise the score over c, the bias included.
+template <bool CAP, bool BIAS>
+struct ScoreTile {
+  float c, k1, slope, x;     // x: the row's nearest key, from the lane's first key of the block on
+  __device__ __forceinline__ ScoreTile(const ScoreConst& k, float slope2, int x0) : c(k.c), k1(k.k1), slope(CAP ? slope2 : slope2 / k.c), x((float)x0) {}
+  // with both, the exponent itself.  raw: any tile; raw_side: all its keys on one side of the row, and the bias but for that of the
+  // lane's first key
+  __device__ __forceinline__ float raw(float u, int key) const {
+    if (CAP && !BIAS) return cap_r(u, c);
+    const float y = CAP ? fmaf(-2.f * k1, cap_r(u, c), k1) : u;
+    return BIAS ? fmaf(-slope, fabsf(x - (float)key), y) : y;
+  }
+  __device__ __forceinline__ float raw_side(float u, int key, float side) const {
+    if (CAP && !BIAS) return cap_r(u, c);
+    const float y = CAP ? fmaf(-2.f * k1, cap_r(u, c), k1) : u;
+    return BIAS ? fmaf(side, (float)key, y) : y;
+  }
+  __device__ __forceinline__ float lowest() const { return CAP && !BIAS ? INFINITY : -INFINITY; }
+  __device__ __forceinline__ float higher(float a, float b) const { return CAP && !BIAS ? fminf(a, b) : fmaxf(a, b); }
+  // log2 units, less m
+  __device__ __forceinline__ float exponent(float y, float m) const {
+    if (CAP) return BIAS ? y - m : fmaf(-2.f * k1, y, k1 - m);
+    return fmaf(y, c, -m);
+  }
+};
 
 // bf16 pairs with the infinities and NaN among them set to zero; bad collects a bit for each
 __device__ __forceinline__ uint32_t scrub_bf16(uint32_t x, uint32_t& bad) {

@@ -30,17 +30,30 @@ __global__ __launch_bounds__(256) void mask_spans_kernel(const Shape s, const in
   *reinterpret_cast<longlong2*>(spans + 2 * x) = w;
 }
 
-// half a wavefront per run of 32 packed rows
-__global__ __launch_bounds__(256) void score_blocks_kernel(const ScoreArgs a, int32_t n_blk) {
-  const int64_t x = (int64_t)blockIdx.x * 8 + threadIdx.x / 32, n = (int64_t)a.s.B * n_blk;
+// half a wavefront per run of 32 packed rows of a KV head
+__global__ __launch_bounds__(256) void score_rows_kernel(const ScoreArgs a, int32_t n_blk) {
+  const int64_t x = (int64_t)blockIdx.x * 8 + threadIdx.x / 32, n = (int64_t)a.s.B * a.s.Hkv * n_blk;
   const int r = threadIdx.x & 31, G = a.s.Hq / a.s.Hkv, M = a.s.Sq * G;
-  const int64_t at = min(x, n - 1);
-  const int b = (int)(at / n_blk), j = (int)(at - (int64_t)b * n_blk);
-  BlockSpan w = span_of(row_view(a, b, min(32 * j + r, M - 1) / G));
+  const int64_t at = min(x, n - 1), bh = at / n_blk;
+  const int j = (int)(at - bh * n_blk), b = (int)(bh / a.s.Hkv), hk = (int)(bh - (int64_t)b * a.s.Hkv);
+  const int R = 32 * j + r, row = min(R, M - 1), i = row / G, h = hk * G + row - i * G;
+  const RowView see = row_view(a, b, i);
+  BlockSpan w = span_of(see);
 #pragma unroll
   for (int d = 1; d < 32; d *= 2)
     w = span_join(w, BlockSpan{__shfl_xor(w.lo, d), __shfl_xor(w.hi, d), __shfl_xor(w.all_lo, d), __shfl_xor(w.all_hi, d)});
-  if (r == 0 && x < n) a.blocks[x] = make_int4(w.lo, w.hi, w.all_lo, w.all_hi);
+  if (x >= n) return;
+  if (r == 0 && hk == 0) a.blocks[(int64_t)b * n_blk + j] = make_int4(w.lo, w.hi, w.all_lo, w.all_hi);
+  const int64_t stat = ((int64_t)b * a.s.Hq + h) * a.s.Sq + i;
+  const float lse = a.lse_in[stat], slope = a.slopes ? a.slopes[h] : 0.f;
+  const bool none = R >= M || lse == -INFINITY;        // a row that does not exist, or an empty one: P = 0
+  float* f = a.rows + x * kRowStats + r;
+  f[32 * kRowLse] = none ? INFINITY : fmaf(slope, see.rest, lse) * kScoreLog2e;
+  f[32 * kRowDelta] = -a.delta[stat];
+  f[32 * kRowLo] = __int_as_float(none ? 0 : see.lo);
+  f[32 * kRowHi] = __int_as_float(none ? 0 : see.hi);
+  f[32 * kRowX] = (float)see.x;
+  f[32 * kRowSlope] = slope * kScoreLog2e;
 }
 
 struct PartSum {
@@ -92,12 +105,12 @@ hipError_t launch_mask_spans(const Shape& s, const int64_t* bounds, int32_t n_do
   return hipGetLastError();
 }
 
-hipError_t launch_score_blocks(const ScoreArgs& a, hipStream_t stream) {
-  const int64_t n_blk = ((int64_t)a.s.Sq * (a.s.Hq / a.s.Hkv) + 31) / 32, n = n_blk * a.s.B;
+hipError_t launch_score_rows(const ScoreArgs& a, hipStream_t stream) {
+  const int64_t n_blk = ((int64_t)a.s.Sq * (a.s.Hq / a.s.Hkv) + 31) / 32, n = n_blk * a.s.B * a.s.Hkv;
   if (n <= 0) return hipSuccess;
   if ((n + 7) / 8 > kScoreGridMost) return hipErrorInvalidValue;
-  ProfScope prof("score_blocks", stream);
-  hipLaunchKernelGGL(score_blocks_kernel, dim3((unsigned)((n + 7) / 8)), dim3(256), 0, stream, a, (int32_t)n_blk);
+  ProfScope prof("score_rows", stream);
+  hipLaunchKernelGGL(score_rows_kernel, dim3((unsigned)((n + 7) / 8)), dim3(256), 0, stream, a, (int32_t)n_blk);
   return hipGetLastError();
 }
 

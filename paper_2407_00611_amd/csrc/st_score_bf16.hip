@@ -8,6 +8,7 @@
 // tile the operand's infinities and NaN are set to zero.  The forward adds them to the rows that do see them once O is stored; in
 // the backward, a row that sees a key with such values has NaN in P or dU already, and so has its contribution.
 #include <algorithm>
+#include <type_traits>
 
 #include "st_score.h"
 
@@ -15,30 +16,94 @@ namespace st {
 namespace {
 
 constexpr int kBN = 64;              // keys of a streamed tile
-constexpr float kGap = 8.f;          // log2 units a tile's maximum may exceed the row's exponent reference by
+// A lane's sum over sixteen keys beyond which a row's exponent reference moves up: one of its exponents exceeds the reference by 8
+// log2 units then; while all are below that, none does.
+constexpr float kSumMost = 4096.f;
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
-// Tiles of 64 keys that a query tile's workgroup walks: those its rows' hull touches, its share of them
+// Tiles of 64 keys that a query tile's workgroup walks: those that the hull of its rows touches.  The general ones come first (a
+// mask edge crosses them, or a biased row lies in them), then the rest, the whole ones, in two ranges of the chunk: nearest first,
+// so that a bias that falls with the distance finds the largest exponents early.  The two kinds have loops of their own: as two
+// ways through one loop's body they cost copies of all accumulators and the masks' compares in every tile (32/8 heads x 8192 rows,
+// capped: 358 us).  A share of a split walk is a run of this order.
 struct Walk {
-  int t0, t1;
+  int t0, a0, a1, a2;        // general [t0, a0), [a1, a2) and from a3 on; whole [a0, a1) from its end, [a2, a3) from its start
+  int n_gen, n0, n1;         // general tiles; this share
+  __device__ __forceinline__ int tile(int n) const {
+    if (n < n_gen) {
+      const int g1 = a0 - t0, g2 = g1 + a2 - a1;
+      return n < g1 ? t0 + n : n < g2 ? a1 + n - g1 : a3 + n - g2;
+    }
+    n -= n_gen;
+    return n < a1 - a0 ? a1 - 1 - n : a2 + n - (a1 - a0);
+  }
+  int a3;
 };
-__device__ __forceinline__ Walk walk_of(int lo, int hi, int n_split, int share) {
-  if (lo >= hi) return Walk{0, 0};
-  const int first = lo / kBN, n = (hi + kBN - 1) / kBN - first;
-  const int64_t y = share;
-  return Walk{first + (int)(n * y / n_split), first + (int)(n * (y + 1) / n_split)};
+// x_lo, x_hi: where the rows' nearest keys lie (bias only)
+__device__ __forceinline__ Walk walk_of(const BlockSpan& w, bool bias, int x_lo, int x_hi, int n_split, int share) {
+  Walk y;
+  const bool any = w.lo < w.hi;
+  y.t0 = any ? w.lo / kBN : 0;
+  const int t1 = any ? (w.hi + kBN - 1) / kBN : 0;
+  const int f0 = min(max((w.all_lo + kBN - 1) / kBN, y.t0), t1), f1 = max(min(w.all_hi / kBN, t1), f0);   // whole tiles
+  y.a0 = f0;
+  y.a1 = f1;
+  y.a2 = y.a3 = f1;
+  if (bias) {                                          // only those with all rows on one side
+    y.a1 = max(min(f1, (x_lo + 1) / kBN), f0);
+    y.a2 = min(max(y.a1, (x_hi + kBN - 1) / kBN), f1);
+    y.a3 = f1;
+    if (y.a2 < y.a1) y.a2 = y.a1;
+  }
+  const int whole = y.a1 - y.a0 + y.a3 - y.a2, n = t1 - y.t0;
+  y.n_gen = n - whole;
+  const int64_t s = share;
+  y.n0 = (int)(n * s / n_split);
+  y.n1 = (int)(n * (s + 1) / n_split);
+  return y;
 }
 
 // Block id -> (row tile, KV head, batch entry).  Every XCD has a contiguous range of the (KV head, batch entry) pairs, whose keys and
-// values stay in its L2; under a causal mask the later tiles, which see more, come first.
+// values stay in its L2; under a causal mask the later tiles, which see more, come first (spans mostly are such masks too).
 __device__ __forceinline__ void tile_block(const ScoreArgs& a, int n_qt, int& qt, int& hk, int& b) {
   int hb;
-  qtile_block(blockIdx.x, gridDim.x, n_qt, a.s.causal, qt, hb);
+  qtile_block(blockIdx.x, gridDim.x, n_qt, a.s.causal || a.spans, qt, hb);
   hk = uniform(hb % a.s.Hkv);
   b = uniform(hb / a.s.Hkv);
   qt = uniform(qt);
 }
+
+// what the rows of the workgroup see together, from what those of each wavefront do; hull: 6 x 4 ints of LDS
+__device__ __forceinline__ BlockSpan workgroup_span(int* hull, const BlockSpan& w, int x_lo, int x_hi, int wave, int lane, int& wg_x_lo, int& wg_x_hi) {
+  if (lane == 0) {
+    hull[wave] = w.lo; hull[4 + wave] = w.hi; hull[8 + wave] = w.all_lo; hull[12 + wave] = w.all_hi; hull[16 + wave] = x_lo; hull[20 + wave] = x_hi;
+  }
+  __syncthreads();
+  auto lowest = [&](int o) { return uniform(min(min(hull[o], hull[o + 1]), min(hull[o + 2], hull[o + 3]))); };
+  auto highest = [&](int o) { return uniform(max(max(hull[o], hull[o + 1]), max(hull[o + 2], hull[o + 3]))); };
+  wg_x_lo = lowest(16);
+  wg_x_hi = highest(20);
+  return BlockSpan{lowest(0), highest(4), highest(8), lowest(12)};
+}
+
+// Direct loads of a whole 64-key tile: the lane's place in the tile's first rows, the rest of the address is uniform
+template <int D>
+struct TileLoads {
+  const char* at;
+  int64_t row;               // bytes
+  __device__ __forceinline__ TileLoads(const char* base, int64_t stride, int lane, int wave) : row(stride * 2) {
+    constexpr int PPR = D / 8, RPI = 64 / PPR;
+    const int r = wave * RPI + lane / PPR, f = swz<D>(r, 0) - r * D * 2;
+    at = base + r * row + (((lane % PPR) << 4) ^ f);
+  }
+  __device__ __forceinline__ void issue(int key0, ST_LDS char* tile, int wave) const {
+    constexpr int N = kBN * D * 2 / 4096, STEP = 4 * 64 / (D / 8);
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      __builtin_amdgcn_global_load_lds((st_global_ptr)(at + (key0 + STEP * j) * row), (st_lds_ptr)(tile + (4 * j + wave) * 1024), 16, 0, 0);
+  }
+};
 
 // =============================================================================================
 // forward: 128 rows per workgroup, 32 per wavefront; lane = row (C layout column)
@@ -47,8 +112,9 @@ template <int D, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, 2) void score_fwd_kernel(const ScoreArgs a) {
   constexpr int KB = kBN / 32, KS = D / 16, DB = D / 32;
   constexpr int kTile = kBN * D * 2;
+  constexpr float kUnset = -1e30f;                     // reference of a row that has met no key: whatever comes exceeds it
   __shared__ __attribute__((aligned(1024))) char smem_raw[4 * kTile];   // 2 stages x (K, V)
-  __shared__ int hull[8];
+  __shared__ int hull[24];
   ST_LDS char* smem = (ST_LDS char*)smem_raw;
   const Shape& s = a.s;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
@@ -61,13 +127,8 @@ __global__ __launch_bounds__(256, 2) void score_fwd_kernel(const ScoreArgs a) {
   const int R = qt * kScoreRows + wave * 32 + r, row = min(R, M - 1);
   const int i = row / G, h = hk * G + row % G;
   const RowView see = row_view(a, b, i);
-  const BlockSpan own = span_of(see);
-  BlockSpan w;                                         // of the wavefront's rows
-  w.lo = wave_min(own.lo); w.hi = wave_max(own.hi); w.all_lo = wave_max(own.all_lo); w.all_hi = wave_min(own.all_hi);
-  if (lane == 0) {
-    hull[wave] = w.lo;
-    hull[4 + wave] = w.hi;
-  }
+  BlockSpan w = span_of(see);                          // of the wavefront's rows
+  w.lo = wave_min(w.lo); w.hi = wave_max(w.hi); w.all_lo = wave_max(w.all_lo); w.all_hi = wave_min(w.all_hi);
   // Q fragments (B operand): row r, elements 16 ks + 8 g .. + 7
   bf16x8 qf[KS];
   const char* qrow = (const char*)a.q.ptr + ((int64_t)b * a.q.sb + (int64_t)i * a.q.ss + (int64_t)h * a.q.sh) * 2;
@@ -75,105 +136,117 @@ __global__ __launch_bounds__(256, 2) void score_fwd_kernel(const ScoreArgs a) {
   for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8*>(qrow + (16 * ks + 8 * g) * 2);
   const ScoreConst k = score_const(a);
   const float slope2 = BIAS ? a.slopes[h] * kScoreLog2e : 0.f;
-  __syncthreads();
-  const int lo = uniform(min(min(hull[0], hull[1]), min(hull[2], hull[3]))), hi = uniform(max(max(hull[4], hull[5]), max(hull[6], hull[7])));
-  const Walk walk = walk_of(lo, hi, a.n_split, blockIdx.y);
+  int x_lo = 0, x_hi = 0;
+  if (BIAS) x_lo = wave_min(see.x), x_hi = wave_max(see.x);
+  const BlockSpan wg = workgroup_span(hull, w, x_lo, x_hi, wave, lane, x_lo, x_hi);
+  const Walk walk = walk_of(wg, BIAS, x_lo, x_hi, a.n_split, blockIdx.y);
 
   f32x16 acc[DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db)
 #pragma unroll
     for (int v = 0; v < 16; ++v) acc[db][v] = 0.f;
-  float m_run = -INFINITY, l_run = 0.f;
+  float m_run = kUnset, l_run = 0.f;
   uint32_t bad = 0;
 
   const char* kb_ = (const char*)a.k.ptr + ((int64_t)b * a.k.sb + (int64_t)hk * a.k.sh) * 2;
   const char* vb_ = (const char*)a.v.ptr + ((int64_t)b * a.v.sb + (int64_t)hk * a.v.sh) * 2;
-  auto issue_load = [&](int t, int stage) {
-    stage_dma<D, kBN>(kb_, a.k.ss, t * kBN, s.Sk, smem + stage * 2 * kTile, tid);
-    stage_dma<D, kBN>(vb_, a.v.ss, t * kBN, s.Sk, smem + stage * 2 * kTile + kTile, tid);
-  };
-  int buf = 0;
-  if (walk.t0 < walk.t1) issue_load(walk.t0, 0);
-  __syncthreads();
-  for (int t = walk.t0; t < walk.t1; ++t) {
-    if (t + 1 < walk.t1) issue_load(t + 1, buf ^ 1);
-    const int key0 = t * kBN;
-    if (w.lo < key0 + kBN && w.hi > key0) {            // some row of this wavefront sees some key of the tile
-      const bool masked = w.all_lo > key0 || w.all_hi < key0 + kBN;
-      const ST_LDS char* ktile = smem + buf * 2 * kTile;
-      const ST_LDS char* vtile = ktile + kTile;
-      f32x16 sc[KB];
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) sc[kb][v] = 0.f;
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb) sc[kb] = mfma32(lds_frag<D>(ktile, 32 * kb, ks, lane), qf[ks], sc[kb]);
-      const float x = (float)(see.x - key0 - 4 * g);
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          float e = CAP ? fmaf(-2.f * k.k1, cap_r(sc[kb][v], k.c), k.k1) : BIAS ? sc[kb][v] * k.c : sc[kb][v];
-          if (BIAS) e = fmaf(-slope2, fabsf(x - (float)(32 * kb + 8 * (v / 4) + v % 4)), e);
-          sc[kb][v] = e;
-        }
-      constexpr bool kRaw = !CAP && !BIAS;             // the exponents are c times what sc holds
-      if (masked) {
-        const int l0 = see.lo - key0 - 4 * g, h0 = see.hi - key0 - 4 * g;
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-          for (int v = 0; v < 16; ++v) {
-            const int key = 32 * kb + 8 * (v / 4) + v % 4;
-            if (key < l0 || key >= h0) sc[kb][v] = -INFINITY;
-          }
-      }
-      float mx = sc[0][0];
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) mx = fmaxf(mx, sc[kb][v]);
-      mx = xhalf_max(mx);
-      if (kRaw) mx *= k.c;
-      // The reference of the exponents moves only when a tile exceeds it by more than kGap, which is rare after the first tiles
-      const bool jump = mx - m_run > kGap || (m_run == -INFINITY && mx != -INFINITY);
-      if (__builtin_expect(__any(jump), 0)) {
-        const float m_new = fmaxf(m_run, mx), m_use = m_new == -INFINITY ? 0.f : m_new;
-        const float alpha = __builtin_amdgcn_exp2f(m_run - m_use);
-        l_run *= alpha;
-        m_run = m_new;
-#pragma unroll
-        for (int db = 0; db < DB; ++db) scale_in_place(acc[db], alpha);
-      }
-      const float mc = m_run == -INFINITY ? 0.f : m_run;
-      float sum = 0.f;
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          const float p = __builtin_amdgcn_exp2f(kRaw ? fmaf(sc[kb][v], k.c, -mc) : sc[kb][v] - mc);
-          sc[kb][v] = p;
-          sum += p;
-        }
-      l_run += sum;
-      auto contract = [&](auto scrub) {
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-          for (int m = 0; m < 2; ++m) {
-            const bf16x8 pf = pack_c_as_b(sc[kb], m);
-#pragma unroll
-            for (int db = 0; db < DB; ++db)
-              acc[db] = mfma32(scrub(lds_frag_tr<D>(vtile, 32 * kb + 16 * m, 32 * db, lane)), pf, acc[db]);
-          }
-      };
-      if (masked) contract([&](bf16x8 f) { return scrub_bf16(f, bad); });
-      else contract([](bf16x8 f) { return f; });
+  const TileLoads<D> k_loads(kb_, a.k.ss, lane, wave), v_loads(vb_, a.v.ss, lane, wave);
+  auto issue_load = [&](int n, int stage) {
+    const int t = walk.tile(n);
+    ST_LDS char* at = smem + stage * 2 * kTile;
+    if (n < walk.n_gen) {                              // it may be the ragged end of the chunk
+      stage_dma<D, kBN>(kb_, a.k.ss, t * kBN, s.Sk, at, tid);
+      stage_dma<D, kBN>(vb_, a.v.ss, t * kBN, s.Sk, at + kTile, tid);
+    } else {
+      k_loads.issue(t * kBN, at, wave);
+      v_loads.issue(t * kBN, at + kTile, wave);
     }
+  };
+  const LaneReads<D> reads(lane);
+  const uint32_t smem_addr = (uint32_t)(uintptr_t)smem;
+
+  // 32 keys against the wavefront's rows.  In a whole tile the bias is slope (key - x) or slope (x - key) for all of them: its part
+  // that no key changes goes into the reference.
+  auto block = [&](auto general, uint32_t ktile, uint32_t vtile, int key0) {
+    constexpr bool GEN = decltype(general)::value;
+    f32x16 sc;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) sc[v] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) sc = mfma32(reads.frag(ktile, 0, ks), qf[ks], sc);
+    const int x0 = see.x - key0 - 4 * g;
+    const ScoreTile<CAP, BIAS> f(k, slope2, x0);
+    const float side = x0 > 0 ? f.slope : -f.slope;    // (left of the row the bias rises with the key)
+    const float off = BIAS && !GEN ? slope2 * fabsf((float)x0) : 0.f;
+    const int l0 = see.lo - key0 - 4 * g, h0 = see.hi - key0 - 4 * g;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      const int key = 8 * (v / 4) + v % 4;
+      sc[v] = GEN ? f.raw(sc[v], key) : f.raw_side(sc[v], key, side);
+      if (GEN) sc[v] = key >= l0 && key < h0 ? sc[v] : f.lowest();
+    }
+    // The reference m_run of the exponents is lazy.  It moves where the block's sum says that some exponent was large (or too large
+    // for its exponential): nothing of the block has been used by then.
+    float p[16], sum;
+    auto softmax = [&]() {
+      sum = 0.f;
+      const float m = m_run + off;
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        p[v] = __builtin_amdgcn_exp2f(f.exponent(sc[v], m));
+        sum += p[v];
+      }
+    };
+    softmax();
+    if (__builtin_expect(__any(sum > kSumMost), 0)) {
+      float top = f.lowest();
+#pragma unroll
+      for (int v = 0; v < 16; ++v) top = f.higher(top, sc[v]);
+      const float m_new = fmaxf(m_run, xhalf_max(f.exponent(top, off)));
+      const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+      l_run *= alpha;
+      m_run = m_new;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) acc[db][v] *= alpha;
+      softmax();
+    }
+    l_run += sum;
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      const bf16x8 pf = __builtin_bit_cast(bf16x8, u32x4{pack_bf16(p[8 * m], p[8 * m + 1]), pack_bf16(p[8 * m + 2], p[8 * m + 3]),
+                                                         pack_bf16(p[8 * m + 4], p[8 * m + 5]), pack_bf16(p[8 * m + 6], p[8 * m + 7])});
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        const bf16x8 vf = reads.frag_tr(vtile, 16 * m, db);
+        acc[db] = mfma32(GEN ? scrub_bf16(vf, bad) : vf, pf, acc[db]);
+      }
+    }
+  };
+
+  int buf = 0, n = walk.n0;
+  if (n < walk.n1) issue_load(n, 0);
+  __syncthreads();
+  for (; n < min(walk.n1, walk.n_gen); ++n) {
+    if (n + 1 < walk.n1) issue_load(n + 1, buf ^ 1);
+    const int key0 = walk.tile(n) * kBN;
+    const uint32_t ktile = smem_addr + buf * 2 * kTile;
+    if (w.lo < key0 + kBN && w.hi > key0)              // some row of this wavefront sees some key of the tile
+#pragma unroll 1
+      for (int kb = 0; kb < KB; ++kb)
+        block(std::true_type(), ktile + 32 * kb * D * 2, ktile + kTile + 32 * kb * D * 2, key0 + 32 * kb);
+    __syncthreads();
+    buf ^= 1;
+  }
+  for (; n < walk.n1; ++n) {
+    if (n + 1 < walk.n1) issue_load(n + 1, buf ^ 1);
+    const int key0 = walk.tile(n) * kBN;
+    const uint32_t ktile = smem_addr + buf * 2 * kTile;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+      block(std::false_type(), ktile + 32 * kb * D * 2, ktile + kTile + 32 * kb * D * 2, key0 + 32 * kb);
     __syncthreads();
     buf ^= 1;
   }
@@ -187,38 +260,37 @@ __global__ __launch_bounds__(256, 2) void score_fwd_kernel(const ScoreArgs a) {
   uint16_t* olow = part ? nullptr : (uint16_t*)a.o_lowp;
   const int64_t orow = (((int64_t)b * s.Sq + i) * s.Hq + h) * D;
   const bool any_bad = __any(bad != 0);
-  if (R < M) {
+  if (R >= M) return;
 #pragma unroll
-    for (int db = 0; db < DB; ++db)
+  for (int db = 0; db < DB; ++db)
 #pragma unroll
-      for (int q4 = 0; q4 < 4; ++q4) {
-        const int d = 32 * db + 8 * q4 + 4 * g;
-        const float4 y = make_float4(acc[db][4 * q4] * inv, acc[db][4 * q4 + 1] * inv, acc[db][4 * q4 + 2] * inv, acc[db][4 * q4 + 3] * inv);
-        if (o) *reinterpret_cast<float4*>(o + orow + d) = y;
-        if (olow) *reinterpret_cast<uint2*>(olow + orow + d) = make_uint2(pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
-      }
-    if (g == 0) {
-      float x = l != 0.f ? m_run * kScoreLn2 + logf(l) : -INFINITY;
-      if (BIAS) x = fmaf(-a.slopes[h], see.rest, x);
-      (part ? a.part_lse + blockIdx.y * n_o : a.lse)[((int64_t)b * s.Hq + h) * s.Sq + i] = x;
+    for (int q4 = 0; q4 < 4; ++q4) {
+      const int d = 32 * db + 8 * q4 + 4 * g;
+      const float4 y = make_float4(acc[db][4 * q4] * inv, acc[db][4 * q4 + 1] * inv, acc[db][4 * q4 + 2] * inv, acc[db][4 * q4 + 3] * inv);
+      if (o) *reinterpret_cast<float4*>(o + orow + d) = y;
+      if (olow) *reinterpret_cast<uint2*>(olow + orow + d) = make_uint2(pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
     }
-    if (any_bad)
-      // what the masked tiles of this wavefront left out: V[t][d] of the keys that this row sees
-      for (int t = walk.t0; t < walk.t1; ++t) {
-        if (!(w.all_lo > t * kBN || w.all_hi < (t + 1) * kBN)) continue;
-        for (int key = max(see.lo, t * kBN); key < min(see.hi, (t + 1) * kBN); ++key)
-          for (int d = 4 * g; d < D; d += 8)
-            for (int e = 0; e < 4; ++e) {
-              const float y = __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(vb_ + ((int64_t)key * a.v.ss + d + e) * 2) << 16);
-              if (fabsf(y) <= 3.402823466e38f) continue;
-              if (o) o[orow + d + e] += y;
-              if (olow) {
-                const float z = __uint_as_float((uint32_t)olow[orow + d + e] << 16) + y;
-                olow[orow + d + e] = (uint16_t)pack_bf16(z, z);
-              }
-            }
-      }
+  if (g == 0) {
+    float x = l != 0.f ? m_run * kScoreLn2 + logf(l) : -INFINITY;
+    if (BIAS) x = fmaf(-a.slopes[h], see.rest, x);
+    (part ? a.part_lse + blockIdx.y * n_o : a.lse)[((int64_t)b * s.Hq + h) * s.Sq + i] = x;
   }
+  if (any_bad)
+    // what the general tiles of this wavefront left out: V[t][d] of the keys that this row sees
+    for (int y = walk.n0; y < min(walk.n1, walk.n_gen); ++y) {
+      const int key0 = walk.tile(y) * kBN;
+      for (int key = max(see.lo, key0); key < min(see.hi, key0 + kBN); ++key)
+        for (int d = 4 * g; d < D; d += 8)
+          for (int e = 0; e < 4; ++e) {
+            const float x = __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(vb_ + ((int64_t)key * a.v.ss + d + e) * 2) << 16);
+            if (fabsf(x) <= 3.402823466e38f) continue;
+            if (o) o[orow + d + e] += x;
+            if (olow) {
+              const float z = __uint_as_float((uint32_t)olow[orow + d + e] << 16) + x;
+              olow[orow + d + e] = (uint16_t)pack_bf16(z, z);
+            }
+          }
+    }
 }
 
 // =============================================================================================
@@ -229,7 +301,7 @@ __global__ __launch_bounds__(256, 2) void score_dq_kernel(const ScoreArgs a) {
   constexpr int KB = kBN / 32, KS = D / 16, DB = D / 32;
   constexpr int kTile = kBN * D * 2;
   __shared__ __attribute__((aligned(1024))) char smem_raw[4 * kTile];
-  __shared__ int hull[8];
+  __shared__ int hull[24];
   ST_LDS char* smem = (ST_LDS char*)smem_raw;
   const Shape& s = a.s;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
@@ -248,13 +320,8 @@ __global__ __launch_bounds__(256, 2) void score_dq_kernel(const ScoreArgs a) {
   if (lse == -INFINITY) see.lo = see.hi = 0;           // an empty row
   // the row's constant: s log2 e = e + const with e from the nearest key on
   const float lse2 = (BIAS ? fmaf(slope, see.rest, lse) : lse) * kScoreLog2e;
-  const BlockSpan own = span_of(see);
-  BlockSpan w;
-  w.lo = wave_min(own.lo); w.hi = wave_max(own.hi); w.all_lo = wave_max(own.all_lo); w.all_hi = wave_min(own.all_hi);
-  if (lane == 0) {
-    hull[wave] = w.lo;
-    hull[4 + wave] = w.hi;
-  }
+  BlockSpan w = span_of(see);
+  w.lo = wave_min(w.lo); w.hi = wave_max(w.hi); w.all_lo = wave_max(w.all_lo); w.all_hi = wave_min(w.all_hi);
   bf16x8 qf[KS], dof[KS];
   const char* qrow = (const char*)a.q.ptr + ((int64_t)b * a.q.sb + (int64_t)i * a.q.ss + (int64_t)h * a.q.sh) * 2;
   const char* drow = (const char*)a.d_o.ptr + ((int64_t)b * a.d_o.sb + (int64_t)i * a.d_o.ss + (int64_t)h * a.d_o.sh) * 2;
@@ -264,9 +331,9 @@ __global__ __launch_bounds__(256, 2) void score_dq_kernel(const ScoreArgs a) {
     dof[ks] = *reinterpret_cast<const bf16x8*>(drow + (16 * ks + 8 * g) * 2);
   }
   const ScoreConst k = score_const(a);
-  __syncthreads();
-  const int lo = uniform(min(min(hull[0], hull[1]), min(hull[2], hull[3]))), hi = uniform(max(max(hull[4], hull[5]), max(hull[6], hull[7])));
-  const Walk walk = walk_of(lo, hi, a.q_split, blockIdx.y);
+  int unused;
+  const BlockSpan wg = workgroup_span(hull, w, 0, 0, wave, lane, unused, unused);
+  const Walk walk = walk_of(wg, false, 0, 0, a.q_split, blockIdx.y);
 
   f32x16 acc[DB];
 #pragma unroll
@@ -276,62 +343,80 @@ __global__ __launch_bounds__(256, 2) void score_dq_kernel(const ScoreArgs a) {
   uint32_t bad = 0;
   const char* kb_ = (const char*)a.k.ptr + ((int64_t)b * a.k.sb + (int64_t)hk * a.k.sh) * 2;
   const char* vb_ = (const char*)a.v.ptr + ((int64_t)b * a.v.sb + (int64_t)hk * a.v.sh) * 2;
-  auto issue_load = [&](int t, int stage) {
-    stage_dma<D, kBN>(kb_, a.k.ss, t * kBN, s.Sk, smem + stage * 2 * kTile, tid);
-    stage_dma<D, kBN>(vb_, a.v.ss, t * kBN, s.Sk, smem + stage * 2 * kTile + kTile, tid);
+  const TileLoads<D> k_loads(kb_, a.k.ss, lane, wave), v_loads(vb_, a.v.ss, lane, wave);
+  auto issue_load = [&](int n, int stage) {
+    const int t = walk.tile(n);
+    ST_LDS char* at = smem + stage * 2 * kTile;
+    if (n < walk.n_gen) {
+      stage_dma<D, kBN>(kb_, a.k.ss, t * kBN, s.Sk, at, tid);
+      stage_dma<D, kBN>(vb_, a.v.ss, t * kBN, s.Sk, at + kTile, tid);
+    } else {
+      k_loads.issue(t * kBN, at, wave);
+      v_loads.issue(t * kBN, at + kTile, wave);
+    }
   };
-  int buf = 0;
-  if (walk.t0 < walk.t1) issue_load(walk.t0, 0);
-  __syncthreads();
-  for (int t = walk.t0; t < walk.t1; ++t) {
-    if (t + 1 < walk.t1) issue_load(t + 1, buf ^ 1);
-    const int key0 = t * kBN;
-    if (w.lo < key0 + kBN && w.hi > key0) {
-      const bool masked = w.all_lo > key0 || w.all_hi < key0 + kBN;
-      const ST_LDS char* ktile = smem + buf * 2 * kTile;
-      const ST_LDS char* vtile = ktile + kTile;
+  const LaneReads<D> reads(lane);
+  const uint32_t smem_addr = (uint32_t)(uintptr_t)smem;
+  auto block = [&](auto general, uint32_t ktile, uint32_t vtile, int key0) {
+    constexpr bool GEN = decltype(general)::value;
+    f32x16 sc, dp;
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb) {
-        f32x16 sc, dp;
+    for (int v = 0; v < 16; ++v) sc[v] = dp[v] = 0.f;
 #pragma unroll
-        for (int v = 0; v < 16; ++v) sc[v] = dp[v] = 0.f;
+    for (int ks = 0; ks < KS; ++ks) {
+      sc = mfma32(reads.frag(ktile, 0, ks), qf[ks], sc);
+      dp = mfma32(reads.frag(vtile, 0, ks), dof[ks], dp);
+    }
+    const float x = (float)(see.x - key0 - 4 * g);
+    const int l0 = see.lo - key0 - 4 * g, h0 = see.hi - key0 - 4 * g;
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          sc = mfma32(lds_frag<D>(ktile, 32 * kb, ks, lane), qf[ks], sc);
-          dp = mfma32(lds_frag<D>(vtile, 32 * kb, ks, lane), dof[ks], dp);
-        }
-        const float x = (float)(see.x - key0 - 32 * kb - 4 * g);
-        const int l0 = see.lo - key0 - 32 * kb - 4 * g, h0 = see.hi - key0 - 32 * kb - 4 * g;
+    for (int v = 0; v < 16; ++v) {
+      const int key = 8 * (v / 4) + v % 4;
+      float e, f = 1.f;
+      if (CAP) {
+        const float rr = cap_r(sc[v], k.c);
+        e = fmaf(-2.f * k.k1, rr, k.k1 - lse2);
+        f = 4.f * rr * (1.f - rr);
+      } else {
+        e = fmaf(sc[v], k.c, -lse2);
+      }
+      if (BIAS) e = fmaf(-slope2, fabsf(x - (float)key), e);
+      float ds = __builtin_amdgcn_exp2f(e) * (dp[v] - dlt);
+      if (CAP) ds *= f;
+      if (GEN) ds = key >= l0 && key < h0 ? ds : 0.f;
+      sc[v] = ds;
+    }
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          const int key = 8 * (v / 4) + v % 4;
-          float e, f = 1.f;
-          if (CAP) {
-            const float rr = cap_r(sc[v], k.c);
-            e = fmaf(-2.f * k.k1, rr, k.k1 - lse2);
-            f = 4.f * rr * (1.f - rr);
-          } else {
-            e = fmaf(sc[v], k.c, -lse2);
-          }
-          if (BIAS) e = fmaf(-slope2, fabsf(x - (float)key), e);
-          float ds = __builtin_amdgcn_exp2f(e) * (dp[v] - dlt);
-          if (CAP) ds *= f;
-          if (masked) ds = key >= l0 && key < h0 ? ds : 0.f;
-          sc[v] = ds;
-        }
-        auto contract = [&](auto scrub) {
+    for (int m = 0; m < 2; ++m) {
+      const bf16x8 dsf = pack_c_as_b(sc, m);
 #pragma unroll
-          for (int m = 0; m < 2; ++m) {
-            const bf16x8 dsf = pack_c_as_b(sc, m);
-#pragma unroll
-            for (int db = 0; db < DB; ++db)
-              acc[db] = mfma32(scrub(lds_frag_tr<D>(ktile, 32 * kb + 16 * m, 32 * db, lane)), dsf, acc[db]);
-          }
-        };
-        if (masked) contract([&](bf16x8 f) { return scrub_bf16(f, bad); });
-        else contract([](bf16x8 f) { return f; });
+      for (int db = 0; db < DB; ++db) {
+        const bf16x8 ktf = reads.frag_tr(ktile, 16 * m, db);
+        acc[db] = mfma32(GEN ? scrub_bf16(ktf, bad) : ktf, dsf, acc[db]);
       }
     }
+  };
+  int buf = 0, n = walk.n0;
+  if (n < walk.n1) issue_load(n, 0);
+  __syncthreads();
+  for (; n < min(walk.n1, walk.n_gen); ++n) {
+    if (n + 1 < walk.n1) issue_load(n + 1, buf ^ 1);
+    const int key0 = walk.tile(n) * kBN;
+    const uint32_t ktile = smem_addr + buf * 2 * kTile;
+    if (w.lo < key0 + kBN && w.hi > key0)
+#pragma unroll 1
+      for (int kb = 0; kb < KB; ++kb)
+        block(std::true_type(), ktile + 32 * kb * D * 2, ktile + kTile + 32 * kb * D * 2, key0 + 32 * kb);
+    __syncthreads();
+    buf ^= 1;
+  }
+  for (; n < walk.n1; ++n) {
+    if (n + 1 < walk.n1) issue_load(n + 1, buf ^ 1);
+    const int key0 = walk.tile(n) * kBN;
+    const uint32_t ktile = smem_addr + buf * 2 * kTile;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+      block(std::false_type(), ktile + 32 * kb * D * 2, ktile + kTile + 32 * kb * D * 2, key0 + 32 * kb);
     __syncthreads();
     buf ^= 1;
   }
@@ -357,20 +442,22 @@ __global__ __launch_bounds__(256, 2) void score_dq_kernel(const ScoreArgs a) {
 }
 
 // =============================================================================================
-// dK, dV: 128 keys of one KV head per workgroup, 32 per wavefront, K and V fragments resident; the group's rows stream by in blocks
-// of 32.  lane = key (C layout column), registers = 16 rows
+// dK, dV: 128 keys of one KV head per workgroup, 32 per wavefront; the group's rows stream by in blocks of 32.  lane = key (C layout
+// column), registers = 16 rows.  K fragments stay in registers, V in LDS, so that two workgroups fit a compute unit: one's softmax
+// runs under the other's products.
 // =============================================================================================
-constexpr int kBlockList = 1024;     // row blocks that a workgroup looks through at a time
+constexpr int kBlockList = 512;      // row blocks that a workgroup looks through at a time
 
 template <int D, bool CAP, bool BIAS>
-__global__ __launch_bounds__(256, 1) void score_dkv_kernel(const ScoreArgs a) {
+__global__ __launch_bounds__(256, 2) void score_dkv_kernel(const ScoreArgs a) {
   constexpr int KS = D / 16, DB = D / 32;
-  constexpr int kTile = 32 * D * 2, kStats = 6 * 32 * 4;
-  constexpr int kStage = 2 * kTile + kStats;           // Q, dO, and of each row lse, Delta, lo, hi, x, slope
-  __shared__ __attribute__((aligned(16))) char smem_raw[2 * kStage];
-  __shared__ int4 list[kBlockList];                    // block, hull of its rows, 1: every row sees every key of the workgroup
-  __shared__ int count[5];
+  constexpr int kTile = 32 * D * 2, kStage = 2 * kTile + kRowStats * 4;   // Q, dO and the statistics of 32 rows
+  constexpr int kKeyTile = kScoreKeys * D * 2;
+  __shared__ __attribute__((aligned(1024))) char smem_raw[kKeyTile + 2 * kStage];
+  __shared__ int4 list[kBlockList];                    // block and hull of its rows: whole ones from the front, the others from the back
+  __shared__ int count[8];
   ST_LDS char* smem = (ST_LDS char*)smem_raw;
+  ST_LDS char* stages = smem + kKeyTile;
   const Shape& s = a.s;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int g = lane >> 5, r = lane & 31;
@@ -384,14 +471,11 @@ __global__ __launch_bounds__(256, 1) void score_dkv_kernel(const ScoreArgs a) {
   const int key = wkey0 + r, key_row = min(key, s.Sk - 1);
   const uint32_t inv_g = G > 1 ? 0xffffffffu / (uint32_t)G + 1 : 0;      // x / G = x inv_g / 2^32 for the small x below
 
+  stage_dma<D, kScoreKeys>((const char*)a.v.ptr + ((int64_t)b * a.v.sb + (int64_t)hk * a.v.sh) * 2, a.v.ss, key0, s.Sk, smem, tid);
   const char* kp = (const char*)a.k.ptr + ((int64_t)b * a.k.sb + (int64_t)hk * a.k.sh + (int64_t)key_row * a.k.ss) * 2;
-  const char* vp = (const char*)a.v.ptr + ((int64_t)b * a.v.sb + (int64_t)hk * a.v.sh + (int64_t)key_row * a.v.ss) * 2;
-  bf16x8 kf[KS], vf[KS];
+  bf16x8 kf[KS];
 #pragma unroll
-  for (int ks = 0; ks < KS; ++ks) {
-    kf[ks] = *reinterpret_cast<const bf16x8*>(kp + (16 * ks + 8 * g) * 2);
-    vf[ks] = *reinterpret_cast<const bf16x8*>(vp + (16 * ks + 8 * g) * 2);
-  }
+  for (int ks = 0; ks < KS; ++ks) kf[ks] = *reinterpret_cast<const bf16x8*>(kp + (16 * ks + 8 * g) * 2);
   const ScoreConst k = score_const(a);
   f32x16 acc_k[DB], acc_v[DB];
 #pragma unroll
@@ -400,73 +484,84 @@ __global__ __launch_bounds__(256, 1) void score_dkv_kernel(const ScoreArgs a) {
     for (int v = 0; v < 16; ++v) acc_k[db][v] = acc_v[db][v] = 0.f;
   uint32_t bad = 0;
 
-  // what the rows of block j see; without spans a row sees a run from the chunk's first key on, longer from row to row
-  auto block_span = [&](int j) {
-    if (a.blocks) {
-      const int4 x = a.blocks[(int64_t)b * n_blk + j];
-      return BlockSpan{x.x, x.y, x.z, x.w};
+  // a block's rows and statistics, straight to LDS: two of the 16-byte pieces of each tile a lane (one at head size 64)
+  constexpr int PPR = D / 8, RPI = 64 / PPR;
+  const int piece_row = wave * RPI + lane / PPR, piece = ((lane % PPR) << 4) ^ (swz<D>(piece_row, 0) - piece_row * D * 2);
+  const char* q_base = (const char*)a.q.ptr + ((int64_t)b * a.q.sb + (int64_t)hk * G * a.q.sh) * 2 + piece;
+  const char* d_base = (const char*)a.d_o.ptr + ((int64_t)b * a.d_o.sb + (int64_t)hk * G * a.d_o.sh) * 2 + piece;
+  const char* stat_base = (const char*)(a.rows + ((int64_t)b * s.Hkv + hk) * n_blk * kRowStats) + lane * 16;
+  auto load_block = [&](int j, int stage) {
+    j = uniform(j);
+    ST_LDS char* at = stages + stage * kStage;
+    const int base = 32 * j / G, rem = 32 * j - base * G;                // uniform
+#pragma unroll
+    for (int u = 0; u < 32 / (4 * RPI); ++u) {
+      const uint32_t x = (uint32_t)(rem + min(piece_row + 4 * RPI * u, M - 1 - 32 * j)), q = G > 1 ? __umulhi(x, inv_g) : x;
+      const int64_t i = base + (int)q, h = (int)(x - q * (uint32_t)G);
+      __builtin_amdgcn_global_load_lds((st_global_ptr)(q_base + (i * a.q.ss + h * a.q.sh) * 2), (st_lds_ptr)(at + (4 * u + wave) * 1024), 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((st_global_ptr)(d_base + (i * a.d_o.ss + h * a.d_o.sh) * 2), (st_lds_ptr)(at + kTile + (4 * u + wave) * 1024), 16, 0, 0);
     }
-    if (!s.causal) return BlockSpan{0, s.Sk, 0, s.Sk};
-    auto seen = [&](int i) {
-      const int64_t pos = q_pos(s, i);
-      return pos < a.k_offset ? 0 : key_clamp(pos + 1, a.k_offset, s.Sk);
-    };
-    const int first = seen(32 * j / G), last = seen(min(32 * j + 31, M - 1) / G);
-    return BlockSpan{last > 0 ? 0 : 0x7fffffff, last, 0, first};
+    if (wave == 0) __builtin_amdgcn_global_load_lds((st_global_ptr)(stat_base + (int64_t)j * kRowStats * 4), (st_lds_ptr)(at + 2 * kTile), 16, 0, 0);
   };
 
-  u32x4 rq[D / 64], rd[D / 64];                        // a block on its way: 32 rows x D / 8 pieces over 256 threads
-  float st_lse = 0.f, st_dlt = 0.f, st_x = 0.f, st_slope = 0.f;
-  int st_lo = 0, st_hi = 0;
-  auto row_at = [&](int j, int x, int& i, int& h) {    // row x of block j
-    const int base = 32 * j / G;                       // uniform
-    const uint32_t n = (uint32_t)(32 * j - base * G + x), q = G > 1 ? __umulhi(n, inv_g) : n;
-    i = base + (int)q;
-    h = hk * G + (int)(n - q * (uint32_t)G);
-  };
-  auto load_block = [&](int j) {
-    j = uniform(j);
+  const LaneReads<D> reads(lane);
+  const uint32_t v_rows = (uint32_t)(uintptr_t)smem + wave * 32 * D * 2, stage_addr = (uint32_t)(uintptr_t)stages;
+  const float kx = (float)key;
+  auto block = [&](auto general, int stage) {
+    constexpr bool GEN = decltype(general)::value;
+    const uint32_t qtile = stage_addr + stage * kStage, dotile = qtile + kTile;
+    const ST_LDS float* stats = reinterpret_cast<const ST_LDS float*>(stages + stage * kStage + 2 * kTile);
+    auto rows4 = [&](int what, int j4) { return *reinterpret_cast<const ST_LDS f32x4*>(stats + 32 * what + 8 * j4 + 4 * g); };
+    f32x16 sc, dp;
 #pragma unroll
-    for (int u = 0; u < D / 64; ++u) {
-      const int p = tid + 256 * u;
-      int i, h;
-      row_at(j, min(p / (D / 8), M - 1 - 32 * j), i, h);
-      rq[u] = *reinterpret_cast<const u32x4*>((const char*)a.q.ptr + ((int64_t)b * a.q.sb + (int64_t)i * a.q.ss + (int64_t)h * a.q.sh + p % (D / 8) * 8) * 2);
-      rd[u] = *reinterpret_cast<const u32x4*>((const char*)a.d_o.ptr + ((int64_t)b * a.d_o.sb + (int64_t)i * a.d_o.ss + (int64_t)h * a.d_o.sh + p % (D / 8) * 8) * 2);
-    }
-    if (tid < 32) {
-      int i, h;
-      const int x = min(tid, M - 1 - 32 * j);
-      row_at(j, x, i, h);
-      const RowView see = row_view(a, b, i);
-      const int64_t stat = ((int64_t)b * s.Hq + h) * s.Sq + i;
-      const float lse = a.lse_in[stat];
-      st_slope = BIAS ? a.slopes[h] : 0.f;
-      const bool none = x < tid || lse == -INFINITY;   // a row that does not exist, or an empty one: P = 0
-      st_lse = none ? INFINITY : (BIAS ? fmaf(st_slope, see.rest, lse) : lse) * kScoreLog2e;
-      st_slope *= kScoreLog2e;
-      st_dlt = a.delta[stat];
-      st_lo = none ? 0 : see.lo;
-      st_hi = none ? 0 : see.hi;
-      st_x = (float)see.x;
-    }
-  };
-  auto store_block = [&](int stage) {
-    ST_LDS char* p0 = smem + stage * kStage;
+    for (int j4 = 0; j4 < 4; ++j4) {
+      const f32x4 dlt = rows4(kRowDelta, j4);          // minus Delta: what the products of dP are added to
 #pragma unroll
-    for (int u = 0; u < D / 64; ++u) {
-      const int p = tid + 256 * u;
-      *reinterpret_cast<ST_LDS u32x4*>(p0 + swz<D>(p / (D / 8), p % (D / 8))) = rq[u];
-      *reinterpret_cast<ST_LDS u32x4*>(p0 + kTile + swz<D>(p / (D / 8), p % (D / 8))) = rd[u];
+      for (int e = 0; e < 4; ++e) sc[4 * j4 + e] = 0.f, dp[4 * j4 + e] = dlt[e];
     }
-    if (tid < 32) {
-      ST_LDS float* f = reinterpret_cast<ST_LDS float*>(p0 + 2 * kTile) + tid;
-      f[0] = st_lse;
-      f[32] = st_dlt;
-      f[64] = __int_as_float(st_lo);
-      f[96] = __int_as_float(st_hi);
-      f[128] = st_x;
-      f[160] = st_slope;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      sc = mfma32(reads.frag(qtile, 0, ks), kf[ks], sc);
+      dp = mfma32(reads.frag(dotile, 0, ks), reads.frag(v_rows, 0, ks), dp);
+    }
+#pragma unroll
+    for (int j4 = 0; j4 < 4; ++j4) {
+      const f32x4 lse2 = rows4(kRowLse, j4);
+      f32x4 x = {}, slope2 = {}, lo = {}, hi = {};
+      if (BIAS) x = rows4(kRowX, j4), slope2 = rows4(kRowSlope, j4);
+      if (GEN) lo = rows4(kRowLo, j4), hi = rows4(kRowHi, j4);
+#pragma unroll
+      for (int e4 = 0; e4 < 4; ++e4) {
+        const int v = 4 * j4 + e4;
+        float e, f = 1.f;
+        if (CAP) {
+          const float rr = cap_r(sc[v], k.c);
+          e = fmaf(-2.f * k.k1, rr, k.k1) - lse2[e4];
+          f = 4.f * rr * (1.f - rr);
+        } else {
+          e = fmaf(sc[v], k.c, -lse2[e4]);
+        }
+        if (BIAS) e = fmaf(-slope2[e4], fabsf(x[e4] - kx), e);
+        float p = __builtin_amdgcn_exp2f(e), ds = p * dp[v];
+        if (CAP) ds *= f;
+        if (GEN) {
+          const bool see = key >= __float_as_int(lo[e4]) && key < __float_as_int(hi[e4]);
+          p = see ? fmaf(0.f, ds, p) : 0.f;            // (a row whose dO is not finite: NaN, as the scrubbed dO no longer says it)
+          ds = see ? ds : 0.f;
+        }
+        sc[v] = p;
+        dp[v] = ds;
+      }
+    }
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      const bf16x8 pf = pack_c_as_b(sc, m), dsf = pack_c_as_b(dp, m);
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        const bf16x8 x = reads.frag_tr(dotile, 16 * m, db), y = reads.frag_tr(qtile, 16 * m, db);
+        acc_v[db] = mfma32(GEN ? scrub_bf16(x, bad) : x, pf, acc_v[db]);
+        acc_k[db] = mfma32(GEN ? scrub_bf16(y, bad) : y, dsf, acc_k[db]);
+      }
     }
   };
 
@@ -474,107 +569,49 @@ __global__ __launch_bounds__(256, 1) void score_dkv_kernel(const ScoreArgs a) {
   const int n_share = a.kv_split, share = blockIdx.y, mine = (n_blk - share + n_share - 1) / n_share;
   for (int at = 0; at < mine; at += kBlockList) {
     // ---- the visible ones among the next blocks, in order
-    int total = 0;
-    for (int c0 = 0; c0 < kBlockList; c0 += 256) {
+    int whole = 0, edge = 0;
+    for (int c0 = 0; c0 < kBlockList && at + c0 < mine; c0 += 256) {
       const int x = at + c0 + tid, j = share + x * n_share;
-      BlockSpan y{0x7fffffff, 0, 0, 0};
-      if (x < mine) y = block_span(j);
-      const bool seen = y.lo < key_end && y.hi > key0;
-      const uint64_t votes = __ballot(seen);
-      if (lane == 0) count[wave] = __popcll(votes);
+      int4 y = make_int4(0x7fffffff, 0, 0, 0);
+      if (x < mine) y = a.blocks[(int64_t)b * n_blk + j];
+      const bool seen = y.x < key_end && y.y > key0, all = seen && y.z <= key0 && y.w >= key_end && 32 * j + 32 <= M;
+      const uint64_t v_all = __ballot(all), v_edge = __ballot(seen && !all), before = ((uint64_t)1 << lane) - 1;
+      if (lane == 0) {
+        count[wave] = __popcll(v_all);
+        count[4 + wave] = __popcll(v_edge);
+      }
       __syncthreads();
-      int before = total;
-      for (int x2 = 0; x2 < wave; ++x2) before += count[x2];
-      if (seen) list[before + __popcll(votes & (((uint64_t)1 << lane) - 1))] =
-          make_int4(j, y.lo, y.hi, y.all_lo <= key0 && y.all_hi >= key_end && 32 * j + 32 <= M ? 1 : 0);
-      total += count[0] + count[1] + count[2] + count[3];
+      int p = whole, q = edge;
+      for (int x2 = 0; x2 < wave; ++x2) p += count[x2], q += count[4 + x2];
+      if (seen) list[all ? p + __popcll(v_all & before) : kBlockList - 1 - q - __popcll(v_edge & before)] = make_int4(j, y.x, y.y, 0);
+      whole += count[0] + count[1] + count[2] + count[3];
+      edge += count[4] + count[5] + count[6] + count[7];
       __syncthreads();
     }
-    total = uniform(total);
+    whole = uniform(whole);
+    edge = uniform(edge);
+    const int total = whole + edge;
     if (total == 0) continue;
-    load_block(list[0].x);
-    store_block(0);
+    auto entry = [&](int n) { return n < edge ? kBlockList - 1 - n : n - edge; };
+    load_block(list[entry(0)].x, 0);
     __syncthreads();
-    int buf = 0;
-    for (int n = 0; n < total; ++n) {
-      const int4 blk = list[n];
-      const bool more = n + 1 < total;
-      if (more) load_block(list[n + 1].x);
-      const int blk_lo = uniform(blk.y), blk_hi = uniform(blk.z);
-      const bool masked = !uniform(blk.w);
-      if (blk_lo < wkey_end && blk_hi > wkey0) {
-        const ST_LDS char* qtile = smem + buf * kStage;
-        const ST_LDS char* dotile = qtile + kTile;
-        const ST_LDS float* stats = reinterpret_cast<const ST_LDS float*>(qtile + 2 * kTile);
-        f32x16 sc, dp;
-#pragma unroll
-        for (int v = 0; v < 16; ++v) sc[v] = dp[v] = 0.f;
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          sc = mfma32(lds_frag<D>(qtile, 0, ks, lane), kf[ks], sc);
-          dp = mfma32(lds_frag<D>(dotile, 0, ks, lane), vf[ks], dp);
-        }
-        const float kx = (float)key;
-#pragma unroll
-        for (int j4 = 0; j4 < 4; ++j4) {
-          const int at4 = 8 * j4 + 4 * g;
-          const f32x4 lse2 = *reinterpret_cast<const ST_LDS f32x4*>(stats + at4);
-          const f32x4 dlt = *reinterpret_cast<const ST_LDS f32x4*>(stats + 32 + at4);
-          f32x4 x = {}, slope2 = {};
-          if (BIAS) {
-            x = *reinterpret_cast<const ST_LDS f32x4*>(stats + 128 + at4);
-            slope2 = *reinterpret_cast<const ST_LDS f32x4*>(stats + 160 + at4);
-          }
-#pragma unroll
-          for (int e4 = 0; e4 < 4; ++e4) {
-            const int v = 4 * j4 + e4;
-            float e, f = 1.f;
-            if (CAP) {
-              const float rr = cap_r(sc[v], k.c);
-              e = fmaf(-2.f * k.k1, rr, k.k1) - lse2[e4];
-              f = 4.f * rr * (1.f - rr);
-            } else {
-              e = fmaf(sc[v], k.c, -lse2[e4]);
-            }
-            if (BIAS) e = fmaf(-slope2[e4], fabsf(x[e4] - kx), e);
-            const float p = __builtin_amdgcn_exp2f(e);
-            float ds = p * (dp[v] - dlt[e4]);
-            if (CAP) ds *= f;
-            sc[v] = p;
-            dp[v] = ds;
-          }
-        }
-        auto contract = [&](auto scrub) {
-#pragma unroll
-          for (int m = 0; m < 2; ++m) {
-            const bf16x8 pf = pack_c_as_b(sc, m), dsf = pack_c_as_b(dp, m);
-#pragma unroll
-            for (int db = 0; db < DB; ++db) {
-              acc_v[db] = mfma32(scrub(lds_frag_tr<D>(dotile, 16 * m, 32 * db, lane)), pf, acc_v[db]);
-              acc_k[db] = mfma32(scrub(lds_frag_tr<D>(qtile, 16 * m, 32 * db, lane)), dsf, acc_k[db]);
-            }
-          }
-        };
-        if (masked) {
-#pragma unroll
-          for (int v = 0; v < 16; ++v) {
-            const int row = 8 * (v / 4) + 4 * g + v % 4;
-            const int lo = __float_as_int(stats[64 + row]), hi = __float_as_int(stats[96 + row]);
-            const bool see = key >= lo && key < hi;
-            sc[v] = see ? fmaf(0.f, dp[v], sc[v]) : 0.f;   // (a row whose dO is not finite: NaN, as the scrubbed dO no longer says it)
-            dp[v] = see ? dp[v] : 0.f;
-          }
-          contract([&](bf16x8 f) { return scrub_bf16(f, bad); });
-        } else {
-          contract([](bf16x8 f) { return f; });
-        }
-      }
-      if (more) store_block(buf ^ 1);
+    int buf = 0, n = 0;
+    for (; n < edge; ++n) {
+      if (n + 1 < total) load_block(list[entry(n + 1)].x, buf ^ 1);
+      const int4 y = list[entry(n)];
+      if (uniform(y.y) < wkey_end && uniform(y.z) > wkey0) block(std::true_type(), buf);
+      __syncthreads();
+      buf ^= 1;
+    }
+    for (; n < total; ++n) {
+      if (n + 1 < total) load_block(list[n + 1 - edge].x, buf ^ 1);
+      block(std::false_type(), buf);
       __syncthreads();
       buf ^= 1;
     }
   }
 
+  __syncthreads();                                     // (the direct loads have landed, also where no block was visible)
   if (key >= s.Sk) return;
   const int64_t n_kv = (int64_t)s.B * s.Sk * s.Hkv * D, orow = (((int64_t)b * s.Sk + key) * s.Hkv + hk) * D;
   const bool part = n_share > 1, add = !part && !a.assign;

@@ -62,7 +62,7 @@ def test_workspaces():
     m = api.st_score(0.0, None, PTR)
     assert lib.st_attn_score_workspace_bytes(C.byref(few), None, 0) > 0
     assert _fwd(few) == 5 and _fwd(few, ws=PTR, size=1000) == 5 and _fwd(few, ws=PTR + 128, size=1 << 30) == 3
-    assert _bwd(m=m) == 5                                                # the table of what rows see
+    assert _bwd(m=m) == 5                                                # the statistics of the rows
     assert lib.st_attn_score_workspace_bytes(C.byref(_desc(Sq=0)), None, 1) == 0
     assert lib.st_attn_score_workspace_bytes(C.byref(_desc(D=80)), None, 1) == 0
     # enough places for every tile: nothing is split
