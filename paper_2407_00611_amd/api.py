@@ -369,9 +369,11 @@ def st_attn_combine(o_parts, lse_parts, row0: int = 0, Sq_out: int = None, out_d
 
 
 def st_attn_delta(d_o, o, delta=None, stream=None) -> torch.Tensor:
+    B, Sq, Hq, D = d_o.shape
+    if delta is None and stream is None and d_o.is_cuda:
+        delta = torch.empty((B, Hq, Sq), dtype=torch.float32, device=d_o.device)
     if delta is not None and _done(_binding.delta(d_o, o, delta, _raw_stream(stream)), "st_attn_delta"):
         return delta
-    B, Sq, Hq, D = d_o.shape
     delta = torch.empty((B, Hq, Sq), dtype=torch.float32, device=d_o.device) if delta is None else \
         _f32_dense(delta, (B, Hq, Sq), "delta")
     d = st_block_desc(_dtype_code(d_o), B, Hq, Hq, D, Sq, 0, 0, 0, 0, 1.0)
@@ -642,6 +644,16 @@ def _on_device(stream, *tensors):
     return _AS_IT_IS if stream is None and device.index == torch._C._cuda_getDevice() else _switched(device, stream)
 
 
+def _short(call, stream, *args):
+    """The outputs of a native call that makes its own, on the current stream; None where it leaves the call to ctypes (which raises
+    the error of a call that failed, too)."""
+    if stream is not None or not torch.cuda.is_initialized():
+        return None
+    device = torch._C._cuda_getDevice()
+    done = call(*args, device, torch._C._cuda_getCurrentRawStream(device))
+    return done[1:] if done is not None and done[0] == 0 else None
+
+
 def _dense(t, shape, dtype, name):
     if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}")
@@ -675,6 +687,9 @@ def _score_workspace(d, m, backward: bool, workspace, device):
 def st_mask_spans(bounds, Sq: int, q_offset, causal: bool, prefix=None, spans=None, stream=None) -> torch.Tensor:
     """Spans [B, Sq, 2] of the rows of packed documents: bounds int64 [B, n_docs + 1] (rising positions at which the documents
     start, and the end of the last one), prefix int64 [B, n_docs] or None (first tokens that a whole document sees)."""
+    done = _short(_binding.mask_spans, stream, bounds, Sq, q_offset, causal, prefix, spans)
+    if done is not None:
+        return done[0]
     with _on_device(stream, bounds, prefix, spans):
         if bounds.dim() != 2 or bounds.shape[1] < 1:
             raise ValueError("bounds must be [B, n_docs + 1]")
@@ -700,6 +715,10 @@ def st_attn_score_fwd(q, k, v, q_offset, k_offset: int, causal: bool, scale: flo
                       o_part=None, lse_part=None, o_lowp=None, lowp: bool = False, workspace=None, stream=None):
     """(O, lse) of a query shard against one chunk.  O is the fp32 partial state, or with lowp=True alone O in the dtype of q; both
     are written where both o_part and o_lowp are given (the fp32 one is returned)."""
+    done = _short(_binding.score_fwd, stream, q, k, v, q_offset, k_offset, causal, scale, softcap, slopes, spans, o_part, lse_part, o_lowp,
+                  lowp, workspace)
+    if done is not None:
+        return done
     with _on_device(stream, q, k, v, slopes, spans, o_part, lse_part, o_lowp, workspace):
         d, m = _score_desc(q, k, v, q_offset, k_offset, causal, scale, softcap, slopes, spans)
         B, Sq, Hq, D = q.shape
@@ -726,6 +745,11 @@ def st_attn_score_bwd(q, k, v, d_o, lse_final, delta, q_offset, k_offset: int, c
     """Gradients of the pair.  With accumulators (all three, fp32) they are added to, or overwritten with assign=True, and the
     *_lowp given are their values in the dtype of q; without accumulators the gradients are written in the dtype of q, into the
     *_lowp given or new tensors.  Returns (dq, dk, dv): the accumulators, or those."""
+    if dq_lowp is None and dk_lowp is None and dv_lowp is None:
+        done = _short(_binding.score_bwd, stream, q, k, v, q_offset, k_offset, causal, scale, softcap, slopes, spans, d_o, lse_final, delta,
+                      dq_acc, dk_acc, dv_acc, assign, workspace)
+        if done is not None:
+            return done
     with _on_device(stream, q, k, v, d_o, lse_final, delta, slopes, spans, dq_acc, dk_acc, dv_acc, dq_lowp, dk_lowp, dv_lowp, workspace):
         d, m = _score_desc(q, k, v, q_offset, k_offset, causal, scale, softcap, slopes, spans)
         B, Sq, Hq, D = q.shape
@@ -751,11 +775,14 @@ def st_attn_score_bwd(q, k, v, d_o, lse_final, delta, q_offset, k_offset: int, c
     return tuple(low) if alone else tuple(acc)
 
 
+_PAIRS = {"halves": ST_ROPE_HALVES, "neighbours": ST_ROPE_NEIGHBOURS}
+
+
 def _rope_desc(q, k, freq, offset, positions, axes, pairs, norm, eps, q_weight, k_weight):
     B, S, Hq, D = q.shape
     if k is not None and (k.dim() != 4 or k.shape[:2] != q.shape[:2] or k.shape[3] != D or k.dtype != q.dtype):
         raise ValueError("expected q [B,S,Hq,D] and k [B,S,Hkv,D] of one dtype")
-    if pairs not in ("halves", "neighbours"):
+    if pairs not in _PAIRS:
         raise ValueError(f"pairs must be 'halves' or 'neighbours', not {pairs!r}")
     n = freq.numel()
     _dense(freq, (n,), torch.float64, "freq")
@@ -769,7 +796,7 @@ def _rope_desc(q, k, freq, offset, positions, axes, pairs, norm, eps, q_weight, 
             _dense(w, (D,), torch.float32, name)
     off, seg, off2 = _q_runs(offset)
     return st_rope_desc(_dtype_code(q), B, S, Hq, k.shape[2] if k is not None else 0, D, 2 * n,
-                        ST_ROPE_NEIGHBOURS if pairs == "neighbours" else ST_ROPE_HALVES, 1 if norm else 0, float(eps), len(axes),
+                        _PAIRS[pairs], 1 if norm else 0, float(eps), len(axes),
                         (C.c_int32 * ST_ROPE_MAX_AXES)(*axes), off, seg, off2)
 
 
@@ -789,6 +816,9 @@ def st_qk_rope_fwd(q, k, freq, offset=0, positions=None, axes=None, pairs: str =
     the rotation of its first 2 len(freq) values: freq fp64 radians per position.  Positions are those of a shard's rows (offset: the
     first one's, or (offset, rows of the first run, offset of the second)), or `positions` int32 [axes,B,S] with `axes` the numbers
     of pairs that each axis turns.  Returns (q_out, k_out), new tensors unless given; they may be q and k."""
+    done = _short(_binding.rope_fwd, stream, q, k, freq, offset, positions, axes, _PAIRS.get(pairs), norm, eps, q_weight, k_weight, q_out, k_out)
+    if done is not None:
+        return done
     with _on_device(stream, q, k, freq, positions, q_weight, k_weight, q_out, k_out):
         d = _rope_desc(q, k, freq, offset, positions, axes, pairs, norm, eps, q_weight, k_weight)
         q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else _like(q_out, q, "q_out")
@@ -805,6 +835,11 @@ def st_qk_rope_bwd(q, k, d_q, d_k, freq, offset=0, positions=None, axes=None, pa
                    workspace=None, stream=None):
     """Gradients of st_qk_rope_fwd: d_q, d_k those of its outputs, fp32 or in the dtype of q.  Returns (dx_q, dx_k, dw_q, dw_k); the
     weights' (None without weights) are added to the dw_q, dw_k given, or overwrite them with assign=True."""
+    if dw_q is None and dw_k is None:
+        done = _short(_binding.rope_bwd, stream, q, k, freq, offset, positions, axes, _PAIRS.get(pairs), norm, eps, q_weight, k_weight, d_q, d_k,
+                      dx_q, dx_k, workspace)
+        if done is not None:
+            return done
     with _on_device(stream, q, k, d_q, d_k, freq, positions, q_weight, k_weight, dx_q, dx_k, dw_q, dw_k, workspace):
         d = _rope_desc(q, k, freq, offset, positions, axes, pairs, norm, eps, q_weight, k_weight)
         if d_q.shape != q.shape or (k is not None and (d_k.shape != k.shape or d_k.dtype != d_q.dtype)):

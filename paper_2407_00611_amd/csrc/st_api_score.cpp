@@ -46,9 +46,11 @@ st::ScoreArgs score_args(const st_block_desc* d, const st_score* m) {
   return a;
 }
 
-// How the launches are split and where in the workspace their sums lie (byte offsets).  Places of the chip: two workgroups on each
-// of 256 compute units.
+// How the launches are split and where in the workspace their sums lie (byte offsets).
 constexpr int64_t kSplitBytesMost = (int64_t)256 << 20;
+// A share is at least so many products (16 blocks of 32 rows): 12/4 heads x 2 x 1000 rows 44 + 10 us so, 55 + 8 with twice as many, 128
+// without shares.
+constexpr int64_t kLeastShare = 64;
 struct ScorePlan {
   int n_split, q_split, kv_split;
   size_t lse, dk, dv, blocks, rows, bytes;
@@ -56,10 +58,13 @@ struct ScorePlan {
 ScorePlan fwd_plan(const st::Shape& s, int dtype) {
   const int G = s.Hq / s.Hkv;
   const bool bf16 = dtype == ST_BF16;
-  const int64_t jobs = bf16 ? ((int64_t)s.Sq * G + st::kScoreRows - 1) / st::kScoreRows * s.Hkv * s.B : ((int64_t)s.Sq + 31) / 32 * s.Hq * s.B;
+  const int64_t tiles = bf16 ? ((int64_t)s.Sq * G + st::kScoreRows - 1) / st::kScoreRows : ((int64_t)s.Sq + 31) / 32;
   const int64_t n_o = (int64_t)s.B * s.Sq * s.Hq * s.D * 4, n_l = (int64_t)s.B * s.Sq * s.Hq * 4;
   ScorePlan p{};
-  p.n_split = st::score_split(jobs, 512, bf16 ? ((int64_t)s.Sk + 63) / 64 : ((int64_t)s.Sk + 255) / 256, bf16 ? 4 : 1, st::kMaxTable);
+  // One row tile of a token or a few is a stream of keys from memory, which two workgroups on each of 256 compute units keep
+  // busy; more rows are work enough for one.
+  p.n_split = st::score_split(tiles * (bf16 ? s.Hkv : s.Hq) * s.B, tiles == 1 ? 512 : 256, bf16 ? ((int64_t)s.Sk + 63) / 64 : ((int64_t)s.Sk + 255) / 256, bf16 ? 4 : 1,
+                              st::kMaxTable);
   while (p.n_split > 1 && p.n_split * n_o > kSplitBytesMost) --p.n_split;
   if (p.n_split > 1) {
     p.lse = align_up((size_t)(p.n_split * n_o), 256);
@@ -67,16 +72,22 @@ ScorePlan fwd_plan(const st::Shape& s, int dtype) {
   }
   return p;
 }
+// Key tiles and query tiles share a launch.  A share of one is at most what a place of the chip has to do on the average, where a
+// tile is longer; the work is counted in products of 32 x 32 x D, four of a key tile's 32 rows for each 32 keys and three of a query
+// tile's.
 ScorePlan bwd_plan(const st::Shape& s, int dtype) {
   const int G = s.Hq / s.Hkv;
   const bool bf16 = dtype == ST_BF16;
+  const int64_t row_blocks = bf16 ? ((int64_t)s.Sq * G + 31) / 32 : ((int64_t)s.Sq + 31) / 32 * G, key_blocks = ((int64_t)s.Sk + 31) / 32;
   const int64_t rows = bf16 ? ((int64_t)s.Sq * G + st::kScoreRows - 1) / st::kScoreRows * s.Hkv * s.B : ((int64_t)s.Sq + 31) / 32 * s.Hq * s.B;
-  const int64_t keys = bf16 ? ((int64_t)s.Sk + st::kScoreKeys - 1) / st::kScoreKeys * s.Hkv * s.B : ((int64_t)s.Sk + 31) / 32 * s.Hkv * s.B;
+  const int64_t keys = bf16 ? ((int64_t)s.Sk + st::kScoreKeys - 1) / st::kScoreKeys * s.Hkv * s.B : key_blocks * s.Hkv * s.B;
   const int64_t n_q = (int64_t)s.B * s.Sq * s.Hq * s.D * 4, n_kv = (int64_t)s.B * s.Sk * s.Hkv * s.D * 4;
+  const int64_t kv_len = 4 * row_blocks, q_len = 3 * key_blocks;
+  const int64_t each = std::max<int64_t>((keys * kv_len + rows * q_len) / 512, bf16 ? kLeastShare : 8);
   ScorePlan p{};
-  p.q_split = st::score_split(rows, 512, bf16 ? ((int64_t)s.Sk + 63) / 64 : ((int64_t)s.Sk + 255) / 256, bf16 ? 4 : 1, 16);
+  p.q_split = (int)std::min<int64_t>(std::max<int64_t>((2 * q_len + each) / (2 * each), 1), 16);
   while (p.q_split > 1 && p.q_split * n_q > kSplitBytesMost) --p.q_split;
-  p.kv_split = st::score_split(keys, 512, ((int64_t)s.Sq * G + 31) / 32, 8, 16);
+  p.kv_split = (int)std::min<int64_t>(std::max<int64_t>((2 * kv_len + each) / (2 * each), 1), 16);
   while (p.kv_split > 1 && p.kv_split * n_kv * 2 > kSplitBytesMost) --p.kv_split;
   p.dk = p.q_split > 1 ? align_up((size_t)(p.q_split * n_q), 256) : 0;
   const size_t kv = p.kv_split > 1 ? align_up((size_t)(p.kv_split * n_kv), 256) : 0;
@@ -198,6 +209,10 @@ st_status st_attn_score_fwd(const st_block_desc* d, const st_score* m, const st_
   a.part_lse = (float*)((char*)workspace + p.lse);
   ST_HIP(d->dtype == ST_BF16 ? st::launch_score_fwd_bf16(a, (hipStream_t)hip_stream) : st::launch_score_fwd_f32(a, (hipStream_t)hip_stream), "st_attn_score_fwd launch");
   if (a.n_split <= 1) return ST_OK;
+  if (a.n_split > 16) {
+    ST_HIP(st::launch_score_combine(a, d->dtype == ST_BF16, (hipStream_t)hip_stream), "st_attn_score_fwd combine");
+    return ST_OK;
+  }
   st::CombineArgs c;
   memset(&c, 0, sizeof(c));
   c.n = a.n_split;

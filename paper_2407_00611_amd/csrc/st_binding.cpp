@@ -6,6 +6,7 @@
 // Every function returns the status of the call, or None without having called anything when an argument is not what the
 // short way takes (another sequence type, a tensor subclass, a shape or dtype that does not fit ...): the Python wrapper
 // then goes the general way, which accepts what is acceptable and raises the error that belongs to the rest.
+#include <ATen/ops/empty.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "../../include/startrail.h"
@@ -383,9 +384,241 @@ PyObject* cast(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return call([&] { return st_cast_from_f32(from, to, count, out, stream); });
 }
 
+// ---- the calls that make their own outputs: (status, outputs...) or None.  Tensors have to be on the current device, which the
+// caller says, as the outputs and the workspace are made on it.
+struct Made {
+  at::Tensor t[4];
+  at::TensorOptions on;
+  float* f32(int i, at::IntArrayRef s) { return (float*)made(i, s, at::kFloat); }
+  void* made(int i, at::IntArrayRef s, at::ScalarType type) {
+    t[i] = at::empty(s, on.dtype(type));
+    return address(&t[i]);
+  }
+};
+bool here(Tensor t, int64_t device) { return t->get_device() == device; }
+bool dense_of(PyObject* o, at::IntArrayRef shape, at::ScalarType type, int64_t device, void** p) {
+  Tensor t;
+  if (!tensor(o, &t) || t->scalar_type() != type || t->sizes() != shape || !t->is_contiguous() || !here(t, device)) return false;
+  *p = address(t);
+  return true;
+}
+bool dense_or_none(PyObject* o, at::IntArrayRef shape, at::ScalarType type, int64_t device, void** p) {
+  *p = nullptr;
+  return o == Py_None || dense_of(o, shape, type, device, p);
+}
+// a workspace that the caller gives, or one of `need` bytes
+bool workspace_of(PyObject* o, size_t need, int64_t device, Made* m, int slot, void** p, size_t* n) {
+  *p = nullptr;
+  *n = 0;
+  if (o != Py_None) {
+    Tensor t;
+    return tensor(o, &t) && here(t, device) && bytes_of(o, p, n);
+  }
+  if (need == 0) return true;
+  *p = m->made(slot, {(int64_t)need}, at::kByte);    // (the allocator's blocks lie on 512-byte boundaries)
+  *n = need;
+  return (uintptr_t)*p % 256 == 0;
+}
+PyObject* answer(PyObject* status, std::initializer_list<PyObject*> out) {
+  if (status == nullptr) return nullptr;
+  PyObject* all = PyTuple_New(1 + (Py_ssize_t)out.size());
+  if (all == nullptr) return nullptr;
+  PyTuple_SET_ITEM(all, 0, status);
+  Py_ssize_t i = 1;
+  for (PyObject* x : out) PyTuple_SET_ITEM(all, i++, x);
+  return all;
+}
+PyObject* given_or(PyObject* o, const at::Tensor& t) {
+  if (!t.defined()) {
+    Py_INCREF(o);
+    return o;
+  }
+  return THPVariable_Wrap(t);
+}
+
+// mask_spans(bounds, rows, where, causal, prefix, spans, device, stream)
+PyObject* mask_spans(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  ST_SHORT(n == 8);
+  Tensor b;
+  st_block_desc d;
+  int64_t device;
+  int32_t causal;
+  void *prefix, *spans, *stream;
+  ST_SHORT(tensor(a[0], &b) && b->dim() == 2 && b->size(1) >= 1 && b->scalar_type() == at::kLong && b->is_contiguous() && integer(a[6], &device) && here(b, device));
+  ST_SHORT(b->size(0) <= INT32_MAX && b->size(1) <= INT32_MAX && integer(a[1], &d.Sq) && d.Sq >= 0 && where(a[2], &d) && truth(a[3], &causal));
+  const int64_t B = b->size(0), docs = b->size(1) - 1;
+  ST_SHORT(dense_or_none(a[4], {B, docs}, at::kLong, device, &prefix) && dense_or_none(a[5], {B, d.Sq, 2}, at::kLong, device, &spans) && handle(a[7], &stream));
+  Made m;
+  m.on = b->options();
+  if (a[5] == Py_None) spans = m.made(0, {B, d.Sq, 2}, at::kLong);
+  const int64_t* bounds = (const int64_t*)address(b);
+  PyObject* s = call([&] {
+    return st_mask_spans((int32_t)B, d.Sq, d.q_offset, d.q_seg, d.q_offset2, causal, bounds, (int32_t)docs, (const int64_t*)prefix, (int64_t*)spans, stream);
+  });
+  return answer(s, {given_or(a[5], m.t[0])});
+}
+
+// q, k, v, where, k_offset, causal, scale at a[0 .. 6]; softcap, slopes, spans at a[at]
+bool scored(PyObject* const* a, PyObject* const* mods, int64_t device, st_block_desc* d, st_score* m, Tensor* q, Tensor* k, st_tensor* tq, st_tensor* tk, st_tensor* tv) {
+  Tensor v;
+  if (!block(a[0], a[1], a[2], a[3], a[4], a[5], a[6], d, q, k, tq, tk, tv) || !tensor(a[2], &v)) return false;
+  if (v->sizes() != (*k)->sizes() || (*k)->size(0) != d->B || (*k)->size(3) != d->D || (*k)->scalar_type() != (*q)->scalar_type() || v->scalar_type() != (*q)->scalar_type()) return false;
+  if (!here(*q, device) || !here(*k, device) || !here(v, device) || !real(mods[0], &m->softcap)) return false;
+  return dense_or_none(mods[1], {d->Hq}, at::kFloat, device, (void**)&m->slopes) && dense_or_none(mods[2], {d->B, d->Sq, 2}, at::kLong, device, (void**)&m->spans);
+}
+
+// score_fwd(q, k, v, where, k_offset, causal, scale, softcap, slopes, spans, o, lse, o_low, lowp, workspace, device, stream): O (the
+// fp32 one where it is written) and lse
+PyObject* score_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  ST_SHORT(n == 17);
+  st_block_desc d;
+  st_score m;
+  Tensor q, k;
+  st_tensor tq, tk, tv;
+  int64_t device;
+  int32_t lowp;
+  void *o, *lse, *low, *ws, *stream;
+  size_t ws_bytes;
+  ST_SHORT(integer(a[15], &device) && scored(a, a + 7, device, &d, &m, &q, &k, &tq, &tk, &tv) && truth(a[13], &lowp) && handle(a[16], &stream));
+  ST_SHORT(dense_or_none(a[10], q->sizes(), at::kFloat, device, &o) && dense_or_none(a[11], {d.B, d.Hq, d.Sq}, at::kFloat, device, &lse) &&
+           dense_or_none(a[12], q->sizes(), q->scalar_type(), device, &low));
+  Made x;
+  x.on = q->options();
+  const bool want_low = a[12] == Py_None && lowp, want_o = a[10] == Py_None && a[12] == Py_None && !lowp;
+  ST_SHORT(workspace_of(a[14], st_attn_score_workspace_bytes(&d, &m, 0), device, &x, 2, &ws, &ws_bytes));
+  if (want_low) low = x.made(0, q->sizes(), q->scalar_type());
+  if (want_o) o = x.f32(0, q->sizes());
+  if (a[11] == Py_None) lse = x.f32(1, {d.B, d.Hq, d.Sq});
+  PyObject* s = call([&] { return st_attn_score_fwd(&d, &m, &tq, &tk, &tv, (float*)o, (float*)lse, low, ws, ws_bytes, stream); });
+  PyObject* first = a[10] != Py_None ? given_or(a[10], at::Tensor()) : given_or(a[12], x.t[0]);
+  return answer(s, {first, given_or(a[11], x.t[1])});
+}
+
+// score_bwd(q, k, v, where, k_offset, causal, scale, softcap, slopes, spans, d_o, lse, delta, dq, dk, dv, assign, workspace, device, stream):
+// the fp32 accumulators, or, where they are None, new gradients in the dtype of q
+PyObject* score_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  ST_SHORT(n == 20);
+  st_block_desc d;
+  st_score m;
+  Tensor q, k, t_do;
+  st_tensor tq, tk, tv, tdo;
+  int64_t device;
+  int32_t assign;
+  void *lse, *delta, *acc[3], *low[3] = {nullptr, nullptr, nullptr}, *ws, *stream;
+  size_t ws_bytes;
+  ST_SHORT(integer(a[18], &device) && scored(a, a + 7, device, &d, &m, &q, &k, &tq, &tk, &tv) && truth(a[16], &assign) && handle(a[19], &stream));
+  ST_SHORT(view(a[10], &t_do, &tdo) && here(t_do, device) && t_do->sizes() == q->sizes() && t_do->scalar_type() == q->scalar_type() &&
+           dense_of(a[11], {d.B, d.Hq, d.Sq}, at::kFloat, device, &lse) && dense_of(a[12], {d.B, d.Hq, d.Sq}, at::kFloat, device, &delta));
+  const bool alone = a[13] == Py_None;
+  ST_SHORT((a[14] == Py_None) == alone && (a[15] == Py_None) == alone);
+  for (int i = 0; i < 3; ++i) ST_SHORT(dense_or_none(a[13 + i], i ? k->sizes() : q->sizes(), at::kFloat, device, &acc[i]));
+  Made x;
+  x.on = q->options();
+  ST_SHORT(workspace_of(a[17], st_attn_score_workspace_bytes(&d, &m, 1), device, &x, 3, &ws, &ws_bytes));
+  if (alone)
+    for (int i = 0; i < 3; ++i) low[i] = x.made(i, i ? k->sizes() : q->sizes(), q->scalar_type());
+  PyObject* s = call([&] {
+    return st_attn_score_bwd(&d, &m, &tq, &tk, &tv, &tdo, (float*)lse, (float*)delta, assign || alone ? ST_GRAD_ASSIGN : 0, (float*)acc[0], (float*)acc[1],
+                             (float*)acc[2], low[0], low[1], low[2], ws, ws_bytes, stream);
+  });
+  return answer(s, {given_or(a[13], x.t[0]), given_or(a[14], x.t[1]), given_or(a[15], x.t[2])});
+}
+
+// q, k, freq, where, positions, axes, pairing, norm, eps, q_weight, k_weight at a[0 .. 10]
+struct Rope {
+  st_rope_desc d;
+  Tensor q, k = nullptr;
+  st_tensor tq, tk = {nullptr, 0, 0, 0};
+  void *freq, *positions, *qw, *kw;
+  bool read(PyObject* const* a, int64_t device) {
+    Tensor f;
+    st_block_desc at_rows;
+    if (!view(a[0], &q, &tq) || !here(q, device) || !dtype_code(q, &d.dtype) || !tensor(a[2], &f)) return false;
+    for (int i = 0; i < 4; ++i)
+      if (q->size(i) > INT32_MAX) return false;
+    d.B = (int32_t)q->size(0); d.S = (int32_t)q->size(1); d.Hq = (int32_t)q->size(2); d.D = (int32_t)q->size(3);
+    d.Hkv = 0;
+    if (a[1] != Py_None) {
+      if (!view(a[1], &k, &tk) || !here(k, device) || k->scalar_type() != q->scalar_type() || k->size(0) != d.B || k->size(1) != d.S || k->size(3) != d.D ||
+          k->size(2) > INT32_MAX)
+        return false;
+      d.Hkv = (int32_t)k->size(2);
+    }
+    const int64_t half = f->numel();
+    if (half > 1 << 20 || !dense_of(a[2], {half}, at::kDouble, device, &freq) || !where(a[3], &at_rows)) return false;
+    d.rot = (int32_t)(2 * half);
+    d.offset = at_rows.q_offset; d.seg = at_rows.q_seg; d.offset2 = at_rows.q_offset2;
+    Py_ssize_t n = 1;
+    int64_t sum = 0;
+    memset(d.axis_pairs, 0, sizeof(d.axis_pairs));
+    d.axis_pairs[0] = (int32_t)half;
+    if (a[5] != Py_None && !integers(a[5], d.axis_pairs, ST_ROPE_MAX_AXES, &n)) return false;
+    for (Py_ssize_t i = 0; i < n; ++i) sum += d.axis_pairs[i];
+    if (n < 1 || sum != half) return false;
+    d.n_axes = (int32_t)n;
+    return dense_or_none(a[4], {(int64_t)n, d.B, d.S}, at::kInt, device, &positions) && integer(a[6], &d.pairing) && truth(a[7], &d.norm) && real(a[8], &d.eps) &&
+           dense_or_none(a[9], {d.D}, at::kFloat, device, &qw) && dense_or_none(a[10], {d.D}, at::kFloat, device, &kw);
+  }
+  // an output like `t`: the one given (None: a new one)
+  bool out(PyObject* o, Tensor t, int64_t device, Made* m, int slot, st_tensor* v) {
+    if (o == Py_None) {
+      m->made(slot, t->sizes(), t->scalar_type());
+      *v = st_tensor{address(&m->t[slot]), m->t[slot].stride(0), m->t[slot].stride(1), m->t[slot].stride(2)};
+      return true;
+    }
+    Tensor x;
+    return view(o, &x, v) && here(x, device) && x->sizes() == t->sizes() && x->scalar_type() == t->scalar_type();
+  }
+};
+
+// rope_fwd(..., q_out, k_out, device, stream)
+PyObject* rope_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  ST_SHORT(n == 15);
+  Rope r;
+  Made m;
+  st_tensor oq, ok = {nullptr, 0, 0, 0};
+  int64_t device;
+  void* stream;
+  ST_SHORT(integer(a[13], &device) && handle(a[14], &stream) && r.read(a, device));
+  m.on = r.q->options();
+  ST_SHORT(r.out(a[11], r.q, device, &m, 0, &oq) && (r.k == nullptr ? a[12] == Py_None : r.out(a[12], r.k, device, &m, 1, &ok)));
+  PyObject* s = call([&] {
+    return st_qk_rope_fwd(&r.d, &r.tq, &r.tk, (const float*)r.qw, (const float*)r.kw, (const double*)r.freq, (const int32_t*)r.positions, &oq, &ok, stream);
+  });
+  return answer(s, {given_or(a[11], m.t[0]), given_or(a[12], m.t[1])});
+}
+
+// rope_bwd(..., d_q, d_k, dx_q, dx_k, workspace, device, stream): gradients of the weights in new tensors where there are weights
+PyObject* rope_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  ST_SHORT(n == 18);
+  Rope r;
+  Made m, w;
+  Tensor gq, gk = nullptr;
+  st_tensor tgq, tgk = {nullptr, 0, 0, 0}, oq, ok = {nullptr, 0, 0, 0};
+  int64_t device;
+  int32_t d_dtype;
+  void *ws = nullptr, *stream;
+  size_t ws_bytes = 0;
+  ST_SHORT(integer(a[16], &device) && handle(a[17], &stream) && r.read(a, device));
+  ST_SHORT(view(a[11], &gq, &tgq) && here(gq, device) && gq->sizes() == r.q->sizes() && dtype_code(gq, &d_dtype));
+  if (r.k != nullptr) ST_SHORT(view(a[12], &gk, &tgk) && here(gk, device) && gk->sizes() == r.k->sizes() && gk->scalar_type() == gq->scalar_type());
+  m.on = w.on = r.q->options();
+  ST_SHORT(r.out(a[13], r.q, device, &m, 0, &oq) && (r.k == nullptr ? a[14] == Py_None : r.out(a[14], r.k, device, &m, 1, &ok)));
+  float *dwq = nullptr, *dwk = nullptr;
+  if (r.qw) dwq = w.f32(0, {r.d.D});
+  if (r.kw && r.k != nullptr) dwk = w.f32(1, {r.d.D});
+  if (dwq || dwk) ST_SHORT(workspace_of(a[15], st_qk_rope_bwd_workspace_bytes(&r.d), device, &w, 2, &ws, &ws_bytes));
+  PyObject* s = call([&] {
+    return st_qk_rope_bwd(&r.d, &r.tq, &r.tk, &tgq, &tgk, d_dtype, (const float*)r.qw, (const float*)r.kw, (const double*)r.freq, (const int32_t*)r.positions,
+                          ST_GRAD_ASSIGN, &oq, &ok, dwq, dwk, ws, ws_bytes, stream);
+  });
+  return answer(s, {given_or(a[13], m.t[0]), given_or(a[14], m.t[1]), given_or(Py_None, w.t[0]), given_or(Py_None, w.t[1])});
+}
+
 #define ST_METHOD(f) {#f, (PyCFunction)(void*)guarded<f>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ST_METHOD(ring_fwd), ST_METHOD(ring_bwd), ST_METHOD(block_fwd), ST_METHOD(block_bwd), ST_METHOD(merge),
-                         ST_METHOD(combine),  ST_METHOD(delta),    ST_METHOD(cast),      {nullptr, nullptr, 0, nullptr}};
+                         ST_METHOD(combine),  ST_METHOD(delta),    ST_METHOD(cast),
+                         ST_METHOD(mask_spans), ST_METHOD(score_fwd), ST_METHOD(score_bwd), ST_METHOD(rope_fwd), ST_METHOD(rope_bwd), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -370,13 +370,19 @@ __global__ __launch_bounds__(kThreads) void rope_bwd_kernel(const RopeArgs g, in
   }
 }
 
-// dw += (or =) the workgroups' sums in their order: 16 columns a workgroup, sixteenths of the sums side by side
-__global__ __launch_bounds__(256) void rope_dw_kernel(const float* __restrict__ parts, int32_t n, int32_t D, float* dwq, float* dwk, int32_t assign) {
-  __shared__ float fold[16][17];
+// dw += (or =) the workgroups' sums in their order: 16 columns a workgroup, sixty-four runs of the sums side by side, four loads
+// of each in flight
+__global__ __launch_bounds__(1024) void rope_dw_kernel(const float* __restrict__ parts, int32_t n, int32_t D, float* dwq, float* dwk, int32_t assign) {
+  __shared__ float fold[64][17];
   const int c = blockIdx.x * 16 + (threadIdx.x & 15), y = threadIdx.x >> 4;
   float sum = 0.f;
   if (c < 2 * D)
-    for (int k = y; k < n; k += 16) sum += parts[(int64_t)k * 2 * D + c];
+    for (int k = y; k < n; k += 256) {
+      float x[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) x[u] = k + 64 * u < n ? parts[(int64_t)(k + 64 * u) * 2 * D + c] : 0.f;
+      sum += (x[0] + x[1]) + (x[2] + x[3]);
+    }
   fold[y][threadIdx.x & 15] = sum;
   __syncthreads();
   if (y != 0 || c >= 2 * D) return;
@@ -384,7 +390,7 @@ __global__ __launch_bounds__(256) void rope_dw_kernel(const float* __restrict__ 
   if (!out) return;
   out += c < D ? c : c - D;
   float all = assign ? 0.f : *out;
-  for (int k = 0; k < 16; ++k) all += fold[k][threadIdx.x & 15];
+  for (int k = 0; k < 64; ++k) all += fold[k][threadIdx.x & 15];
   *out = all;
 }
 
@@ -464,7 +470,7 @@ hipError_t launch_rope_bwd(const RopeArgs& g, bool bf16, bool d_bf16, float* dwq
   }
   if (!dwq && !dwk) return hipSuccess;
   ProfScope prof("qk_rope_dw", stream);
-  hipLaunchKernelGGL(rope_dw_kernel, dim3((unsigned)((2 * g.D + 15) / 16)), dim3(256), 0, stream, g.dw_parts, tokens > 0 ? rope_dw_blocks(tokens) : 0, g.D, dwq, dwk, assign ? 1 : 0);
+  hipLaunchKernelGGL(rope_dw_kernel, dim3((unsigned)((2 * g.D + 15) / 16)), dim3(1024), 0, stream, g.dw_parts, tokens > 0 ? rope_dw_blocks(tokens) : 0, g.D, dwq, dwk, assign ? 1 : 0);
   return hipGetLastError();
 }
 

@@ -57,6 +57,7 @@ constexpr float kScoreLn2 = 0.6931471805599453f;
 hipError_t launch_mask_spans(const Shape& s, const int64_t* bounds, int32_t n_docs, const int64_t* prefix, int64_t* spans, hipStream_t stream);
 hipError_t launch_score_fwd_bf16(const ScoreArgs& a, hipStream_t stream);
 hipError_t launch_score_fwd_f32(const ScoreArgs& a, hipStream_t stream);
+hipError_t launch_score_combine(const ScoreArgs& a, int bf16, hipStream_t stream);
 hipError_t launch_score_rows(const ScoreArgs& a, hipStream_t stream);
 hipError_t launch_score_bwd_bf16(const ScoreArgs& a, hipStream_t stream);
 hipError_t launch_score_bwd_f32(const ScoreArgs& a, hipStream_t stream);

@@ -56,6 +56,47 @@ __global__ __launch_bounds__(256) void score_rows_kernel(const ScoreArgs a, int3
   f[32 * kRowSlope] = slope * kScoreLog2e;
 }
 
+// Many partial states of few rows (a split walk of a token or a few): a workgroup per row, eight states side by side, where the
+// general combine has a thread go through all of them (64 states of 32 rows of 128: 55 us).  Weights as there: an empty state is 0
+// whatever its O holds, a row that is empty in all of them stays empty.
+__global__ __launch_bounds__(256) void score_combine_kernel(const float* __restrict__ o, const float* __restrict__ lse, int32_t n, int32_t Sq, int32_t Hq, int32_t D,
+                                                            int64_t n_rows, float* o_out, float* __restrict__ lse_out, void* low, int32_t bf16) {
+  __shared__ float w[kMaxTable];
+  __shared__ float4 fold[256];
+  const int64_t row = blockIdx.x;                      // (b Sq + i) Hq + h
+  const int64_t bi = row / Hq, h = row - bi * Hq, b = bi / Sq, i = bi - b * Sq, stat = (b * Hq + h) * Sq + i;
+  const int tid = threadIdx.x, vecs = D / 4, lanes = 256 / vecs;
+  if (tid < 64) {
+    const float l = tid < n ? lse[tid * n_rows + stat] : -INFINITY;
+    float m = l;
+    for (int d = 1; d < 64; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
+    const float e = m == -INFINITY ? 0.f : expf(l - m);
+    float sum = e;
+    for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+    w[tid] = m == -INFINITY ? 0.f : e / sum;
+    if (tid == 0) lse_out[stat] = m == -INFINITY ? -INFINITY : m + logf(sum);
+  }
+  __syncthreads();
+  const int x = tid % vecs, y = tid / vecs;
+  float4 r = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (y < lanes)
+    for (int k = y; k < n; k += lanes) {
+      const float4 p = *reinterpret_cast<const float4*>(o + (k * n_rows + row) * D + 4 * x);
+      const float c = w[k];
+      if (c != 0.f) r = make_float4(fmaf(c, p.x, r.x), fmaf(c, p.y, r.y), fmaf(c, p.z, r.z), fmaf(c, p.w, r.w));
+    }
+  fold[tid] = r;
+  __syncthreads();
+  if (y != 0) return;
+  for (int k = 1; k < lanes; ++k) {
+    const float4 p = fold[k * vecs + x];
+    r.x += p.x; r.y += p.y; r.z += p.z; r.w += p.w;
+  }
+  if (o_out) *reinterpret_cast<float4*>(o_out + row * D + 4 * x) = r;
+  if (low && bf16) *reinterpret_cast<uint2*>((uint16_t*)low + row * D + 4 * x) = make_uint2(pack_bf16(r.x, r.y), pack_bf16(r.z, r.w));
+  else if (low) *reinterpret_cast<float4*>((float*)low + row * D + 4 * x) = r;
+}
+
 struct PartSum {
   const float* part;         // n sums of `floats` floats, one behind the other; null: nothing to add up
   float* out;                // nullable; added to unless assign
@@ -102,6 +143,14 @@ hipError_t launch_mask_spans(const Shape& s, const int64_t* bounds, int32_t n_do
   if ((n + 255) / 256 > kScoreGridMost) return hipErrorInvalidValue;
   ProfScope prof("mask_spans", stream);
   hipLaunchKernelGGL(mask_spans_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, stream, s, bounds, n_docs, prefix, spans);
+  return hipGetLastError();
+}
+
+hipError_t launch_score_combine(const ScoreArgs& a, int bf16, hipStream_t stream) {
+  const int64_t rows = (int64_t)a.s.B * a.s.Sq * a.s.Hq;
+  if (rows > kScoreGridMost || a.n_split > kMaxTable) return hipErrorInvalidValue;
+  ProfScope prof("score_combine", stream);
+  hipLaunchKernelGGL(score_combine_kernel, dim3((unsigned)rows), dim3(256), 0, stream, a.part_o, a.part_lse, a.n_split, a.s.Sq, a.s.Hq, a.s.D, rows, a.o, a.lse, a.o_lowp, bf16);
   return hipGetLastError();
 }
 

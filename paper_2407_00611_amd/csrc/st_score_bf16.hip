@@ -66,9 +66,9 @@ __device__ __forceinline__ Walk walk_of(const BlockSpan& w, bool bias, int x_lo,
 
 // Block id -> (row tile, KV head, batch entry).  Every XCD has a contiguous range of the (KV head, batch entry) pairs, whose keys and
 // values stay in its L2; under a causal mask the later tiles, which see more, come first (spans mostly are such masks too).
-__device__ __forceinline__ void tile_block(const ScoreArgs& a, int n_qt, int& qt, int& hk, int& b) {
+__device__ __forceinline__ void tile_block(const ScoreArgs& a, int block, int blocks, int n_qt, int& qt, int& hk, int& b) {
   int hb;
-  qtile_block(blockIdx.x, gridDim.x, n_qt, a.s.causal || a.spans, qt, hb);
+  qtile_block(block, blocks, n_qt, a.s.causal || a.spans, qt, hb);
   hk = uniform(hb % a.s.Hkv);
   b = uniform(hb / a.s.Hkv);
   qt = uniform(qt);
@@ -122,7 +122,7 @@ __global__ __launch_bounds__(256, 2) void score_fwd_kernel(const ScoreArgs a) {
   const int G = s.Hq / s.Hkv, M = s.Sq * G;
   const int n_qt = (M + kScoreRows - 1) / kScoreRows;
   int qt, hk, b;
-  tile_block(a, n_qt, qt, hk, b);
+  tile_block(a, blockIdx.x, gridDim.x, n_qt, qt, hk, b);
 
   const int R = qt * kScoreRows + wave * 32 + r, row = min(R, M - 1);
   const int i = row / G, h = hk * G + row % G;
@@ -297,11 +297,10 @@ __global__ __launch_bounds__(256, 2) void score_fwd_kernel(const ScoreArgs a) {
 // dQ: as the forward, with dP beside S
 // =============================================================================================
 template <int D, bool CAP, bool BIAS>
-__global__ __launch_bounds__(256, 2) void score_dq_kernel(const ScoreArgs a) {
+__device__ __forceinline__ void score_dq(const ScoreArgs& a, int block_x, int blocks, int share, char* smem_raw) {
   constexpr int KB = kBN / 32, KS = D / 16, DB = D / 32;
   constexpr int kTile = kBN * D * 2;
-  __shared__ __attribute__((aligned(1024))) char smem_raw[4 * kTile];
-  __shared__ int hull[24];
+  int* hull = (int*)(smem_raw + 4 * kTile);
   ST_LDS char* smem = (ST_LDS char*)smem_raw;
   const Shape& s = a.s;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
@@ -309,7 +308,7 @@ __global__ __launch_bounds__(256, 2) void score_dq_kernel(const ScoreArgs a) {
   const int G = s.Hq / s.Hkv, M = s.Sq * G;
   const int n_qt = (M + kScoreRows - 1) / kScoreRows;
   int qt, hk, b;
-  tile_block(a, n_qt, qt, hk, b);
+  tile_block(a, block_x, blocks, n_qt, qt, hk, b);
 
   const int R = qt * kScoreRows + wave * 32 + r, row = min(R, M - 1);
   const int i = row / G, h = hk * G + row % G;
@@ -333,7 +332,7 @@ __global__ __launch_bounds__(256, 2) void score_dq_kernel(const ScoreArgs a) {
   const ScoreConst k = score_const(a);
   int unused;
   const BlockSpan wg = workgroup_span(hull, w, 0, 0, wave, lane, unused, unused);
-  const Walk walk = walk_of(wg, false, 0, 0, a.q_split, blockIdx.y);
+  const Walk walk = walk_of(wg, false, 0, 0, a.q_split, share);
 
   f32x16 acc[DB];
 #pragma unroll
@@ -423,7 +422,7 @@ __global__ __launch_bounds__(256, 2) void score_dq_kernel(const ScoreArgs a) {
   if (R >= M) return;
   const int64_t orow = (((int64_t)b * s.Sq + i) * s.Hq + h) * D;
   const bool part = a.q_split > 1;
-  float* out = part ? a.part_dq + blockIdx.y * ((int64_t)s.B * s.Sq * s.Hq * D) : a.dq;
+  float* out = part ? a.part_dq + share * ((int64_t)s.B * s.Sq * s.Hq * D) : a.dq;
   uint16_t* low = part ? nullptr : (uint16_t*)a.dq_lowp;
   const bool add = !part && !a.assign;
 #pragma unroll
@@ -448,14 +447,16 @@ __global__ __launch_bounds__(256, 2) void score_dq_kernel(const ScoreArgs a) {
 // =============================================================================================
 constexpr int kBlockList = 512;      // row blocks that a workgroup looks through at a time
 
+template <int D>
+constexpr int dkv_lds() { return kScoreKeys * D * 2 + 2 * (2 * 32 * D * 2 + kRowStats * 4) + kBlockList * 16 + 8 * 4; }
+
 template <int D, bool CAP, bool BIAS>
-__global__ __launch_bounds__(256, 2) void score_dkv_kernel(const ScoreArgs a) {
+__device__ __forceinline__ void score_dkv(const ScoreArgs& a, int block_x, int blocks, int share, char* smem_raw) {
   constexpr int KS = D / 16, DB = D / 32;
   constexpr int kTile = 32 * D * 2, kStage = 2 * kTile + kRowStats * 4;   // Q, dO and the statistics of 32 rows
   constexpr int kKeyTile = kScoreKeys * D * 2;
-  __shared__ __attribute__((aligned(1024))) char smem_raw[kKeyTile + 2 * kStage];
-  __shared__ int4 list[kBlockList];                    // block and hull of its rows: whole ones from the front, the others from the back
-  __shared__ int count[8];
+  int4* list = (int4*)(smem_raw + kKeyTile + 2 * kStage);                 // block and hull of its rows: whole ones from the front, the others from the back
+  int* count = (int*)(list + kBlockList);
   ST_LDS char* smem = (ST_LDS char*)smem_raw;
   ST_LDS char* stages = smem + kKeyTile;
   const Shape& s = a.s;
@@ -463,7 +464,7 @@ __global__ __launch_bounds__(256, 2) void score_dkv_kernel(const ScoreArgs a) {
   const int g = lane >> 5, r = lane & 31;
   const int G = s.Hq / s.Hkv, M = s.Sq * G, n_blk = (M + 31) / 32;
   const int n_kt = (s.Sk + kScoreKeys - 1) / kScoreKeys;
-  const int logical = xcd_logical_block(blockIdx.x, gridDim.x);
+  const int logical = xcd_logical_block(block_x, blocks);
   const int kt = uniform(logical % n_kt), bh = logical / n_kt;
   const int b = uniform(bh % s.B), hk = uniform(bh / s.B);
   const int key0 = kt * kScoreKeys, key_end = min(key0 + kScoreKeys, s.Sk);
@@ -566,7 +567,7 @@ __global__ __launch_bounds__(256, 2) void score_dkv_kernel(const ScoreArgs a) {
   };
 
   // the blocks of this share: every kv_split-th, so that shares of a mask's edge and of its inside are alike
-  const int n_share = a.kv_split, share = blockIdx.y, mine = (n_blk - share + n_share - 1) / n_share;
+  const int n_share = a.kv_split, mine = (n_blk - share + n_share - 1) / n_share;
   for (int at = 0; at < mine; at += kBlockList) {
     // ---- the visible ones among the next blocks, in order
     int whole = 0, edge = 0;
@@ -634,6 +635,17 @@ __global__ __launch_bounds__(256, 2) void score_dkv_kernel(const ScoreArgs a) {
   store(acc_v, 1.f, part ? a.part_dv + share * n_kv : a.dv, part ? nullptr : (uint16_t*)a.dv_lowp);
 }
 
+// Both in one launch, the key tiles first: those of a causal or packed batch do unlike amounts of work, and the query tiles fill
+// the places that the short ones leave (32/8 heads x 8192 packed rows: 1111 and 419 us in launches of their own).
+template <int D, bool CAP, bool BIAS>
+__global__ __launch_bounds__(256, 2) void score_bwd_kernel(const ScoreArgs a, int key_tiles, int query_tiles) {
+  constexpr int kQueryLds = 4 * kBN * D * 2 + 24 * 4;
+  __shared__ __attribute__((aligned(1024))) char smem[dkv_lds<D>() > kQueryLds ? dkv_lds<D>() : kQueryLds];
+  const int n_kv = key_tiles * a.kv_split, block = blockIdx.x;      // (either number of tiles may be zero)
+  if (block < n_kv) score_dkv<D, CAP, BIAS>(a, block % key_tiles, key_tiles, block / key_tiles, smem);
+  else score_dq<D, CAP, BIAS>(a, (block - n_kv) % query_tiles, query_tiles, (block - n_kv) / query_tiles, smem);
+}
+
 // f(integral D, cap, bias)
 template <typename F>
 hipError_t with_score(const ScoreArgs& a, F f) {
@@ -668,20 +680,14 @@ hipError_t launch_score_fwd_bf16(const ScoreArgs& a, hipStream_t stream) {
 }
 
 hipError_t launch_score_bwd_bf16(const ScoreArgs& a, hipStream_t stream) {
-  const int64_t total = row_tiles(a.s), keys = (int64_t)((a.s.Sk + kScoreKeys - 1) / kScoreKeys) * a.s.Hkv * a.s.B;
-  if (total > kScoreGridMost || keys > kScoreGridMost) return hipErrorInvalidValue;
-  if (keys > 0) {
-    ProfScope prof("score_dkv_bf16", stream);
-    const hipError_t e = with_score(a, [&](auto d, auto cap, auto bias) {
-      hipLaunchKernelGGL((score_dkv_kernel<decltype(d)::value, decltype(cap)::value, decltype(bias)::value>), dim3((unsigned)keys, (unsigned)a.kv_split), dim3(256), 0, stream, a);
-      return hipGetLastError();
-    });
-    if (e != hipSuccess) return e;
-  }
+  const int64_t rows = row_tiles(a.s), keys = (int64_t)((a.s.Sk + kScoreKeys - 1) / kScoreKeys) * a.s.Hkv * a.s.B;
+  const int64_t total = keys * a.kv_split + rows * a.q_split;
   if (total <= 0) return hipSuccess;
-  ProfScope prof("score_dq_bf16", stream);
+  if (total > 4 * kScoreGridMost - 1) return hipErrorInvalidValue;
+  ProfScope prof("score_bwd_bf16", stream);
   return with_score(a, [&](auto d, auto cap, auto bias) {
-    hipLaunchKernelGGL((score_dq_kernel<decltype(d)::value, decltype(cap)::value, decltype(bias)::value>), dim3((unsigned)total, (unsigned)a.q_split), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((score_bwd_kernel<decltype(d)::value, decltype(cap)::value, decltype(bias)::value>), dim3((unsigned)total), dim3(256), 0, stream, a,
+                       (int)keys, (int)rows);
     return hipGetLastError();
   });
 }
