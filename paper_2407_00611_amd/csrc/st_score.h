@@ -194,17 +194,13 @@ struct ScoreTile {
   }
 };
 
-// bf16 pairs with the infinities and NaN among them set to zero; bad collects a bit for each
-__device__ __forceinline__ uint32_t scrub_bf16(uint32_t x, uint32_t& bad) {
-  const uint32_t b = ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
-  bad |= b;
-  return x & ~(b | (b - (b >> 15)));
-}
-__device__ __forceinline__ bf16x8 scrub_bf16(bf16x8 x, uint32_t& bad) {
-  u32x4 u = __builtin_bit_cast(u32x4, x);
-#pragma unroll
-  for (int j = 0; j < 4; ++j) u[j] = scrub_bf16(u[j], bad);
-  return __builtin_bit_cast(bf16x8, u);
+// bf16 values with the infinities and NaN among them made the largest finite value of their sign.  As signed integers those with a
+// plus are the highest, as unsigned ones those with a minus: two packed instructions for a pair.
+__device__ __forceinline__ bf16x8 finite_bf16(bf16x8 x) {
+  typedef short s16x8 __attribute__((ext_vector_type(8)));
+  typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
+  const s16x8 y = __builtin_elementwise_min(__builtin_bit_cast(s16x8, x), (s16x8)(short)0x7f7f);
+  return __builtin_bit_cast(bf16x8, __builtin_elementwise_min(__builtin_bit_cast(u16x8, y), (u16x8)(unsigned short)0xff7f));
 }
 
 }  // namespace st

@@ -5,8 +5,8 @@
 // bf16 kernels here; sums and statistics stay fp32.
 //
 // Rows whose tile a mask edge crosses: the matrix unit multiplies what a row does not see by zero, and 0 * inf is NaN.  In such a
-// tile the operand's infinities and NaN are set to zero.  The forward adds them to the rows that do see them once O is stored; in
-// the backward, a row that sees a key with such values has NaN in P or dU already, and so has its contribution.
+// tile the operand's infinities and NaN are made finite.  The forward adds them to the rows that do see them once O is stored; in
+// the backward, P or dU of a row that sees a key with such values is NaN, and so is its contribution.
 #include <algorithm>
 #include <type_traits>
 
@@ -21,6 +21,24 @@ constexpr int kBN = 64;              // keys of a streamed tile
 constexpr float kSumMost = 4096.f;
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// Whether 32 rows of an LDS tile hold an infinity or NaN: their products with zeros are NaN then.  Eight matrix instructions, where a
+// look at every operand's bits is some 380 others; operands are scrubbed only where it is true.
+template <int D>
+__device__ __forceinline__ bool not_finite(const LaneReads<D>& reads, uint32_t tile) {
+  f32x16 z;
+#pragma unroll
+  for (int v = 0; v < 16; ++v) z[v] = 0.f;
+  const bf16x8 zero = __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
+#pragma unroll
+  for (int m = 0; m < 2; ++m)
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) z = mfma32(reads.frag_tr(tile, 16 * m, db), zero, z);
+  float sum = 0.f;
+#pragma unroll
+  for (int v = 0; v < 16; ++v) sum += z[v];
+  return __any(sum != 0.f);
+}
 
 // Tiles of 64 keys that a query tile's workgroup walks: those that the hull of its rows touches.  The general ones come first (a
 // mask edge crosses them, or a biased row lies in them), then the rest, the whole ones, in two ranges of the chunk: nearest first,
@@ -87,7 +105,12 @@ __device__ __forceinline__ BlockSpan workgroup_span(int* hull, const BlockSpan& 
   return BlockSpan{lowest(0), highest(4), highest(8), lowest(12)};
 }
 
-// Direct loads of a whole 64-key tile: the lane's place in the tile's first rows, the rest of the address is uniform
+// Direct loads of a whole 64-key tile (in assembly: the compiler would wait for builtin ones ahead of every LDS read, those of the
+// tile in hand too; landed() is the wait): the lane's place in the tile's first rows, the rest of the address is uniform
+__device__ __forceinline__ void landed() {
+  wait_vmcnt<0>();
+  __syncthreads();
+}
 template <int D>
 struct TileLoads {
   const char* at;
@@ -97,11 +120,10 @@ struct TileLoads {
     const int r = wave * RPI + lane / PPR, f = swz<D>(r, 0) - r * D * 2;
     at = base + r * row + (((lane % PPR) << 4) ^ f);
   }
-  __device__ __forceinline__ void issue(int key0, ST_LDS char* tile, int wave) const {
+  __device__ __forceinline__ void issue(int key0, uint32_t tile, int wave) const {
     constexpr int N = kBN * D * 2 / 4096, STEP = 4 * 64 / (D / 8);
 #pragma unroll
-    for (int j = 0; j < N; ++j)
-      __builtin_amdgcn_global_load_lds((st_global_ptr)(at + (key0 + STEP * j) * row), (st_lds_ptr)(tile + (4 * j + wave) * 1024), 16, 0, 0);
+    for (int j = 0; j < N; ++j) dma16_asm(at + (key0 + STEP * j) * row, tile + (4 * j + wave) * 1024);
   }
 };
 
@@ -147,34 +169,39 @@ __global__ __launch_bounds__(256, 2) void score_fwd_kernel(const ScoreArgs a) {
 #pragma unroll
     for (int v = 0; v < 16; ++v) acc[db][v] = 0.f;
   float m_run = kUnset, l_run = 0.f;
-  uint32_t bad = 0;
+  bool bad = false;
 
   const char* kb_ = (const char*)a.k.ptr + ((int64_t)b * a.k.sb + (int64_t)hk * a.k.sh) * 2;
   const char* vb_ = (const char*)a.v.ptr + ((int64_t)b * a.v.sb + (int64_t)hk * a.v.sh) * 2;
+  const uint32_t smem_addr = (uint32_t)(uintptr_t)smem;
   const TileLoads<D> k_loads(kb_, a.k.ss, lane, wave), v_loads(vb_, a.v.ss, lane, wave);
   auto issue_load = [&](int n, int stage) {
     const int t = walk.tile(n);
-    ST_LDS char* at = smem + stage * 2 * kTile;
+    const uint32_t at = smem_addr + stage * 2 * kTile;
     if (n < walk.n_gen) {                              // it may be the ragged end of the chunk
-      stage_dma<D, kBN>(kb_, a.k.ss, t * kBN, s.Sk, at, tid);
-      stage_dma<D, kBN>(vb_, a.v.ss, t * kBN, s.Sk, at + kTile, tid);
+      stage_dma_asm<D, kBN>(kb_, a.k.ss, t * kBN, s.Sk, at, tid);
+      stage_dma_asm<D, kBN>(vb_, a.v.ss, t * kBN, s.Sk, at + kTile, tid);
     } else {
       k_loads.issue(t * kBN, at, wave);
       v_loads.issue(t * kBN, at + kTile, wave);
     }
   };
   const LaneReads<D> reads(lane);
-  const uint32_t smem_addr = (uint32_t)(uintptr_t)smem;
 
-  // 32 keys against the wavefront's rows.  In a whole tile the bias is slope (key - x) or slope (x - key) for all of them: its part
-  // that no key changes goes into the reference.
-  auto block = [&](auto general, uint32_t ktile, uint32_t vtile, int key0) {
-    constexpr bool GEN = decltype(general)::value;
+  // 32 keys against the wavefront's rows, in three steps
+  struct Block {
     f32x16 sc;
+    u32x4 pf[2];
+  };
+  auto products = [&](Block& y, uint32_t ktile) {
 #pragma unroll
-    for (int v = 0; v < 16; ++v) sc[v] = 0.f;
+    for (int v = 0; v < 16; ++v) y.sc[v] = 0.f;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) sc = mfma32(reads.frag(ktile, 0, ks), qf[ks], sc);
+    for (int ks = 0; ks < KS; ++ks) y.sc = mfma32(reads.frag(ktile, 0, ks), qf[ks], y.sc);
+  };
+  // In a whole tile the bias is slope (key - x) or slope (x - key) for all keys: the part of it that no key changes goes into the reference.
+  auto softmax = [&](auto general, Block& y, int key0) {
+    constexpr bool GEN = decltype(general)::value;
     const int x0 = see.x - key0 - 4 * g;
     const ScoreTile<CAP, BIAS> f(k, slope2, x0);
     const float side = x0 > 0 ? f.slope : -f.slope;    // (left of the row the bias rises with the key)
@@ -183,26 +210,26 @@ __global__ __launch_bounds__(256, 2) void score_fwd_kernel(const ScoreArgs a) {
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
       const int key = 8 * (v / 4) + v % 4;
-      sc[v] = GEN ? f.raw(sc[v], key) : f.raw_side(sc[v], key, side);
-      if (GEN) sc[v] = key >= l0 && key < h0 ? sc[v] : f.lowest();
+      y.sc[v] = GEN ? f.raw(y.sc[v], key) : f.raw_side(y.sc[v], key, side);
+      if (GEN) y.sc[v] = key >= l0 && key < h0 ? y.sc[v] : f.lowest();
     }
     // The reference m_run of the exponents is lazy.  It moves where the block's sum says that some exponent was large (or too large
     // for its exponential): nothing of the block has been used by then.
     float p[16], sum;
-    auto softmax = [&]() {
-      sum = 0.f;
+    auto exponentials = [&]() {
       const float m = m_run + off;
+      sum = 0.f;
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
-        p[v] = __builtin_amdgcn_exp2f(f.exponent(sc[v], m));
+        p[v] = __builtin_amdgcn_exp2f(f.exponent(y.sc[v], m));
         sum += p[v];
       }
     };
-    softmax();
+    exponentials();
     if (__builtin_expect(__any(sum > kSumMost), 0)) {
       float top = f.lowest();
 #pragma unroll
-      for (int v = 0; v < 16; ++v) top = f.higher(top, sc[v]);
+      for (int v = 0; v < 16; ++v) top = f.higher(top, y.sc[v]);
       const float m_new = fmaxf(m_run, xhalf_max(f.exponent(top, off)));
       const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
       l_run *= alpha;
@@ -211,43 +238,61 @@ __global__ __launch_bounds__(256, 2) void score_fwd_kernel(const ScoreArgs a) {
       for (int db = 0; db < DB; ++db)
 #pragma unroll
         for (int v = 0; v < 16; ++v) acc[db][v] *= alpha;
-      softmax();
+      exponentials();
     }
     l_run += sum;
 #pragma unroll
-    for (int m = 0; m < 2; ++m) {
-      const bf16x8 pf = __builtin_bit_cast(bf16x8, u32x4{pack_bf16(p[8 * m], p[8 * m + 1]), pack_bf16(p[8 * m + 2], p[8 * m + 3]),
-                                                         pack_bf16(p[8 * m + 4], p[8 * m + 5]), pack_bf16(p[8 * m + 6], p[8 * m + 7])});
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y.pf[m][e] = pack_bf16(p[8 * m + 2 * e], p[8 * m + 2 * e + 1]);
+  };
+  auto contract = [&](auto scrub, const Block& y, uint32_t vtile) {
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
 #pragma unroll
       for (int db = 0; db < DB; ++db) {
         const bf16x8 vf = reads.frag_tr(vtile, 16 * m, db);
-        acc[db] = mfma32(GEN ? scrub_bf16(vf, bad) : vf, pf, acc[db]);
+        acc[db] = mfma32(decltype(scrub)::value ? finite_bf16(vf) : vf, __builtin_bit_cast(bf16x8, y.pf[m]), acc[db]);
       }
-    }
   };
 
   int buf = 0, n = walk.n0;
   if (n < walk.n1) issue_load(n, 0);
-  __syncthreads();
+  landed();
   for (; n < min(walk.n1, walk.n_gen); ++n) {
     if (n + 1 < walk.n1) issue_load(n + 1, buf ^ 1);
     const int key0 = walk.tile(n) * kBN;
     const uint32_t ktile = smem_addr + buf * 2 * kTile;
     if (w.lo < key0 + kBN && w.hi > key0)              // some row of this wavefront sees some key of the tile
 #pragma unroll 1
-      for (int kb = 0; kb < KB; ++kb)
-        block(std::true_type(), ktile + 32 * kb * D * 2, ktile + kTile + 32 * kb * D * 2, key0 + 32 * kb);
-    __syncthreads();
+      for (int kb = 0; kb < KB; ++kb) {
+        const uint32_t vblock = ktile + kTile + 32 * kb * D * 2;
+        const int block0 = key0 + 32 * kb;
+        Block y;
+        products(y, ktile + 32 * kb * D * 2);
+        softmax(std::true_type(), y, block0);
+        const bool dirty = (w.all_lo > block0 || w.all_hi < block0 + 32) && not_finite<D>(reads, vblock);
+        bad = bad || dirty;
+        if (__builtin_expect(dirty, 0)) contract(std::true_type(), y, vblock);
+        else contract(std::false_type(), y, vblock);
+      }
+    landed();
     buf ^= 1;
   }
   for (; n < walk.n1; ++n) {
     if (n + 1 < walk.n1) issue_load(n + 1, buf ^ 1);
     const int key0 = walk.tile(n) * kBN;
     const uint32_t ktile = smem_addr + buf * 2 * kTile;
+    // both blocks' products first: the second's run over the softmax of the first
+    Block y[KB];
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
-      block(std::false_type(), ktile + 32 * kb * D * 2, ktile + kTile + 32 * kb * D * 2, key0 + 32 * kb);
-    __syncthreads();
+    for (int kb = 0; kb < KB; ++kb) products(y[kb], ktile + 32 * kb * D * 2);
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+      softmax(std::false_type(), y[kb], key0 + 32 * kb);
+      contract(std::false_type(), y[kb], ktile + kTile + 32 * kb * D * 2);
+    }
+    landed();
     buf ^= 1;
   }
 
@@ -259,7 +304,6 @@ __global__ __launch_bounds__(256, 2) void score_fwd_kernel(const ScoreArgs a) {
   float* o = part ? a.part_o + blockIdx.y * n_o * D : a.o;
   uint16_t* olow = part ? nullptr : (uint16_t*)a.o_lowp;
   const int64_t orow = (((int64_t)b * s.Sq + i) * s.Hq + h) * D;
-  const bool any_bad = __any(bad != 0);
   if (R >= M) return;
 #pragma unroll
   for (int db = 0; db < DB; ++db)
@@ -275,7 +319,7 @@ __global__ __launch_bounds__(256, 2) void score_fwd_kernel(const ScoreArgs a) {
     if (BIAS) x = fmaf(-a.slopes[h], see.rest, x);
     (part ? a.part_lse + blockIdx.y * n_o : a.lse)[((int64_t)b * s.Hq + h) * s.Sq + i] = x;
   }
-  if (any_bad)
+  if (bad)
     // what the general tiles of this wavefront left out: V[t][d] of the keys that this row sees
     for (int y = walk.n0; y < min(walk.n1, walk.n_gen); ++y) {
       const int key0 = walk.tile(y) * kBN;
@@ -339,23 +383,22 @@ __device__ __forceinline__ void score_dq(const ScoreArgs& a, int block_x, int bl
   for (int db = 0; db < DB; ++db)
 #pragma unroll
     for (int v = 0; v < 16; ++v) acc[db][v] = 0.f;
-  uint32_t bad = 0;
   const char* kb_ = (const char*)a.k.ptr + ((int64_t)b * a.k.sb + (int64_t)hk * a.k.sh) * 2;
   const char* vb_ = (const char*)a.v.ptr + ((int64_t)b * a.v.sb + (int64_t)hk * a.v.sh) * 2;
+  const uint32_t smem_addr = (uint32_t)(uintptr_t)smem;
   const TileLoads<D> k_loads(kb_, a.k.ss, lane, wave), v_loads(vb_, a.v.ss, lane, wave);
   auto issue_load = [&](int n, int stage) {
     const int t = walk.tile(n);
-    ST_LDS char* at = smem + stage * 2 * kTile;
+    const uint32_t at = smem_addr + stage * 2 * kTile;
     if (n < walk.n_gen) {
-      stage_dma<D, kBN>(kb_, a.k.ss, t * kBN, s.Sk, at, tid);
-      stage_dma<D, kBN>(vb_, a.v.ss, t * kBN, s.Sk, at + kTile, tid);
+      stage_dma_asm<D, kBN>(kb_, a.k.ss, t * kBN, s.Sk, at, tid);
+      stage_dma_asm<D, kBN>(vb_, a.v.ss, t * kBN, s.Sk, at + kTile, tid);
     } else {
       k_loads.issue(t * kBN, at, wave);
       v_loads.issue(t * kBN, at + kTile, wave);
     }
   };
   const LaneReads<D> reads(lane);
-  const uint32_t smem_addr = (uint32_t)(uintptr_t)smem;
   auto block = [&](auto general, uint32_t ktile, uint32_t vtile, int key0) {
     constexpr bool GEN = decltype(general)::value;
     f32x16 sc, dp;
@@ -382,7 +425,7 @@ __device__ __forceinline__ void score_dq(const ScoreArgs& a, int block_x, int bl
       if (BIAS) e = fmaf(-slope2, fabsf(x - (float)key), e);
       float ds = __builtin_amdgcn_exp2f(e) * (dp[v] - dlt);
       if (CAP) ds *= f;
-      if (GEN) ds = key >= l0 && key < h0 ? ds : 0.f;
+      if (GEN) ds = key >= l0 && key < h0 ? fmaf(0.f, sc[v], ds) : 0.f;
       sc[v] = ds;
     }
 #pragma unroll
@@ -391,13 +434,13 @@ __device__ __forceinline__ void score_dq(const ScoreArgs& a, int block_x, int bl
 #pragma unroll
       for (int db = 0; db < DB; ++db) {
         const bf16x8 ktf = reads.frag_tr(ktile, 16 * m, db);
-        acc[db] = mfma32(GEN ? scrub_bf16(ktf, bad) : ktf, dsf, acc[db]);
+        acc[db] = mfma32(GEN ? finite_bf16(ktf) : ktf, dsf, acc[db]);
       }
     }
   };
   int buf = 0, n = walk.n0;
   if (n < walk.n1) issue_load(n, 0);
-  __syncthreads();
+  landed();
   for (; n < min(walk.n1, walk.n_gen); ++n) {
     if (n + 1 < walk.n1) issue_load(n + 1, buf ^ 1);
     const int key0 = walk.tile(n) * kBN;
@@ -406,7 +449,7 @@ __device__ __forceinline__ void score_dq(const ScoreArgs& a, int block_x, int bl
 #pragma unroll 1
       for (int kb = 0; kb < KB; ++kb)
         block(std::true_type(), ktile + 32 * kb * D * 2, ktile + kTile + 32 * kb * D * 2, key0 + 32 * kb);
-    __syncthreads();
+    landed();
     buf ^= 1;
   }
   for (; n < walk.n1; ++n) {
@@ -416,7 +459,7 @@ __device__ __forceinline__ void score_dq(const ScoreArgs& a, int block_x, int bl
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
       block(std::false_type(), ktile + 32 * kb * D * 2, ktile + kTile + 32 * kb * D * 2, key0 + 32 * kb);
-    __syncthreads();
+    landed();
     buf ^= 1;
   }
   if (R >= M) return;
@@ -472,7 +515,7 @@ __device__ __forceinline__ void score_dkv(const ScoreArgs& a, int block_x, int b
   const int key = wkey0 + r, key_row = min(key, s.Sk - 1);
   const uint32_t inv_g = G > 1 ? 0xffffffffu / (uint32_t)G + 1 : 0;      // x / G = x inv_g / 2^32 for the small x below
 
-  stage_dma<D, kScoreKeys>((const char*)a.v.ptr + ((int64_t)b * a.v.sb + (int64_t)hk * a.v.sh) * 2, a.v.ss, key0, s.Sk, smem, tid);
+  stage_dma_asm<D, kScoreKeys>((const char*)a.v.ptr + ((int64_t)b * a.v.sb + (int64_t)hk * a.v.sh) * 2, a.v.ss, key0, s.Sk, (uint32_t)(uintptr_t)smem, tid);
   const char* kp = (const char*)a.k.ptr + ((int64_t)b * a.k.sb + (int64_t)hk * a.k.sh + (int64_t)key_row * a.k.ss) * 2;
   bf16x8 kf[KS];
 #pragma unroll
@@ -483,7 +526,6 @@ __device__ __forceinline__ void score_dkv(const ScoreArgs& a, int block_x, int b
   for (int db = 0; db < DB; ++db)
 #pragma unroll
     for (int v = 0; v < 16; ++v) acc_k[db][v] = acc_v[db][v] = 0.f;
-  uint32_t bad = 0;
 
   // a block's rows and statistics, straight to LDS: two of the 16-byte pieces of each tile a lane (one at head size 64)
   constexpr int PPR = D / 8, RPI = 64 / PPR;
@@ -493,16 +535,16 @@ __device__ __forceinline__ void score_dkv(const ScoreArgs& a, int block_x, int b
   const char* stat_base = (const char*)(a.rows + ((int64_t)b * s.Hkv + hk) * n_blk * kRowStats) + lane * 16;
   auto load_block = [&](int j, int stage) {
     j = uniform(j);
-    ST_LDS char* at = stages + stage * kStage;
+    const uint32_t at = (uint32_t)(uintptr_t)stages + stage * kStage;
     const int base = 32 * j / G, rem = 32 * j - base * G;                // uniform
 #pragma unroll
     for (int u = 0; u < 32 / (4 * RPI); ++u) {
       const uint32_t x = (uint32_t)(rem + min(piece_row + 4 * RPI * u, M - 1 - 32 * j)), q = G > 1 ? __umulhi(x, inv_g) : x;
       const int64_t i = base + (int)q, h = (int)(x - q * (uint32_t)G);
-      __builtin_amdgcn_global_load_lds((st_global_ptr)(q_base + (i * a.q.ss + h * a.q.sh) * 2), (st_lds_ptr)(at + (4 * u + wave) * 1024), 16, 0, 0);
-      __builtin_amdgcn_global_load_lds((st_global_ptr)(d_base + (i * a.d_o.ss + h * a.d_o.sh) * 2), (st_lds_ptr)(at + kTile + (4 * u + wave) * 1024), 16, 0, 0);
+      dma16_asm(q_base + (i * a.q.ss + h * a.q.sh) * 2, at + (4 * u + wave) * 1024);
+      dma16_asm(d_base + (i * a.d_o.ss + h * a.d_o.sh) * 2, at + kTile + (4 * u + wave) * 1024);
     }
-    if (wave == 0) __builtin_amdgcn_global_load_lds((st_global_ptr)(stat_base + (int64_t)j * kRowStats * 4), (st_lds_ptr)(at + 2 * kTile), 16, 0, 0);
+    if (wave == 0) dma16_asm(stat_base + (int64_t)j * kRowStats * 4, at + 2 * kTile);
   };
 
   const LaneReads<D> reads(lane);
@@ -547,8 +589,8 @@ __device__ __forceinline__ void score_dkv(const ScoreArgs& a, int block_x, int b
         if (CAP) ds *= f;
         if (GEN) {
           const bool see = key >= __float_as_int(lo[e4]) && key < __float_as_int(hi[e4]);
-          p = see ? fmaf(0.f, ds, p) : 0.f;            // (a row whose dO is not finite: NaN, as the scrubbed dO no longer says it)
-          ds = see ? ds : 0.f;
+          p = see ? fmaf(0.f, ds, p) : 0.f;            // (NaN for a row whose dO, or below Q, is not finite: the operand no longer says it)
+          ds = see ? fmaf(0.f, sc[v], ds) : 0.f;
         }
         sc[v] = p;
         dp[v] = ds;
@@ -560,8 +602,8 @@ __device__ __forceinline__ void score_dkv(const ScoreArgs& a, int block_x, int b
 #pragma unroll
       for (int db = 0; db < DB; ++db) {
         const bf16x8 x = reads.frag_tr(dotile, 16 * m, db), y = reads.frag_tr(qtile, 16 * m, db);
-        acc_v[db] = mfma32(GEN ? scrub_bf16(x, bad) : x, pf, acc_v[db]);
-        acc_k[db] = mfma32(GEN ? scrub_bf16(y, bad) : y, dsf, acc_k[db]);
+        acc_v[db] = mfma32(GEN ? finite_bf16(x) : x, pf, acc_v[db]);
+        acc_k[db] = mfma32(GEN ? finite_bf16(y) : y, dsf, acc_k[db]);
       }
     }
   };
@@ -595,24 +637,24 @@ __device__ __forceinline__ void score_dkv(const ScoreArgs& a, int block_x, int b
     if (total == 0) continue;
     auto entry = [&](int n) { return n < edge ? kBlockList - 1 - n : n - edge; };
     load_block(list[entry(0)].x, 0);
-    __syncthreads();
+    landed();
     int buf = 0, n = 0;
     for (; n < edge; ++n) {
       if (n + 1 < total) load_block(list[entry(n + 1)].x, buf ^ 1);
       const int4 y = list[entry(n)];
       if (uniform(y.y) < wkey_end && uniform(y.z) > wkey0) block(std::true_type(), buf);
-      __syncthreads();
+      landed();
       buf ^= 1;
     }
     for (; n < total; ++n) {
       if (n + 1 < total) load_block(list[n + 1 - edge].x, buf ^ 1);
       block(std::false_type(), buf);
-      __syncthreads();
+      landed();
       buf ^= 1;
     }
   }
 
-  __syncthreads();                                     // (the direct loads have landed, also where no block was visible)
+  landed();                                            // (V, also where no block was visible)
   if (key >= s.Sk) return;
   const int64_t n_kv = (int64_t)s.B * s.Sk * s.Hkv * D, orow = (((int64_t)b * s.Sk + key) * s.Hkv + hk) * D;
   const bool part = n_share > 1, add = !part && !a.assign;
