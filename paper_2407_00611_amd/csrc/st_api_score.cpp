@@ -72,10 +72,12 @@ ScorePlan fwd_plan(const st::Shape& s, int dtype) {
   }
   return p;
 }
-// Key tiles and query tiles share a launch.  A share of one is at most what a place of the chip has to do on the average, where a
-// tile is longer; the work is counted in products of 32 x 32 x D, four of a key tile's 32 rows for each 32 keys and three of a query
-// tile's.
-ScorePlan bwd_plan(const st::Shape& s, int dtype) {
+// Key tiles and query tiles share a launch.  A share of one is about what a place of the chip has to do on the average, where a tile
+// is longer; the work is counted in products of 32 x 32 x D, four of a key tile's 32 rows for each 32 keys and three of a query
+// tile's.  A mask leaves the longest key tiles, which come first, and takes from the average: half of it, or, where one of two runs
+// of rows is past most keys, a quarter.  (The size of the workspace must not depend on the offsets.)  32/8 heads x 8192 packed
+// rows, capped: 857 + 33 us in two shares, 947 in one; x 4096 rows in two runs and 2048 keys: 403 + 12 in three, 470 + 10 in two.
+ScorePlan bwd_plan(const st::Shape& s, int dtype, bool spans) {
   const int G = s.Hq / s.Hkv;
   const bool bf16 = dtype == ST_BF16;
   const int64_t row_blocks = bf16 ? ((int64_t)s.Sq * G + 31) / 32 : ((int64_t)s.Sq + 31) / 32 * G, key_blocks = ((int64_t)s.Sk + 31) / 32;
@@ -83,11 +85,13 @@ ScorePlan bwd_plan(const st::Shape& s, int dtype) {
   const int64_t keys = bf16 ? ((int64_t)s.Sk + st::kScoreKeys - 1) / st::kScoreKeys * s.Hkv * s.B : key_blocks * s.Hkv * s.B;
   const int64_t n_q = (int64_t)s.B * s.Sq * s.Hq * s.D * 4, n_kv = (int64_t)s.B * s.Sk * s.Hkv * s.D * 4;
   const int64_t kv_len = 4 * row_blocks, q_len = 3 * key_blocks;
-  const int64_t each = std::max<int64_t>((keys * kv_len + rows * q_len) / 512, bf16 ? kLeastShare : 8);
+  const int64_t each = (keys * kv_len + rows * q_len) / 512, least = bf16 ? kLeastShare : 8;
+  const int quarters = !bf16 ? 4 : spans || (s.causal && s.q_seg <= 0) ? 2 : s.causal ? 3 : 4;
   ScorePlan p{};
-  p.q_split = (int)std::min<int64_t>(std::max<int64_t>((2 * q_len + each) / (2 * each), 1), 16);
+  auto shares = [](int64_t len, int64_t most, int64_t eighths) { return (int)std::min<int64_t>(std::max<int64_t>((8 * len + eighths * most) / (8 * most), 1), 16); };
+  p.q_split = shares(q_len, std::max(each, least), 4);
   while (p.q_split > 1 && p.q_split * n_q > kSplitBytesMost) --p.q_split;
-  p.kv_split = (int)std::min<int64_t>(std::max<int64_t>((2 * kv_len + each) / (2 * each), 1), 16);
+  p.kv_split = shares(kv_len, std::max(each * quarters / 4, least), quarters < 4 ? 7 : 4);
   while (p.kv_split > 1 && p.kv_split * n_kv * 2 > kSplitBytesMost) --p.kv_split;
   p.dk = p.q_split > 1 ? align_up((size_t)(p.q_split * n_q), 256) : 0;
   const size_t kv = p.kv_split > 1 ? align_up((size_t)(p.kv_split * n_kv), 256) : 0;
@@ -179,7 +183,7 @@ st_status st_mask_spans(int32_t B, int32_t Sq, int64_t q_offset, int32_t q_seg, 
 size_t st_attn_score_workspace_bytes(const st_block_desc* d, const st_score* m, int32_t backward) {
   if (check_score(d, m) != ST_OK || (int64_t)d->B * d->Sq == 0) return 0;
   const st::Shape s = shape_of(d);
-  return backward ? bwd_plan(s, d->dtype).bytes : fwd_plan(s, d->dtype).bytes;
+  return backward ? bwd_plan(s, d->dtype, true).bytes : fwd_plan(s, d->dtype).bytes;   // (with spans, which need the most)
 }
 
 st_status st_attn_score_fwd(const st_block_desc* d, const st_score* m, const st_tensor* q, const st_tensor* k, const st_tensor* v,
@@ -263,7 +267,7 @@ st_status st_attn_score_bwd(const st_block_desc* d, const st_score* m, const st_
   a.dq = dq_acc; a.dk = dk_acc; a.dv = dv_acc;
   a.dq_lowp = dq_lowp; a.dk_lowp = dk_lowp; a.dv_lowp = dv_lowp;
   if (n_q > 0) {
-    const ScorePlan p = bwd_plan(a.s, d->dtype);
+    const ScorePlan p = bwd_plan(a.s, d->dtype, a.spans != nullptr);
     ST_TRY(check_workspace(workspace, workspace_bytes, p.bytes, "score backward"));
     a.q_split = p.q_split;
     a.kv_split = p.kv_split;

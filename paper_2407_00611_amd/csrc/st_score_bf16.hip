@@ -82,14 +82,50 @@ __device__ __forceinline__ Walk walk_of(const BlockSpan& w, bool bias, int x_lo,
   return y;
 }
 
+// The nth of a batch entry's row tiles, of 256 at a time those with the most keys first: what spans leave to a tile differs, and one
+// that holds the end of a document and the start of the next walks both, behind the mask of each.  Launched last such a tile runs on
+// while the chip is empty.  The order is by half octaves of the keys that the first and the last row see, and the tile's number.
+constexpr int kTileLevels = 16;
+__device__ __forceinline__ int ordered_tile(const ScoreArgs& a, int b, int n_qt, int nth, int* lds) {   // lds: 4 kTileLevels + 1 ints
+  const Shape& s = a.s;
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), G = s.Hq / s.Hkv;
+  const int c0 = nth & ~255, t = n_qt - 1 - (c0 + tid);
+  int level = -1;
+  if (t >= 0) {
+    const BlockSpan w = span_join(span_of(row_view(a, b, t * kScoreRows / G)), span_of(row_view(a, b, min((t * kScoreRows + kScoreRows - 1) / G, s.Sq - 1))));
+    const int hull = max(w.hi - w.lo, 0), cost = max(2 * hull - max(w.all_hi - w.all_lo, 0), 0);
+    const int below = (__float_as_int(2.f * (float)s.Sk) >> 22) - (__float_as_int((float)cost) >> 22);
+    level = max(kTileLevels - 1 - below, 0);
+  }
+  uint64_t mine = 0;
+#pragma unroll
+  for (int x = 0; x < kTileLevels; ++x) {
+    const uint64_t m = __ballot(level == x);
+    if (level == x) mine = m;
+    if (lane == 0) lds[4 * x + wave] = __popcll(m);
+  }
+  __syncthreads();
+  int rank = __popcll(mine & (((uint64_t)1 << lane) - 1));
+#pragma unroll
+  for (int x = 0; x < kTileLevels; ++x)
+#pragma unroll
+    for (int y = 0; y < 4; ++y)
+      if (x > level || (x == level && y < wave)) rank += lds[4 * x + y];
+  if (level >= 0 && rank == nth - c0) lds[4 * kTileLevels] = t;
+  __syncthreads();
+  return uniform(lds[4 * kTileLevels]);
+}
+
 // Block id -> (row tile, KV head, batch entry).  Every XCD has a contiguous range of the (KV head, batch entry) pairs, whose keys and
-// values stay in its L2; under a causal mask the later tiles, which see more, come first (spans mostly are such masks too).
-__device__ __forceinline__ void tile_block(const ScoreArgs& a, int block, int blocks, int n_qt, int& qt, int& hk, int& b) {
+// values stay in its L2; under a causal mask the later tiles, which see more, come first.
+constexpr int kOrderFrom = 512;      // workgroups that the chip holds at once: with no more, their order says nothing
+__device__ __forceinline__ void tile_block(const ScoreArgs& a, int block, int blocks, int n_qt, int* lds, int& qt, int& hk, int& b) {
   int hb;
   qtile_block(block, blocks, n_qt, a.s.causal || a.spans, qt, hb);
   hk = uniform(hb % a.s.Hkv);
   b = uniform(hb / a.s.Hkv);
   qt = uniform(qt);
+  if (a.spans && blocks > kOrderFrom) qt = ordered_tile(a, b, n_qt, n_qt - 1 - qt, lds);
 }
 
 // what the rows of the workgroup see together, from what those of each wavefront do; hull: 6 x 4 ints of LDS
@@ -136,7 +172,7 @@ __global__ __launch_bounds__(256, 2) void score_fwd_kernel(const ScoreArgs a) {
   constexpr int kTile = kBN * D * 2;
   constexpr float kUnset = -1e30f;                     // reference of a row that has met no key: whatever comes exceeds it
   __shared__ __attribute__((aligned(1024))) char smem_raw[4 * kTile];   // 2 stages x (K, V)
-  __shared__ int hull[24];
+  __shared__ int hull[24], order[4 * kTileLevels + 1];
   ST_LDS char* smem = (ST_LDS char*)smem_raw;
   const Shape& s = a.s;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
@@ -144,7 +180,7 @@ __global__ __launch_bounds__(256, 2) void score_fwd_kernel(const ScoreArgs a) {
   const int G = s.Hq / s.Hkv, M = s.Sq * G;
   const int n_qt = (M + kScoreRows - 1) / kScoreRows;
   int qt, hk, b;
-  tile_block(a, blockIdx.x, gridDim.x, n_qt, qt, hk, b);
+  tile_block(a, blockIdx.x, gridDim.x, n_qt, order, qt, hk, b);
 
   const int R = qt * kScoreRows + wave * 32 + r, row = min(R, M - 1);
   const int i = row / G, h = hk * G + row % G;
@@ -352,7 +388,7 @@ __device__ __forceinline__ void score_dq(const ScoreArgs& a, int block_x, int bl
   const int G = s.Hq / s.Hkv, M = s.Sq * G;
   const int n_qt = (M + kScoreRows - 1) / kScoreRows;
   int qt, hk, b;
-  tile_block(a, block_x, blocks, n_qt, qt, hk, b);
+  tile_block(a, block_x, blocks, n_qt, hull + 24, qt, hk, b);
 
   const int R = qt * kScoreRows + wave * 32 + r, row = min(R, M - 1);
   const int i = row / G, h = hk * G + row % G;
@@ -681,7 +717,7 @@ __device__ __forceinline__ void score_dkv(const ScoreArgs& a, int block_x, int b
 // the places that the short ones leave (32/8 heads x 8192 packed rows: 1111 and 419 us in launches of their own).
 template <int D, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, 2) void score_bwd_kernel(const ScoreArgs a, int key_tiles, int query_tiles) {
-  constexpr int kQueryLds = 4 * kBN * D * 2 + 24 * 4;
+  constexpr int kQueryLds = 4 * kBN * D * 2 + (24 + 4 * kTileLevels + 1) * 4;
   __shared__ __attribute__((aligned(1024))) char smem[dkv_lds<D>() > kQueryLds ? dkv_lds<D>() : kQueryLds];
   const int n_kv = key_tiles * a.kv_split, block = blockIdx.x;      // (either number of tiles may be zero)
   if (block < n_kv) score_dkv<D, CAP, BIAS>(a, block % key_tiles, key_tiles, block / key_tiles, smem);
