@@ -93,8 +93,8 @@ __device__ __forceinline__ int ordered_tile(const ScoreArgs& a, int b, int n_qt,
   int level = -1;
   if (t >= 0) {
     const BlockSpan w = span_join(span_of(row_view(a, b, t * kScoreRows / G)), span_of(row_view(a, b, min((t * kScoreRows + kScoreRows - 1) / G, s.Sq - 1))));
-    const int hull = max(w.hi - w.lo, 0), cost = max(2 * hull - max(w.all_hi - w.all_lo, 0), 0);
-    const int below = (__float_as_int(2.f * (float)s.Sk) >> 22) - (__float_as_int((float)cost) >> 22);
+    const float hull = (float)max(w.hi - w.lo, 0), cost = fmaxf(2.f * hull - (float)max(w.all_hi - w.all_lo, 0), 0.f);
+    const int below = (__float_as_int(2.f * (float)s.Sk) >> 22) - (__float_as_int(cost) >> 22);
     level = max(kTileLevels - 1 - below, 0);
   }
   uint64_t mine = 0;
