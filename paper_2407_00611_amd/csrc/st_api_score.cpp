@@ -316,7 +316,7 @@ st_status st_qk_rope_fwd(const st_rope_desc* d, const st_tensor* q, const st_ten
 
 size_t st_qk_rope_bwd_workspace_bytes(const st_rope_desc* d) {
   if (d == nullptr || d->B <= 0 || d->S <= 0 || d->D <= 0 || !d->norm) return 0;
-  return align_up((size_t)st::rope_dw_blocks((int64_t)d->B * d->S) * 2 * d->D * 4, 256);
+  return align_up((size_t)std::min<int64_t>((int64_t)d->B * d->S, st::kRopeBlocksMost) * 2 * d->D * 4, 256);
 }
 
 st_status st_qk_rope_bwd(const st_rope_desc* d, const st_tensor* q, const st_tensor* k, const st_tensor* d_q, const st_tensor* d_k,

@@ -18,10 +18,10 @@ struct RopeArgs {
   const float *q_weight, *k_weight;
   const double* freq;        // [rot / 2], radians per position
   const int32_t* positions;  // nullable, [n_axes, B, S]
-  float* dw_parts;           // backward, nullable: [rope_dw_blocks][2][D]
+  float* dw_parts;           // backward, nullable: [min(kRopeBlocksMost, B S)][2][D]
 };
 
-int rope_dw_blocks(int64_t tokens);      // workgroups of the backward, each with sums of its own
+constexpr int kRopeBlocksMost = 1024;    // workgroups of the backward, each with sums of its own: so many, or one a token
 hipError_t launch_rope_fwd(const RopeArgs& g, bool bf16, hipStream_t stream);
 hipError_t launch_rope_bwd(const RopeArgs& g, bool bf16, bool d_bf16, float* dwq, float* dwk, bool assign, hipStream_t stream);
 

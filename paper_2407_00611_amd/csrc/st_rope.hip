@@ -423,20 +423,26 @@ void with_pairs(const RopeArgs& g, F f) {
   }
 }
 
-// tokens of a workgroup: one while that does not fill the chip, then as many as keep four workgroups for every compute unit
-int tokens_each(int64_t tokens) { return (int)std::min<int64_t>(std::max<int64_t>(tokens / 1024, 1), kTokensMost); }
+// tokens of a workgroup: one while that does not fill the chip, then as many as keep four workgroups for every compute unit; where
+// there are more of them than compute units, as many as give every lane a row
+int tokens_each(const RopeArgs& g) {
+  const int64_t tokens = (int64_t)g.B * g.S, groups = kThreads / lanes_of(g.D, pairs_per_lane(g.D, g.rot));
+  const int64_t full = std::min<int64_t>((groups + g.Hq + g.Hkv - 1) / (g.Hq + g.Hkv), std::max<int64_t>(tokens / 256, 1));
+  return (int)std::min<int64_t>(std::max<int64_t>(tokens / 1024, full), kTokensMost);
+}
+
+int bwd_blocks(const RopeArgs& g) {
+  const int64_t tokens = (int64_t)g.B * g.S;
+  const int each = tokens_each(g);
+  return (int)std::min<int64_t>((tokens + each - 1) / each, kRopeBlocksMost);
+}
 
 }  // namespace
-
-int rope_dw_blocks(int64_t tokens) {
-  const int each = tokens_each(tokens);
-  return (int)std::min<int64_t>((tokens + each - 1) / each, 1024);
-}
 
 hipError_t launch_rope_fwd(const RopeArgs& g, bool bf16, hipStream_t stream) {
   const int64_t tokens = (int64_t)g.B * g.S;
   if (tokens <= 0) return hipSuccess;
-  const int each = tokens_each(tokens);
+  const int each = tokens_each(g);
   const int64_t blocks = (tokens + each - 1) / each;
   if (blocks > (1 << 23)) return hipErrorInvalidValue;
   ProfScope prof("qk_rope_fwd", stream);
@@ -452,11 +458,11 @@ hipError_t launch_rope_fwd(const RopeArgs& g, bool bf16, hipStream_t stream) {
 
 hipError_t launch_rope_bwd(const RopeArgs& g, bool bf16, bool d_bf16, float* dwq, float* dwk, bool assign, hipStream_t stream) {
   const int64_t tokens = (int64_t)g.B * g.S;
-  const int each = tokens_each(tokens);
+  const int each = tokens_each(g);
   const int64_t blocks = (tokens + each - 1) / each;
   if (tokens > 0) {
     ProfScope prof("qk_rope_bwd", stream);
-    const dim3 grid((unsigned)rope_dw_blocks(tokens)), block(kThreads);
+    const dim3 grid((unsigned)bwd_blocks(g)), block(kThreads);
     with_pairs(g, [&](auto v, auto u, auto next) {
       constexpr int V = decltype(v)::value, U = decltype(u)::value;
       constexpr bool NEXT = decltype(next)::value;
@@ -470,7 +476,7 @@ hipError_t launch_rope_bwd(const RopeArgs& g, bool bf16, bool d_bf16, float* dwq
   }
   if (!dwq && !dwk) return hipSuccess;
   ProfScope prof("qk_rope_dw", stream);
-  hipLaunchKernelGGL(rope_dw_kernel, dim3((unsigned)((2 * g.D + 15) / 16)), dim3(1024), 0, stream, g.dw_parts, tokens > 0 ? rope_dw_blocks(tokens) : 0, g.D, dwq, dwk, assign ? 1 : 0);
+  hipLaunchKernelGGL(rope_dw_kernel, dim3((unsigned)((2 * g.D + 15) / 16)), dim3(1024), 0, stream, g.dw_parts, tokens > 0 ? bwd_blocks(g) : 0, g.D, dwq, dwk, assign ? 1 : 0);
   return hipGetLastError();
 }
 
