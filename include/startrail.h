@@ -296,13 +296,17 @@ st_status st_ring_bwd_last(const st_ring_desc* desc, const st_tensor* q, const s
  *   u = scale <q, k>,   y = softcap tanh(u / softcap),   s = y - slope_h |p_q - p_k|
  * over the keys of the row's span.  The states fold with st_attn_merge and st_attn_combine, Delta comes from st_attn_delta.
  *   softcap  0: scores are not capped; otherwise finite and positive
- *   slopes   nullable; device fp32 [Hq], finite: what a unit of distance between the positions of query and key takes off the score
+ *   slopes   nullable; device fp32 [Hq], finite, as their products with the distances have to be: what a unit of distance between
+ *            the positions of query and key takes off the score
  *   spans    nullable; device int64 [B,Sq,2], 16-byte aligned: query row i of batch entry b sees the keys at global positions
  *            spans[b][i][0] <= p < spans[b][i][1] (and, with desc->causal, p <= its own); an empty span is legal (O = 0,
  *            lse = -inf, no gradient).  st_mask_spans makes them; any other interval (a sliding window) is as good.
  * Precision of ST_BF16: scores, softmax, sums in fp32 from the stored Q and K (Q is not scaled and rounded first, as the kernels
  * of the plain scores do); P and the gradient of the scores are rounded to bf16 before the second contractions.
- * Infinities and NaN in rows of Q, K, V, dO reach the results of the rows and keys that see them, and no others. */
+ * The states' lse is fp32, like everything that is folded from it: with a bias, where a row sees nothing of a sequence but keys
+ * far away, its probabilities in the backward carry half a step of an lse of that size, 2^-24 slope distance.
+ * Infinities and NaN in rows of Q, K, V, dO reach the results of the rows and keys that see them, and no others.  Outputs overlap
+ * neither each other nor an input. */
 typedef struct {
   float softcap;
   const float* slopes;      /* device */
@@ -349,7 +353,7 @@ st_status st_attn_score_bwd(const st_block_desc* desc, const st_score* score, co
  *   freq        device fp64 [rot/2], radians per position (any: scaled ones too); angles are made in fp64, for far positions
  *   q_weight, k_weight  nullable (ones); device fp32 [D], for norm = 1 only
  * q, k: [B,S,Hq,D] and [B,S,Hkv,D] views (k is not read where Hkv = 0); arithmetic is fp32, rounded once.  q_out, k_out: views of
- * the same type, which may be q and k themselves.  D <= 256, D % 8 == 0, rot even, 0 <= rot <= D. */
+ * the same type, which may be q and k themselves.  D <= 256, D % 8 == 0, rot even, 0 <= rot <= D, Hq + Hkv <= 16384, B S <= 2^25. */
 enum { ST_ROPE_HALVES = 0, ST_ROPE_NEIGHBOURS = 1, ST_ROPE_MAX_AXES = 4 };
 typedef struct {
   int32_t dtype, B, S, Hq, Hkv, D;

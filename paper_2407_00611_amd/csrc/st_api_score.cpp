@@ -97,9 +97,9 @@ ScorePlan bwd_plan(const st::Shape& s, int dtype, bool spans) {
   const size_t kv = p.kv_split > 1 ? align_up((size_t)(p.kv_split * n_kv), 256) : 0;
   p.dv = p.dk + kv;
   p.blocks = p.dv + kv;
-  const int64_t blocks = ((int64_t)s.Sq * G + 31) / 32 * s.B;
+  const int64_t blocks = ((int64_t)s.Sq * G + 31) / 32 * s.Hkv * s.B;
   p.rows = p.blocks + (bf16 ? align_up((size_t)blocks * sizeof(int4), 256) : 0);
-  p.bytes = p.rows + (bf16 ? (size_t)blocks * s.Hkv * st::kRowStats * 4 : 0);
+  p.bytes = p.rows + (bf16 ? (size_t)blocks * st::kRowStats * 4 : 0);
   return p;
 }
 
@@ -121,7 +121,7 @@ st_status check_rope(const st_rope_desc* d, const int32_t* positions, const doub
   if (d->B < 0 || d->S < 0 || d->Hkv < 0) return fail(ST_ERR_INVALID_ARG, "negative size");
   if (d->Hq <= 0 || d->D <= 0) return fail(ST_ERR_INVALID_ARG, "Hq and D must be positive");
   if (d->D > 256 || d->D % 8 != 0) return fail(ST_ERR_UNSUPPORTED, "D <= 256 and D %% 8 == 0 are needed (D=%d)", d->D);
-  if (d->Hq > 65535 || d->Hkv > 65535) return fail(ST_ERR_UNSUPPORTED, "Hq and Hkv must not exceed 65535");
+  if ((int64_t)d->Hq + d->Hkv > 16384) return fail(ST_ERR_UNSUPPORTED, "more than 16384 heads");
   if ((int64_t)d->B * d->S > (int64_t)1 << 25) return fail(ST_ERR_UNSUPPORTED, "more than 2^25 tokens");
   if (d->rot < 0 || d->rot > d->D || d->rot % 2) return fail(ST_ERR_INVALID_ARG, "rot = %d must be even, 0 .. D", d->rot);
   if (d->pairing != ST_ROPE_HALVES && d->pairing != ST_ROPE_NEIGHBOURS) return fail(ST_ERR_INVALID_ARG, "unknown pairing %d", d->pairing);
@@ -255,6 +255,10 @@ st_status st_attn_score_bwd(const st_block_desc* d, const st_score* m, const st_
     if (o.acc) ST_TRY(check_f32(o.name, o.acc, o.n));
     ST_TRY(check_low(o.name, o.low));
   }
+  const void* written[] = {dq_acc, dk_acc, dv_acc, dq_lowp, dk_lowp, dv_lowp};
+  for (int x = 0; x < 6; ++x)
+    for (int y = 0; y < x; ++y)
+      if (written[x] && written[x] == written[y]) return fail(ST_ERR_INVALID_ARG, "two gradients share their memory");
   if (n_q == 0 && n_kv == 0) return ST_OK;
   st::ScoreArgs a = score_args(d, m);
   a.q = view_of(q);

@@ -152,8 +152,12 @@ __device__ __forceinline__ void make_angles(const RopeArgs& g, int64_t t0, int n
     const int i = (int)(token - b * g.S);
     double p;
     if (g.positions) {
-      int axis = 0, end = g.axis_pairs[0];
-      while (j >= end && axis + 1 < g.n_axes) end += g.axis_pairs[++axis];
+      int axis = 0, end = 0;                         // (no index that is known at run time only: the list would be copied to memory)
+#pragma unroll
+      for (int y = 0; y + 1 < ST_ROPE_MAX_AXES; ++y) {
+        end += g.axis_pairs[y];
+        axis += y + 1 < g.n_axes && j >= end;
+      }
       p = (double)g.positions[((int64_t)axis * g.B + b) * g.S + i];
     } else {
       p = (double)(g.seg > 0 && i >= g.seg ? g.offset2 + (i - g.seg) : g.offset + i);
@@ -205,6 +209,7 @@ __global__ __launch_bounds__(kThreads) void rope_fwd_kernel(const RopeArgs g, in
   const int tid = threadIdx.x, chunk = tid & (lanes - 1), group = tid / lanes, groups = kThreads / lanes;
   const int64_t all = (int64_t)g.B * g.S, t0 = (int64_t)blockIdx.x * tokens;
   const int n = (int)min((int64_t)tokens, all - t0);
+  // row / heads = row inv_heads / 2^32 while rows x heads stay below 2^32: at most 16384 heads of eight tokens
   const uint32_t heads = (uint32_t)(g.Hq + g.Hkv), rows = heads * (uint32_t)n, inv_heads = 0xffffffffu / heads + 1;
   Place<V, NEXT> p[U];
 #pragma unroll

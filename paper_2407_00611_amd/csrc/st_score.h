@@ -41,8 +41,8 @@ struct ScoreArgs {
   // (part_dk, part_dv + y B Sk Hkv D), and a last launch adds them up in order
   int32_t q_split, kv_split;
   float *part_dq, *part_dk, *part_dv;
-  // bf16, made by launch_score_rows: what every run of 32 rows sees (BlockSpan), [B, ceil(Sq G / 32)], and the statistics of its
-  // rows, kRowStats floats, [B, Hkv, ceil(Sq G / 32)]
+  // bf16, made by launch_score_rows, [B, Hkv, ceil(Sq G / 32)]: what every run of 32 rows sees (BlockSpan), and the statistics of its
+  // rows, kRowStats floats
   int4* blocks;
   float* rows;
 };

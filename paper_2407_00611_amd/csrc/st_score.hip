@@ -37,21 +37,22 @@ __global__ __launch_bounds__(256) void score_rows_kernel(const ScoreArgs a, int3
   const int64_t at = min(x, n - 1), bh = at / n_blk;
   const int j = (int)(at - bh * n_blk), b = (int)(bh / a.s.Hkv), hk = (int)(bh - (int64_t)b * a.s.Hkv);
   const int R = 32 * j + r, row = min(R, M - 1), i = row / G, h = hk * G + row - i * G;
-  const RowView see = row_view(a, b, i);
+  const int64_t stat = ((int64_t)b * a.s.Hq + h) * a.s.Sq + i;
+  const float lse = a.lse_in[stat], slope = a.slopes ? a.slopes[h] : 0.f;
+  RowView see = row_view(a, b, i);
+  const bool none = R >= M || lse == -INFINITY;        // a row that does not exist, or an empty one: P = 0
+  if (none) see.lo = see.hi = 0;
   BlockSpan w = span_of(see);
 #pragma unroll
   for (int d = 1; d < 32; d *= 2)
     w = span_join(w, BlockSpan{__shfl_xor(w.lo, d), __shfl_xor(w.hi, d), __shfl_xor(w.all_lo, d), __shfl_xor(w.all_hi, d)});
   if (x >= n) return;
-  if (r == 0 && hk == 0) a.blocks[(int64_t)b * n_blk + j] = make_int4(w.lo, w.hi, w.all_lo, w.all_hi);
-  const int64_t stat = ((int64_t)b * a.s.Hq + h) * a.s.Sq + i;
-  const float lse = a.lse_in[stat], slope = a.slopes ? a.slopes[h] : 0.f;
-  const bool none = R >= M || lse == -INFINITY;        // a row that does not exist, or an empty one: P = 0
+  if (r == 0) a.blocks[x] = make_int4(w.lo, w.hi, w.all_lo, w.all_hi);
   float* f = a.rows + x * kRowStats + r;
   f[32 * kRowLse] = none ? INFINITY : fmaf(slope, see.rest, lse) * kScoreLog2e;
   f[32 * kRowDelta] = -a.delta[stat];
-  f[32 * kRowLo] = __int_as_float(none ? 0 : see.lo);
-  f[32 * kRowHi] = __int_as_float(none ? 0 : see.hi);
+  f[32 * kRowLo] = __int_as_float(see.lo);
+  f[32 * kRowHi] = __int_as_float(see.hi);
   f[32 * kRowX] = (float)see.x;
   f[32 * kRowSlope] = slope * kScoreLog2e;
 }

@@ -652,8 +652,8 @@ __device__ __forceinline__ void score_dkv(const ScoreArgs& a, int block_x, int b
     for (int c0 = 0; c0 < kBlockList && at + c0 < mine; c0 += 256) {
       const int x = at + c0 + tid, j = share + x * n_share;
       int4 y = make_int4(0x7fffffff, 0, 0, 0);
-      if (x < mine) y = a.blocks[(int64_t)b * n_blk + j];
-      const bool seen = y.x < key_end && y.y > key0, all = seen && y.z <= key0 && y.w >= key_end && 32 * j + 32 <= M;
+      if (x < mine) y = a.blocks[((int64_t)b * s.Hkv + hk) * n_blk + j];
+      const bool seen = y.x < key_end && y.y > key0, all = seen && y.z <= key0 && y.w >= key_end;
       const uint64_t v_all = __ballot(all), v_edge = __ballot(seen && !all), before = ((uint64_t)1 << lane) - 1;
       if (lane == 0) {
         count[wave] = __popcll(v_all);

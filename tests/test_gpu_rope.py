@@ -176,4 +176,4 @@ def test_a_layer_from_projections_to_their_gradients():
         # fp32 throughout: 1e-5 as the attention's gradients, four of its steps
         y = torch.nan_to_num(y.grad)
         assert float((x.double() - y).norm()) <= 4e-5 * float(y.norm()), name
-    assert float((o.double() - ref)[inside].norm()) <= 1e-5 * float(ref[inside].norm())
+    assert float((o.double() - ref.detach())[inside].norm()) <= 1e-5 * float(ref.detach()[inside].norm())

@@ -26,7 +26,7 @@ def _fwd(d=None, m=None, q=None, k=None, v=None, o=PTR, lse=PTR, low=None, ws=No
     return lib.st_attn_score_fwd(C.byref(d), C.byref(m) if m else None, C.byref(q), C.byref(k), C.byref(v), o, lse, low, ws, size, None)
 
 
-def _bwd(d=None, m=None, flags=0, acc=(PTR, PTR, PTR), low=(None, None, None), ws=None, size=0, lse=PTR, q=None):
+def _bwd(d=None, m=None, flags=0, acc=(PTR, 2 * PTR, 3 * PTR), low=(None, None, None), ws=None, size=0, lse=PTR, q=None):
     d, q, x = d or _desc(), q or _view(), _view()
     return lib.st_attn_score_bwd(C.byref(d), C.byref(m) if m else None, C.byref(q), C.byref(x), C.byref(x), C.byref(x), lse, PTR, flags, *acc, *low,
                                  ws, size, None)
@@ -52,9 +52,10 @@ def test_forward_outputs():
 
 def test_backward_outputs():
     assert _bwd(flags=2) == 1 and _bwd(lse=None) == 1
-    assert _bwd(acc=(None, PTR, PTR), low=(PTR, None, None)) == 1        # nothing to add to
-    assert _bwd(flags=1, acc=(PTR, None, PTR)) == 1 and _bwd(flags=1, low=(None, PTR, None)) == 1
-    assert _bwd(acc=(PTR, PTR + 8, PTR)) == 3 and _bwd(low=(0x20008, None, None)) == 3
+    assert _bwd(acc=(None, 2 * PTR, 3 * PTR), low=(PTR, None, None)) == 1        # nothing to add to
+    assert _bwd(flags=1, acc=(PTR, None, 3 * PTR)) == 1 and _bwd(flags=1, low=(None, 2 * PTR, None)) == 1
+    assert _bwd(acc=(PTR, PTR, 3 * PTR)) == 1 and _bwd(low=(None, 3 * PTR, None)) == 1 and _bwd(low=(None, 5 * PTR, 5 * PTR)) == 1   # shared memory
+    assert _bwd(acc=(PTR, PTR + 8, 3 * PTR)) == 3 and _bwd(low=(0x20008, None, None)) == 3
 
 
 def test_workspaces():
@@ -101,7 +102,7 @@ def test_rope_descriptors():
                     dict(axis_pairs=(32, 32), n_axes=2), dict(seg=4, offset2=9), dict(seg=2, offset2=1)):
             assert call(_rope(**bad)) == 1, bad
         assert call(_rope(D=260, rot=64, axis_pairs=(32,))) == 2 and call(_rope(D=12, rot=0, axis_pairs=(0,))) == 2
-        assert call(_rope(S=1 << 26)) == 2 and call(_rope(Hq=70000)) == 2
+        assert call(_rope(S=1 << 26)) == 2 and call(_rope(Hq=70000)) == 2 and call(_rope(Hq=16000, Hkv=400)) == 2
         assert call(freq=None) == 1 and call(freq=PTR + 4) == 3 and call(pos=PTR + 2) == 3 and call(wq=PTR + 4) == 3
         assert call(_rope(seg=2, offset2=9), pos=PTR) == 1
         assert call(_rope(norm=0), wq=PTR) == 1
