@@ -5,7 +5,7 @@ from test_kernel_resources import _kernels
 
 def test_the_kernels_of_modified_scores_and_rotations_stay_in_registers():
     kernels = _kernels()
-    # capped and biased scores of head size 128 have three registers waiting in memory, none in a loop; in fp32 the accumulators of
+    # capped and biased scores of head size 128 have an address waiting in memory, read outside the inner loops; in fp32 the accumulators of
     # both gradients of 32 keys of 160 values and more exceed the registers, as those of the plain scores do
     for part, most in (("score_fwd_kernel", 0), ("score_bwd_kernel", 16), ("score_rows_kernel", 0), ("score_combine_kernel", 0),
                        ("score_add_parts_kernel", 0), ("mask_spans_kernel", 0), ("score_fwd_f32_kernelILi128", 0), ("score_dq_f32_kernelILi128", 0),
