@@ -22,22 +22,18 @@ constexpr float kSumMost = 4096.f;
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
-// Whether 32 rows of an LDS tile hold an infinity or NaN: their products with zeros are NaN then.  Eight matrix instructions, where a
-// look at every operand's bits is some 380 others; operands are scrubbed only where it is true.
+// Whether 32 rows of an LDS tile hold an infinity or NaN: their products with zeros are NaN then, whatever place a matrix instruction
+// takes an operand's values for.  Eight short ones, where a look at every operand's bits is some 96 others; operands are made finite
+// only where it is true.
 template <int D>
 __device__ __forceinline__ bool not_finite(const LaneReads<D>& reads, uint32_t tile) {
-  f32x16 z;
-#pragma unroll
-  for (int v = 0; v < 16; ++v) z[v] = 0.f;
+  f32x4 z = {0.f, 0.f, 0.f, 0.f};
   const bf16x8 zero = __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
 #pragma unroll
   for (int m = 0; m < 2; ++m)
 #pragma unroll
-    for (int db = 0; db < D / 32; ++db) z = mfma32(reads.frag_tr(tile, 16 * m, db), zero, z);
-  float sum = 0.f;
-#pragma unroll
-  for (int v = 0; v < 16; ++v) sum += z[v];
-  return __any(sum != 0.f);
+    for (int db = 0; db < D / 32; ++db) z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(reads.frag_tr(tile, 16 * m, db), zero, z, 0, 0, 0);
+  return __any((z[0] + z[1]) + (z[2] + z[3]) != 0.f);
 }
 
 // Tiles of 64 keys that a query tile's workgroup walks: those that the hull of its rows touches.  The general ones come first (a
@@ -299,19 +295,21 @@ __global__ __launch_bounds__(256, 2) void score_fwd_kernel(const ScoreArgs a) {
     if (n + 1 < walk.n1) issue_load(n + 1, buf ^ 1);
     const int key0 = walk.tile(n) * kBN;
     const uint32_t ktile = smem_addr + buf * 2 * kTile;
-    if (w.lo < key0 + kBN && w.hi > key0)              // some row of this wavefront sees some key of the tile
-#pragma unroll 1
+    if (w.lo < key0 + kBN && w.hi > key0) {            // some row of this wavefront sees some key of the tile
+      Block y[KB];
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) products(y[kb], ktile + 32 * kb * D * 2);
+      const bool dirty = (w.all_lo > key0 || w.all_hi < key0 + kBN) &&
+                         (not_finite<D>(reads, ktile + kTile) || not_finite<D>(reads, ktile + kTile + 32 * D * 2));
+      bad = bad || dirty;
+#pragma unroll
       for (int kb = 0; kb < KB; ++kb) {
         const uint32_t vblock = ktile + kTile + 32 * kb * D * 2;
-        const int block0 = key0 + 32 * kb;
-        Block y;
-        products(y, ktile + 32 * kb * D * 2);
-        softmax(std::true_type(), y, block0);
-        const bool dirty = (w.all_lo > block0 || w.all_hi < block0 + 32) && not_finite<D>(reads, vblock);
-        bad = bad || dirty;
-        if (__builtin_expect(dirty, 0)) contract(std::true_type(), y, vblock);
-        else contract(std::false_type(), y, vblock);
+        softmax(std::true_type(), y[kb], key0 + 32 * kb);
+        if (__builtin_expect(dirty, 0)) contract(std::true_type(), y[kb], vblock);
+        else contract(std::false_type(), y[kb], vblock);
       }
+    }
     landed();
     buf ^= 1;
   }
