@@ -48,9 +48,10 @@ st::ScoreArgs score_args(const st_block_desc* d, const st_score* m) {
 
 // How the launches are split and where in the workspace their sums lie (byte offsets).
 constexpr int64_t kSplitBytesMost = (int64_t)256 << 20;
-// A share is at least so many products (16 blocks of 32 rows): 12/4 heads x 2 x 1000 rows 44 + 10 us so, 55 + 8 with twice as many, 128
-// without shares.
-constexpr int64_t kLeastShare = 64;
+// A share is at least so many products of a tile; fewer where that leaves compute units without a workgroup.  Forward and backward of
+// 12/4 heads x 2 x 1000 packed rows take 78 us with 96, 83 with 64 and 80 with 128; of 16/4 x 200, too few for the chip, 41 us with
+// 32, 50 with 64.
+constexpr int64_t kLeastShare = 96, kLeastShareOfFew = 32;
 struct ScorePlan {
   int n_split, q_split, kv_split;
   size_t lse, dk, dv, blocks, rows, bytes;
@@ -85,13 +86,17 @@ ScorePlan bwd_plan(const st::Shape& s, int dtype, bool spans) {
   const int64_t keys = bf16 ? ((int64_t)s.Sk + st::kScoreKeys - 1) / st::kScoreKeys * s.Hkv * s.B : key_blocks * s.Hkv * s.B;
   const int64_t n_q = (int64_t)s.B * s.Sq * s.Hq * s.D * 4, n_kv = (int64_t)s.B * s.Sk * s.Hkv * s.D * 4;
   const int64_t kv_len = 4 * row_blocks, q_len = 3 * key_blocks;
-  const int64_t each = (keys * kv_len + rows * q_len) / 512, least = bf16 ? kLeastShare : 8;
+  const int64_t each = (keys * kv_len + rows * q_len) / 512;
   const int quarters = !bf16 ? 4 : spans || (s.causal && s.q_seg <= 0) ? 2 : s.causal ? 3 : 4;
   ScorePlan p{};
   auto shares = [](int64_t len, int64_t most, int64_t eighths) { return (int)std::min<int64_t>(std::max<int64_t>((8 * len + eighths * most) / (8 * most), 1), 16); };
-  p.q_split = shares(q_len, std::max(each, least), 4);
+  auto split = [&](int64_t least) {
+    p.q_split = shares(q_len, std::max(each, least), 4);
+    p.kv_split = shares(kv_len, std::max(each * quarters / 4, least), quarters < 4 ? 7 : 4);
+  };
+  split(bf16 ? kLeastShare : 8);
+  if (bf16 && keys * p.kv_split + rows * p.q_split < 256) split(kLeastShareOfFew);
   while (p.q_split > 1 && p.q_split * n_q > kSplitBytesMost) --p.q_split;
-  p.kv_split = shares(kv_len, std::max(each * quarters / 4, least), quarters < 4 ? 7 : 4);
   while (p.kv_split > 1 && p.kv_split * n_kv * 2 > kSplitBytesMost) --p.kv_split;
   p.dk = p.q_split > 1 ? align_up((size_t)(p.q_split * n_q), 256) : 0;
   const size_t kv = p.kv_split > 1 ? align_up((size_t)(p.kv_split * n_kv), 256) : 0;
@@ -183,7 +188,7 @@ st_status st_mask_spans(int32_t B, int32_t Sq, int64_t q_offset, int32_t q_seg, 
 size_t st_attn_score_workspace_bytes(const st_block_desc* d, const st_score* m, int32_t backward) {
   if (check_score(d, m) != ST_OK || (int64_t)d->B * d->Sq == 0) return 0;
   const st::Shape s = shape_of(d);
-  return backward ? bwd_plan(s, d->dtype, true).bytes : fwd_plan(s, d->dtype).bytes;   // (with spans, which need the most)
+  return backward ? std::max(bwd_plan(s, d->dtype, true).bytes, bwd_plan(s, d->dtype, false).bytes) : fwd_plan(s, d->dtype).bytes;
 }
 
 st_status st_attn_score_fwd(const st_block_desc* d, const st_score* m, const st_tensor* q, const st_tensor* k, const st_tensor* v,
