@@ -18,9 +18,24 @@ __device__ __forceinline__ float score_of(float u, const ScoreArgs& a, float& f)
   return a.cap * t;
 }
 
+// A piece of a tile that a mask edge crosses, with its infinities and NaN taken as zero; true if it had some.  (Looking at the tile
+// once more beforehand was a chain of loads: 8/2 heads x 500 rows of 80, forward and backward, 95 us, 89 so.)
+template <int DP, int N>
+__device__ __forceinline__ bool make_finite(Piece<N>& f) {
+  bool bad = false;
+#pragma unroll
+  for (int k = 0; k < piece_rows<DP, N>() * (DP / 32); ++k) {
+    const bool fine = finite(f.x[k]);
+    bad = bad || !fine;
+    f.x[k] = fine ? f.x[k] : 0.f;
+  }
+  return bad;
+}
+
 template <int DP, bool FULL, bool CAP>
 __global__ __launch_bounds__(waves<DP>() * 64) void score_fwd_f32_kernel(const ScoreArgs a) {
-  constexpr int NW = waves<DP>(), DB = DP / 32, N = 32, NR = row_pieces<DP, N>(), NC = col_pieces<DP, N>();
+  constexpr int NW = waves<DP>(), DB = DP / 32, N = DP == 128 ? 16 : 32, R = DP < 128 ? 3 : DP == 128 ? 4 : 2;
+  constexpr int NR = row_pieces<DP, N>(), NC = col_pieces<DP, N>(), kPieces = NR + NC;
   __shared__ __attribute__((aligned(16))) float qs[kT * lds_stride<DP>()];
   __shared__ float fold[NW / 2 * DB * 16 * 64];
   __shared__ float fold_m[NW / 2 * 64], fold_l[NW / 2 * 64];
@@ -53,20 +68,22 @@ __global__ __launch_bounds__(waves<DP>() * 64) void score_fwd_f32_kernel(const S
     const float *kb = k0 + (int64_t)key0 * a.k.ss, *vb = v0 + (int64_t)key0 * a.v.ss;
     const bool masked = w.all_lo > key0 || w.all_hi < key0 + kT;
     const float* krow = kb + (int64_t)min(r, limit - 1) * a.k.ss;
-    Piece<N> f[2];
+    Piece<N> f[R];
     auto load = [&](int x) {
-      if (x < NR) load_rows<DP, FULL>(f[x & 1], krow, x, s.D, g);
-      else load_cols<DP, FULL>(f[x & 1], vb, a.v.ss, limit, x - NR, s.D, r, g);
+      if (x >= kPieces) return;
+      if (x < NR) load_rows<DP, FULL>(f[x % R], krow, x, s.D, g);
+      else load_cols<DP, FULL>(f[x % R], vb, a.v.ss, limit, x - NR, s.D, r, g);
       __builtin_amdgcn_sched_barrier(0);
     };
     f32x16 p;
 #pragma unroll
     for (int v = 0; v < 16; ++v) p[v] = 0.f;
-    load(0);
+#pragma unroll
+    for (int x = 0; x < R - 1; ++x) load(x);
 #pragma unroll
     for (int x = 0; x < NR; ++x) {
-      load(x + 1);
-      contract_d<DP>(p, f[x & 1], qs, x, r, g);
+      load(x + R - 1);
+      contract_d<DP>(p, f[x % R], qs, x, r, g);
     }
     float mx = -INFINITY;
 #pragma unroll
@@ -94,14 +111,14 @@ __global__ __launch_bounds__(waves<DP>() * 64) void score_fwd_f32_kernel(const S
 #pragma unroll
         for (int v = 0; v < 16; ++v) acc[db][v] *= alpha;
     }
-    const bool dirty = masked && tile_dirty(vb, a.v.ss, limit, s.D, lane);
-    if (dirty) any_dirty = 1;
+    bool bad = false;
 #pragma unroll
-    for (int x = NR; x < NR + NC; ++x) {
-      if (x + 1 < NR + NC) load(x + 1);
-      if (dirty) scrub(f[x & 1]);
-      contract_rows<DP>(acc, f[x & 1], p, x - NR);
+    for (int x = NR; x < kPieces; ++x) {
+      load(x + R - 1);
+      if (masked) bad = make_finite<DP>(f[x % R]) || bad;
+      contract_rows<DP>(acc, f[x % R], p, x - NR);
     }
+    if (bad) any_dirty = 1;
   }
   for (int y = NW / 2; y > 0; y /= 2) {
     if (wave >= y && wave < 2 * y) {
@@ -152,7 +169,8 @@ __global__ __launch_bounds__(waves<DP>() * 64) void score_fwd_f32_kernel(const S
 // ---------------------------------------------------------------- dQ
 template <int DP, bool FULL, bool CAP>
 __global__ __launch_bounds__(waves<DP>() * 64) void score_dq_f32_kernel(const ScoreArgs a) {
-  constexpr int NW = waves<DP>(), DB = DP / 32, N = 32, NR = row_pieces<DP, N>(), NC = col_pieces<DP, N>();
+  constexpr int NW = waves<DP>(), DB = DP / 32, N = DP == 128 ? 16 : 32, R = DP < 128 ? 3 : DP == 128 ? 4 : 2;
+  constexpr int NR = row_pieces<DP, N>(), NC = col_pieces<DP, N>(), kPieces = 2 * NR + NC;
   __shared__ __attribute__((aligned(16))) float qs[kT * lds_stride<DP>()];
   __shared__ __attribute__((aligned(16))) float dos[kT * lds_stride<DP>()];
   __shared__ float fold[NW / 2 * DB * 16 * 64];
@@ -189,21 +207,23 @@ __global__ __launch_bounds__(waves<DP>() * 64) void score_dq_f32_kernel(const Sc
     const bool masked = w.all_lo > key0 || w.all_hi < key0 + kT;
     const float* krow = kb + (int64_t)min(r, limit - 1) * a.k.ss;
     const float* vrow = vb + (int64_t)min(r, limit - 1) * a.v.ss;
-    Piece<N> f[2];
+    Piece<N> f[R];
     auto load = [&](int x) {
-      if (x < 2 * NR) load_rows<DP, FULL>(f[x & 1], x < NR ? krow : vrow, x < NR ? x : x - NR, s.D, g);
-      else load_cols<DP, FULL>(f[x & 1], kb, a.k.ss, limit, x - 2 * NR, s.D, r, g);
+      if (x >= kPieces) return;
+      if (x < 2 * NR) load_rows<DP, FULL>(f[x % R], x < NR ? krow : vrow, x < NR ? x : x - NR, s.D, g);
+      else load_cols<DP, FULL>(f[x % R], kb, a.k.ss, limit, x - 2 * NR, s.D, r, g);
       __builtin_amdgcn_sched_barrier(0);
     };
     f32x16 p, ds;
 #pragma unroll
     for (int v = 0; v < 16; ++v) p[v] = ds[v] = 0.f;
-    load(0);
+#pragma unroll
+    for (int x = 0; x < R - 1; ++x) load(x);
 #pragma unroll
     for (int x = 0; x < 2 * NR; ++x) {
-      load(x + 1);
-      if (x < NR) contract_d<DP>(p, f[x & 1], qs, x, r, g);
-      else contract_d<DP>(ds, f[x & 1], dos, x - NR, r, g);
+      load(x + R - 1);
+      if (x < NR) contract_d<DP>(p, f[x % R], qs, x, r, g);
+      else contract_d<DP>(ds, f[x % R], dos, x - NR, r, g);
     }
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
@@ -212,14 +232,14 @@ __global__ __launch_bounds__(waves<DP>() * 64) void score_dq_f32_kernel(const Sc
       const float e = fmaf(-slope, fabsf((float)(see.x - key)), score_of<CAP>(p[v], a, f2));
       ds[v] = key >= see.lo && key < see.hi ? expf(e - lse) * (ds[v] - dl) * f2 : 0.f;
     }
-    const bool dirty = masked && tile_dirty(kb, a.k.ss, limit, s.D, lane);
-    if (dirty) any_dirty = 1;
+    bool bad = false;
 #pragma unroll
-    for (int x = 2 * NR; x < 2 * NR + NC; ++x) {
-      if (x + 1 < 2 * NR + NC) load(x + 1);
-      if (dirty) scrub(f[x & 1]);
-      contract_rows<DP>(acc, f[x & 1], ds, x - 2 * NR);
+    for (int x = 2 * NR; x < kPieces; ++x) {
+      load(x + R - 1);
+      if (masked) bad = make_finite<DP>(f[x % R]) || bad;
+      contract_rows<DP>(acc, f[x % R], ds, x - 2 * NR);
     }
+    if (bad) any_dirty = 1;
   }
   for (int y = NW / 2; y > 0; y /= 2) {
     if (wave >= y && wave < 2 * y) put_acc(fold + (wave - y) * DB * 16 * 64, acc, lane);
@@ -258,7 +278,8 @@ __global__ __launch_bounds__(waves<DP>() * 64) void score_dq_f32_kernel(const Sc
 // block = key tile + ceil(Sk / 32) (KV head + Hkv batch entry); share y takes every kv_split-th group of a wavefront each's pairs
 template <int DP, bool FULL, bool CAP>
 __global__ __launch_bounds__(waves<DP>() * 64) void score_dkv_f32_kernel(const ScoreArgs a) {
-  constexpr int NW = waves<DP>(), DB = DP / 32, N = DP < 128 ? 32 : 16, NR = row_pieces<DP, N>(), NC = col_pieces<DP, N>();
+  constexpr int NW = waves<DP>(), DB = DP / 32, N = 16, R = DP < 128 ? 4 : 2;
+  constexpr int NR = row_pieces<DP, N>(), NC = col_pieces<DP, N>(), kPieces = 2 * NR + 2 * NC;
   constexpr int kStat = 6 * kT;                              // of every row lse, Delta, lo, hi, x
   __shared__ __attribute__((aligned(16))) float ks[kT * lds_stride<DP>()];
   __shared__ __attribute__((aligned(16))) float vs[kT * lds_stride<DP>()];
@@ -297,22 +318,24 @@ __global__ __launch_bounds__(waves<DP>() * 64) void score_dkv_f32_kernel(const S
     const float* db_ = (const float*)a.d_o.ptr + b * a.d_o.sb + h * a.d_o.sh + (int64_t)i0 * a.d_o.ss;
     const float* qrow = qb + (int64_t)min(r, limit - 1) * a.q.ss;
     const float* drow = db_ + (int64_t)min(r, limit - 1) * a.d_o.ss;
-    Piece<N> f[2];
+    Piece<N> f[R];
     auto load = [&](int x) {
-      if (x < 2 * NR) load_rows<DP, FULL>(f[x & 1], x < NR ? qrow : drow, x < NR ? x : x - NR, s.D, g);
-      else if (x < 2 * NR + NC) load_cols<DP, FULL>(f[x & 1], db_, a.d_o.ss, limit, x - 2 * NR, s.D, r, g);
-      else load_cols<DP, FULL>(f[x & 1], qb, a.q.ss, limit, x - 2 * NR - NC, s.D, r, g);
+      if (x >= kPieces) return;
+      if (x < 2 * NR) load_rows<DP, FULL>(f[x % R], x < NR ? qrow : drow, x < NR ? x : x - NR, s.D, g);
+      else if (x < 2 * NR + NC) load_cols<DP, FULL>(f[x % R], db_, a.d_o.ss, limit, x - 2 * NR, s.D, r, g);
+      else load_cols<DP, FULL>(f[x % R], qb, a.q.ss, limit, x - 2 * NR - NC, s.D, r, g);
       __builtin_amdgcn_sched_barrier(0);
     };
     f32x16 p, ds;
 #pragma unroll
     for (int v = 0; v < 16; ++v) p[v] = ds[v] = 0.f;
-    load(0);
+#pragma unroll
+    for (int x = 0; x < R - 1; ++x) load(x);
 #pragma unroll
     for (int x = 0; x < 2 * NR; ++x) {
-      load(x + 1);
-      if (x < NR) contract_d<DP>(p, f[x & 1], ks, x, r, g);
-      else contract_d<DP>(ds, f[x & 1], vs, x - NR, r, g);
+      load(x + R - 1);
+      if (x < NR) contract_d<DP>(p, f[x % R], ks, x, r, g);
+      else contract_d<DP>(ds, f[x % R], vs, x - NR, r, g);
     }
     if (g == 0) {
       st[r] = fmaf(slope, see.rest, lse_row);
@@ -333,15 +356,15 @@ __global__ __launch_bounds__(waves<DP>() * 64) void score_dkv_f32_kernel(const S
       ds[v] = live ? p[v] * (ds[v] - st[kT + row]) * f2 : 0.f;
     }
     __builtin_amdgcn_wave_barrier();
-    const bool dirty = masked && (tile_dirty(db_, a.d_o.ss, limit, s.D, lane) || tile_dirty(qb, a.q.ss, limit, s.D, lane));
-    if (dirty) any_dirty = 1;
+    bool bad = false;
 #pragma unroll
-    for (int x = 2 * NR; x < 2 * NR + 2 * NC; ++x) {
-      if (x + 1 < 2 * NR + 2 * NC) load(x + 1);
-      if (dirty) scrub(f[x & 1]);
-      if (x < 2 * NR + NC) contract_rows<DP>(acc_v, f[x & 1], p, x - 2 * NR);
-      else contract_rows<DP>(acc_k, f[x & 1], ds, x - 2 * NR - NC);
+    for (int x = 2 * NR; x < kPieces; ++x) {
+      load(x + R - 1);
+      if (masked) bad = make_finite<DP>(f[x % R]) || bad;
+      if (x < 2 * NR + NC) contract_rows<DP>(acc_v, f[x % R], p, x - 2 * NR);
+      else contract_rows<DP>(acc_k, f[x % R], ds, x - 2 * NR - NC);
     }
+    if (bad) any_dirty = 1;
   }
   for (int n = NW / 2; n > 0; n /= 2) {
     float* slot = fold + (wave - (wave >= n ? n : 0)) * DB * 16 * 64;
