@@ -30,7 +30,8 @@ __global__ __launch_bounds__(256) void mask_spans_kernel(const Shape s, const in
   *reinterpret_cast<longlong2*>(spans + 2 * x) = w;
 }
 
-// half a wavefront per run of 32 packed rows of a KV head
+// Half a wavefront per run of 32 packed rows of a KV head: what every key tile needs to know of them, made once (2 us of kernel for
+// 32/8 heads x 8192 rows; every key tile reads 128 bytes a row otherwise strewn over lse, Delta and spans).
 __global__ __launch_bounds__(256) void score_rows_kernel(const ScoreArgs a, int32_t n_blk) {
   const int64_t x = (int64_t)blockIdx.x * 8 + threadIdx.x / 32, n = (int64_t)a.s.B * a.s.Hkv * n_blk;
   const int r = threadIdx.x & 31, G = a.s.Hq / a.s.Hkv, M = a.s.Sq * G;
@@ -109,7 +110,8 @@ struct PartSums {
   PartSum x[3];
   int32_t assign, bf16;
 };
-// four neighbouring floats a thread, in the order of the shares
+// Four neighbouring floats a thread, in the order of the shares: memory-bound (two shares of dK and dV of 8 KV heads x 8192 keys of 128,
+// to bf16: 33 us, 5 TB/s).
 __global__ __launch_bounds__(256) void score_add_parts_kernel(const PartSums a) {
   const PartSum& p = a.x[blockIdx.y];
   for (int64_t e = 4 * ((int64_t)blockIdx.x * 256 + threadIdx.x); e < p.floats && p.part; e += (int64_t)gridDim.x * 1024) {

@@ -160,7 +160,16 @@ struct TileLoads {
 };
 
 // =============================================================================================
-// forward: 128 rows per workgroup, 32 per wavefront; lane = row (C layout column)
+// Forward: S^T = K Q^T and O^T += V^T P^T, so that a lane has one row (C layout column) of a wavefront's 32: its reference, sum and
+// span are registers, and the exponentials of S^T are the second product's operand as they stand.  128 rows a workgroup, packed over
+// the heads of a KV head, two workgroups a compute unit at head size 128, three at 64.  One pass over the keys: O and the row sum
+// against a reference m, O = acc / l, lse = m ln 2 + ln l.
+//
+// Bound by the matrix units and the vector unit together, whose work hardly overlaps with two wavefronts on a SIMD (two runs of rows,
+// 32/8 heads x 4096 x 2048 keys: busy 42 % and 61 % of the time), and by power: 32/8 heads x 8192 x 4096 keys of 128 take 590 us,
+// 930 TFLOP/s at 1.8 GHz (capped 650 us; 24 or 32 heads of 64, vector unit busy 82 %: 900 TFLOP/s).  Wavefronts of 64 rows, half the
+// operand reads a product, leave one on a SIMD and took 951 us; products and softmax interleaved by hand gained 3 % there and
+// nothing where masks are.  Packed images (24 heads of 64 x 8192 rows) 109 us, prompts with prefixes (32/8 x 4096) 50 us.
 // =============================================================================================
 template <int D, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, 2) void score_fwd_kernel(const ScoreArgs a) {
@@ -372,7 +381,8 @@ __global__ __launch_bounds__(256, 2) void score_fwd_kernel(const ScoreArgs a) {
 }
 
 // =============================================================================================
-// dQ: as the forward, with dP beside S
+// dQ: as the forward, with dP^T = V dO^T beside S^T and P from the final lse: dQ^T += K^T dU^T.  Seven contractions for both passes of
+// the backward, where five would do in one: dQ of one pass would be added up by atomics, in no order.
 // =============================================================================================
 template <int D, bool CAP, bool BIAS>
 __device__ __forceinline__ void score_dq(const ScoreArgs& a, int block_x, int blocks, int share, char* smem_raw) {
@@ -518,9 +528,11 @@ __device__ __forceinline__ void score_dq(const ScoreArgs& a, int block_x, int bl
 }
 
 // =============================================================================================
-// dK, dV: 128 keys of one KV head per workgroup, 32 per wavefront; the group's rows stream by in blocks of 32.  lane = key (C layout
-// column), registers = 16 rows.  K fragments stay in registers, V in LDS, so that two workgroups fit a compute unit: one's softmax
-// runs under the other's products.
+// dK, dV: 128 keys of one KV head per workgroup, 32 per wavefront; the group's rows stream by in blocks of 32, so that the gradients
+// of shared heads are sums in registers.  lane = key (C layout column), registers = 16 rows.  K fragments stay in registers, V in LDS,
+// so that two workgroups fit a compute unit: one's softmax runs under the other's products (with V in registers too and one workgroup:
+// 516 us for 32/8 heads x 4096 x 2048 keys, biased; 301 so, with rows and statistics straight to LDS).  Both gradients and dQ of 32/8 heads x 8192 x 4096 keys of 128: 1.9 ms, 1010
+// TFLOP/s of the seven contractions (capped 2.05 ms; 32 heads of 64: 1.0 ms, 960).
 // =============================================================================================
 constexpr int kBlockList = 512;      // row blocks that a workgroup looks through at a time
 
