@@ -114,14 +114,17 @@ __device__ __forceinline__ int ordered_tile(const ScoreArgs& a, int b, int n_qt,
 
 // Block id -> (row tile, KV head, batch entry).  Every XCD has a contiguous range of the (KV head, batch entry) pairs, whose keys and
 // values stay in its L2; under a causal mask the later tiles, which see more, come first.
-constexpr int kOrderFrom = 512;      // workgroups that the chip holds at once: with no more, their order says nothing
+// Workgroups whose order is worth its making, 2 us of each: more than the chip holds at once, and so few turns of them that a long
+// last one shows.  24 heads of 64 x 8192 packed rows, 1536 workgroups, 155 us without an order, 111 with one; a window of 64 keys on
+// 32/8 heads x 16384 rows, 4096 workgroups, 119 without, 137 with one.
+constexpr int kOrderFrom = 512, kOrderUpTo = 2048;
 __device__ __forceinline__ void tile_block(const ScoreArgs& a, int block, int blocks, int n_qt, int* lds, int& qt, int& hk, int& b) {
   int hb;
   qtile_block(block, blocks, n_qt, a.s.causal || a.spans, qt, hb);
   hk = uniform(hb % a.s.Hkv);
   b = uniform(hb / a.s.Hkv);
   qt = uniform(qt);
-  if (a.spans && blocks > kOrderFrom) qt = ordered_tile(a, b, n_qt, n_qt - 1 - qt, lds);
+  if (a.spans && blocks > kOrderFrom && blocks <= kOrderUpTo) qt = ordered_tile(a, b, n_qt, n_qt - 1 - qt, lds);
 }
 
 // what the rows of the workgroup see together, from what those of each wavefront do; hull: 6 x 4 ints of LDS
@@ -169,7 +172,8 @@ struct TileLoads {
 // 32/8 heads x 4096 x 2048 keys: busy 42 % and 61 % of the time), and by power: 32/8 heads x 8192 x 4096 keys of 128 take 590 us,
 // 930 TFLOP/s at 1.8 GHz (capped 650 us; 24 or 32 heads of 64, vector unit busy 82 %: 900 TFLOP/s).  Wavefronts of 64 rows, half the
 // operand reads a product, leave one on a SIMD and took 951 us; products and softmax interleaved by hand gained 3 % there and
-// nothing where masks are.  Packed images (24 heads of 64 x 8192 rows) 109 us, prompts with prefixes (32/8 x 4096) 50 us.
+// nothing where masks are.  Packed images (24 heads of 64 x 8192 rows) take 111 us, prompts with prefixes (32/8
+// x 4096) 53 us, spans included.
 // =============================================================================================
 template <int D, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, 2) void score_fwd_kernel(const ScoreArgs a) {
