@@ -166,3 +166,31 @@ def test_values_that_are_not_finite_in_tiles_with_an_edge(D, value):
             assert not torch.isfinite(dv[0, seen][:, 0]).any() and not torch.isfinite(dq[0, at, 1]).any() and torch.equal(o, clean[0])
         else:
             assert not torch.isfinite(dk[0, seen][:, 0]).any() and not torch.isfinite(dq[0, at, 1]).any()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_strides_that_pass_32_bits(dtype):
+    """Heads of a buffer of more than 2^31 elements: as those of dense copies, bit for bit."""
+    S, heads, D, Sq = 70000, 264, 128, 40
+    big = torch.empty((1, S, heads, D), dtype=dtype, device="cuda")
+    assert big.numel() > 2 ** 31
+    g = torch.Generator(device="cuda").manual_seed(4)
+    places = {"q": (0, 2), "k": (10, 11), "v": (262, 263), "d": (260, 262)}
+    for a, b in places.values():
+        big[:, :, a:b] = torch.randn((1, S, b - a, D), generator=g, device="cuda").to(dtype)
+    wide = {n: big[:, :, a:b] for n, (a, b) in places.items()}
+    wide["q"], wide["d"] = wide["q"][:, S - Sq:], wide["d"][:, S - Sq:]
+    dense = {n: t.contiguous() for n, t in wide.items()}
+    freq = (10000.0 ** (-torch.arange(64, dtype=torch.float64) / 64)).cuda()
+    spans = st.st_mask_spans(torch.tensor([[3, 30000, S - 20, S]]).cuda(), Sq, S - Sq, True)
+    runs = []
+    for x in (wide, dense):
+        lse = st.st_attn_score_fwd(x["q"], x["k"], x["v"], S - Sq, 0, True, 0.1, softcap=9.0)[1]
+        o = st.st_attn_score_fwd(x["q"], x["k"], x["v"], S - Sq, 0, False, 0.1, spans=spans, lowp=True)
+        delta = st.st_attn_delta(x["d"], o[0])
+        runs.append((lse,) + tuple(o) + tuple(st.st_attn_score_bwd(x["q"], x["k"], x["v"], x["d"], o[1], delta, S - Sq, 0, False, 0.1, spans=spans)) +
+                    tuple(st.st_qk_rope_fwd(x["q"], x["v"][:, S - Sq:], freq=freq, offset=S - Sq)))
+    for a, b in zip(*runs):
+        assert torch.equal(a, b)
+    dk = runs[0][4]                                  # what the spans leave: the last two documents' keys from row S - 40 on
+    assert float(dk[0, 30000:].float().norm()) > 0 and not dk[0, :30000].any()
