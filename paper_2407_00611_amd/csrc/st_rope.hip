@@ -4,8 +4,8 @@
 //   (a, b) -> (a cos t - b sin t, a sin t + b cos t),  t = p f    for each rotated pair, p its axis' position, f its frequency
 //   backward  dn = R^T dy,  g = dn w,  dx = r (g - xh mean(g xh)),  dw = sum dn xh,  xh = x r,  r = rsqrt(mean(x^2) + eps)
 //
-// Bounded by HBM: x is read and y written once (24 heads of 64 x 16384 tokens, three axes: 201 MB in 45 us, 4.5 TB/s; the gradients of
-// 32/8 heads x 4096 tokens behind their forward: 252 MB in 59 us).  A token's angles serve all of its heads: a workgroup takes some tokens, makes their
+// Bounded by HBM: x is read and y written once (24 heads of 64 x 16384 tokens, three axes: 201 MB in 40.5 us, 5.0 TB/s; the gradients of
+// 32/8 heads x 4096 tokens behind their forward: 252 MB in 55 us).  A token's angles serve all of its heads: a workgroup takes some tokens, makes their
 // sines and cosines once (LDS), and its lanes then take the heads' rows.  Angles of far positions need more than fp32: p f / 2 pi is
 // taken in fp64 and only its fraction rounded (positions below 2^31: 1e-7 of a turn at most, from the fp64 frequency itself).
 //
@@ -64,9 +64,11 @@ __device__ __forceinline__ Vec<V> load(const float* p) {
   }
   return y;
 }
+// Results are said to be read by nobody soon: that leaves the caches to the inputs, 24 heads of 64 x 16384 tokens 45 us, 40.5 so, and an
+// attention that reads them next is none the slower.  (Inputs loaded so: 52 us.)
 template <int V>
 __device__ __forceinline__ void store(uint16_t* p, const Vec<V>& y) {
-  if constexpr (V == 8) *reinterpret_cast<u32x4*>(p) = u32x4{pack_bf16(y.x[0], y.x[1]), pack_bf16(y.x[2], y.x[3]), pack_bf16(y.x[4], y.x[5]), pack_bf16(y.x[6], y.x[7])};
+  if constexpr (V == 8) __builtin_nontemporal_store(u32x4{pack_bf16(y.x[0], y.x[1]), pack_bf16(y.x[2], y.x[3]), pack_bf16(y.x[4], y.x[5]), pack_bf16(y.x[6], y.x[7])}, reinterpret_cast<u32x4*>(p));
   else if constexpr (V == 4) *reinterpret_cast<u32x2*>(p) = u32x2{pack_bf16(y.x[0], y.x[1]), pack_bf16(y.x[2], y.x[3])};
   else if constexpr (V == 2) *reinterpret_cast<uint32_t*>(p) = pack_bf16(y.x[0], y.x[1]);
   else *p = (uint16_t)pack_bf16(y.x[0], y.x[0]);
@@ -75,7 +77,7 @@ template <int V>
 __device__ __forceinline__ void store(float* p, const Vec<V>& y) {
   if constexpr (V >= 4) {
 #pragma unroll
-    for (int j = 0; j < V / 4; ++j) *reinterpret_cast<f32x4*>(p + 4 * j) = f32x4{y.x[4 * j], y.x[4 * j + 1], y.x[4 * j + 2], y.x[4 * j + 3]};
+    for (int j = 0; j < V / 4; ++j) __builtin_nontemporal_store(f32x4{y.x[4 * j], y.x[4 * j + 1], y.x[4 * j + 2], y.x[4 * j + 3]}, reinterpret_cast<f32x4*>(p + 4 * j));
   } else {
 #pragma unroll
     for (int j = 0; j < V; ++j) p[j] = y.x[j];
