@@ -295,7 +295,8 @@ st_status st_ring_bwd_last(const st_ring_desc* desc, const st_tensor* q, const s
  * One (Q shard, KV chunk) pair as in st_attn_block_fwd / st_attn_block_bwd, with scores
  *   u = scale <q, k>,   y = softcap tanh(u / softcap),   s = y - slope_h |p_q - p_k|
  * over the keys of the row's span.  The states fold with st_attn_merge and st_attn_combine, Delta comes from st_attn_delta.
- *   softcap  0: scores are not capped; otherwise finite and positive
+ *   softcap  0: scores are not capped; otherwise finite and positive.  ST_BF16: at most 1024, and capped scores are some 2^-22 softcap
+ *            off (the hardware's exponential and reciprocal); ST_F32: tanhf
  *   slopes   nullable; device fp32 [Hq], finite, as their products with the distances have to be: what a unit of distance between
  *            the positions of query and key takes off the score
  *   spans    nullable; device int64 [B,Sq,2], 16-byte aligned: query row i of batch entry b sees the keys at global positions

@@ -46,7 +46,7 @@ struct ScoreArgs {
   int4* blocks;
   float* rows;
 };
-// of 32 rows: lse (log2 units, as if the nearest key had no bias; inf: a row without gradients), minus Delta, the keys it sees and
+// of 32 rows: lse less the cap (log2 units, as if the nearest key had no bias; inf: a row without gradients), minus Delta, the keys it sees and
 // the nearest of them, slope (log2 units)
 constexpr int kRowStats = 8 * 32;
 enum { kRowLse = 0, kRowDelta = 1, kRowLo = 2, kRowHi = 3, kRowX = 4, kRowSlope = 5 };
@@ -137,7 +137,9 @@ __device__ __forceinline__ ScoreConst score_const(const ScoreArgs& a) {
   k.k1 = a.cap * kScoreLog2e;
   return k;
 }
-// r = 1 / (1 + e^(2 u / cap)): tanh(u / cap) = 1 - 2 r and 1 - tanh^2 = 4 r (1 - r), for any u
+// r = 1 / (1 + e^(2 u / cap)): tanh(u / cap) = 1 - 2 r and 1 - tanh^2 = 4 r (1 - r), for any u.  Both functions are the hardware's, r some
+// 2^-24 off, and the score 2 cap times that: caps are at most kCapMost.
+constexpr float kCapMost = 1024.f;
 __device__ __forceinline__ float cap_r(float u, float c) {
   return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(u * c));
 }

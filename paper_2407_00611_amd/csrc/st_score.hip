@@ -50,7 +50,7 @@ __global__ __launch_bounds__(256) void score_rows_kernel(const ScoreArgs a, int3
   if (x >= n) return;
   if (r == 0) a.blocks[x] = make_int4(w.lo, w.hi, w.all_lo, w.all_hi);
   float* f = a.rows + x * kRowStats + r;
-  f[32 * kRowLse] = none ? INFINITY : fmaf(slope, see.rest, lse) * kScoreLog2e;
+  f[32 * kRowLse] = none ? INFINITY : (fmaf(slope, see.rest, lse) - a.cap) * kScoreLog2e;
   f[32 * kRowDelta] = -a.delta[stat];
   f[32 * kRowLo] = __int_as_float(see.lo);
   f[32 * kRowHi] = __int_as_float(see.hi);

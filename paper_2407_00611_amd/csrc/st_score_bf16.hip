@@ -466,7 +466,7 @@ __device__ __forceinline__ void score_dq(const ScoreArgs& a, int block_x, int bl
       if (CAP) {
         const float rr = cap_r(sc[v], k.c);
         e = fmaf(-2.f * k.k1, rr, k.k1 - lse2);
-        f = 4.f * rr * (1.f - rr);
+        f = fmaf(-rr, rr, rr);                         // a quarter of 1 - tanh^2
       } else {
         e = fmaf(sc[v], k.c, -lse2);
       }
@@ -516,12 +516,13 @@ __device__ __forceinline__ void score_dq(const ScoreArgs& a, int block_x, int bl
   float* out = part ? a.part_dq + share * ((int64_t)s.B * s.Sq * s.Hq * D) : a.dq;
   uint16_t* low = part ? nullptr : (uint16_t*)a.dq_lowp;
   const bool add = !part && !a.assign;
+  const float c = CAP ? 4.f * s.scale : s.scale;
 #pragma unroll
   for (int db = 0; db < DB; ++db)
 #pragma unroll
     for (int q4 = 0; q4 < 4; ++q4) {
       const int d = 32 * db + 8 * q4 + 4 * g;
-      float4 y = make_float4(acc[db][4 * q4] * s.scale, acc[db][4 * q4 + 1] * s.scale, acc[db][4 * q4 + 2] * s.scale, acc[db][4 * q4 + 3] * s.scale);
+      float4 y = make_float4(acc[db][4 * q4] * c, acc[db][4 * q4 + 1] * c, acc[db][4 * q4 + 2] * c, acc[db][4 * q4 + 3] * c);
       if (add) {
         const float4 z = *reinterpret_cast<const float4*>(out + orow + d);
         y.x += z.x; y.y += z.y; y.z += z.z; y.w += z.w;
@@ -629,8 +630,8 @@ __device__ __forceinline__ void score_dkv(const ScoreArgs& a, int block_x, int b
         float e, f = 1.f;
         if (CAP) {
           const float rr = cap_r(sc[v], k.c);
-          e = fmaf(-2.f * k.k1, rr, k.k1) - lse2[e4];
-          f = 4.f * rr * (1.f - rr);
+          e = fmaf(-2.f * k.k1, rr, -lse2[e4]);        // (k1 is in the row's statistics)
+          f = fmaf(-rr, rr, rr);                       // a quarter of 1 - tanh^2
         } else {
           e = fmaf(sc[v], k.c, -lse2[e4]);
         }
@@ -723,7 +724,7 @@ __device__ __forceinline__ void score_dkv(const ScoreArgs& a, int block_x, int b
         if (low) *reinterpret_cast<uint2*>(low + orow + d) = make_uint2(pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
       }
   };
-  store(acc_k, s.scale, part ? a.part_dk + share * n_kv : a.dk, part ? nullptr : (uint16_t*)a.dk_lowp);
+  store(acc_k, CAP ? 4.f * s.scale : s.scale, part ? a.part_dk + share * n_kv : a.dk, part ? nullptr : (uint16_t*)a.dk_lowp);
   store(acc_v, 1.f, part ? a.part_dv + share * n_kv : a.dv, part ? nullptr : (uint16_t*)a.dv_lowp);
 }
 

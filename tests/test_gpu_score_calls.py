@@ -194,3 +194,18 @@ def test_strides_that_pass_32_bits(dtype):
         assert torch.equal(a, b)
     dk = runs[0][4]                                  # what the spans leave: the last two documents' keys from row S - 40 on
     assert float(dk[0, 30000:].float().norm()) > 0 and not dk[0, :30000].any()
+
+
+@pytest.mark.parametrize("dtype,cap", [("bf16", 1024.0), ("f32", 1e6)])
+def test_caps_far_above_the_scores(dtype, cap):
+    """A cap that hardly bends anything: 1 - 2 / (1 + e^2x) cancels there, in the bf16 kernels 2^-22 cap of a score is lost."""
+    g = torch.Generator().manual_seed(29)
+    t = torch.bfloat16 if dtype == "bf16" else torch.float32
+    q, k, v = (torch.randn((1, 200, h, 64), generator=g).to(t).cuda() for h in (4, 2, 2))
+    pos = _positions(0, 200)
+    o, lse = st.st_attn_score_fwd(q, k, v, 0, 0, True, 0.125, softcap=cap)
+    o_ref, lse_ref = so.forward(q, k, v, pos, pos, True, 0.125, cap=cap)
+    off = 2.0 ** -22 * cap if dtype == "bf16" else 1e-5
+    assert float((lse - lse_ref).abs().max()) <= off + 1e-5
+    # the errors of a row's scores change P by as much, beside its rounding by 2^-8 in bf16 and the sums' in fp32
+    assert float((o - o_ref).norm()) <= ((2.0 ** -8 if dtype == "bf16" else 1e-5) + 2 * off) * float(o_ref.norm())
