@@ -82,10 +82,15 @@ __global__ __launch_bounds__(256) void score_combine_kernel(const float* __restr
   const int x = tid % vecs, y = tid / vecs;
   float4 r = make_float4(0.f, 0.f, 0.f, 0.f);
   if (y < lanes)
-    for (int k = y; k < n; k += lanes) {
-      const float4 p = *reinterpret_cast<const float4*>(o + (k * n_rows + row) * D + 4 * x);
-      const float c = w[k];
-      if (c != 0.f) r = make_float4(fmaf(c, p.x, r.x), fmaf(c, p.y, r.y), fmaf(c, p.z, r.z), fmaf(c, p.w, r.w));
+    for (int k0 = y; k0 < n; k0 += 4 * lanes) {        // four loads in flight
+      float4 p[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) p[u] = *reinterpret_cast<const float4*>(o + (min(k0 + u * lanes, n - 1) * n_rows + row) * D + 4 * x);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const float c = k0 + u * lanes < n ? w[k0 + u * lanes] : 0.f;
+        if (c != 0.f) r = make_float4(fmaf(c, p[u].x, r.x), fmaf(c, p[u].y, r.y), fmaf(c, p[u].z, r.z), fmaf(c, p[u].w, r.w));
+      }
     }
   fold[tid] = r;
   __syncthreads();
