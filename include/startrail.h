@@ -298,7 +298,7 @@ st_status st_ring_bwd_last(const st_ring_desc* desc, const st_tensor* q, const s
  *   softcap  0: scores are not capped; otherwise finite and positive.  ST_BF16: at most 1024, and capped scores are some 2^-22 softcap
  *            off (the hardware's exponential and reciprocal); ST_F32: tanhf
  *   slopes   nullable; device fp32 [Hq], finite, as their products with the distances have to be: what a unit of distance between
- *            the positions of query and key takes off the score
+ *            the positions of query and key takes off the score; chunks of at most 2^24 keys
  *   spans    nullable; device int64 [B,Sq,2], 16-byte aligned: query row i of batch entry b sees the keys at global positions
  *            spans[b][i][0] <= p < spans[b][i][1] (and, with desc->causal, p <= its own); an empty span is legal (O = 0,
  *            lse = -inf, no gradient).  st_mask_spans makes them; any other interval (a sliding window) is as good.

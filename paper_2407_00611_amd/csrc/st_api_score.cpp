@@ -28,6 +28,7 @@ st_status check_score(const st_block_desc* d, const st_score* m) {
   if (m->softcap > 0.f && !std::isfinite(2.f * st::kScoreLog2e * (d->scale / m->softcap))) return fail(ST_ERR_INVALID_ARG, "scale / softcap is too large");
   if (m->softcap > 0.f && !std::isfinite(m->softcap * st::kScoreLog2e)) return fail(ST_ERR_INVALID_ARG, "softcap is too large");
   if (d->dtype == ST_BF16 && m->softcap > st::kCapMost) return fail(ST_ERR_UNSUPPORTED, "bf16 path needs softcap <= %g (0: no cap)", (double)st::kCapMost);
+  if (m->slopes && d->Sk > 1 << 24) return fail(ST_ERR_UNSUPPORTED, "slopes need chunks of at most 2^24 keys, whose numbers fp32 holds");
   if (reinterpret_cast<uintptr_t>(m->slopes) % 4) return fail(ST_ERR_ALIGNMENT, "slopes: not 4-byte aligned");
   if (reinterpret_cast<uintptr_t>(m->spans) % 16) return fail(ST_ERR_ALIGNMENT, "spans: not 16-byte aligned");
   return ST_OK;

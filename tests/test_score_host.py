@@ -40,6 +40,7 @@ def test_score_shapes_and_modifications():
         assert call(_desc(Sq=1 << 30, B=64)) == 2 and call(_desc(Sq=1 << 30, Hq=64)) == 2
         for cap in (-1.0, float("nan"), float("inf"), 3.4e38, 1e-40):
             assert call(m=api.st_score(cap, None, None)) == 1, cap
+        assert call(_desc(Sk=(1 << 24) + 1), m=api.st_score(0.0, PTR, None)) == 2
         assert call(m=api.st_score(1025.0, None, None)) == 2                 # the hardware's exponential is not exact enough
         assert call(m=api.st_score(0.0, PTR + 2, None)) == 3 and call(m=api.st_score(0.0, None, PTR + 8)) == 3
         assert call(q=_view(PTR + 8)) == 3 and call(q=_view(s=513)) == 3 and call(q=_view(None)) == 1 and call(q=_view(b=-4096)) == 1
