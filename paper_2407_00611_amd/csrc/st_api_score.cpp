@@ -21,7 +21,7 @@ st_status check_score(const st_block_desc* d, const st_score* m) {
   ST_TRY(check_segments(d->Sq, d->q_offset, d->q_seg, d->q_offset2));
   if ((int64_t)d->Sq * (d->Hq / d->Hkv) > 0x7fffff00) return fail(ST_ERR_UNSUPPORTED, "more than 2^31 rows of a KV head's group");
   const int64_t rows = d->dtype == ST_BF16 ? ((int64_t)d->Sq * (d->Hq / d->Hkv) + st::kScoreRows - 1) / st::kScoreRows * d->Hkv : ((int64_t)d->Sq + 31) / 32 * d->Hq;
-  const int64_t keys = ((int64_t)d->Sk + 31) / 32 * d->Hkv;
+  const int64_t keys = ((int64_t)d->Sk + 31) / 32 * d->Hkv * (d->dtype == ST_F32 ? st::score_f32_halves(d->D) : 1);
   if (std::max(rows, keys) * d->B > st::kScoreGridMost) return fail(ST_ERR_UNSUPPORTED, "more than %lld tiles", (long long)st::kScoreGridMost);
   if (m == nullptr) return ST_OK;
   if (!(m->softcap >= 0.f) || m->softcap > 3.0e38f) return fail(ST_ERR_INVALID_ARG, "softcap must be 0 or finite and positive");
@@ -87,10 +87,11 @@ ScorePlan bwd_plan(const st::Shape& s, int dtype, bool spans) {
   const int G = s.Hq / s.Hkv;
   const bool bf16 = dtype == ST_BF16;
   const int64_t row_blocks = bf16 ? ((int64_t)s.Sq * G + 31) / 32 : ((int64_t)s.Sq + 31) / 32 * G, key_blocks = ((int64_t)s.Sk + 31) / 32;
+  const int halves = bf16 ? 1 : st::score_f32_halves(s.D);
   const int64_t rows = bf16 ? ((int64_t)s.Sq * G + st::kScoreRows - 1) / st::kScoreRows * s.Hkv * s.B : ((int64_t)s.Sq + 31) / 32 * s.Hq * s.B;
-  const int64_t keys = bf16 ? ((int64_t)s.Sk + st::kScoreKeys - 1) / st::kScoreKeys * s.Hkv * s.B : key_blocks * s.Hkv * s.B;
+  const int64_t keys = bf16 ? ((int64_t)s.Sk + st::kScoreKeys - 1) / st::kScoreKeys * s.Hkv * s.B : key_blocks * s.Hkv * s.B * halves;
   const int64_t n_q = (int64_t)s.B * s.Sq * s.Hq * s.D * 4, n_kv = (int64_t)s.B * s.Sk * s.Hkv * s.D * 4;
-  const int64_t kv_len = 4 * row_blocks, q_len = 3 * key_blocks;
+  const int64_t kv_len = (halves > 1 ? 3 : 4) * row_blocks, q_len = 3 * key_blocks;
   const int64_t each = (keys * kv_len + rows * q_len) / 512;
   const int quarters = !bf16 ? 4 : spans || (s.causal && s.q_seg <= 0) ? 2 : s.causal ? 3 : 4;
   ScorePlan p{};

@@ -68,6 +68,8 @@ hipError_t launch_score_add_parts(const ScoreArgs& a, int bf16, hipStream_t stre
 constexpr int kScoreRows = 128;      // bf16: rows of a query tile's workgroup
 constexpr int kScoreKeys = 128;      // bf16: keys of a key tile's workgroup
 
+constexpr int score_f32_halves(int D) { return D > 128 ? 2 : 1; }   // fp32: workgroups that share a key tile, by columns
+
 constexpr int64_t kScoreGridMost = 1 << 22;   // workgroups of a launch: a dimension of a grid holds fewer than 2^32 threads
 
 // shares of each of `jobs` workgroups that fill `slots` places, where a workgroup walks `steps` tiles

@@ -280,10 +280,13 @@ __global__ __launch_bounds__(waves<DP>() * 64) void score_dq_f32_kernel(const Sc
 
 // ---------------------------------------------------------------- dK, dV
 // block = key tile + ceil(Sk / 32) (KV head + Hkv batch entry); share y takes every kv_split-th group of a wavefront each's pairs
+// Head sizes beyond 128: the accumulators of 32 keys are more than the registers, so a workgroup has half of the gradients' columns and
+// makes S and dP for itself (8/2 heads x 400 rows of 256, forward and backward: 163 us; 229 with all columns, 640 values of them in
+// scratch memory).
 template <int DP, bool FULL, bool CAP>
-__global__ __launch_bounds__(waves<DP>() * 64) void score_dkv_f32_kernel(const ScoreArgs a) {
-  constexpr int NW = waves<DP>(), DB = DP / 32, N = 16, R = DP < 128 ? 4 : 2;
-  constexpr int NR = row_pieces<DP, N>(), NC = col_pieces<DP, N>(), kPieces = 2 * NR + 2 * NC;
+__global__ __launch_bounds__(512) void score_dkv_f32_kernel(const ScoreArgs a) {
+  constexpr int NW = 8, H = score_f32_halves(DP), DH = DP / H, DB = DH / 32, N = 16, R = DP < 128 ? 4 : 2;   // DH: columns of this workgroup
+  constexpr int NR = row_pieces<DP, N>(), NC = col_pieces<DH, N>(), kPieces = 2 * NR + 2 * NC;
   constexpr int kStat = 6 * kT;                              // of every row lse, Delta, lo, hi, x
   __shared__ __attribute__((aligned(16))) float ks[kT * lds_stride<DP>()];
   __shared__ __attribute__((aligned(16))) float vs[kT * lds_stride<DP>()];
@@ -293,12 +296,15 @@ __global__ __launch_bounds__(waves<DP>() * 64) void score_dkv_f32_kernel(const S
   const Shape& s = a.s;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 5, r = lane & 31;
-  const int n_kt = (s.Sk + kT - 1) / kT, outer = (int)(blockIdx.x / n_kt);
-  const int key0 = (int)sgpr(((int)blockIdx.x - outer * n_kt) * kT), hk = (int)sgpr(outer % s.Hkv), b = (int)sgpr(outer / s.Hkv);
+  const int tile = (int)(blockIdx.x / H), first = (int)sgpr((int)(blockIdx.x % H) * DH), columns = min(DH, s.D - first);
+  const int n_kt = (s.Sk + kT - 1) / kT, outer = tile / n_kt;
+  const int key0 = (int)sgpr((tile - outer * n_kt) * kT), hk = (int)sgpr(outer % s.Hkv), b = (int)sgpr(outer / s.Hkv);
   const int keys = min(kT, s.Sk - key0), key = key0 + r;
   const int G = s.Hq / s.Hkv;
-  stage_tile<DP>(ks, (const float*)a.k.ptr + b * a.k.sb + hk * a.k.sh, a.k.ss, key0, s.Sk, s.D, tid);
-  stage_tile<DP>(vs, (const float*)a.v.ptr + b * a.v.sb + hk * a.v.sh, a.v.ss, key0, s.Sk, s.D, tid);
+  if (tid < waves<DP>() * 64) {
+    stage_tile<DP>(ks, (const float*)a.k.ptr + b * a.k.sb + hk * a.k.sh, a.k.ss, key0, s.Sk, s.D, tid);
+    stage_tile<DP>(vs, (const float*)a.v.ptr + b * a.v.sb + hk * a.v.sh, a.v.ss, key0, s.Sk, s.D, tid);
+  }
   if (tid == 0) any_dirty = 0;
   __syncthreads();
   f32x16 acc_k[DB], acc_v[DB];
@@ -326,8 +332,8 @@ __global__ __launch_bounds__(waves<DP>() * 64) void score_dkv_f32_kernel(const S
     auto load = [&](int x) {
       if (x >= kPieces) return;
       if (x < 2 * NR) load_rows<DP, FULL>(f[x % R], x < NR ? qrow : drow, x < NR ? x : x - NR, s.D, g);
-      else if (x < 2 * NR + NC) load_cols<DP, FULL>(f[x % R], db_, a.d_o.ss, limit, x - 2 * NR, s.D, r, g);
-      else load_cols<DP, FULL>(f[x % R], qb, a.q.ss, limit, x - 2 * NR - NC, s.D, r, g);
+      else if (x < 2 * NR + NC) load_cols<DH, FULL>(f[x % R], db_ + first, a.d_o.ss, limit, x - 2 * NR, columns, r, g);
+      else load_cols<DH, FULL>(f[x % R], qb + first, a.q.ss, limit, x - 2 * NR - NC, columns, r, g);
       __builtin_amdgcn_sched_barrier(0);
     };
     f32x16 p, ds;
@@ -364,9 +370,9 @@ __global__ __launch_bounds__(waves<DP>() * 64) void score_dkv_f32_kernel(const S
 #pragma unroll
     for (int x = 2 * NR; x < kPieces; ++x) {
       load(x + R - 1);
-      if (masked) bad = make_finite<DP>(f[x % R]) || bad;
-      if (x < 2 * NR + NC) contract_rows<DP>(acc_v, f[x % R], p, x - 2 * NR);
-      else contract_rows<DP>(acc_k, f[x % R], ds, x - 2 * NR - NC);
+      if (masked) bad = make_finite<DH>(f[x % R]) || bad;
+      if (x < 2 * NR + NC) contract_rows<DH>(acc_v, f[x % R], p, x - 2 * NR);
+      else contract_rows<DH>(acc_k, f[x % R], ds, x - 2 * NR - NC);
     }
     if (bad) any_dirty = 1;
   }
@@ -383,7 +389,7 @@ __global__ __launch_bounds__(waves<DP>() * 64) void score_dkv_f32_kernel(const S
   }
   if (wave != 0 || key >= s.Sk) return;
   const bool part = a.kv_split > 1, add_old = !part && !a.assign;
-  const int64_t n_kv = (int64_t)s.B * s.Sk * s.Hkv * s.D, at = (((int64_t)b * s.Sk + key) * s.Hkv + hk) * s.D;
+  const int64_t n_kv = (int64_t)s.B * s.Sk * s.Hkv * s.D, at = (((int64_t)b * s.Sk + key) * s.Hkv + hk) * s.D + first;
   auto place = [&](float* parts, float* out, void* low, float*& o, float*& o2) {
     o = part ? parts + blockIdx.y * n_kv + at : out ? out + at : nullptr;
     o2 = !part && low ? (float*)low + at : nullptr;
@@ -400,7 +406,7 @@ __global__ __launch_bounds__(waves<DP>() * 64) void score_dkv_f32_kernel(const S
 #pragma unroll
     for (int q = 0; q < DB; ++q) {
       const int d = block_column<DB>(j, q, g);
-      if (d >= s.D) continue;
+      if (d >= columns) continue;
       float4 x = acc_block(acc_k, j, q, s.scale), y = acc_block(acc_v, j, q, 1.f);
       if (add_old) {
         x = add(x, *reinterpret_cast<const float4*>(ok + d));
@@ -421,8 +427,8 @@ __global__ __launch_bounds__(waves<DP>() * 64) void score_dkv_f32_kernel(const S
       for (int i = i0; i < min(i0 + kT, s.Sq); ++i) {
         const RowView see = row_view(a, b, i);
         if (key < see.lo || key >= see.hi || a.lse_in[((int64_t)b * s.Hq + h) * s.Sq + i] == -INFINITY) continue;
-        add_nonfinite<DB>(ok, ok2, qb, a.q.ss, i, i + 1, s.D, g, true);
-        add_nonfinite<DB>(ov, ov2, db_, a.d_o.ss, i, i + 1, s.D, g, false);
+        add_nonfinite<DB>(ok, ok2, qb + first, a.q.ss, i, i + 1, columns, g, true);
+        add_nonfinite<DB>(ov, ov2, db_ + first, a.d_o.ss, i, i + 1, columns, g, false);
       }
     }
 }
@@ -446,16 +452,16 @@ hipError_t launch_score_fwd_f32(const ScoreArgs& a, hipStream_t stream) {
 
 hipError_t launch_score_bwd_f32(const ScoreArgs& a, hipStream_t stream) {
   const int64_t rows = (int64_t)((a.s.Sq + kT - 1) / kT) * a.s.Hq * a.s.B, keys = (int64_t)((a.s.Sk + kT - 1) / kT) * a.s.Hkv * a.s.B;
-  if (rows > kScoreGridMost || keys > kScoreGridMost) return hipErrorInvalidValue;
+  if (rows > kScoreGridMost || keys * score_f32_halves(a.s.D) > kScoreGridMost) return hipErrorInvalidValue;
   return with_padded_d(a.s.D, [&](auto dp, auto full) {
     constexpr int DP = decltype(dp)::value;
     constexpr bool FULL = decltype(full)::value;
     const dim3 block(waves<DP>() * 64);
     if (keys > 0) {
       ProfScope prof("score_dkv_f32", stream);
-      const dim3 grid((unsigned)keys, (unsigned)a.kv_split);
-      if (a.cap > 0.f) hipLaunchKernelGGL((score_dkv_f32_kernel<DP, FULL, true>), grid, block, 0, stream, a);
-      else hipLaunchKernelGGL((score_dkv_f32_kernel<DP, FULL, false>), grid, block, 0, stream, a);
+      const dim3 grid((unsigned)(keys * score_f32_halves(DP)), (unsigned)a.kv_split);
+      if (a.cap > 0.f) hipLaunchKernelGGL((score_dkv_f32_kernel<DP, FULL, true>), grid, dim3(512), 0, stream, a);
+      else hipLaunchKernelGGL((score_dkv_f32_kernel<DP, FULL, false>), grid, dim3(512), 0, stream, a);
       const hipError_t e = hipGetLastError();
       if (e != hipSuccess) return e;
     }

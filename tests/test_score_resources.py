@@ -5,11 +5,10 @@ from test_kernel_resources import _kernels
 
 def test_the_kernels_of_modified_scores_and_rotations_stay_in_registers():
     kernels = _kernels()
-    # capped and biased scores of head size 128 have an address waiting in memory, read outside the inner loops; in fp32 the accumulators of
-    # both gradients of 32 keys of 160 values and more exceed the registers, as those of the plain scores do
+    # capped and biased scores of head size 128 have an address waiting in memory, read outside the inner loops
     for part, most in (("score_fwd_kernel", 0), ("score_bwd_kernel", 16), ("score_rows_kernel", 0), ("score_combine_kernel", 0),
-                       ("score_add_parts_kernel", 0), ("mask_spans_kernel", 0), ("score_fwd_f32_kernelILi128", 0), ("score_dq_f32_kernelILi128", 0),
-                       ("score_dkv_f32_kernelILi128", 24), ("score_dkv_f32_kernelILi96", 0), ("rope_fwd_kernel", 0), ("rope_bwd_kernel", 0),
+                       ("score_add_parts_kernel", 0), ("mask_spans_kernel", 0), ("score_fwd_f32_kernel", 0), ("score_dq_f32_kernel", 0),
+                       ("score_dkv_f32_kernel", 8), ("rope_fwd_kernel", 0), ("rope_bwd_kernel", 0),
                        ("rope_dw_kernel", 0)):
         found = {name: k for name, k in kernels.items() if part in name}
         assert found, part
