@@ -140,7 +140,8 @@ st_status st_attn_merge(float* o_acc, float* lse_acc, const float* o_part, const
  *   o_parts, lse_parts  host arrays [n_states] of device pointers: fp32 [B,Sq_in,Hq,D] / fp32 [B,Hq,Sq_in]
  *   o_out fp32 [B,Sq_out,Hq,D], lse_out fp32 [B,Hq,Sq_out] (overwritten; may not alias an input)
  *   o_out_lowp (nullable): O' rounded to out_dtype, dense [B,Sq_out,Hq,D]
- * A state with lse = -inf on a row is empty there; a row empty in every state gives O = 0, lse = -inf.
+ * A state with lse = -inf on a row is empty there; a row empty in every state gives O = 0, lse = -inf, and one whose lse is NaN
+ * in some state gives NaN.
  * Requires 1 <= n_states <= 64, D <= 256, D % 8 == 0, 0 <= row0, row0 + Sq_out <= Sq_in. */
 st_status st_attn_combine(const float* const* o_parts, const float* const* lse_parts, int32_t n_states,
                           int32_t B, int32_t Sq_in, int32_t Hq, int32_t D, int32_t row0, int32_t Sq_out,

@@ -102,7 +102,8 @@ __global__ __launch_bounds__(256) void merge_kernel(float* __restrict__ o_acc, f
 // ---- combine: n partial states of the same rows -> one state, keeping a run of rows -----------
 // Thread = one float4 of one kept (b, i, h) row, lanes per row as in the merge.  The weights are
 // w_x = exp(lse_x - m) / sum_y exp(lse_y - m) with m the largest lse, so an empty state (lse = -inf)
-// weighs 0 and (-inf) - (-inf) is never formed; a row empty in every state gives O = 0, lse = -inf.
+// weighs 0 and (-inf) - (-inf) is never formed; a row empty in every state gives O = 0, lse = -inf, and one whose lse is
+// NaN in any state gives NaN.
 // kFew: at most that many states, each lse of which is read once and kept (0: any number, lse read three times, one wait
 // after the other).  O loads in flight together: all for up to 4 and 9 to 16 states, otherwise kCombineUnroll (8 states of
 // 8 x 1024 rows of 128: 12.0 us, 12.4 with all eight at once).  16 states of 4 x 256 rows, the split of a short shard: 17.5
@@ -139,6 +140,12 @@ __global__ __launch_bounds__(256) void combine_kernel(const CombineArgs a, int32
       r.z = fmaf(w, p.z, r.z);
       r.w = fmaf(w, p.w, r.w);
     }
+  };
+  // fmaxf passes over NaN, so a largest lse of -inf says that no state holds more than NaN; the sum of all lse is NaN then, or -inf
+  // where all are empty.
+  auto empty_or_nan = [](float l) {
+    const float x = l == -INFINITY ? 0.f : l;
+    return make_float4(x, x, x, x);
   };
   float4 r = make_float4(0.f, 0.f, 0.f, 0.f);
   float lnew = -INFINITY;
@@ -178,6 +185,10 @@ __global__ __launch_bounds__(256) void combine_kernel(const CombineArgs a, int32
 #pragma unroll
         for (int u = 0; u < U; ++u) add(r, x0 + u < n ? l[x0 + u] * inv : 0.f, p[u]);
       }
+    } else {
+#pragma unroll
+      for (int x = 0; x < N; ++x) lnew += l[x];
+      r = empty_or_nan(lnew);
     }
   } else {
     float m = -INFINITY;
@@ -199,6 +210,9 @@ __global__ __launch_bounds__(256) void combine_kernel(const CombineArgs a, int32
 #pragma unroll
         for (int u = 0; u < kCombineUnroll; ++u) add(r, w[u], p[u]);
       }
+    } else {
+      for (int x = 0; x < a.n; ++x) lnew += a.lse[x][l_in];
+      r = empty_or_nan(lnew);
     }
   }
   const int64_t v_out = row * vec_per_row + sub;

@@ -61,7 +61,7 @@ __global__ __launch_bounds__(256) void score_rows_kernel(const ScoreArgs a, int3
 
 // Many partial states of few rows (a split walk of a token or a few): a workgroup per row, eight states side by side, where the
 // general combine has a thread go through all of them (64 states of 32 rows of 128: 55 us).  Weights as there: an empty state is 0
-// whatever its O holds, a row that is empty in all of them stays empty.
+// whatever its O holds, a row that is empty in all of them stays empty, one that is NaN in any of them becomes NaN.
 __global__ __launch_bounds__(256) void score_combine_kernel(const float* __restrict__ o, const float* __restrict__ lse, int32_t n, int32_t Sq, int32_t Hq, int32_t D,
                                                             int64_t n_rows, float* o_out, float* __restrict__ lse_out, void* low, int32_t bf16) {
   __shared__ float w[kMaxTable];
@@ -73,11 +73,13 @@ __global__ __launch_bounds__(256) void score_combine_kernel(const float* __restr
     const float l = tid < n ? lse[tid * n_rows + stat] : -INFINITY;
     float m = l;
     for (int d = 1; d < 64; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
-    const float e = m == -INFINITY ? 0.f : expf(l - m);
+    // (fmaxf passes over NaN: with none but such states beside empty ones the sum of all lse is NaN, with empty ones alone -inf)
+    const bool none = m == -INFINITY;
+    const float e = none ? l : expf(l - m);
     float sum = e;
     for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
-    w[tid] = m == -INFINITY ? 0.f : e / sum;
-    if (tid == 0) lse_out[stat] = m == -INFINITY ? -INFINITY : m + logf(sum);
+    w[tid] = !none ? e / sum : sum == -INFINITY ? 0.f : sum;
+    if (tid == 0) lse_out[stat] = none ? sum : m + logf(sum);
   }
   __syncthreads();
   const int x = tid % vecs, y = tid / vecs;
