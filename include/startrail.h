@@ -126,6 +126,7 @@ st_status st_attn_block_fwd(const st_block_desc* desc, const st_tensor* q, const
  *   lse' = log(exp(lse_acc) + exp(lse_part)),
  *   O'   = exp(lse_acc - lse') O_acc + exp(lse_part - lse') O_part.
  * A state with lse = -inf is empty (the neutral element; start from O = 0, lse = -inf).
+ * One whose lse is NaN makes the row NaN.
  * o_out_lowp (nullable): also write O' rounded to out_dtype, dense [B,Sq,Hq,D].
  * o_acc/o_part fp32 [B,Sq,Hq,D]; lse_acc/lse_part fp32 [B,Hq,Sq].  o_part may not alias o_acc. */
 st_status st_attn_merge(float* o_acc, float* lse_acc, const float* o_part, const float* lse_part,

@@ -166,16 +166,16 @@ def merge(o_a, lse_a, o_b, lse_b):
         lse' = log(exp(lse_a) + exp(lse_b))
         O'   = exp(lse_a - lse') O_a + exp(lse_b - lse') O_b
     o_*: [B,Sq,Hq,D]; lse_*: [B,Hq,Sq].  A state with lse = -inf is empty and
-    acts as the identity."""
+    acts as the identity; one whose lse is NaN makes the row NaN."""
     o_a, o_b, lse_a, lse_b = _f64(o_a), _f64(o_b), _f64(lse_a), _f64(lse_b)
     m = np.maximum(lse_a, lse_b)
-    m_safe = np.where(np.isfinite(m), m, 0.0)
+    m_safe = np.where(m != NEG_INF, m, 0.0)
     with np.errstate(divide="ignore"):
         lse = m_safe + np.log(np.exp(lse_a - m_safe) + np.exp(lse_b - m_safe))
-    lse = np.where(np.isfinite(m), lse, NEG_INF)
-    lse_safe = np.where(np.isfinite(lse), lse, 0.0)
-    w_a = np.where(np.isfinite(lse_a), np.exp(lse_a - lse_safe), 0.0)   # [B,Hq,Sq]
-    w_b = np.where(np.isfinite(lse_b), np.exp(lse_b - lse_safe), 0.0)
+    lse = np.where(m != NEG_INF, lse, NEG_INF)
+    lse_safe = np.where(lse != NEG_INF, lse, 0.0)
+    w_a = np.where(lse_a != NEG_INF, np.exp(lse_a - lse_safe), 0.0)   # [B,Hq,Sq]
+    w_b = np.where(lse_b != NEG_INF, np.exp(lse_b - lse_safe), 0.0)
     o = w_a.transpose(0, 2, 1)[..., None] * o_a + w_b.transpose(0, 2, 1)[..., None] * o_b
     return o, lse
 

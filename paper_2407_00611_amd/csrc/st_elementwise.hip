@@ -44,6 +44,7 @@ __device__ __forceinline__ RowOf row_of(int64_t row, int64_t rows, int32_t S, in
 // The group never straddles a wavefront: every lane of the row has read lse_acc before lane 0 overwrites it.
 // Weights: w_acc = exp(lse_acc - lse'), w_part = exp(lse_part - lse'), lse' = max + log(sum).
 // A side with lse = -inf gets weight 0 without ever forming (-inf) - (-inf), and its O is not read into the sum.
+// A side whose lse is NaN makes the row NaN.
 // U = vectors per thread (1, 2 or 4): all loads of a thread are in flight before its first store.
 template <bool kLowp, int U>
 __global__ __launch_bounds__(256) void merge_kernel(float* __restrict__ o_acc, float* __restrict__ lse_acc,
@@ -80,6 +81,9 @@ __global__ __launch_bounds__(256) void merge_kernel(float* __restrict__ o_acc, f
     const float inv = 1.f / sum;
     wa = ea * inv;
     wp = ep * inv;
+  } else {
+    lnew = la + lp;                                    // fmaxf passes over NaN: with one in either lse the row is NaN, else empty
+    wa = wp = lnew == -INFINITY ? 0.f : lnew;
   }
 #pragma unroll
   for (int u = 0; u < U; ++u) {

@@ -89,3 +89,28 @@ def test_combining_a_state_of_nan(n):
     assert got[gone].isnan().all() and low[gone].isnan().all() and l.transpose(1, 2)[gone].isnan().all()
     assert not got[~gone].isnan().any() and not low[~gone].isnan().any() and not l.transpose(1, 2)[~gone].isnan().any()
     assert (got[0, 6, 0] == 0).all() and l[0, 0, 6] == -math.inf
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_chunks_with_nan_fold_to_nan(dtype):
+    """A fold starts from the empty state, and some chunks hold nothing for a row: a chunk in which its scores are NaN still shows."""
+    g = torch.Generator().manual_seed(2)
+    q, k, v = (torch.randn((2, 40, h, 64), generator=g).to(dtype).cuda() for h in (4, 2, 2))
+    spans = torch.tensor([[50, 60]] * 40).expand(2, 40, 2).contiguous().cuda()          # in the second of three chunks
+    bad = q.clone()
+    bad[0, 7, 2] = math.nan
+    for order in ((0, 1, 2), (1, 0, 2), (2, 0, 1)):
+        parts = [[st.st_attn_score_fwd(x, k, v, 0, 40 * j, False, 0.1, spans=spans) for j in order] for x in (q, bad)]
+        out = []
+        for p in parts:
+            o, lse = torch.zeros(q.shape, device="cuda"), torch.full((2, 4, 40), -math.inf, device="cuda")
+            for part in p:
+                st.st_attn_merge(o, lse, *part)
+            out.append((o, lse))
+            both = st.st_attn_combine([x[0] for x in p], [x[1] for x in p])
+            assert both[0].isnan().equal(o.isnan()) and both[1].isnan().equal(lse.isnan())
+        (o, lse), (o2, lse2) = out
+        assert torch.isfinite(o).all() and torch.isfinite(lse).all()
+        assert o2[0, 7, 2].isnan().all() and lse2[0, 2, 7].isnan()
+        o2[0, 7, 2], lse2[0, 2, 7] = o[0, 7, 2], lse[0, 2, 7]
+        assert torch.equal(o, o2) and torch.equal(lse, lse2)

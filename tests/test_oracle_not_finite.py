@@ -23,3 +23,12 @@ def _check(o, lse):
 def test_combine_keeps_nan():
     for n in (1, 2, 5):
         _check(*oa.combine(*_states(n)))
+
+
+def test_merge_keeps_nan():
+    for order in ((0, 1, 2, 3), (3, 0, 1, 2)):
+        parts_o, parts_l = _states(4)
+        o, lse = oa.empty_state(1, 3, 2, 4)
+        for x in order:
+            o, lse = oa.merge(o, lse, parts_o[x], parts_l[x])
+        _check(o, lse)
