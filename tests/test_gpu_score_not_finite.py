@@ -6,6 +6,7 @@ import pytest
 import torch
 
 import paper_2407_00611_amd as st
+from test_gpu_score import _all, _packed
 
 pytestmark = pytest.mark.gpu
 
@@ -114,3 +115,38 @@ def test_chunks_with_nan_fold_to_nan(dtype):
         assert o2[0, 7, 2].isnan().all() and lse2[0, 2, 7].isnan()
         o2[0, 7, 2], lse2[0, 2, 7] = o[0, 7, 2], lse[0, 2, 7]
         assert torch.equal(o, o2) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("D", [64, 80, 96, 192, 200, 256])
+@pytest.mark.parametrize("value", [math.inf, -math.inf, math.nan])
+def test_fp32_gradients_of_values_that_are_not_finite(D, value):
+    """One value of one key's V or K, one row's dO or Q, in tiles that a document's edge crosses, in either half of the columns: who
+    sees it has it, nobody else does."""
+    q, k, v, d_o, bounds = _packed(19, torch.float32, D=D)
+    spans = st.st_mask_spans(bounds, q.shape[1], 0, False)
+    clean = _all(q, k, v, d_o, 0, 0, 0.1, dict(spans=spans))
+    at = 120                                         # of entry 0: in the document 101 .. 259
+    seen = (spans[0, :, 0] <= at) & (at < spans[0, :, 1])
+    for column in (3, D - 2):
+        for what in "vkdq":
+            x = dict(q=q.clone(), k=k.clone(), v=v.clone(), d=d_o.clone())
+            x[what][0, at, 1, column] = value       # (KV head 1: query heads 3, 4, 5; query head 1: KV head 0)
+            o, lse, dq, dk, dv = _all(x["q"], x["k"], x["v"], x["d"], 0, 0, 0.1, dict(spans=spans))
+            for a, b, name in zip((o, dq, dk, dv), (clean[0],) + clean[2:], ("o", "dq", "dk", "dv")):
+                assert torch.equal(a[1], b[1]) and torch.equal(a[0, ~seen], b[0, ~seen]), f"{what}, {column}: {name} of those that see nothing of it"
+            fine = torch.isfinite
+            rest = torch.arange(D, device="cuda") != column
+            if what == "d":                          # P is what it was: dV has the value where its row looks, in its column
+                assert not fine(dv[0, seen, 0, column]).any() and torch.equal(dv[0, :, 0, rest], clean[4][0, :, 0, rest])
+                assert dv[0, seen, 0, column].isnan().all() if math.isnan(value) else (dv[0, seen, 0, column] == value).all()
+                assert not fine(dq[0, at, 1]).any() and not fine(dk[0, seen, 0]).any() and torch.equal(o, clean[0])
+                assert torch.equal(dv[0, :, 1], clean[4][0, :, 1]) and torch.equal(dk[0, :, 1], clean[3][0, :, 1])
+            elif what == "v":                        # O has it in its column, Delta and the rows' dS everywhere
+                assert not fine(o[0, seen][:, 3:, column]).any() and torch.equal(o[0][:, 3:, rest], clean[0][0][:, 3:, rest])
+                assert not fine(dq[0, seen][:, 3:]).any() and not fine(dk[0, seen, 1]).any() and torch.equal(dv, clean[4])
+                assert torch.equal(dq[0][:, :3], clean[2][0][:, :3])
+            elif what == "q":
+                assert not fine(dq[0, at, 1]).any() and not fine(dk[0, seen, 0]).any() and torch.equal(dk[0, :, 1], clean[3][0, :, 1])
+            elif math.isnan(value):
+                assert not fine(o[0, seen][:, 3:]).any() and not fine(dq[0, seen][:, 3:]).any() and not fine(dk[0, seen, 1]).any()
+                assert torch.equal(dq[0][:, :3], clean[2][0][:, :3])
