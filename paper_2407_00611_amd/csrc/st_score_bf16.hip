@@ -114,9 +114,14 @@ __device__ __forceinline__ int ordered_tile(const ScoreArgs& a, int b, int n_qt,
 
 // Block id -> (row tile, KV head, batch entry).  Every XCD has a contiguous range of the (KV head, batch entry) pairs, whose keys and
 // values stay in its L2; under a causal mask the later tiles, which see more, come first.
-// Workgroups whose order is worth its making, 2 us of each: more than the chip holds at once, and so few turns of them that a long
-// last one shows.  24 heads of 64 x 8192 packed rows, 1536 workgroups, 155 us without an order, 111 with one; a window of 64 keys on
-// 32/8 heads x 16384 rows, 4096 workgroups, 119 without, 137 with one.
+// Workgroups whose order is worth its making, 2 us of each.  The spans are on the device, so a rule on the host goes by the number of
+// workgroups: more than the chip holds at once, and so few turns of them that a long last one shows.  Forward without and with an
+// order, in us:
+//   long documents   24 heads of 64 x 8192 rows, six of them (1536 workgroups) 135, 114; 32/8 heads of 128, eight x 4096 (1024) 56, 53,
+//                    three x 8192 (2048) 258, 243
+//   what has the same work in every tile loses: 32/8 heads x 8192 rows, 31 documents 72, 79, a window of 64 keys 60, 69
+//   beyond 2048      32/8 heads, three documents x 16384 (4096) 896, 890, x 32768 (8192) 3370, 3430; window of 64 keys x 16384 121, 138;
+//                    but six documents, 24 heads of 64 x 16384 (3072), 448, 407
 constexpr int kOrderFrom = 512, kOrderUpTo = 2048;
 __device__ __forceinline__ void tile_block(const ScoreArgs& a, int block, int blocks, int n_qt, int* lds, int& qt, int& hk, int& b) {
   int hb;

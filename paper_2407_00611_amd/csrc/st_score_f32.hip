@@ -287,7 +287,7 @@ template <int DP, bool FULL, bool CAP>
 __global__ __launch_bounds__(512) void score_dkv_f32_kernel(const ScoreArgs a) {
   constexpr int NW = 8, H = score_f32_halves(DP), DH = DP / H, DB = DH / 32, N = 16, R = DP < 128 ? 4 : 2;   // DH: columns of this workgroup
   constexpr int NR = row_pieces<DP, N>(), NC = col_pieces<DH, N>(), kPieces = 2 * NR + 2 * NC;
-  constexpr int kStat = 6 * kT;                              // of every row lse, Delta, lo, hi, x
+  constexpr int kStat = 5 * kT;                              // of every row lse, Delta, lo, hi, x
   __shared__ __attribute__((aligned(16))) float ks[kT * lds_stride<DP>()];
   __shared__ __attribute__((aligned(16))) float vs[kT * lds_stride<DP>()];
   __shared__ __attribute__((aligned(16))) float stats[NW * kStat];
