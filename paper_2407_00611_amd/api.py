@@ -233,7 +233,7 @@ def _ptr(t: Optional[torch.Tensor]) -> C.c_void_p:
 def _aligned(buf: torch.Tensor, a: int) -> Tuple[int, int]:
     """First a-byte aligned address inside a byte buffer and the bytes from there to its end."""
     ptr = (buf.data_ptr() + a - 1) // a * a
-    return ptr, buf.numel() * buf.element_size() - (ptr - buf.data_ptr())
+    return ptr, max(buf.numel() * buf.element_size() - (ptr - buf.data_ptr()), 0)      # (the buffer may end before the boundary)
 
 
 def _f32_dense(t: torch.Tensor, shape, name: str) -> torch.Tensor:
