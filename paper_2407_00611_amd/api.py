@@ -242,19 +242,38 @@ def _f32_dense(t: torch.Tensor, shape, name: str) -> torch.Tensor:
     return t
 
 
+_INT32, _INT64 = 1 << 31, 1 << 63
+
+
+def _fit(end: int, *xs: int) -> None:
+    """ctypes cuts off what does not fit a field of the structs or an argument."""
+    for x in xs:
+        if not -end <= x < end:
+            raise ValueError(f"{x} does not fit {end.bit_length()} bits")
+
+
 def _q_runs(q_offset) -> Tuple[int, int, int]:
     """q_offset is the position of query row 0, or (position of row 0, rows in the first run, position of the
     first row of the second run) for a shard made of two runs of the sequence."""
     if isinstance(q_offset, (tuple, list)):
         off, seg, off2 = q_offset
-        return int(off), int(seg), int(off2)
-    return int(q_offset), 0, 0
+        off, seg, off2 = int(off), int(seg), int(off2)
+        _fit(_INT64, off, off2)
+        _fit(_INT32, seg)
+        return off, seg, off2
+    off = int(q_offset)
+    _fit(_INT64, off)
+    return off, 0, 0
 
 
 def _block_desc(q, k, q_offset, k_offset, causal, scale) -> st_block_desc:
     B, Sq, Hq, D = q.shape
+    _, Sk, Hkv, _ = k.shape
     off, seg, off2 = _q_runs(q_offset)
-    return st_block_desc(_dtype_code(q), B, Hq, k.shape[2], D, Sq, k.shape[1], off, int(k_offset),
+    k_off = int(k_offset)
+    _fit(_INT32, max(B, Sq, Hq, D, Sk, Hkv))
+    _fit(_INT64, k_off)
+    return st_block_desc(_dtype_code(q), B, Hq, Hkv, D, Sq, Sk, off, k_off,
                          1 if causal else 0, float(scale), seg, off2)
 
 
@@ -694,6 +713,7 @@ def st_mask_spans(bounds, Sq: int, q_offset, causal: bool, prefix=None, spans=No
         if bounds.dim() != 2 or bounds.shape[1] < 1:
             raise ValueError("bounds must be [B, n_docs + 1]")
         B, n = bounds.shape[0], bounds.shape[1] - 1
+        _fit(_INT32, B, int(Sq), n)
         _dense(bounds, (B, n + 1), torch.int64, "bounds")
         if prefix is not None:
             _dense(prefix, (B, n), torch.int64, "prefix")
@@ -795,6 +815,7 @@ def _rope_desc(q, k, freq, offset, positions, axes, pairs, norm, eps, q_weight, 
         if w is not None:
             _dense(w, (D,), torch.float32, name)
     off, seg, off2 = _q_runs(offset)
+    _fit(_INT32, *q.shape, *(k.shape if k is not None else ()), *axes, 2 * n)
     return st_rope_desc(_dtype_code(q), B, S, Hq, k.shape[2] if k is not None else 0, D, 2 * n,
                         _PAIRS[pairs], 1 if norm else 0, float(eps), len(axes),
                         (C.c_int32 * ST_ROPE_MAX_AXES)(*axes), off, seg, off2)
