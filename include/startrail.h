@@ -321,7 +321,7 @@ typedef struct {
  *   prefix  nullable, int64 [B,n_docs]: so many first tokens of document d are seen by all of its tokens, whatever `causal` says
  *   spans   int64 [B,Sq,2] (out): a row sees its own document, with `causal` up to its own position or the prefix' end;
  *           a row in no document gets an empty span.  Hand them on with desc->causal = 0: the causal order is in them.
- * q_offset, q_seg, q_offset2 place the rows as in st_block_desc. */
+ * q_offset, q_seg, q_offset2 place the rows as in st_block_desc.  B Sq <= 2^30, n_docs < 2^30. */
 st_status st_mask_spans(int32_t B, int32_t Sq, int64_t q_offset, int32_t q_seg, int64_t q_offset2, int32_t causal,
                         const int64_t* bounds, int32_t n_docs, const int64_t* prefix, int64_t* spans, void* hip_stream);
 

@@ -184,6 +184,7 @@ st_status st_mask_spans(int32_t B, int32_t Sq, int64_t q_offset, int32_t q_seg, 
   if (reinterpret_cast<uintptr_t>(bounds) % 8 || reinterpret_cast<uintptr_t>(prefix) % 8 || reinterpret_cast<uintptr_t>(spans) % 16)
     return fail(ST_ERR_ALIGNMENT, "bounds and prefix need 8-byte, spans 16-byte alignment");
   if (((int64_t)B * Sq + 255) / 256 > st::kScoreGridMost) return fail(ST_ERR_UNSUPPORTED, "more than 2^30 rows");
+  if (n_docs >= 1 << 30) return fail(ST_ERR_UNSUPPORTED, "2^30 documents or more");   // (the search adds two of their numbers)
   st::Shape s;
   memset(&s, 0, sizeof(s));
   s.B = B; s.Sq = Sq; s.q_offset = q_offset; s.q_seg = q_seg; s.q_offset2 = q_offset2; s.causal = causal ? 1 : 0;
