@@ -299,13 +299,14 @@ st_status st_ring_bwd_last(const st_ring_desc* desc, const st_tensor* q, const s
  * over the keys of the row's span.  The states fold with st_attn_merge and st_attn_combine, Delta comes from st_attn_delta.
  *   softcap  0: scores are not capped; otherwise finite and positive.  ST_BF16: at most 1024, and capped scores are some 2^-22 softcap
  *            off (the hardware's exponential and reciprocal); ST_F32: tanhf
- *   slopes   nullable; device fp32 [Hq], finite, as their products with the distances have to be: what a unit of distance between
- *            the positions of query and key takes off the score; chunks of at most 2^24 keys
+ *   slopes   nullable; device fp32 [Hq], finite, as their products with the distances have to be (ST_BF16: and those over scale):
+ *            what a unit of distance between the positions of query and key takes off the score; chunks of at most 2^24 keys
  *   spans    nullable; device int64 [B,Sq,2], 16-byte aligned: query row i of batch entry b sees the keys at global positions
  *            spans[b][i][0] <= p < spans[b][i][1] (and, with desc->causal, p <= its own); an empty span is legal (O = 0,
  *            lse = -inf, no gradient).  st_mask_spans makes them; any other interval (a sliding window) is as good.
  * Precision of ST_BF16: scores, softmax, sums in fp32 from the stored Q and K (Q is not scaled and rounded first, as the kernels
  * of the plain scores do); P and the gradient of the scores are rounded to bf16 before the second contractions.
+ * Delta has the rounding of the O that st_attn_delta is handed: none with o_part, half a step of bf16 a value with o_lowp.
  * The states' lse is fp32, like everything that is folded from it: with a bias, where a row sees nothing of a sequence but keys
  * far away, its probabilities in the backward carry half a step of an lse of that size, 2^-24 slope distance.
  * Infinities and NaN in rows of Q, K, V, dO reach the results of the rows and keys that see them, and no others.  Outputs overlap
@@ -353,7 +354,8 @@ st_status st_attn_score_bwd(const st_block_desc* desc, const st_score* score, co
  *               those of axis 1 (time, height, width of a video patch); they add up to rot / 2
  *   positions   nullable; device int32 [n_axes,B,S].  NULL (one axis): the rows are those of a shard, at offset, and from row seg
  *               on at offset2 (q_offset, q_seg, q_offset2 of st_block_desc)
- *   freq        device fp64 [rot/2], radians per position (any: scaled ones too); angles are made in fp64, for far positions
+ *   freq        device fp64 [rot/2], radians per position (any: scaled ones too); angles are made in fp64, for far positions, and
+ *               their fraction of a turn is rounded to fp32, 1e-7 radians at most, before its sine and cosine
  *   q_weight, k_weight  nullable (ones); device fp32 [D], for norm = 1 only
  * q, k: [B,S,Hq,D] and [B,S,Hkv,D] views (k is not read where Hkv = 0); arithmetic is fp32, rounded once.  q_out, k_out: views of
  * the same type, which may be q and k themselves.  D <= 256, D % 8 == 0, rot even, 0 <= rot <= D, Hq + Hkv <= 16384, B S <= 2^25. */

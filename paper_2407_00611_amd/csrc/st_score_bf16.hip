@@ -1,7 +1,7 @@
 // bf16 attention with modified scores (st_score.h), head size 128 or 64: forward, dQ and dK/dV on v_mfma_f32_32x32x16_bf16.
 //
 // Products <q, k> of the stored values are exact in the matrix unit's fp32 sums; scale, cap, bias and softmax are fp32, Q itself is
-// not rounded again.  P and dU are rounded to bf16 for the second contractions, relative 2^-9 at most each, as those of the other
+// not rounded again.  P and dU are rounded to bf16 for the second contractions, relative 2^-8 at most each, as those of the other
 // bf16 kernels here; sums and statistics stay fp32.
 //
 // Rows whose tile a mask edge crosses: the matrix unit multiplies what a row does not see by zero, and 0 * inf is NaN.  In such a
@@ -177,8 +177,8 @@ struct TileLoads {
 // 32/8 heads x 4096 x 2048 keys: busy 42 % and 61 % of the time), and by power: 32/8 heads x 8192 x 4096 keys of 128 take 590 us,
 // 930 TFLOP/s at 1.8 GHz (capped 650 us; 24 or 32 heads of 64, vector unit busy 82 %: 900 TFLOP/s).  Wavefronts of 64 rows, half the
 // operand reads a product, leave one on a SIMD and took 951 us; products and softmax interleaved by hand gained 3 % there and
-// nothing where masks are.  Packed images (24 heads of 64 x 8192 rows) take 111 us, prompts with prefixes (32/8
-// x 4096) 53 us, spans included.
+// nothing where masks are.  Packed images (24 heads of 64 x 8192 rows) take 110 us, prompts with prefixes (32/8
+// x 4096) 53 to 56 us, spans included.
 // =============================================================================================
 template <int D, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, 2) void score_fwd_kernel(const ScoreArgs a) {
