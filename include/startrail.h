@@ -60,7 +60,7 @@ typedef enum {
   ST_ERR_WORKSPACE = 5      /* workspace missing or smaller than st_ring_workspace_bytes() */
 } st_status;
 
-typedef enum { ST_F32 = 0, ST_BF16 = 1 } st_dtype;
+typedef enum { ST_F32 = 0, ST_BF16 = 1, ST_E4M3 = 2 /* of a cache's pages only */ } st_dtype;
 
 /* How the driver walks the visit order. */
 typedef enum {
@@ -385,6 +385,66 @@ st_status st_qk_rope_bwd(const st_rope_desc* desc, const st_tensor* q, const st_
                          const double* freq, const int32_t* positions, int32_t flags, const st_tensor* dx_q,
                          const st_tensor* dx_k, float* dw_q, float* dw_k, void* workspace, size_t workspace_bytes,
                          void* hip_stream);
+
+/* ---- a cache of keys and values in pages, for serving: appending to it, reading chunks of it, attention that reads it ----
+ * Token x of sequence b lies in page table[b][x / page] at row x % page.  Every size that changes from step to step (tokens of the
+ * sequences, their new rows, the pages) is read from device memory by the kernels, so that a captured call can be replayed.
+ *   dtype          what the pages hold: the dtype of the calls' tensors, or ST_E4M3
+ *   page           16, 32, 64, 128 or 256
+ *   k, v           [n_pages, page, Hkv, D] views (stride_b of a page, stride_s of a token, stride_h of a head), rows 16-byte aligned
+ *   k_scale, v_scale  ST_E4M3 only: device bytes [n_pages, Hkv]; a stored value stands for its e4m3 value times 2^(scale - 127)
+ *                  (1 <= scale <= 254).  Whole powers of two: every value is exact in bf16, and a page whose scale grows keeps its
+ *                  rows but for what falls below the least e4m3 value
+ *   table          device int32 [B, width].  An entry that is no page (negative, or >= n_pages: a page that a window has left behind)
+ *                  holds nothing: its tokens are not stored, not seen, and read as zeros
+ *   lens           device int32 [B]: tokens of every sequence, those that a call appends among them; at most width page of them
+ * Rows of a call are packed: T rows, of which sequence b has the n_b = starts[b + 1] - starts[b] from starts[b] on (device int32
+ * [B + 1], rising, in 0 .. T; n_b may be 0).  Row i of sequence b is its token lens[b] - n_b + i.  Rows of no sequence (T may be
+ * more than there are, as for a captured call) are left as they were.
+ * A page may be in the tables of several sequences (a common beginning), but only one of them may append to it, in one call at a time.
+ * D: multiples of 8 up to 256 (ST_E4M3: of 16); B <= 65535, T <= 2^25, width page <= 2^30. */
+typedef struct {
+  int32_t  dtype, n_pages, page, Hkv, D, B, width;
+  st_tensor k, v;
+  uint8_t *k_scale, *v_scale;
+  const int32_t *table, *lens;
+} st_cache;
+
+/* The norms and rotations of st_qk_rope_fwd over new rows, and their keys and values into the cache.
+ *   desc        B = 1, S = T, seg = 0; Hq may be 0 (then q and q_out are not read); positions are the tokens' places in their
+ *               sequences + offset, or come from `positions` int32 [n_axes,1,T].  Hkv and D are the cache's
+ *   q, k, v     [1,T,heads,D] views in desc->dtype; q_out as q, which it may be
+ * ST_E4M3: the scale of a page and head is 2^e with the least e for which all new values of the page are within 448 2^e, and not
+ * below what the rows have that were there before, which are rescaled where it grows.  Keys are normed and rotated in fp64 there, so
+ * that each is the nearest stored value to the exact one; values that are not finite are stored as NaN and do not count for the scale.
+ * Repeating a call with the same tensors changes nothing. */
+st_status st_cache_append(const st_rope_desc* desc, const st_cache* cache, const int32_t* starts, const st_tensor* q, const st_tensor* k,
+                          const st_tensor* v, const float* q_weight, const float* k_weight, const double* freq, const int32_t* positions,
+                          const st_tensor* q_out, void* hip_stream);
+
+/* Tokens first[b] .. first[b] + count - 1 of every sequence (first: device int32 [B], NULL: 0) as chunks [B,count,Hkv,D], views in
+ * `dtype` (that of the cache; of ST_E4M3 either other); tokens past a sequence's end are zeros.  k_out or v_out may be NULL. */
+st_status st_cache_read(const st_cache* cache, const int32_t* first, int32_t count, int32_t dtype, const st_tensor* k_out,
+                        const st_tensor* v_out, void* hip_stream);
+
+/* Attention of packed rows against the cache, with the scores of st_score: a row at position p sees the tokens x < lens[b] of its
+ * sequence with x <= p (causal) and p - x < window (window > 0).
+ *   q_first     nullable; device int64 [B]: position of a sequence's first row, counted from the cache's first token (a GPU that has a
+ *               share of a sequence's tokens passes the distance from the share's beginning).  NULL: lens[b] - n_b
+ *   max_rows    no sequence has more rows than this; rows behind are not computed
+ *   softcap, slopes  as in st_score
+ *   o_part fp32 and / or o_lowp in dtype, dense [1,T,Hq,D]; lse_part fp32 [1,Hq,T]: a state that st_attn_merge and st_attn_combine fold
+ *   (B = 1, Sq = T).  A row that sees nothing has O = 0, lse = -inf.
+ * ST_BF16 with D = 64 or 128 (pages of ST_BF16 or ST_E4M3), ST_F32 with any D (pages of ST_F32 or ST_E4M3).  Scores, softmax and sums
+ * are fp32; infinities and NaN reach the rows that see them, and no others.  Results do not depend on the order of the pages. */
+typedef struct {
+  int32_t dtype, T, Hq, max_rows, causal, window;
+  float   scale, softcap;
+  const float* slopes;      /* device */
+} st_cache_rows;
+size_t st_attn_cache_workspace_bytes(const st_cache_rows* rows, const st_cache* cache);   /* device, 256-byte aligned; as for st_attn_score_fwd */
+st_status st_attn_cache(const st_cache_rows* rows, const st_cache* cache, const int32_t* starts, const int64_t* q_first, const st_tensor* q,
+                        float* o_part, float* lse_part, void* o_lowp, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /* ---- per-kernel timing for benchmarks (not part of the method) ----
  * Between st_profile_begin() and st_profile_end() the library records a HIP event on the launch

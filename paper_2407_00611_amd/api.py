@@ -16,11 +16,11 @@ import ctypes as C
 import os
 import sys
 import warnings
-from typing import List, Optional, Sequence, Tuple
+from typing import List, NamedTuple, Optional, Sequence, Tuple
 
 import torch
 
-ST_F32, ST_BF16 = 0, 1
+ST_F32, ST_BF16, ST_E4M3 = 0, 1, 2
 ST_RING_STEPWISE, ST_RING_FUSED = 0, 1
 ST_KV_ASSIGN = 1
 ST_GRAD_ASSIGN = 1
@@ -66,6 +66,17 @@ class st_rope_desc(C.Structure):
                 ("axis_pairs", C.c_int32 * 4), ("offset", C.c_int64), ("seg", C.c_int32), ("offset2", C.c_int64)]
 
 
+class st_cache(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("n_pages", C.c_int32), ("page", C.c_int32), ("Hkv", C.c_int32), ("D", C.c_int32), ("B", C.c_int32),
+                ("width", C.c_int32), ("k", st_tensor), ("v", st_tensor), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("table", C.c_void_p), ("lens", C.c_void_p)]
+
+
+class st_cache_rows(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("T", C.c_int32), ("Hq", C.c_int32), ("max_rows", C.c_int32), ("causal", C.c_int32),
+                ("window", C.c_int32), ("scale", C.c_float), ("softcap", C.c_float), ("slopes", C.c_void_p)]
+
+
 class st_comm_report(C.Structure):
     _fields_ = [("ring_iterations", C.c_int32), ("startrail_iterations", C.c_int32),
                 ("ring_p2p_bytes_per_iter", C.c_int64), ("startrail_p2p_bytes_per_iter", C.c_int64),
@@ -95,6 +106,7 @@ def _load() -> C.CDLL:
     lib = C.CDLL(_LIB_PATH)
     T, D, R = C.POINTER(st_tensor), C.POINTER(st_block_desc), C.POINTER(st_ring_desc)
     M, P = C.POINTER(st_score), C.POINTER(st_rope_desc)
+    K, W = C.POINTER(st_cache), C.POINTER(st_cache_rows)
     vp, f32p, i32p = C.c_void_p, C.c_void_p, C.POINTER(C.c_int32)
     sigs = {
         "st_attn_block_fwd": (C.c_int, [D, T, T, T, f32p, f32p, vp]),
@@ -126,6 +138,10 @@ def _load() -> C.CDLL:
         "st_qk_rope_fwd": (C.c_int, [P, T, T, f32p, f32p, vp, vp, T, T, vp]),
         "st_qk_rope_bwd_workspace_bytes": (C.c_size_t, [P]),
         "st_qk_rope_bwd": (C.c_int, [P, T, T, T, T, C.c_int32, f32p, f32p, vp, vp, C.c_int32, T, T, f32p, f32p, vp, C.c_size_t, vp]),
+        "st_cache_append": (C.c_int, [P, K, vp, T, T, T, f32p, f32p, vp, vp, T, vp]),
+        "st_cache_read": (C.c_int, [K, vp, C.c_int32, C.c_int32, T, T, vp]),
+        "st_attn_cache_workspace_bytes": (C.c_size_t, [W, K]),
+        "st_attn_cache": (C.c_int, [W, K, vp, vp, T, f32p, f32p, vp, vp, C.c_size_t, vp]),
         "st_device_facts": (C.c_int, [C.POINTER(st_device_report)]),
         "st_mfma_probe": (C.c_int, [vp, C.c_int64, C.c_int32, C.c_int32, f32p, C.c_int64, C.POINTER(C.c_double), vp]),
         "st_mfma_probe_mixes": (C.c_int32, []),
@@ -173,7 +189,7 @@ _binding = _native_half()
 
 EXPORTS = ["st_attn_block_fwd", "st_attn_merge", "st_attn_combine", "st_attn_delta", "st_attn_block_bwd", "st_attn_block_bwd_workspace_bytes", "st_cast_from_f32",
            "st_visit_order", "st_team_visit_order", "st_schedule_report", "st_ring_workspace_bytes", "st_ring_fwd", "st_ring_bwd", "st_ring_bwd_noalloc", "st_ring_bwd_noalloc_max_bytes", "st_ring_bwd_last", "st_mask_spans", "st_attn_score_workspace_bytes", "st_attn_score_fwd", "st_attn_score_bwd", "st_qk_rope_fwd",
-           "st_qk_rope_bwd_workspace_bytes", "st_qk_rope_bwd", "st_device_facts", "st_mfma_probe", "st_mfma_probe_mixes", "st_mfma_probe_mix_name", "st_profile_begin",
+           "st_qk_rope_bwd_workspace_bytes", "st_qk_rope_bwd", "st_cache_append", "st_cache_read", "st_attn_cache_workspace_bytes", "st_attn_cache", "st_device_facts", "st_mfma_probe", "st_mfma_probe_mixes", "st_mfma_probe_mix_name", "st_profile_begin",
            "st_profile_end", "st_status_str",
            "st_last_error", "st_version"]
 
@@ -893,3 +909,149 @@ def st_qk_rope_bwd(q, k, d_q, d_k, freq, offset=0, positions=None, axes=None, pa
 
 def st_qk_rope_bwd_workspace_bytes(q, k, freq, norm: bool = True) -> int:
     return int(_lib.st_qk_rope_bwd_workspace_bytes(C.byref(_rope_desc(q, k, freq, 0, None, None, "halves", norm, 1e-6, None, None))))
+
+
+# ---- a cache of keys and values in pages
+
+class KVCache(NamedTuple):
+    """A cache as the calls below take it.  k, v [n_pages, page, Hkv, D] (any strides with D contiguous) in fp32, bf16 or
+    float8_e4m3fn; table int32 [B, width]: the pages of every sequence; lens int32 [B]: its tokens, those of the rows at hand among
+    them; k_scale, v_scale uint8 [n_pages, Hkv], with pages in 8 bits only: a stored value stands for itself times 2^(scale - 127)."""
+    k: torch.Tensor
+    v: torch.Tensor
+    table: torch.Tensor
+    lens: torch.Tensor
+    k_scale: Optional[torch.Tensor] = None
+    v_scale: Optional[torch.Tensor] = None
+
+
+_PAGE_TYPES = {torch.float32: ST_F32, torch.bfloat16: ST_BF16, torch.float8_e4m3fn: ST_E4M3}
+
+
+def _cache_desc(c: KVCache) -> st_cache:
+    if c.k.dim() != 4 or c.v.shape != c.k.shape or c.v.dtype != c.k.dtype:
+        raise ValueError("expected k, v [n_pages,page,Hkv,D] of one shape and dtype")
+    if c.k.dtype not in _PAGE_TYPES:
+        raise TypeError(f"unsupported dtype {c.k.dtype}")
+    n_pages, page, Hkv, D = c.k.shape
+    if c.table.dim() != 2:
+        raise ValueError("table must be [B, width]")
+    B, width = c.table.shape
+    _dense(c.table, (B, width), torch.int32, "table")
+    _dense(c.lens, (B,), torch.int32, "lens")
+    for x, name in ((c.k_scale, "k_scale"), (c.v_scale, "v_scale")):
+        if (x is not None) != (c.k.dtype == torch.float8_e4m3fn):
+            raise ValueError(f"{name}: with pages in 8 bits, and only there")
+        if x is not None:
+            _dense(x, (n_pages, Hkv), torch.uint8, name)
+    _fit(_INT32, n_pages, page, Hkv, D, B, width)
+    return st_cache(_PAGE_TYPES[c.k.dtype], n_pages, page, Hkv, D, B, width, _view(c.k), _view(c.v),
+                    c.k_scale.data_ptr() if c.k_scale is not None else None, c.v_scale.data_ptr() if c.v_scale is not None else None,
+                    c.table.data_ptr(), c.lens.data_ptr())
+
+
+def _starts(starts, c: KVCache):
+    return _dense(starts, (c.lens.shape[0] + 1,), torch.int32, "starts")
+
+
+def st_cache_append(q, k, v, starts, cache: KVCache, freq, offset: int = 0, positions=None, axes=None, pairs: str = "halves",
+                    norm: bool = True, eps: float = 1e-6, q_weight=None, k_weight=None, q_out=None, stream=None):
+    """New rows, packed: q [1,T,Hq,D] (or None), k and v [1,T,Hkv,D], of which sequence b has starts[b] .. starts[b + 1] - 1 (int32
+    [B + 1]), its last tokens.  Norms and rotations as in st_qk_rope_fwd at the tokens' places in their sequences + offset (or at
+    `positions` int32 [axes,1,T]); keys and values go into the cache.  Returns the queries (a new tensor unless q_out is given, which
+    may be q), None without."""
+    with _on_device(stream, k, q, v, starts, *cache, freq, positions, q_weight, k_weight, q_out):
+        c = _cache_desc(cache)
+        if k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype:
+            raise ValueError("expected k and v [1,T,Hkv,D] of one shape and dtype")
+        if q is not None and (q.dim() != 4 or q.shape[:2] != k.shape[:2] or q.shape[3] != k.shape[3] or q.dtype != k.dtype):
+            raise ValueError("expected q [1,T,Hq,D] with the rows and the dtype of k")
+        if q is None and q_out is not None:
+            raise ValueError("q_out without q")
+        _starts(starts, cache)
+        d = _rope_desc(k, k, freq, offset, positions, axes, pairs, norm, eps, q_weight, k_weight)
+        d.Hq = q.shape[2] if q is not None else 0
+        _fit(_INT32, d.Hq)
+        if q is not None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else _like(q_out, q, "q_out")
+        tq, tk, tv, to = _maybe_view(q), _view(k), _view(v), _maybe_view(q_out)
+        _check(_lib.st_cache_append(C.byref(d), C.byref(c), _ptr(starts), C.byref(tq), C.byref(tk), C.byref(tv), _ptr(q_weight), _ptr(k_weight),
+                                    _ptr(freq), _ptr(positions), C.byref(to), _stream(None)), "st_cache_append")
+    return q_out
+
+
+def st_cache_read(cache: KVCache, first, count: int, dtype=None, k_out=None, v_out=None, stream=None):
+    """(k, v) chunks [B,count,Hkv,D]: tokens first[b] .. first[b] + count - 1 of every sequence (int32 [B], None: from 0), zeros past
+    its end.  dtype: that of the pages; of pages in 8 bits torch.bfloat16 (unless given) or torch.float32."""
+    with _on_device(stream, cache.k, *cache[1:], first, k_out, v_out):
+        c = _cache_desc(cache)
+        if dtype is None:
+            dtype = k_out.dtype if k_out is not None else torch.bfloat16 if c.dtype == ST_E4M3 else cache.k.dtype
+        code = {torch.float32: ST_F32, torch.bfloat16: ST_BF16}.get(dtype)
+        if code is None:
+            raise TypeError(f"unsupported dtype {dtype}")
+        if first is not None:
+            _dense(first, (c.B,), torch.int32, "first")
+        _fit(_INT32, int(count))
+        if int(count) < 0:
+            raise ValueError("count must not be negative")
+        shape, out = (c.B, int(count), c.Hkv, c.D), []
+        for x, name in ((k_out, "k_out"), (v_out, "v_out")):
+            if x is None:
+                x = torch.empty(shape, dtype=dtype, device=cache.k.device)
+            elif tuple(x.shape) != shape or x.dtype != dtype:
+                raise ValueError(f"{name} must be a {dtype} tensor of shape {shape}")
+            out.append(x)
+        tk, tv = _view(out[0]), _view(out[1])
+        _check(_lib.st_cache_read(C.byref(c), _ptr(first), int(count), code, C.byref(tk), C.byref(tv), _stream(None)), "st_cache_read")
+    return tuple(out)
+
+
+def _cache_rows(q, cache, causal, scale, max_rows, window, softcap, slopes) -> st_cache_rows:
+    if q.dim() != 4 or q.shape[0] != 1 or q.shape[3] != cache.k.shape[3]:
+        raise ValueError("expected q [1,T,Hq,D] with the head size of the cache")
+    T, Hq = q.shape[1], q.shape[2]
+    if slopes is not None:
+        _dense(slopes, (Hq,), torch.float32, "slopes")
+    max_rows = T if max_rows is None else int(max_rows)
+    _fit(_INT32, T, Hq, max_rows, int(window))
+    return st_cache_rows(_dtype_code(q), T, Hq, max_rows, 1 if causal else 0, int(window), float(scale), float(softcap),
+                         slopes.data_ptr() if slopes is not None else None)
+
+
+def st_attn_cache_workspace_bytes(q, cache: KVCache, max_rows: Optional[int] = None) -> int:
+    r, c = _cache_rows(q, cache, True, 1.0, max_rows, 0, 0.0, None), _cache_desc(cache)
+    return int(_lib.st_attn_cache_workspace_bytes(C.byref(r), C.byref(c)))
+
+
+def st_attn_cache(q, starts, cache: KVCache, causal: bool, scale: float, max_rows: Optional[int] = None, window: int = 0,
+                  softcap: float = 0.0, slopes=None, q_first=None, o_part=None, lse_part=None, o_lowp=None, lowp: bool = False,
+                  workspace=None, stream=None):
+    """(O, lse) of packed rows q [1,T,Hq,D] against the cache: sequence b has rows starts[b] .. starts[b + 1] - 1 (int32 [B + 1]), at
+    positions from q_first[b] on (int64 [B], counted from the cache's first token; None: its last tokens).  A row sees the tokens up
+    to its position (causal), the last `window` of them (0: all).  No sequence has more than max_rows rows (None: T).  O [1,T,Hq,D] is
+    the fp32 state, or with lowp=True alone in the dtype of q; both are written where o_part and o_lowp are given (the fp32 one is
+    returned); lse fp32 [1,Hq,T].  Rows of no sequence are left as they were."""
+    with _on_device(stream, q, starts, *cache, slopes, q_first, o_part, lse_part, o_lowp, workspace):
+        r, c = _cache_rows(q, cache, causal, scale, max_rows, window, softcap, slopes), _cache_desc(cache)
+        T, Hq = r.T, r.Hq
+        _starts(starts, cache)
+        if q_first is not None:
+            _dense(q_first, (c.B,), torch.int64, "q_first")
+        if o_lowp is None and lowp:
+            o_lowp = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        elif o_lowp is not None:
+            _dense(o_lowp, q.shape, q.dtype, "o_lowp")
+        if o_part is None and o_lowp is None:
+            o_part = torch.empty(q.shape, dtype=torch.float32, device=q.device)
+        elif o_part is not None:
+            _f32_dense(o_part, q.shape, "o_part")
+        lse_part = torch.empty((1, Hq, T), dtype=torch.float32, device=q.device) if lse_part is None else _f32_dense(lse_part, (1, Hq, T), "lse_part")
+        if workspace is None:
+            need = int(_lib.st_attn_cache_workspace_bytes(C.byref(r), C.byref(c)))
+            workspace = torch.empty(need + 256, dtype=torch.uint8, device=q.device) if need else None
+        ws, size = _aligned(workspace, 256) if workspace is not None else (None, 0)
+        tq = _view(q)
+        _check(_lib.st_attn_cache(C.byref(r), C.byref(c), _ptr(starts), _ptr(q_first), C.byref(tq), _ptr(o_part), _ptr(lse_part), _ptr(o_lowp),
+                                  C.c_void_p(ws), size, _stream(None)), "st_attn_cache")
+    return (o_part if o_part is not None else o_lowp), lse_part

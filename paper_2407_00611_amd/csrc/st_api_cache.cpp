@@ -1,0 +1,179 @@
+// C ABI of the cache of keys and values in pages: argument checks, workspace layout, launches.
+#include <cmath>
+
+#include "st_cache.h"
+#include "st_checks.h"
+#include "st_score.h"
+
+using namespace st::checks;
+using st::fail;
+using st::hip_fail;
+
+namespace {
+
+st_status check_cache(const st_cache* c) {
+  if (c == nullptr) return fail(ST_ERR_INVALID_ARG, "null cache");
+  if (c->dtype != ST_F32 && c->dtype != ST_BF16 && c->dtype != ST_E4M3) return fail(ST_ERR_INVALID_ARG, "cache: unknown dtype %d", c->dtype);
+  if (c->n_pages < 0 || c->B < 0 || c->width < 0) return fail(ST_ERR_INVALID_ARG, "cache: negative size");
+  if (c->Hkv <= 0 || c->D <= 0) return fail(ST_ERR_INVALID_ARG, "cache: Hkv and D must be positive");
+  if (c->page < 16 || c->page > 256 || (c->page & (c->page - 1))) return fail(ST_ERR_UNSUPPORTED, "cache: pages of 16, 32, 64, 128 or 256 tokens (page=%d)", c->page);
+  if (c->D > 256 || c->D % 8 != 0) return fail(ST_ERR_UNSUPPORTED, "cache: D <= 256 and D %% 8 == 0 are needed (D=%d)", c->D);
+  if (c->dtype == ST_E4M3 && c->D % 16 != 0) return fail(ST_ERR_UNSUPPORTED, "cache: D %% 16 == 0 is needed in 8 bits (D=%d)", c->D);
+  if (c->Hkv > 16384) return fail(ST_ERR_UNSUPPORTED, "cache: more than 16384 heads");
+  if (c->B > 65535) return fail(ST_ERR_UNSUPPORTED, "cache: B must not exceed 65535");
+  if ((int64_t)c->width * c->page > (int64_t)1 << 30) return fail(ST_ERR_UNSUPPORTED, "cache: more than 2^30 tokens a sequence");
+  const int64_t n = (int64_t)c->n_pages * c->page * c->Hkv * c->D;
+  ST_TRY(check_tensor("cache k", &c->k, c->dtype, n));
+  ST_TRY(check_tensor("cache v", &c->v, c->dtype, n));
+  if (c->dtype == ST_E4M3 && n > 0 && (c->k_scale == nullptr || c->v_scale == nullptr)) return fail(ST_ERR_INVALID_ARG, "cache: pages in 8 bits need k_scale and v_scale");
+  if (c->dtype != ST_E4M3 && (c->k_scale || c->v_scale)) return fail(ST_ERR_INVALID_ARG, "cache: scales belong to pages in 8 bits");
+  if (c->B > 0 && (c->lens == nullptr || (c->table == nullptr && c->width > 0))) return fail(ST_ERR_INVALID_ARG, "cache: table / lens: null pointer");
+  if (reinterpret_cast<uintptr_t>(c->table) % 4 || reinterpret_cast<uintptr_t>(c->lens) % 4) return fail(ST_ERR_ALIGNMENT, "cache: table and lens need 4-byte alignment");
+  return ST_OK;
+}
+
+st_status check_starts(const st_cache* c, const int32_t* starts, int64_t T) {
+  if (c->B == 0 || T == 0) return ST_OK;
+  if (starts == nullptr) return fail(ST_ERR_INVALID_ARG, "starts: null pointer");
+  if (reinterpret_cast<uintptr_t>(starts) % 4) return fail(ST_ERR_ALIGNMENT, "starts: not 4-byte aligned");
+  return ST_OK;
+}
+
+st::CacheArgs cache_args(const st_cache* c) {
+  st::CacheArgs a;
+  memset(&a, 0, sizeof(a));
+  a.dtype = c->dtype; a.n_pages = c->n_pages; a.shift = __builtin_ctz((unsigned)c->page); a.Hkv = c->Hkv; a.D = c->D; a.B = c->B; a.width = c->width;
+  a.k = view_of(&c->k);
+  a.v = view_of(&c->v);
+  a.k_scale = c->k_scale; a.v_scale = c->v_scale; a.table = c->table; a.lens = c->lens;
+  return a;
+}
+
+st_status check_rows(const st_cache_rows* r, const st_cache* c) {
+  if (r == nullptr) return fail(ST_ERR_INVALID_ARG, "null descriptor");
+  ST_TRY(check_cache(c));
+  if (r->dtype != ST_F32 && r->dtype != ST_BF16) return fail(ST_ERR_INVALID_ARG, "unknown dtype %d", r->dtype);
+  if (c->dtype != ST_E4M3 && c->dtype != r->dtype) return fail(ST_ERR_UNSUPPORTED, "rows and pages of different dtypes");
+  if (r->T < 0 || r->max_rows < 0 || r->window < 0) return fail(ST_ERR_INVALID_ARG, "negative size");
+  if (r->Hq <= 0 || r->Hq % c->Hkv != 0) return fail(ST_ERR_INVALID_ARG, "need Hq %% Hkv == 0 (Hq=%d Hkv=%d)", r->Hq, c->Hkv);
+  if (r->dtype == ST_BF16 && c->D != 128 && c->D != 64) return fail(ST_ERR_UNSUPPORTED, "bf16 path is built for D = 64 or 128 (D=%d)", c->D);
+  if (r->Hq > 65535) return fail(ST_ERR_UNSUPPORTED, "Hq must not exceed 65535");
+  if (r->T > 1 << 25) return fail(ST_ERR_UNSUPPORTED, "more than 2^25 rows");
+  if ((int64_t)r->T * (r->Hq / c->Hkv) > 0x7fffff00) return fail(ST_ERR_UNSUPPORTED, "more than 2^31 rows of a KV head's group");
+  ST_TRY(check_scale(r->scale));
+  if (!(r->softcap >= 0.f) || r->softcap > 3.0e38f) return fail(ST_ERR_INVALID_ARG, "softcap must be 0 or finite and positive");
+  if (r->softcap > 0.f && !std::isfinite(2.f * st::kScoreLog2e * (r->scale / r->softcap))) return fail(ST_ERR_INVALID_ARG, "scale / softcap is too large");
+  if (r->softcap > 0.f && !std::isfinite(r->softcap * st::kScoreLog2e)) return fail(ST_ERR_INVALID_ARG, "softcap is too large");
+  if (r->dtype == ST_BF16 && r->softcap > st::kCapMost) return fail(ST_ERR_UNSUPPORTED, "bf16 path needs softcap <= %g (0: no cap)", (double)st::kCapMost);
+  if (r->slopes && (int64_t)c->width * c->page > 1 << 24) return fail(ST_ERR_UNSUPPORTED, "slopes need sequences of at most 2^24 tokens, whose numbers fp32 holds");
+  if (reinterpret_cast<uintptr_t>(r->slopes) % 4) return fail(ST_ERR_ALIGNMENT, "slopes: not 4-byte aligned");
+  return ST_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+st_status st_cache_append(const st_rope_desc* d, const st_cache* c, const int32_t* starts, const st_tensor* q, const st_tensor* k, const st_tensor* v,
+                          const float* q_weight, const float* k_weight, const double* freq, const int32_t* positions, const st_tensor* q_out,
+                          void* hip_stream) {
+  ST_TRY(check_cache(c));
+  ST_TRY(check_rope(d, positions, freq, 0));
+  if (d->B != 1 || d->seg != 0) return fail(ST_ERR_INVALID_ARG, "packed rows: B = 1 and seg = 0");
+  if (d->Hkv != c->Hkv || d->D != c->D) return fail(ST_ERR_INVALID_ARG, "the rows have %d heads of %d, the cache %d of %d", d->Hkv, d->D, c->Hkv, c->D);
+  if (c->dtype != ST_E4M3 && c->dtype != d->dtype) return fail(ST_ERR_UNSUPPORTED, "rows and pages of different dtypes");
+  ST_TRY(check_starts(c, starts, d->S));
+  const int64_t n_q = (int64_t)d->S * d->Hq * d->D, n_k = (int64_t)d->S * d->Hkv * d->D;
+  ST_TRY(check_tensor("k", k, d->dtype, n_k));
+  ST_TRY(check_tensor("v", v, d->dtype, n_k));
+  if (n_q > 0) {
+    ST_TRY(check_tensor("q", q, d->dtype, n_q));
+    ST_TRY(check_tensor("q_out", q_out, d->dtype, n_q));
+  }
+  ST_TRY(check_weight("q_weight", q_weight));
+  ST_TRY(check_weight("k_weight", k_weight));
+  if (!d->norm && (q_weight || k_weight)) return fail(ST_ERR_INVALID_ARG, "weights need norm = 1");
+  if (n_k == 0 || c->B == 0) return ST_OK;
+  st::AppendArgs a;
+  memset(&a, 0, sizeof(a));
+  a.g = rope_args(d);
+  a.c = cache_args(c);
+  a.g.k = view_of(k);
+  a.v_in = view_of(v);
+  if (n_q > 0) {
+    a.g.q = view_of(q);
+    a.g.q_out = view_of(q_out);
+  }
+  a.g.q_weight = q_weight;
+  a.g.k_weight = k_weight;
+  a.g.freq = freq;
+  a.g.positions = positions;
+  a.starts = starts;
+  ST_HIP(st::launch_cache_append(a, d->dtype == ST_BF16, (hipStream_t)hip_stream), "st_cache_append launch");
+  return ST_OK;
+}
+
+st_status st_cache_read(const st_cache* c, const int32_t* first, int32_t count, int32_t dtype, const st_tensor* k_out, const st_tensor* v_out,
+                        void* hip_stream) {
+  ST_TRY(check_cache(c));
+  if (dtype != ST_F32 && dtype != ST_BF16) return fail(ST_ERR_INVALID_ARG, "unknown dtype %d", dtype);
+  if (c->dtype != ST_E4M3 && c->dtype != dtype) return fail(ST_ERR_UNSUPPORTED, "chunks and pages of different dtypes");
+  if (count < 0) return fail(ST_ERR_INVALID_ARG, "negative size");
+  if (reinterpret_cast<uintptr_t>(first) % 4) return fail(ST_ERR_ALIGNMENT, "first: not 4-byte aligned");
+  const int64_t n = (int64_t)count * c->Hkv * c->D;
+  if (n / 2048 >= 1 << 23) return fail(ST_ERR_UNSUPPORTED, "2^34 values of a sequence or more");
+  if (n == 0 || c->B == 0) return ST_OK;
+  if (k_out == nullptr && v_out == nullptr) return fail(ST_ERR_INVALID_ARG, "k_out and v_out: one of them is needed");
+  st::ReadArgs a;
+  memset(&a, 0, sizeof(a));
+  a.c = cache_args(c);
+  a.first = first;
+  a.count = count;
+  if (k_out) {
+    ST_TRY(check_tensor("k_out", k_out, dtype, n));
+    a.k_out = view_of(k_out);
+  }
+  if (v_out) {
+    ST_TRY(check_tensor("v_out", v_out, dtype, n));
+    a.v_out = view_of(v_out);
+  }
+  if (a.k_out.ptr == a.v_out.ptr) return fail(ST_ERR_INVALID_ARG, "v_out aliases k_out");
+  ST_HIP(st::launch_cache_read(a, dtype, (hipStream_t)hip_stream), "st_cache_read launch");
+  return ST_OK;
+}
+
+size_t st_attn_cache_workspace_bytes(const st_cache_rows* r, const st_cache* c) {
+  if (check_rows(r, c) != ST_OK) return 0;
+  return 0;
+}
+
+st_status st_attn_cache(const st_cache_rows* r, const st_cache* c, const int32_t* starts, const int64_t* q_first, const st_tensor* q, float* o_part,
+                        float* lse_part, void* o_lowp, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  ST_TRY(check_rows(r, c));
+  ST_TRY(check_starts(c, starts, r->T));
+  if (reinterpret_cast<uintptr_t>(q_first) % 8) return fail(ST_ERR_ALIGNMENT, "q_first: not 8-byte aligned");
+  const int64_t n_q = (int64_t)r->T * r->Hq * c->D;
+  ST_TRY(check_tensor("q", q, r->dtype, n_q));
+  if (n_q == 0 || c->B == 0 || r->max_rows == 0) return ST_OK;
+  if (o_part == nullptr && o_lowp == nullptr) return fail(ST_ERR_INVALID_ARG, "o_part and o_lowp: one of them is needed");
+  if ((void*)o_part == o_lowp) return fail(ST_ERR_INVALID_ARG, "o_lowp aliases o_part");
+  if (o_part) ST_TRY(check_f32("o_part", o_part, n_q));
+  ST_TRY(check_low("o_lowp", o_lowp));
+  ST_TRY(check_f32("lse_part", lse_part, n_q));
+  st::CacheAttnArgs a;
+  memset(&a, 0, sizeof(a));
+  a.c = cache_args(c);
+  a.q = view_of(q);
+  a.starts = starts;
+  a.q_first = q_first;
+  a.T = r->T; a.Hq = r->Hq; a.max_rows = r->max_rows; a.causal = r->causal ? 1 : 0; a.window = r->window;
+  a.scale = r->scale; a.cap = r->softcap; a.slopes = r->slopes;
+  a.o = o_part;
+  a.lse = lse_part;
+  a.o_lowp = o_lowp;
+  ST_TRY(check_workspace(workspace, workspace_bytes, st_attn_cache_workspace_bytes(r, c), "cache attention"));
+  ST_HIP(st::launch_cache_attn(a, r->dtype == ST_BF16, (hipStream_t)hip_stream), "st_attn_cache launch");
+  return ST_OK;
+}
+
+}  // extern "C"

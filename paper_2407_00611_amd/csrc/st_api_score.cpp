@@ -114,63 +114,6 @@ ScorePlan bwd_plan(const st::Shape& s, int dtype, bool spans) {
   return p;
 }
 
-st_status check_workspace(const void* ws, size_t bytes, size_t need, const char* what) {
-  if (need == 0) return ST_OK;
-  if (ws == nullptr || bytes < need) return fail(ST_ERR_WORKSPACE, "%s workspace needs %zu bytes", what, need);
-  if (reinterpret_cast<uintptr_t>(ws) % 256) return fail(ST_ERR_ALIGNMENT, "workspace: not 256-byte aligned");
-  return ST_OK;
-}
-
-st_status check_low(const char* name, const void* p) {
-  if (reinterpret_cast<uintptr_t>(p) % 16) return fail(ST_ERR_ALIGNMENT, "%s: not 16-byte aligned", name);
-  return ST_OK;
-}
-
-st_status check_rope(const st_rope_desc* d, const int32_t* positions, const double* freq) {
-  if (d == nullptr) return fail(ST_ERR_INVALID_ARG, "null descriptor");
-  if (d->dtype != ST_F32 && d->dtype != ST_BF16) return fail(ST_ERR_INVALID_ARG, "unknown dtype %d", d->dtype);
-  if (d->B < 0 || d->S < 0 || d->Hkv < 0) return fail(ST_ERR_INVALID_ARG, "negative size");
-  if (d->Hq <= 0 || d->D <= 0) return fail(ST_ERR_INVALID_ARG, "Hq and D must be positive");
-  if (d->D > 256 || d->D % 8 != 0) return fail(ST_ERR_UNSUPPORTED, "D <= 256 and D %% 8 == 0 are needed (D=%d)", d->D);
-  if ((int64_t)d->Hq + d->Hkv > 16384) return fail(ST_ERR_UNSUPPORTED, "more than 16384 heads");
-  if ((int64_t)d->B * d->S > (int64_t)1 << 25) return fail(ST_ERR_UNSUPPORTED, "more than 2^25 tokens");
-  if (d->rot < 0 || d->rot > d->D || d->rot % 2) return fail(ST_ERR_INVALID_ARG, "rot = %d must be even, 0 .. D", d->rot);
-  if (d->pairing != ST_ROPE_HALVES && d->pairing != ST_ROPE_NEIGHBOURS) return fail(ST_ERR_INVALID_ARG, "unknown pairing %d", d->pairing);
-  if (d->norm != 0 && d->norm != 1) return fail(ST_ERR_INVALID_ARG, "unknown norm %d", d->norm);
-  if (d->norm && !(d->eps >= 0.f && d->eps <= 3.0e38f)) return fail(ST_ERR_INVALID_ARG, "eps must be finite and not negative");
-  if (d->n_axes < 1 || d->n_axes > ST_ROPE_MAX_AXES) return fail(ST_ERR_INVALID_ARG, "n_axes must be in 1..%d", ST_ROPE_MAX_AXES);
-  int64_t pairs = 0;
-  for (int x = 0; x < d->n_axes; ++x) {
-    if (d->axis_pairs[x] < 0) return fail(ST_ERR_INVALID_ARG, "axis_pairs[%d] is negative", x);
-    pairs += d->axis_pairs[x];
-  }
-  if (pairs != d->rot / 2) return fail(ST_ERR_INVALID_ARG, "axis_pairs add up to %lld, rot has %d pairs", (long long)pairs, d->rot / 2);
-  ST_TRY(check_segments(d->S, d->offset, d->seg, d->offset2));
-  if (positions == nullptr && d->n_axes != 1) return fail(ST_ERR_INVALID_ARG, "more than one axis needs positions");
-  if (positions != nullptr && d->seg != 0) return fail(ST_ERR_INVALID_ARG, "positions and a second run of rows exclude each other");
-  if (d->rot > 0 && (int64_t)d->B * d->S > 0 && freq == nullptr) return fail(ST_ERR_INVALID_ARG, "freq: null pointer");
-  if (reinterpret_cast<uintptr_t>(freq) % 8 || reinterpret_cast<uintptr_t>(positions) % 4) return fail(ST_ERR_ALIGNMENT, "freq needs 8-byte, positions 4-byte alignment");
-  return ST_OK;
-}
-
-st_status check_weight(const char* name, const void* p) {
-  if (reinterpret_cast<uintptr_t>(p) % 16) return fail(ST_ERR_ALIGNMENT, "%s: not 16-byte aligned", name);
-  return ST_OK;
-}
-
-st::RopeArgs rope_args(const st_rope_desc* d) {
-  st::RopeArgs g;
-  memset(&g, 0, sizeof(g));
-  g.B = d->B; g.S = d->S; g.Hq = d->Hq; g.Hkv = d->Hkv; g.D = d->D; g.rot = d->rot;
-  g.next = d->pairing == ST_ROPE_NEIGHBOURS;
-  g.norm = d->norm;
-  g.eps = d->eps;
-  g.n_axes = d->n_axes;
-  for (int x = 0; x < ST_ROPE_MAX_AXES; ++x) g.axis_pairs[x] = d->axis_pairs[x];
-  g.offset = d->offset; g.seg = d->seg; g.offset2 = d->offset2;
-  return g;
-}
-
 }  // namespace
 
 extern "C" {

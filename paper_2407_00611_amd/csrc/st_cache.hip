@@ -1,0 +1,361 @@
+// New keys and values into a cache of pages, and chunks of it out again.
+//
+//   n = x rsqrt(mean(x^2) + eps) w,  (a, b) -> (a cos t - b sin t, a sin t + b cos t)      queries and keys, as st_rope.hip
+//   e = max(e of the rows that are there, least e with max |x| <= 448 2^e)                 of a page and head, pages in e4m3
+//   stored = e4m3(x 2^-e);  rows that are there: e4m3(stored 2^(e - e'))                   (exact but below the least value)
+#include <algorithm>
+
+#include "st_cache.h"
+#include "st_rope_rows.h"
+
+namespace st {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kMaxPairs = 128;
+constexpr int kTokensMost = 8;                       // tokens whose angles a workgroup holds for the queries
+constexpr int kQueryRows = 512;                      // rows (token, head) of queries for a workgroup, about
+
+// ---- arithmetic of the keys: fp32 as the queries', or fp64
+
+// sine and cosine of x turns, |x| <= 1/2: x is taken to the nearest quarter, |r| <= pi / 4 from there, and both series of r are cut where the
+// next term is below 1e-12
+__device__ __forceinline__ void sincos_turns(double x, double& s, double& c) {
+  const double n = rint(4.0 * x), r = (x - 0.25 * n) * 6.283185307179586477, z = r * r;
+  const double ps = r * (1.0 + z * (-1.0 / 6 + z * (1.0 / 120 + z * (-1.0 / 5040 + z * (1.0 / 362880 + z * (-1.0 / 39916800 + z * (1.0 / 6227020800.0)))))));
+  const double pc = 1.0 + z * (-0.5 + z * (1.0 / 24 + z * (-1.0 / 720 + z * (1.0 / 40320 + z * (-1.0 / 3628800 + z * (1.0 / 479001600.0))))));
+  const int k = (int)n & 3;
+  const double u = k & 1 ? pc : ps, v = k & 1 ? ps : pc;
+  s = k & 2 ? -u : u;
+  c = (k + 1) & 2 ? -v : v;
+}
+__device__ __forceinline__ void sincos_turns(double x, float& s, float& c) { sincospif((float)(2.0 * x), &s, &c); }
+
+// To fp32 so that a second rounding, to fewer bits, gives what one rounding of x would: towards zero, with a one in the last place where
+// anything was cut off.
+__device__ __forceinline__ float sticky(double x) {
+  const float f = (float)x;
+  if ((double)f == x || f != f) return f;
+  const uint32_t u = __float_as_uint(f) - (fabs((double)f) > fabs(x) ? 1u : 0u);
+  return __uint_as_float(u | 1u);
+}
+__device__ __forceinline__ float sticky(float x) { return x; }
+
+template <typename A>
+__device__ __forceinline__ A lanes_sum(A x, int lanes) {
+  for (int d = 1; d < lanes; d *= 2) x += __shfl_xor(x, d);
+  return x;
+}
+__device__ __forceinline__ float inv_root(float x) { return rsqrtf(x); }
+__device__ __forceinline__ double inv_root(double x) { return 1.0 / sqrt(x); }
+
+__device__ __forceinline__ bool is_finite(float x) { return fabsf(x) <= 3.402823466e38f; }
+// The least e, -126 at the least, with top <= 448 2^e = 1.75 2^(e + 8)
+__device__ __forceinline__ int exponent_for(float top) {
+  const uint32_t u = __float_as_uint(top);
+  return max((int)(u >> 23) - 127 - 8 + ((u & 0x7fffff) > 0x600000 ? 1 : 0), -126);
+}
+__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }   // -126 .. 127
+
+__device__ __forceinline__ double place_of_token(const RopeArgs& g, int64_t token, int t, int pair) {
+  if (!g.positions) return (double)token;
+  int axis = 0, end = 0;                             // (no index that is known at run time only: the list would be copied to memory)
+#pragma unroll
+  for (int y = 0; y + 1 < ST_ROPE_MAX_AXES; ++y) {
+    end += g.axis_pairs[y];
+    axis += y + 1 < g.n_axes && pair >= end;
+  }
+  return (double)g.positions[(int64_t)axis * g.S + t];
+}
+__device__ __forceinline__ double fraction(double turns) { return turns - rint(turns); }
+constexpr double kPerTurn = 0.15915494309189533577;
+
+// What a workgroup has of the new rows: those of sequence b whose tokens lie in one page
+struct Piece {
+  int b, j, slot0;           // sequence, page of its pages, token of its first row
+  int lo, hi;                // tokens
+  int row0;                  // packed row of token lo
+};
+// Sequence b has at most n_b / page + 2 such pieces, so the workgroups from starts[b] / page + 2 b on are enough for it (the number before the
+// next one's is at least that), and a workgroup finds its sequence by a look at all of them, a thread each.
+__device__ __forceinline__ bool find_piece(const AppendArgs& a, Piece& p, int* found) {
+  const int u = blockIdx.x, tid = threadIdx.x, shift = a.c.shift, T = a.g.S;
+  if (tid == 0) *found = -1;
+  __syncthreads();
+  for (int b = tid; b < a.c.B; b += kThreads) {
+    const SeqRows r = seq_rows(a.starts, b, T);
+    if (u >= (r.first >> shift) + 2 * b && u < ((r.first + r.n) >> shift) + 2 * b + 2) *found = b;
+  }
+  __syncthreads();
+  p.b = __builtin_amdgcn_readfirstlane(*found);
+  if (p.b < 0) return false;
+  const SeqRows r = seq_rows(a.starts, p.b, T);
+  const int len = a.c.lens[p.b];
+  p.slot0 = len - r.n;
+  p.j = (max(p.slot0, 0) >> shift) + u - (r.first >> shift) - 2 * p.b;
+  p.lo = (int)min(max((int64_t)max(p.slot0, 0), (int64_t)p.j << shift), (int64_t)max(len, 0));
+  p.hi = (int)min((int64_t)len, ((int64_t)p.j + 1) << shift);
+  p.row0 = r.first + p.lo - p.slot0;
+  return p.lo < p.hi;
+}
+
+// T: of the rows; A: of the arithmetic of keys; S: what the pages hold
+template <typename T, typename A, typename S, int V, int U, bool NEXT>
+__device__ __forceinline__ void append_rows(const AppendArgs& a, const Piece& p, int h, bool key, int lanes, int* shared) {
+  constexpr bool E4M3 = std::is_same<S, uint8_t>::value;
+  const RopeArgs& g = a.g;
+  const int tid = threadIdx.x, chunk = tid & (lanes - 1), group = tid / lanes, groups = kThreads / lanes, half = g.rot / 2;
+  if (p.j >= a.c.width) return;
+  const int page = __builtin_amdgcn_readfirstlane(page_of(a.c, p.b, p.j));
+  if (page < 0) return;
+  const View& in = key ? g.k : a.v_in;
+  const View& to = key ? a.c.k : a.c.v;
+  const T* src = (const T*)in.ptr + (int64_t)p.row0 * in.ss + (int64_t)h * in.sh;
+  S* dst = (S*)const_cast<void*>(to.ptr) + (int64_t)page * to.sb + (int64_t)h * to.sh;
+  const int begun = p.lo & ((1 << a.c.shift) - 1), n = p.hi - p.lo;
+  Place<V, NEXT> at[U];
+  double f[U][V];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    at[u] = place_of<V, NEXT>(g, chunk + u * lanes);
+#pragma unroll
+    for (int e = 0; e < V; ++e) f[u][e] = key && at[u].pair + e < half ? g.freq[at[u].pair + e] * kPerTurn : 0.0;
+  }
+  auto make = [&](int row, Vec<V> (&x)[U], Vec<V> (&z)[U]) {   // of the rows as they are stored, before they are rounded
+#pragma unroll
+    for (int u = 0; u < U; ++u) load_pairs<V, NEXT>(src + row * in.ss, at[u], x[u], z[u]);
+    if (!key) return;
+    A r = 1;
+    if (g.norm) {
+      A sum = 0;
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int e = 0; e < V; ++e) sum += at[u].live ? (A)x[u].x[e] * (A)x[u].x[e] + (A)z[u].x[e] * (A)z[u].x[e] : (A)0;
+      r = inv_root(lanes_sum(sum, lanes) / (A)g.D + (A)g.eps);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      Vec<V> wa, wb;
+      if (g.k_weight) load_pairs<V, NEXT>(g.k_weight, at[u], wa, wb);
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        A y = (A)x[u].x[e], w = (A)z[u].x[e];
+        if (g.norm) {
+          y *= g.k_weight ? r * (A)wa.x[e] : r;
+          w *= g.k_weight ? r * (A)wb.x[e] : r;
+        }
+        if (at[u].pair + e < half) {                   // (others as they are: zero times infinity is NaN)
+          A c, s;
+          sincos_turns(fraction(place_of_token(g, g.offset + p.lo + row, p.row0 + row, at[u].pair + e) * f[u][e]), s, c);
+          const A m = y * c - w * s;
+          w = y * s + w * c;
+          y = m;
+        }
+        x[u].x[e] = E4M3 ? sticky(y) : (float)y;
+        z[u].x[e] = E4M3 ? sticky(w) : (float)w;
+      }
+    }
+  };
+  Vec<V> x[U], z[U];
+  float unit = 1.f;
+  if constexpr (E4M3) {
+    uint8_t* scale = (key ? a.c.k_scale : a.c.v_scale) + (int64_t)page * g.Hkv + h;
+    const int had = begun > 0 ? (int)*scale - 127 : -126;
+    float top = 0.f;
+    for (int row = group; row < n; row += groups) {
+      make(row, x, z);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          if (at[u].live && is_finite(x[u].x[e])) top = fmaxf(top, fabsf(x[u].x[e]));
+          if (at[u].live && is_finite(z[u].x[e])) top = fmaxf(top, fabsf(z[u].x[e]));
+        }
+    }
+    for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+    if ((tid & 63) == 0) shared[tid >> 6] = __float_as_int(top);
+    __syncthreads();
+    top = __int_as_float(max(max(shared[0], shared[1]), max(shared[2], shared[3])));
+    const int e = max(had, exponent_for(top));
+    unit = power_of_two(-e);
+    if (e > had && begun > 0) {
+      const int less = e - had;
+      const float by = less < 32 ? power_of_two(-less) : 0.f;
+      for (int row = group; row < begun; row += groups)
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          S* to_row = dst + (int64_t)row * to.ss;
+          load_pairs<V, NEXT>(to_row, at[u], x[u], z[u]);
+#pragma unroll
+          for (int y = 0; y < V; ++y) x[u].x[y] *= by, z[u].x[y] *= by;
+          if (at[u].live) store_pairs<V, NEXT>(to_row, at[u], x[u], z[u]);
+        }
+    }
+    if (tid == 0) *scale = (uint8_t)(e + 127);
+  }
+  for (int row = group; row < n; row += groups) {
+    make(row, x, z);
+    S* to_row = dst + (int64_t)(begun + row) * to.ss;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if constexpr (E4M3) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          x[u].x[e] = is_finite(x[u].x[e]) ? x[u].x[e] * unit : NAN;
+          z[u].x[e] = is_finite(z[u].x[e]) ? z[u].x[e] * unit : NAN;
+        }
+      }
+      if (at[u].live) store_pairs<V, NEXT>(to_row, at[u], x[u], z[u]);
+    }
+  }
+}
+
+// grid (pieces, 2 Hkv + groups of query heads)
+template <typename T, typename S, int V, int U, bool NEXT>
+__global__ __launch_bounds__(kThreads) void cache_append_kernel(const AppendArgs a, int lanes, int q_heads) {
+  constexpr bool E4M3 = std::is_same<S, uint8_t>::value;
+  __shared__ float2 angles[kTokensMost * kMaxPairs];
+  __shared__ int shared[4];
+  const RopeArgs& g = a.g;
+  Piece p;
+  if (!find_piece(a, p, shared)) return;
+  __syncthreads();
+  const int y = blockIdx.y;
+  if (y < 2 * g.Hkv) {
+    append_rows<T, typename std::conditional<E4M3, double, float>::type, S, V, U, NEXT>(a, p, y >> 1, (y & 1) == 0, lanes, shared);
+    return;
+  }
+  // queries: some heads of the piece's tokens, eight tokens at a time, whose angles serve all heads
+  const int h0 = (y - 2 * g.Hkv) * q_heads, heads = min(q_heads, g.Hq - h0), half = g.rot / 2;
+  const int tid = threadIdx.x, chunk = tid & (lanes - 1), group = tid / lanes, groups = kThreads / lanes;
+  Place<V, NEXT> at[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) at[u] = place_of<V, NEXT>(g, chunk + u * lanes);
+  for (int t0 = 0; t0 < p.hi - p.lo; t0 += kTokensMost) {
+    const int n = min(kTokensMost, p.hi - p.lo - t0);
+    if (t0 > 0) __syncthreads();
+    for (int x = tid; x < n * half; x += kThreads) {
+      const int t = x / half, j = x - t * half;
+      float2 w;
+      sincos_turns(fraction(place_of_token(g, g.offset + p.lo + t0 + t, p.row0 + t0 + t, j) * (g.freq[j] * kPerTurn)), w.y, w.x);
+      angles[x] = w;
+    }
+    __syncthreads();
+    for (int row = group; row < n * heads; row += groups) {
+      const int t = row / heads, h = h0 + row - t * heads;
+      const int64_t i = p.row0 + t0 + t;
+      const T* src = (const T*)g.q.ptr + i * g.q.ss + h * g.q.sh;
+      T* dst = (T*)const_cast<void*>(g.q_out.ptr) + i * g.q_out.ss + h * g.q_out.sh;
+      Vec<V> x[U], z[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) load_pairs<V, NEXT>(src, at[u], x[u], z[u]);
+      float r = 1.f;
+      if (g.norm) {
+        float sum = 0.f;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int e = 0; e < V; ++e) sum += at[u].live ? x[u].x[e] * x[u].x[e] + z[u].x[e] * z[u].x[e] : 0.f;
+        r = rsqrtf(row_sum(sum, lanes) / (float)g.D + g.eps);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        Vec<V> wa, wb, ya, yb;
+        if (g.q_weight) load_pairs<V, NEXT>(g.q_weight, at[u], wa, wb);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          const bool turned = at[u].pair + e < half;
+          const float2 w = turned ? angles[t * half + at[u].pair + e] : make_float2(1.f, 0.f);
+          const float m = g.norm ? x[u].x[e] * (g.q_weight ? r * wa.x[e] : r) : x[u].x[e];
+          const float o = g.norm ? z[u].x[e] * (g.q_weight ? r * wb.x[e] : r) : z[u].x[e];
+          ya.x[e] = turned ? m * w.x - o * w.y : m;
+          yb.x[e] = turned ? m * w.y + o * w.x : o;
+        }
+        if (at[u].live) store_pairs<V, NEXT>(dst, at[u], ya, yb);
+      }
+    }
+  }
+}
+
+// ---- chunks
+
+// V neighbouring values of a row a thread; grid (., B, 2: keys and values)
+template <typename S, typename T, int V>
+__global__ __launch_bounds__(kThreads) void cache_read_kernel(const ReadArgs a) {
+  const CacheArgs& c = a.c;
+  const View& out = blockIdx.z ? a.v_out : a.k_out;
+  if (!out.ptr) return;
+  const View& in = blockIdx.z ? c.v : c.k;
+  const int b = blockIdx.y, len = seq_len(c, b), per = c.D / V, heads = c.Hkv;
+  const int64_t first = a.first ? a.first[b] : 0, x = (int64_t)blockIdx.x * kThreads + threadIdx.x, row = x / per;
+  const int d = (int)(x - row * per) * V;
+  const int64_t i = row / heads;
+  const int h = (int)(row - i * heads);
+  if (i >= a.count) return;
+  const int64_t token = first + i;
+  const int page = token >= 0 && token < len ? page_of(c, b, (int)(token >> c.shift)) : -1;
+  float y[V];
+#pragma unroll
+  for (int e = 0; e < V; ++e) y[e] = 0.f;
+  if (page >= 0) {
+    const S* src = (const S*)in.ptr + (int64_t)page * in.sb + (token & ((1 << c.shift) - 1)) * in.ss + (int64_t)h * in.sh + d;
+    if constexpr (std::is_same<S, uint8_t>::value) {
+      const u32x4 w = *reinterpret_cast<const u32x4*>(src);
+      const float s = scale_value((blockIdx.z ? c.v_scale : c.k_scale)[(int64_t)page * heads + h]);
+#pragma unroll
+      for (int e = 0; e < V; e += 4) {
+        const float2 p = e4m3_pair<false>(w[e / 4]), q = e4m3_pair<true>(w[e / 4]);
+        y[e] = p.x * s; y[e + 1] = p.y * s; y[e + 2] = q.x * s; y[e + 3] = q.y * s;
+      }
+    } else {
+      const Vec<V> w = load<V>(src);
+#pragma unroll
+      for (int e = 0; e < V; ++e) y[e] = w.x[e];
+    }
+  }
+  T* dst = (T*)const_cast<void*>(out.ptr) + b * out.sb + i * out.ss + h * out.sh + d;
+#pragma unroll
+  for (int e = 0; e < V; e += 8) {
+    Vec<8> w;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) w.x[u] = y[e + u];
+    store<8>(dst + e, w);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_cache_append(const AppendArgs& a, bool bf16, hipStream_t stream) {
+  const RopeArgs& g = a.g;
+  if (g.S <= 0 || a.c.B <= 0) return hipSuccess;
+  const int64_t pieces = ((int64_t)g.S >> a.c.shift) + 2 * (int64_t)a.c.B;
+  const int q_heads = std::max(1, kQueryRows >> a.c.shift), y = 2 * g.Hkv + (g.Hq + q_heads - 1) / q_heads;
+  if (pieces > (1 << 23) || y > 65535) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)pieces, (unsigned)y), block(kThreads);
+  ProfScope prof("cache_append", stream);
+  with_pairs(g, [&](auto v, auto u, auto next) {
+    constexpr int V = decltype(v)::value, U = decltype(u)::value;
+    constexpr bool NEXT = decltype(next)::value;
+    const int lanes = lanes_of(g.D, V);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, a, lanes, q_heads); };
+    if (a.c.dtype == ST_E4M3) bf16 ? go(cache_append_kernel<uint16_t, uint8_t, V, U, NEXT>) : go(cache_append_kernel<float, uint8_t, V, U, NEXT>);
+    else bf16 ? go(cache_append_kernel<uint16_t, uint16_t, V, U, NEXT>) : go(cache_append_kernel<float, float, V, U, NEXT>);
+  });
+  return hipGetLastError();
+}
+
+hipError_t launch_cache_read(const ReadArgs& a, int out_dtype, hipStream_t stream) {
+  if (a.count <= 0 || a.c.B <= 0) return hipSuccess;
+  const int V = a.c.dtype == ST_E4M3 ? 16 : 8;
+  const int64_t threads = (int64_t)a.count * a.c.Hkv * (a.c.D / V), blocks = (threads + kThreads - 1) / kThreads;
+  if (blocks > (1 << 23)) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)blocks, (unsigned)a.c.B, 2), block(kThreads);
+  ProfScope prof("cache_read", stream);
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, a); };
+  if (a.c.dtype == ST_E4M3) out_dtype == ST_BF16 ? go(cache_read_kernel<uint8_t, uint16_t, 16>) : go(cache_read_kernel<uint8_t, float, 16>);
+  else out_dtype == ST_BF16 ? go(cache_read_kernel<uint16_t, uint16_t, 8>) : go(cache_read_kernel<float, float, 8>);
+  return hipGetLastError();
+}
+
+}  // namespace st

@@ -1,0 +1,95 @@
+"""Caches for the tests: pages in any order, NaN wherever no sequence has a token, and the oracle's copy of them."""
+import torch
+
+import paper_2407_00611_amd as st
+from oracle import cache as oc
+
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "e4m3": torch.float8_e4m3fn}
+
+
+def rows_of(counts):
+    return torch.tensor([0] + list(counts)).cumsum(0).to(torch.int32)
+
+
+def pages_like(shape, dtype, layout, device):
+    """Storage for keys and values [n_pages, page, Hkv, D], in one of the layouts a program may keep."""
+    n, page, heads, D = shape
+    if layout == "heads_first":
+        return [torch.empty((n, heads, page, D), dtype=torch.float32, device=device).to(dtype).transpose(1, 2) for _ in range(2)]
+    if layout == "together":
+        both = torch.empty((n, 2, page, heads, D), dtype=torch.float32, device=device).to(dtype)
+        return [both[:, 0], both[:, 1]]
+    return [torch.empty(shape, dtype=torch.float32, device=device).to(dtype) for _ in range(2)]
+
+
+class Case:
+    def __init__(self, seed, kind, lens, page, Hkv, D, layout="dense", more=1, stale=True):
+        g = torch.Generator().manual_seed(seed)
+        self.g, self.kind, self.lens, self.page, B = g, kind, list(lens), page, len(lens)
+        width = max([1] + [-(-n // page) for n in lens]) + more
+        n_pages = B * width + 2
+        self.table = torch.randperm(n_pages, generator=g)[:B * width].reshape(B, width).to(torch.int32)
+        shape = (n_pages, page, Hkv, D)
+        self.k, self.v = pages_like(shape, TYPES[kind], layout, "cuda")
+        self.scales, self.oracle = [None, None], []
+        live = torch.zeros((n_pages, page), dtype=torch.bool)
+        for b, n in enumerate(lens):
+            for x in range(n):
+                live[self.table[b, x // page], x % page] = True
+        for i, to in enumerate((self.k, self.v)):
+            x, e = torch.randn(shape, generator=g, dtype=torch.float64), None
+            if kind == "e4m3":
+                e = torch.randint(-10, 3, (n_pages, Hkv), generator=g)
+                x = oc.e4m3_near((x * torch.exp2(-e[:, None, :, None].double())).clamp(-448, 448))
+                self.scales[i] = (e + 127).to(torch.uint8).cuda()
+            else:
+                x = x.to(TYPES[kind]).double()
+            if stale:
+                x = torch.where(live[:, :, None, None], x, torch.nan)
+            to.copy_(x.float().to(TYPES[kind]).cuda())
+            self.oracle.append(oc.Pages(x, e))
+
+    def cache(self, lens=None, table=None):
+        lens = self.lens if lens is None else lens
+        table = self.table if table is None else table
+        return st.KVCache(self.k, self.v, table.cuda(), torch.tensor(lens, dtype=torch.int32).cuda(), *self.scales)
+
+    def held(self, b, lens=None, table=None):
+        lens, table = self.lens if lens is None else lens, self.table if table is None else table
+        (k, there), (v, _) = (p.held(table, lens, b) for p in self.oracle)
+        return k.nan_to_num(0.0) if not there.all() else k, v.nan_to_num(0.0) if not there.all() else v, there
+
+
+def check_attention(case, q, starts, o, lse, causal, scale, window=0, cap=0.0, slopes=None, q_first=None, lens=None, table=None, max_rows=None, lowp=False):
+    """Rows of every sequence against the oracle.  Bounds, from the roundings of the definition's steps: products of D terms in fp32, each
+    2^-24 of its part of sum |q k| (and as much again for scale, cap and reference: 4 D 2^-24 is beyond both), exponentials and sums
+    2^-20 of the result; bf16 rows: probabilities rounded to bf16, 2^-8 of sum p |v|; O in bf16: 2^-8 of itself."""
+    lens = case.lens if lens is None else lens
+    bf16 = q.dtype == torch.bfloat16
+    T = q.shape[1]
+    done = torch.zeros(T, dtype=torch.bool)
+    q, o, lse = q.double().cpu(), o.double().cpu(), lse.double().cpu()
+    for b in range(len(lens)):
+        n = int(starts[b + 1] - starts[b])
+        if max_rows is not None:
+            n = min(n, max_rows)
+        if n <= 0:
+            continue
+        at = slice(int(starts[b]), int(starts[b]) + n)
+        done[at] = True
+        p0 = int(q_first[b]) if q_first is not None else lens[b] - int(starts[b + 1] - starts[b])
+        k, v, there = case.held(b, lens, table)
+        ref, ref_lse, mass, size = oc.attention(q[0, at], k, v, there, torch.arange(n) + p0, causal, scale, window, cap, slopes)
+        far = 0.0 if slopes is None else float(slopes.abs().max()) * (abs(p0) + n + k.shape[0])
+        s_err = 4 * q.shape[3] * 2.0 ** -24 * (size + 1e-3) + (cap + far) * 2.0 ** -21 + 2.0 ** -21
+        empty = ref_lse == -torch.inf
+        got = lse[0, :, at].t()
+        assert torch.equal(got == -torch.inf, empty), f"sequence {b}: empty rows"
+        assert (o[0, at][empty] == 0).all(), f"sequence {b}: an empty row has values"
+        off = torch.where(empty, 0.0, (got - ref_lse).abs())
+        bound = s_err + 2.0 ** -22 * ref_lse.abs().nan_to_num(posinf=0.0) + 2.0 ** -20
+        assert (off <= torch.where(empty, 1.0, bound)).all(), f"sequence {b}: lse {float((off / bound).max()):.2f} of the bound"
+        bound = mass * (2 * s_err[..., None] + 2.0 ** -20 + (2.0 ** -8 if bf16 else 0.0)) + (2.0 ** -8 * ref.abs() if lowp and bf16 else 0.0) + 1e-30
+        off = (o[0, at] - ref).abs()
+        assert (off <= bound).all(), f"sequence {b}: O {float((off / bound).max()):.2f} of the bound"
+    return done

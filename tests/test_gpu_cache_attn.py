@@ -1,0 +1,138 @@
+"""Attention of packed rows against a cache of pages (st_attn_cache) against the 64-bit oracle; bounds in cache_cases.check_attention."""
+import math
+
+import pytest
+import torch
+
+import paper_2407_00611_amd as st
+from cache_cases import TYPES, Case, check_attention, rows_of
+
+pytestmark = pytest.mark.gpu
+
+PAIRS = [("bf16", "e4m3"), ("bf16", "bf16"), ("f32", "e4m3"), ("f32", "f32")]
+
+
+def _attend(dtype, kind, lens, counts, page=16, Hq=4, Hkv=2, D=64, layout="dense", causal=True, window=0, cap=0.0, bias=False, q_first=None, rows="dense",
+            more_rows=0, max_rows=None, table=None, scale=None, lowp=False, change=None, seed=0):
+    dt = TYPES[dtype]
+    case = Case(seed, kind, lens, page, Hkv, D, layout)
+    if change is not None:
+        change(case)
+    T = sum(counts) + more_rows
+    if rows == "packed":
+        q = torch.randn((1, T, Hq + 3, D), generator=case.g).to(dt).cuda()[:, :, 1:Hq + 1]
+    elif rows == "heads_first":
+        q = torch.randn((1, Hq, T, D), generator=case.g).to(dt).cuda().transpose(1, 2)
+    else:
+        q = torch.randn((1, T, Hq, D), generator=case.g).to(dt).cuda()
+    scale = (4.0 if cap else 1.0) / math.sqrt(D) if scale is None else scale
+    slopes = torch.tensor([2.0 ** (-1.0 - h) for h in range(Hq)]) if bias else None
+    starts = rows_of(counts)
+    print(f"[{dtype} from {kind}, {lens} by {counts}, page {page}, {Hq}/{Hkv} D{D} {layout} {rows}, window {window}, cap {cap}, bias {bias}, first {q_first}]", flush=True)
+    o = torch.full((1, T, Hq, D), 7.0, dtype=dt if lowp else torch.float32, device="cuda")
+    lse = torch.full((1, Hq, T), 7.0, device="cuda")
+    first = torch.tensor(q_first, dtype=torch.int64).cuda() if q_first is not None else None
+    how = dict(max_rows=max_rows, window=window, softcap=cap, slopes=slopes.cuda() if bias else None, q_first=first)
+    got, got_lse = st.st_attn_cache(q, starts.cuda(), case.cache(table=table), causal, scale, lse_part=lse, **how, **({"o_lowp": o} if lowp else {"o_part": o}))
+    assert got is o and got_lse is lse
+    done = check_attention(case, q, starts, o, lse, causal, scale, window, cap, slopes, q_first, table=table, max_rows=max_rows, lowp=lowp)
+    assert (o[0, ~done] == 7.0).all() and (lse[0][:, ~done] == 7.0).all(), "rows of no sequence"
+    return case, q, o, lse
+
+
+CASES = [
+    dict(lens=[1], counts=[1]),
+    dict(lens=[16, 17, 5, 64], counts=[1, 1, 1, 1], Hq=8, Hkv=2),
+    dict(lens=[100, 0, 33, 700], counts=[1, 1, 1, 1], Hq=2, Hkv=2, page=32),           # one that sees nothing, no shared heads
+    dict(lens=[90, 200], counts=[5, 3], Hq=8, Hkv=1, page=64, lowp=True),              # some rows each
+    dict(lens=[130], counts=[130], Hq=4, Hkv=4, page=16),                              # a whole prompt
+    dict(lens=[300, 40, 200], counts=[70, 1, 33], Hq=6, Hkv=2, page=128, rows="packed", more_rows=3),
+    dict(lens=[300, 50], counts=[7, 7], window=19, page=16),
+    dict(lens=[300, 50], counts=[1, 1], window=64, q_first=[310, 200], page=256),      # rows ahead of the cache, one past its window
+    dict(lens=[80, 30], counts=[4, 4], q_first=[-2, 10], causal=True),                 # rows before the first token
+    dict(lens=[80, 30], counts=[20, 1], causal=False, layout="heads_first"),
+    dict(lens=[200, 30], counts=[9, 3], cap=15.0, layout="together"),
+    dict(lens=[200, 30], counts=[9, 1], bias=True, Hq=8),
+    dict(lens=[200, 30], counts=[40, 1], bias=True, cap=30.0, window=50, rows="heads_first"),
+    dict(lens=[5000], counts=[1], Hq=1, Hkv=1, page=64),                               # keys of several workgroups
+    dict(lens=[2000, 3, 500], counts=[2, 2, 2], Hq=2, Hkv=1, page=16),
+    dict(lens=[40] * 300, counts=[1] * 300, Hq=1, Hkv=1),                              # more sequences than a workgroup has threads
+    dict(lens=[70, 70], counts=[33, 20], max_rows=25),
+    dict(lens=[60, 60], counts=[0, 2], Hq=64, Hkv=1),
+]
+
+
+@pytest.mark.parametrize("case", range(len(CASES)))
+@pytest.mark.parametrize("dtype,kind", PAIRS)
+def test_rows_against_a_cache(dtype, kind, case):
+    _attend(dtype, kind, seed=case, D=128 if case % 3 == 1 else 64, **CASES[case])
+
+
+@pytest.mark.parametrize("D", [8, 40, 80, 128, 200, 256])
+@pytest.mark.parametrize("kind", ["f32", "e4m3"])
+def test_head_sizes_of_fp32(D, kind):
+    if kind == "e4m3" and D % 16:
+        pytest.skip("pages in 8 bits have head sizes of 16")
+    _attend("f32", kind, [70, 33], [3, 1], D=D, Hq=6, Hkv=2)
+    _attend("f32", kind, [70, 33], [40, 17], D=D, Hq=2, Hkv=1, cap=20.0, bias=True)
+
+
+@pytest.mark.parametrize("dtype,kind", PAIRS)
+def test_pages_that_are_not_there(dtype, kind):
+    """Entries that name no page: their tokens are not seen.  Whole sequences of them see nothing."""
+    case = Case(9, kind, [100, 100, 30], 16, 2, 64)
+    table = case.table.clone()
+    table[0, :3], table[1, 2], table[1, 6], table[2] = -1, 10 ** 9, -2 ** 31, -7
+    for counts in ([1, 1, 1], [40, 3, 30]):
+        _attend(dtype, kind, [100, 100, 30], counts, table=table, seed=9)
+
+
+@pytest.mark.parametrize("kind", ["e4m3", "bf16"])
+def test_lengths_that_are_no_lengths(kind):
+    """Tokens behind the table's end are not there, a negative length is none, starts that fall or leave the rows name none."""
+    case = Case(10, kind, [48, 20], 16, 2, 64, more=0)
+    q = torch.randn((1, 6, 4, 64), generator=case.g).bfloat16().cuda()
+    o, lse = st.st_attn_cache(q, rows_of([3, 3]).cuda(), case.cache([100, -5]), False, 0.125)
+    check_attention(case, q, rows_of([3, 3]), o, lse, False, 0.125, lens=[100, 0], q_first=[97, -8])
+    for starts in ([0, 4, 2], [-3, 2, 100], [5, 2, 1], [2 ** 31 - 1, -2 ** 31, 6]):
+        o, lse = torch.full((1, 6, 4, 64), 7.0).cuda(), torch.full((1, 4, 6), 7.0).cuda()
+        st.st_attn_cache(q, torch.tensor(starts, dtype=torch.int32).cuda(), case.cache(), False, 0.125, o_part=o, lse_part=lse)
+        torch.cuda.synchronize()
+        assert torch.isfinite(o).all() and not torch.isnan(lse).any()
+
+
+@pytest.mark.parametrize("dtype,kind", PAIRS)
+@pytest.mark.parametrize("counts", [[1], [3], [40]])
+def test_what_is_not_finite_reaches_those_who_see_it(dtype, kind, counts):
+    """A NaN (an infinity) in the values of one token, and in the keys of another: rows before it have what they would have without."""
+    L, D, n = 90, 64, counts[0]
+    case = Case(11, kind, [L], 16, 1, D)
+    plant = {}
+    for i, (tok, d) in enumerate(((L - 2, 5), (L - 1, 9))):                   # keys of the last token, values of the last but one
+        pages, x = (case.v, math.nan) if i == 0 else (case.k, math.nan)
+        plant[i] = (pages, int(case.table[0, tok // 16]), tok % 16, d, x)
+    q = torch.randn((1, n, 2, D), generator=case.g).to(TYPES[dtype]).cuda()
+    run = lambda: st.st_attn_cache(q, rows_of([n]).cuda(), case.cache(), True, 0.125)
+    o0, l0 = run()
+    for pages, p, r, d, x in plant.values():
+        pages[p, r, 0, d] = torch.tensor(x, device="cuda").to(pages.dtype)
+    o, lse = run()
+    before = max(0, n - 2)
+    assert torch.equal(o[0, :before], o0[0, :before]) and torch.equal(lse[0, :, :before], l0[0, :, :before])
+    if n > 1:                                                                # sees the value, not the key
+        x, y = o[0, n - 2], o0[0, n - 2]
+        assert torch.isnan(x[:, 5]).all()
+        keep = torch.arange(D, device="cuda") != 5
+        assert torch.equal(x[:, keep], y[:, keep]) and torch.equal(lse[0, :, n - 2], l0[0, :, n - 2])
+    assert torch.isnan(o[0, n - 1]).all() and torch.isnan(lse[0, :, n - 1]).all()
+
+
+@pytest.mark.parametrize("kind", ["bf16"])
+def test_an_infinite_value(kind):
+    case = Case(12, kind, [50], 16, 1, 64)
+    q = torch.randn((1, 5, 2, 64), generator=case.g).bfloat16().cuda()
+    case.v[int(case.table[0, 2]), 15, 0, 3] = math.inf                        # token 47: rows at 47, 48, 49 see it
+    o, lse = st.st_attn_cache(q, rows_of([5]).cuda(), case.cache(), True, 0.125)
+    assert (o[0, 2:, :, 3] == math.inf).all() and torch.isfinite(o[0, :2]).all() and torch.isfinite(lse).all()
+    keep = torch.arange(64, device="cuda") != 3
+    assert torch.isfinite(o[0][:, :, keep]).all()
