@@ -391,7 +391,8 @@ st_status st_qk_rope_bwd(const st_rope_desc* desc, const st_tensor* q, const st_
  * sequences, their new rows, the pages) is read from device memory by the kernels, so that a captured call can be replayed.
  *   dtype          what the pages hold: the dtype of the calls' tensors, or ST_E4M3
  *   page           16, 32, 64, 128 or 256
- *   k, v           [n_pages, page, Hkv, D] views (stride_b of a page, stride_s of a token, stride_h of a head), rows 16-byte aligned
+ *   k, v           [n_pages, page, Hkv, D] views (stride_b of a page, stride_s of a token, below 2^20, stride_h of a head), rows
+ *                  16-byte aligned
  *   k_scale, v_scale  ST_E4M3 only: device bytes [n_pages, Hkv]; a stored value stands for its e4m3 value times 2^(scale - 127)
  *                  (1 <= scale <= 254).  Whole powers of two: every value is exact in bf16, and a page whose scale grows keeps its
  *                  rows but for what falls below the least e4m3 value

@@ -1,4 +1,5 @@
 // C ABI of the cache of keys and values in pages: argument checks, workspace layout, launches.
+#include <algorithm>
 #include <cmath>
 
 #include "st_cache.h"
@@ -10,6 +11,9 @@ using st::fail;
 using st::hip_fail;
 
 namespace {
+
+// A share of a walk is at least so many blocks of 32 keys, two for each of a workgroup's wavefronts; workgroups that shares are made for
+constexpr int kLeastBlocks = 8, kPlaces = 1024;
 
 st_status check_cache(const st_cache* c) {
   if (c == nullptr) return fail(ST_ERR_INVALID_ARG, "null cache");
@@ -25,6 +29,8 @@ st_status check_cache(const st_cache* c) {
   const int64_t n = (int64_t)c->n_pages * c->page * c->Hkv * c->D;
   ST_TRY(check_tensor("cache k", &c->k, c->dtype, n));
   ST_TRY(check_tensor("cache v", &c->v, c->dtype, n));
+  // (kernels add places inside a page in 32 bits)
+  if (std::max(c->k.stride_s, c->v.stride_s) >= (int64_t)1 << 20) return fail(ST_ERR_UNSUPPORTED, "cache: tokens of a page are 2^20 values or more apart");
   if (c->dtype == ST_E4M3 && n > 0 && (c->k_scale == nullptr || c->v_scale == nullptr)) return fail(ST_ERR_INVALID_ARG, "cache: pages in 8 bits need k_scale and v_scale");
   if (c->dtype != ST_E4M3 && (c->k_scale || c->v_scale)) return fail(ST_ERR_INVALID_ARG, "cache: scales belong to pages in 8 bits");
   if (c->B > 0 && (c->lens == nullptr || (c->table == nullptr && c->width > 0))) return fail(ST_ERR_INVALID_ARG, "cache: table / lens: null pointer");
@@ -42,7 +48,8 @@ st_status check_starts(const st_cache* c, const int32_t* starts, int64_t T) {
 st::CacheArgs cache_args(const st_cache* c) {
   st::CacheArgs a;
   memset(&a, 0, sizeof(a));
-  a.dtype = c->dtype; a.n_pages = c->n_pages; a.shift = __builtin_ctz((unsigned)c->page); a.Hkv = c->Hkv; a.D = c->D; a.B = c->B; a.width = c->width;
+  // (without a page no sequence has a token)
+  a.dtype = c->dtype; a.n_pages = c->n_pages; a.shift = __builtin_ctz((unsigned)c->page); a.Hkv = c->Hkv; a.D = c->D; a.B = c->B; a.width = c->n_pages > 0 ? c->width : 0;
   a.k = view_of(&c->k);
   a.v = view_of(&c->v);
   a.k_scale = c->k_scale; a.v_scale = c->v_scale; a.table = c->table; a.lens = c->lens;
@@ -67,7 +74,35 @@ st_status check_rows(const st_cache_rows* r, const st_cache* c) {
   if (r->dtype == ST_BF16 && r->softcap > st::kCapMost) return fail(ST_ERR_UNSUPPORTED, "bf16 path needs softcap <= %g (0: no cap)", (double)st::kCapMost);
   if (r->slopes && (int64_t)c->width * c->page > 1 << 24) return fail(ST_ERR_UNSUPPORTED, "slopes need sequences of at most 2^24 tokens, whose numbers fp32 holds");
   if (reinterpret_cast<uintptr_t>(r->slopes) % 4) return fail(ST_ERR_ALIGNMENT, "slopes: not 4-byte aligned");
+  if (((int64_t)r->T * (r->Hq / c->Hkv) / st::kCacheRows + c->B) * c->Hkv > st::kScoreGridMost / 2) return fail(ST_ERR_UNSUPPORTED, "more than %lld tiles", (long long)st::kScoreGridMost / 2);
   return ST_OK;
+}
+
+// Row tiles of all sequences together there can be, and how their walks are split
+st::CachePlan plan_of(const st_cache_rows* r, const st_cache* c) {
+  const int64_t G = r->Hq / c->Hkv, some = std::min(c->B, r->T), rows = std::min(r->max_rows, r->T);
+  const int64_t tiles = std::min(r->T * G / st::kCacheRows + some, some * ((rows * G + st::kCacheRows - 1) / st::kCacheRows));
+  const int64_t blocks = ((int64_t)c->width * c->page + st::kCacheKeys - 1) / st::kCacheKeys;
+  st::CachePlan p{};
+  p.rows_from = 0;
+  p.rows_to = 0x7fffffff;
+  p.least = kLeastBlocks;
+  p.target = kPlaces;
+  const int64_t jobs = tiles * c->Hkv, most = std::max<int64_t>((blocks + p.least - 1) / p.least, 1);
+  p.grid = std::min(p.target + jobs, jobs * most);
+  p.states = most > 1 ? (int32_t)std::min<int64_t>(2 * p.target, jobs * most) : 0;
+  return p;
+}
+struct Room {
+  size_t rows, info, bytes;
+};
+Room room_of(const st::CachePlan& p, const st_cache_rows* r, const st_cache* c) {
+  Room y{};
+  if (p.states == 0) return y;
+  y.rows = align_up((size_t)p.states * st::kCacheRows * c->D * 4, 256);
+  y.info = y.rows + align_up((size_t)p.states * st::kCacheRows * 16, 256);
+  y.bytes = y.info + align_up((size_t)r->T * 16, 256);
+  return y;
 }
 
 }  // namespace
@@ -143,8 +178,8 @@ st_status st_cache_read(const st_cache* c, const int32_t* first, int32_t count, 
 }
 
 size_t st_attn_cache_workspace_bytes(const st_cache_rows* r, const st_cache* c) {
-  if (check_rows(r, c) != ST_OK) return 0;
-  return 0;
+  if (check_rows(r, c) != ST_OK || c->B == 0 || r->T == 0 || r->max_rows == 0) return 0;
+  return room_of(plan_of(r, c), r, c).bytes;
 }
 
 st_status st_attn_cache(const st_cache_rows* r, const st_cache* c, const int32_t* starts, const int64_t* q_first, const st_tensor* q, float* o_part,
@@ -171,8 +206,16 @@ st_status st_attn_cache(const st_cache_rows* r, const st_cache* c, const int32_t
   a.o = o_part;
   a.lse = lse_part;
   a.o_lowp = o_lowp;
-  ST_TRY(check_workspace(workspace, workspace_bytes, st_attn_cache_workspace_bytes(r, c), "cache attention"));
+  a.plan = plan_of(r, c);
+  const Room room = room_of(a.plan, r, c);
+  ST_TRY(check_workspace(workspace, workspace_bytes, room.bytes, "cache attention"));
+  if (room.bytes > 0) {
+    a.part_o = (float*)workspace;
+    a.part_row = (float4*)((char*)workspace + room.rows);
+    a.info = (int4*)((char*)workspace + room.info);
+  }
   ST_HIP(st::launch_cache_attn(a, r->dtype == ST_BF16, (hipStream_t)hip_stream), "st_attn_cache launch");
+  if (a.plan.states > 0) ST_HIP(st::launch_cache_combine(a, r->dtype == ST_BF16, (hipStream_t)hip_stream), "st_attn_cache combine");
   return ST_OK;
 }
 

@@ -51,7 +51,7 @@ def _read(c=None, first=None, count=4, dtype=1, k=None, v=None):
 BAD_CACHES = [(dict(dtype=3), 1), (dict(n_pages=-1), 1), (dict(B=-1), 1), (dict(width=-1), 1), (dict(Hkv=0), 1), (dict(D=0), 1),
               (dict(page=8), 2), (dict(page=48), 2), (dict(page=512), 2), (dict(page=0), 2), (dict(D=264), 2), (dict(D=12), 2),
               (dict(Hkv=20000), 2), (dict(B=65536), 2), (dict(width=1 << 27), 2), (dict(k=_view(None)), 1), (dict(v=_view(PTR + 8)), 3),
-              (dict(k=_view(s=516)), 3), (dict(v=_view(h=-128)), 1), (dict(k_scale=PTR), 1), (dict(dtype=2), 1), (dict(dtype=2, k_scale=PTR), 1),
+              (dict(k=_view(s=516)), 3), (dict(v=_view(s=1 << 20)), 2), (dict(v=_view(h=-128)), 1), (dict(k_scale=PTR), 1), (dict(dtype=2), 1), (dict(dtype=2, k_scale=PTR), 1),
               (dict(dtype=2, k_scale=PTR, v_scale=PTR, k=_view(s=520)), 3), (dict(lens=None), 1), (dict(table=None), 1), (dict(table=PTR + 2), 3),
               (dict(lens=PTR + 1), 3)]
 
