@@ -925,6 +925,7 @@ class KVCache(NamedTuple):
     v_scale: Optional[torch.Tensor] = None
 
 
+_CHUNK_TYPES = {torch.float32: ST_F32, torch.bfloat16: ST_BF16}
 _PAGE_TYPES = {torch.float32: ST_F32, torch.bfloat16: ST_BF16, torch.float8_e4m3fn: ST_E4M3}
 
 
@@ -960,6 +961,9 @@ def st_cache_append(q, k, v, starts, cache: KVCache, freq, offset: int = 0, posi
     [B + 1]), its last tokens.  Norms and rotations as in st_qk_rope_fwd at the tokens' places in their sequences + offset (or at
     `positions` int32 [axes,1,T]); keys and values go into the cache.  Returns the queries (a new tensor unless q_out is given, which
     may be q), None without."""
+    done = _short(_binding.cache_append, stream, *cache, q, k, v, starts, freq, offset, positions, axes, _PAIRS.get(pairs), norm, eps, q_weight, k_weight, q_out)
+    if done is not None:
+        return done[0]
     with _on_device(stream, k, q, v, starts, *cache, freq, positions, q_weight, k_weight, q_out):
         c = _cache_desc(cache)
         if k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype:
@@ -983,11 +987,15 @@ def st_cache_append(q, k, v, starts, cache: KVCache, freq, offset: int = 0, posi
 def st_cache_read(cache: KVCache, first, count: int, dtype=None, k_out=None, v_out=None, stream=None):
     """(k, v) chunks [B,count,Hkv,D]: tokens first[b] .. first[b] + count - 1 of every sequence (int32 [B], None: from 0), zeros past
     its end.  dtype: that of the pages; of pages in 8 bits torch.bfloat16 (unless given) or torch.float32."""
+    if k_out is None and v_out is None:
+        done = _short(_binding.cache_read, stream, *cache, first, count, None if dtype is None else _CHUNK_TYPES.get(dtype, -1))
+        if done is not None:
+            return done
     with _on_device(stream, cache.k, *cache[1:], first, k_out, v_out):
         c = _cache_desc(cache)
         if dtype is None:
             dtype = k_out.dtype if k_out is not None else torch.bfloat16 if c.dtype == ST_E4M3 else cache.k.dtype
-        code = {torch.float32: ST_F32, torch.bfloat16: ST_BF16}.get(dtype)
+        code = _CHUNK_TYPES.get(dtype)
         if code is None:
             raise TypeError(f"unsupported dtype {dtype}")
         if first is not None:
@@ -1032,6 +1040,10 @@ def st_attn_cache(q, starts, cache: KVCache, causal: bool, scale: float, max_row
     to its position (causal), the last `window` of them (0: all).  No sequence has more than max_rows rows (None: T).  O [1,T,Hq,D] is
     the fp32 state, or with lowp=True alone in the dtype of q; both are written where o_part and o_lowp are given (the fp32 one is
     returned); lse fp32 [1,Hq,T].  Rows of no sequence are left as they were."""
+    done = _short(_binding.cache_attn, stream, *cache, q, starts, causal, scale, max_rows, window, softcap, slopes, q_first, o_part, lse_part, o_lowp, lowp,
+                  workspace)
+    if done is not None:
+        return done
     with _on_device(stream, q, starts, *cache, slopes, q_first, o_part, lse_part, o_lowp, workspace):
         r, c = _cache_rows(q, cache, causal, scale, max_rows, window, softcap, slopes), _cache_desc(cache)
         T, Hq = r.T, r.Hq

@@ -615,10 +615,120 @@ PyObject* rope_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return answer(s, {given_or(a[13], m.t[0]), given_or(a[14], m.t[1]), given_or(Py_None, w.t[0]), given_or(Py_None, w.t[1])});
 }
 
+// k, v, table, lens, k_scale, v_scale of a cache at a[0 .. 5]
+struct Cache {
+  st_cache d;
+  Tensor k;
+  bool read(PyObject* const* a, int64_t device) {
+    Tensor v, table;
+    if (!view(a[0], &k, &d.k) || !view(a[1], &v, &d.v) || !here(k, device) || !here(v, device) || v->sizes() != k->sizes() || v->scalar_type() != k->scalar_type()) return false;
+    const bool low = k->scalar_type() == at::kFloat8_e4m3fn;
+    if (low) d.dtype = ST_E4M3;
+    else if (!dtype_code(k, &d.dtype)) return false;
+    if (!tensor(a[2], &table) || table->dim() != 2) return false;
+    const int64_t B = table->size(0), width = table->size(1);
+    for (int64_t x : {k->size(0), k->size(1), k->size(2), k->size(3), B, width})
+      if (x > INT32_MAX) return false;
+    d.n_pages = (int32_t)k->size(0); d.page = (int32_t)k->size(1); d.Hkv = (int32_t)k->size(2); d.D = (int32_t)k->size(3);
+    d.B = (int32_t)B; d.width = (int32_t)width;
+    if ((a[4] != Py_None) != low || (a[5] != Py_None) != low) return false;
+    return dense_of(a[2], {B, width}, at::kInt, device, (void**)&d.table) && dense_of(a[3], {B}, at::kInt, device, (void**)&d.lens) &&
+           dense_or_none(a[4], {d.n_pages, d.Hkv}, at::kByte, device, (void**)&d.k_scale) && dense_or_none(a[5], {d.n_pages, d.Hkv}, at::kByte, device, (void**)&d.v_scale);
+  }
+};
+
+// cache_append(cache ..., q, k, v, starts, freq, offset, positions, axes, pairing, norm, eps, q_weight, k_weight, q_out, device, stream)
+PyObject* cache_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  ST_SHORT(n == 22);
+  Cache c;
+  Rope r;
+  Made m;
+  Tensor q = nullptr, v;
+  st_tensor tq = {nullptr, 0, 0, 0}, tv, out = {nullptr, 0, 0, 0};
+  int64_t device;
+  void *starts, *qw, *stream;
+  PyObject* const keys[11] = {a[7], Py_None, a[10], a[11], a[12], a[13], a[14], a[15], a[16], Py_None, a[18]};
+  ST_SHORT(integer(a[20], &device) && handle(a[21], &stream) && c.read(a, device) && r.read(keys, device));
+  ST_SHORT(view(a[8], &v, &tv) && here(v, device) && v->sizes() == r.q->sizes() && v->scalar_type() == r.q->scalar_type());
+  ST_SHORT(dense_of(a[9], {(int64_t)c.d.B + 1}, at::kInt, device, &starts) && dense_or_none(a[17], {r.d.D}, at::kFloat, device, &qw));
+  r.d.Hkv = r.d.Hq;
+  r.d.Hq = 0;
+  m.on = r.q->options();
+  if (a[6] != Py_None) {
+    ST_SHORT(view(a[6], &q, &tq) && here(q, device) && q->dim() == 4 && q->scalar_type() == r.q->scalar_type() && q->size(0) == r.d.B && q->size(1) == r.d.S &&
+             q->size(3) == r.d.D && q->size(2) <= INT32_MAX);
+    r.d.Hq = (int32_t)q->size(2);
+    ST_SHORT(r.out(a[19], q, device, &m, 0, &out));
+  } else {
+    ST_SHORT(a[19] == Py_None);
+  }
+  PyObject* s = call([&] {
+    return st_cache_append(&r.d, &c.d, (const int32_t*)starts, &tq, &r.tq, &tv, (const float*)qw, (const float*)r.kw, (const double*)r.freq, (const int32_t*)r.positions,
+                           &out, stream);
+  });
+  return answer(s, {given_or(a[19], m.t[0])});
+}
+
+// cache_read(cache ..., first, count, dtype (a code, or None: of the pages, bf16 from those in 8 bits), device, stream): new chunks
+PyObject* cache_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  ST_SHORT(n == 11);
+  Cache c;
+  int32_t count, code;
+  int64_t device;
+  void *first, *stream;
+  ST_SHORT(integer(a[9], &device) && handle(a[10], &stream) && c.read(a, device) && integer(a[7], &count) && count >= 0);
+  ST_SHORT(dense_or_none(a[6], {c.d.B}, at::kInt, device, &first));
+  if (a[8] == Py_None) code = c.d.dtype == ST_E4M3 ? ST_BF16 : c.d.dtype;
+  else ST_SHORT(integer(a[8], &code) && (code == ST_F32 || code == ST_BF16));
+  Made m;
+  m.on = c.k->options();
+  st_tensor out[2];
+  for (int i = 0; i < 2; ++i) {
+    m.made(i, {c.d.B, count, c.d.Hkv, c.d.D}, code == ST_F32 ? at::kFloat : at::kBFloat16);
+    out[i] = st_tensor{address(&m.t[i]), m.t[i].stride(0), m.t[i].stride(1), m.t[i].stride(2)};
+  }
+  PyObject* s = call([&] { return st_cache_read(&c.d, (const int32_t*)first, count, code, &out[0], &out[1], stream); });
+  return answer(s, {given_or(Py_None, m.t[0]), given_or(Py_None, m.t[1])});
+}
+
+// cache_attn(cache ..., q, starts, causal, scale, max_rows (None: all), window, softcap, slopes, q_first, o, lse, o_low, lowp, workspace, device, stream)
+PyObject* cache_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  ST_SHORT(n == 22);
+  Cache c;
+  st_cache_rows d;
+  Tensor q;
+  st_tensor tq;
+  int64_t device;
+  int32_t lowp;
+  void *starts, *first, *o, *lse, *low, *ws, *stream;
+  size_t ws_bytes;
+  ST_SHORT(integer(a[20], &device) && handle(a[21], &stream) && c.read(a, device) && view(a[6], &q, &tq) && here(q, device) && dtype_code(q, &d.dtype));
+  ST_SHORT(q->size(0) == 1 && q->size(3) == c.d.D && q->size(1) <= INT32_MAX && q->size(2) <= INT32_MAX);
+  d.T = (int32_t)q->size(1);
+  d.Hq = (int32_t)q->size(2);
+  d.max_rows = d.T;
+  ST_SHORT(truth(a[8], &d.causal) && real(a[9], &d.scale) && (a[10] == Py_None || integer(a[10], &d.max_rows)) && integer(a[11], &d.window) && real(a[12], &d.softcap));
+  ST_SHORT(dense_of(a[7], {(int64_t)c.d.B + 1}, at::kInt, device, &starts) && dense_or_none(a[13], {d.Hq}, at::kFloat, device, (void**)&d.slopes) &&
+           dense_or_none(a[14], {c.d.B}, at::kLong, device, &first) && truth(a[18], &lowp));
+  ST_SHORT(dense_or_none(a[15], q->sizes(), at::kFloat, device, &o) && dense_or_none(a[16], {1, d.Hq, d.T}, at::kFloat, device, &lse) &&
+           dense_or_none(a[17], q->sizes(), q->scalar_type(), device, &low));
+  Made x;
+  x.on = q->options();
+  const bool want_low = a[17] == Py_None && lowp, want_o = a[15] == Py_None && a[17] == Py_None && !lowp;
+  ST_SHORT(workspace_of(a[19], st_attn_cache_workspace_bytes(&d, &c.d), device, &x, 2, &ws, &ws_bytes));
+  if (want_low) low = x.made(0, q->sizes(), q->scalar_type());
+  if (want_o) o = x.f32(0, q->sizes());
+  if (a[16] == Py_None) lse = x.f32(1, {1, d.Hq, d.T});
+  PyObject* s = call([&] { return st_attn_cache(&d, &c.d, (const int32_t*)starts, (const int64_t*)first, &tq, (float*)o, (float*)lse, low, ws, ws_bytes, stream); });
+  PyObject* out = a[15] != Py_None ? given_or(a[15], at::Tensor()) : given_or(a[17], x.t[0]);
+  return answer(s, {out, given_or(a[16], x.t[1])});
+}
+
 #define ST_METHOD(f) {#f, (PyCFunction)(void*)guarded<f>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ST_METHOD(ring_fwd), ST_METHOD(ring_bwd), ST_METHOD(block_fwd), ST_METHOD(block_bwd), ST_METHOD(merge),
                          ST_METHOD(combine),  ST_METHOD(delta),    ST_METHOD(cast),
-                         ST_METHOD(mask_spans), ST_METHOD(score_fwd), ST_METHOD(score_bwd), ST_METHOD(rope_fwd), ST_METHOD(rope_bwd), {nullptr, nullptr, 0, nullptr}};
+                         ST_METHOD(mask_spans), ST_METHOD(score_fwd), ST_METHOD(score_bwd), ST_METHOD(rope_fwd), ST_METHOD(rope_bwd),
+                         ST_METHOD(cache_append), ST_METHOD(cache_read), ST_METHOD(cache_attn), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
