@@ -14,6 +14,8 @@ namespace {
 
 // A share of a walk is at least so many blocks of 32 keys, two for each of a workgroup's wavefronts; workgroups that shares are made for
 constexpr int kLeastBlocks = 8, kPlaces = 1024;
+// Batches whose sequences all have at most so many rows have one launch for them
+constexpr int kFewRows = 64;
 
 st_status check_cache(const st_cache* c) {
   if (c == nullptr) return fail(ST_ERR_INVALID_ARG, "null cache");
@@ -74,33 +76,59 @@ st_status check_rows(const st_cache_rows* r, const st_cache* c) {
   if (r->dtype == ST_BF16 && r->softcap > st::kCapMost) return fail(ST_ERR_UNSUPPORTED, "bf16 path needs softcap <= %g (0: no cap)", (double)st::kCapMost);
   if (r->slopes && (int64_t)c->width * c->page > 1 << 24) return fail(ST_ERR_UNSUPPORTED, "slopes need sequences of at most 2^24 tokens, whose numbers fp32 holds");
   if (reinterpret_cast<uintptr_t>(r->slopes) % 4) return fail(ST_ERR_ALIGNMENT, "slopes: not 4-byte aligned");
-  if (((int64_t)r->T * (r->Hq / c->Hkv) / st::kCacheRows + c->B) * c->Hkv > st::kScoreGridMost / 2) return fail(ST_ERR_UNSUPPORTED, "more than %lld tiles", (long long)st::kScoreGridMost / 2);
+  if (((int64_t)r->T * (r->Hq / c->Hkv) / 16 + c->B) * c->Hkv > st::kScoreGridMost / 2) return fail(ST_ERR_UNSUPPORTED, "more than %lld tiles", (long long)st::kScoreGridMost / 2);
   return ST_OK;
 }
 
-// Row tiles of all sequences together there can be, and how their walks are split
-st::CachePlan plan_of(const st_cache_rows* r, const st_cache* c) {
-  const int64_t G = r->Hq / c->Hkv, some = std::min(c->B, r->T), rows = std::min(r->max_rows, r->T);
-  const int64_t tiles = std::min(r->T * G / st::kCacheRows + some, some * ((rows * G + st::kCacheRows - 1) / st::kCacheRows));
+// Row tiles of all sequences together there can be, and how their walks are split: a launch for tiles of `rows` rows
+st::CachePlan launch_plan(const st_cache_rows* r, const st_cache* c, int rows, int from, int to, int64_t base) {
+  const int64_t G = r->Hq / c->Hkv, some = std::min(c->B, r->T), most_rows = std::min<int64_t>((int64_t)std::min(r->max_rows, r->T) * G, to);
+  const int64_t tiles = std::min(r->T * G / rows + some, some * ((most_rows + rows - 1) / rows));
   const int64_t blocks = ((int64_t)c->width * c->page + st::kCacheKeys - 1) / st::kCacheKeys;
   st::CachePlan p{};
-  p.rows_from = 0;
-  p.rows_to = 0x7fffffff;
+  p.rows = rows;
+  p.rows_from = from;
+  p.rows_to = to;
   p.least = kLeastBlocks;
   p.target = kPlaces;
-  const int64_t jobs = tiles * c->Hkv, most = std::max<int64_t>((blocks + p.least - 1) / p.least, 1);
+  const int64_t jobs = tiles * c->Hkv, most = std::max<int64_t>((blocks + p.least / 2) / p.least, 1);
   p.grid = std::min(p.target + jobs, jobs * most);
-  p.states = most > 1 ? (int32_t)std::min<int64_t>(2 * p.target, jobs * most) : 0;
+  p.states = most > 1 ? (int32_t)std::min<int64_t>(p.target * 4 / 3 + 1, jobs * most) : 0;
+  p.base = base;
   return p;
+}
+// The launches of a call: sequences of up to 16 rows and those of more have kernels of their own where there may be both
+struct Plans {
+  int n;
+  st::CachePlan p[2];
+  int64_t rows;              // of all states
+};
+Plans plans_of(const st_cache_rows* r, const st_cache* c) {
+  constexpr int kAll = 0x7fffffff;
+  const int64_t most = (int64_t)std::min(r->max_rows, r->T) * (r->Hq / c->Hkv);
+  Plans y{};
+  if (most <= 16) {
+    y.n = 1;
+    y.p[0] = launch_plan(r, c, 16, 0, kAll, 0);
+  } else if (most <= kFewRows || c->B == 1) {
+    y.n = 1;
+    y.p[0] = launch_plan(r, c, 32, 0, kAll, 0);
+  } else {
+    y.n = 2;
+    y.p[0] = launch_plan(r, c, 32, 16, kAll, 0);
+    y.p[1] = launch_plan(r, c, 16, 0, 16, (int64_t)y.p[0].states * 32);
+  }
+  for (int x = 0; x < y.n; ++x) y.rows += (int64_t)y.p[x].states * y.p[x].rows;
+  return y;
 }
 struct Room {
   size_t rows, info, bytes;
 };
-Room room_of(const st::CachePlan& p, const st_cache_rows* r, const st_cache* c) {
+Room room_of(const Plans& p, const st_cache_rows* r, const st_cache* c) {
   Room y{};
-  if (p.states == 0) return y;
-  y.rows = align_up((size_t)p.states * st::kCacheRows * c->D * 4, 256);
-  y.info = y.rows + align_up((size_t)p.states * st::kCacheRows * 16, 256);
+  if (p.rows == 0) return y;
+  y.rows = align_up((size_t)p.rows * c->D * 4, 256);
+  y.info = y.rows + align_up((size_t)p.rows * 16, 256);
   y.bytes = y.info + align_up((size_t)r->T * 16, 256);
   return y;
 }
@@ -179,7 +207,7 @@ st_status st_cache_read(const st_cache* c, const int32_t* first, int32_t count, 
 
 size_t st_attn_cache_workspace_bytes(const st_cache_rows* r, const st_cache* c) {
   if (check_rows(r, c) != ST_OK || c->B == 0 || r->T == 0 || r->max_rows == 0) return 0;
-  return room_of(plan_of(r, c), r, c).bytes;
+  return room_of(plans_of(r, c), r, c).bytes;
 }
 
 st_status st_attn_cache(const st_cache_rows* r, const st_cache* c, const int32_t* starts, const int64_t* q_first, const st_tensor* q, float* o_part,
@@ -206,16 +234,20 @@ st_status st_attn_cache(const st_cache_rows* r, const st_cache* c, const int32_t
   a.o = o_part;
   a.lse = lse_part;
   a.o_lowp = o_lowp;
-  a.plan = plan_of(r, c);
-  const Room room = room_of(a.plan, r, c);
+  const Plans plans = plans_of(r, c);
+  const Room room = room_of(plans, r, c);
   ST_TRY(check_workspace(workspace, workspace_bytes, room.bytes, "cache attention"));
   if (room.bytes > 0) {
     a.part_o = (float*)workspace;
     a.part_row = (float4*)((char*)workspace + room.rows);
     a.info = (int4*)((char*)workspace + room.info);
   }
-  ST_HIP(st::launch_cache_attn(a, r->dtype == ST_BF16, (hipStream_t)hip_stream), "st_attn_cache launch");
-  if (a.plan.states > 0) ST_HIP(st::launch_cache_combine(a, r->dtype == ST_BF16, (hipStream_t)hip_stream), "st_attn_cache combine");
+  a.state_rows = plans.rows;
+  for (int x = 0; x < plans.n; ++x) {
+    a.plan = plans.p[x];
+    ST_HIP(st::launch_cache_attn(a, r->dtype == ST_BF16, (hipStream_t)hip_stream), "st_attn_cache launch");
+  }
+  if (plans.rows > 0) ST_HIP(st::launch_cache_combine(a, r->dtype == ST_BF16, (hipStream_t)hip_stream), "st_attn_cache combine");
   return ST_OK;
 }
 

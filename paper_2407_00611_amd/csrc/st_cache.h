@@ -31,12 +31,14 @@ struct ReadArgs {
   View k_out, v_out;                                 // ptr null: not asked for
 };
 
-// Which rows a launch takes and how it is split (st_cache_plan.h)
+// Which sequences a launch takes and how it is split (st_cache_plan.h)
 struct CachePlan {
+  int32_t rows;                                      // of a tile: 16 or 32
   int32_t rows_from, rows_to;                        // packed rows (token, head of a group) of a sequence: rows_from < rows <= rows_to
   int32_t least;                                     // key blocks of a share, at least
   int32_t target;                                    // workgroups that the shares are made for
   int32_t states;                                    // partial states there is room for
+  int64_t base;                                      // rows of the states of launches before
   int64_t grid;
 };
 
@@ -52,14 +54,14 @@ struct CacheAttnArgs {
   float* lse;                                        // [Hq,T]
   void* o_lowp;                                      // nullable
   CachePlan plan;
-  // of a split walk: state s has the rows of its tile, O not divided by its row sum yet, and for each row the reference of its exponents,
+  // of a split walk: a state has the rows of its tile, O not divided by its row sum yet, and for each row the reference of its exponents,
   // the sum, and what its lse has besides
-  float* part_o;                                     // [states, rows of a tile, D]
-  float4* part_row;                                  // [states, rows of a tile]
-  int4* info;                                        // [T]: first state of the sequence, shares, row tiles, row of the sequence
+  float* part_o;                                     // [state rows, D]
+  float4* part_row;                                  // [state rows]
+  int64_t state_rows;
+  int4* info;                                        // [T]: row of the sequence's first state, shares | rows of a tile << 16, row tiles, row of the sequence
 };
 
-constexpr int kCacheRows = 32;                       // rows of a tile
 constexpr int kCacheKeys = 32;                       // keys of a block
 
 hipError_t launch_cache_append(const AppendArgs& a, bool bf16, hipStream_t stream);

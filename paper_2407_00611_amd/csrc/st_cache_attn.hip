@@ -1,13 +1,13 @@
 // Attention of packed rows against a cache of pages.
 //
-// A tile is 32 rows, packed over the heads of a KV head (row R is token R / G, head R % G of the group), so that a key is read once for all of
-// them.  The four wavefronts of a workgroup share the tile's walk over the keys, 32 keys a step, and fold in LDS; walks are split over
+// A tile is 16 or 32 rows, packed over the heads of a KV head (row R is token R / G, head R % G of the group), so that a key is read once for
+// all of them.  The four wavefronts of a workgroup share the tile's walk over the keys, 32 keys a step, and fold in LDS; walks are split over
 // workgroups as st_cache_plan.h says, and their states joined by a second launch.
 //
-//   S^T = K Q^T and O^T += V^T P^T: a lane has one row (C layout column l % 32), its reference, sum and span in registers.
-// Keys and values go from memory to the operand registers: the order of a contraction is free as long as both sides agree, so lane (r, g)
-// takes 16-byte pieces of key r's row as they lie, and for the second product the values of DP / 32 neighbouring columns of the eight keys
-// that its exponentials belong to.
+//   S^T = K Q^T and O^T += V^T P^T: a lane has one row (C layout column), its reference, sum and span in registers.
+// Keys and values go from memory to the operand registers: the order of a contraction is free as long as both sides agree, so a lane takes
+// 16-byte pieces of its key's row as they lie, and for the second product the values of D / tile neighbouring columns of the eight (sixteen)
+// keys that its exponentials belong to.
 #include <type_traits>
 
 #include "st_cache_plan.h"
@@ -16,13 +16,39 @@
 namespace st {
 namespace {
 
-constexpr int kKeys = kCacheKeys, kRows = kCacheRows;
+constexpr int kKeys = kCacheKeys;
 constexpr float kUnset = -1e30f;                     // reference of a row that has met no key: whatever comes exceeds it
-constexpr float kSumMost = 4096.f;                   // a lane's sum over sixteen keys beyond which a row's reference moves
+constexpr float kSumMost = 4096.f;                   // a lane's sum over its keys of a block beyond which a row's reference moves
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
-__device__ __forceinline__ f32x16 mfma_f32(float a, float b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0); }
+// The matrix instructions of a tile of 32 or 16 rows: lane l holds row (column) l % ROWS of both operands, C rows as Tile::row says
+template <int ROWS>
+struct Tile;
+template <>
+struct Tile<32> {
+  typedef f32x16 Acc;
+  static __device__ __forceinline__ int row(int v, int g) { return 8 * (v / 4) + 4 * g + v % 4; }   // g = l / 32; also the key of score v
+  static __device__ __forceinline__ Acc mul(bf16x8 a, bf16x8 b, Acc c) { return mfma32(a, b, c); }
+  static __device__ __forceinline__ Acc mul(float a, float b, Acc c) { return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0); }
+  static __device__ __forceinline__ float sum(float x) { return xhalf_sum(x); }
+  static __device__ __forceinline__ float max(float x) { return xhalf_max(x); }
+};
+template <>
+struct Tile<16> {
+  typedef f32x4 Acc;
+  static __device__ __forceinline__ int row(int v, int g) { return 16 * (v / 4) + 4 * g + v % 4; }  // g = l / 16; scores 4 .. 7 are a second tile's
+  static __device__ __forceinline__ Acc mul(bf16x8 a, bf16x8 b, Acc c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+  static __device__ __forceinline__ Acc mul(float a, float b, Acc c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
+  static __device__ __forceinline__ float sum(float x) {
+    x += __shfl_xor(x, 16);
+    return xhalf_sum(x);
+  }
+  static __device__ __forceinline__ float max(float x) {
+    x = fmaxf(x, __shfl_xor(x, 16));
+    return xhalf_max(x);
+  }
+};
 // two values of a half of x, times a power of two: exact
 template <bool HIGH>
 __device__ __forceinline__ uint32_t bf16_of_e4m3(uint32_t x, float scale) {
@@ -51,43 +77,66 @@ __device__ __forceinline__ float stored(const float* p, uint8_t) { return *p; }
 __device__ __forceinline__ float stored(const uint16_t* p, uint8_t) { return __uint_as_float((uint32_t)*p << 16); }
 __device__ __forceinline__ float stored(const uint8_t* p, uint8_t scale) { return e4m3_pair<false>(*p).x * scale_value(scale); }
 
+// wavefronts on a SIMD that the registers leave room for
+template <typename T, typename S, int ROWS, int DP>
+constexpr int stream_waves() {
+  return DP > 128 ? (ROWS == 16 ? 2 : 1) : ROWS == 16 ? (DP <= 64 ? 4 : sizeof(S) == 1 ? 3 : 2) : 2;
+}
+
 // T: of the rows (bf16: on the bf16 matrix unit, D = DP; fp32: on the fp32 one, D <= DP); S: what the pages hold; MOD: scores may be capped, biased
-template <typename T, typename S, int DP, bool MOD>
-__global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void cache_stream_kernel(const CacheAttnArgs a) {
+template <typename T, typename S, int ROWS, int DP, bool MOD>
+__global__ __launch_bounds__(256, (stream_waves<T, S, ROWS, DP>())) void cache_stream_kernel(const CacheAttnArgs a) {
   constexpr bool BF = std::is_same<T, uint16_t>::value, E4M3 = std::is_same<S, uint8_t>::value;
-  constexpr int DB = DP / 32, EPC = 16 / (int)sizeof(S), NJ = DP / (2 * EPC);
-  constexpr int VB = DB * (int)sizeof(S), VW = VB < 4 ? 1 : VB / 4;
-  constexpr int PW = DB < 4 ? DB : 4, PASSES = DB / PW, FS = 32 * PW + 4;
+  typedef Tile<ROWS> M;
+  typedef typename M::Acc Acc;
+  constexpr int GROUPS = 64 / ROWS;                    // lanes of a row
+  constexpr int NS = kKeys / GROUPS, NA = NS < 16 ? 4 : 16, TILES = NS / NA;   // scores of a lane, as TILES tiles of keys of NA registers
+  constexpr int DB = DP / ROWS;                        // columns of O of a lane's matrix row
+  constexpr int EPC = 16 / (int)sizeof(S), NJ = DP / (GROUPS * EPC);           // values of a piece, pieces of a key's row a lane
+  constexpr int VB = DB * (int)sizeof(S), VW = VB < 4 ? 1 : VB / 4;            // bytes and words of a lane's columns
+  constexpr int PW = DB < 4 ? DB : 4, PASSES = DB / PW, FS = ROWS * PW + 4;    // folding: columns at a time
   constexpr int QS = DP + 4;
-  constexpr int kFold = 4 * kRows * FS * 4, kQ = BF ? 0 : kRows * QS * 4;
+  constexpr int kFold = 4 * ROWS * FS * 4, kQ = BF ? 0 : ROWS * QS * 4;
+  static_assert(NJ >= 1 && VB >= 2 && DB >= 2, "a lane takes part in every product");
   __shared__ __attribute__((aligned(16))) char smem[kFold > kQ ? kFold : kQ];
-  __shared__ float stat_m[4][kRows], stat_l[4][kRows];
-  __shared__ PlanRoom room;
+  __shared__ float stat_m[4][ROWS], stat_l[4][ROWS];
   __shared__ int any_bad;
   const CacheArgs& c = a.c;
-  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), g = lane >> 5, r = lane & 31;
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), g = lane / ROWS, r = lane % ROWS;
   const int G = a.Hq / c.Hkv, D = BF ? DP : c.D;
-  const CacheItem t = find_item<kRows, kKeys>(a, &room);
+  SeqSpan s;
+  const CacheItem t = find_item<ROWS, kKeys>(a, s);
   if (t.b < 0) return;
-  const SeqSpan s = seq_span(a, t.b);
-  const CacheWalk w = cache_walk<kRows, kKeys>(a, s, t, G);
-  tell_rows<kRows>(a, s, t, G);
-  const int M = s.r.n * G, live = min(M - t.tile * kRows, kRows);
-  const int row = min(t.tile * kRows + r, M - 1), i = row / G, h = t.hk * G + row - i * G;
+  const CacheWalk w = cache_walk<ROWS, kKeys>(a, s, t, G);
+  tell_rows<ROWS>(a, s, t, G);
+  const int all_rows = s.r.n * G, live = min(all_rows - t.tile * ROWS, ROWS);
+  const int row = min(t.tile * ROWS + r, all_rows - 1), i = row / G, h = t.hk * G + row - i * G;
   const RowSpan see = row_span(a, s, i);
   const char* qrow = (const char*)a.q.ptr + ((int64_t)(s.r.first + i) * a.q.ss + (int64_t)h * a.q.sh) * (int)sizeof(T);
 
-  bf16x8 qf[BF ? DP / 16 : 1];
+  // the pages of a block, one for its first 16 keys and one for the others
+  const int32_t* table = c.table + (int64_t)t.b * c.width;
+  auto table_at = [&](int n) { return table[min((n * kKeys + 16 * (lane & 1)) >> c.shift, c.width - 1)]; };
+  // wavefront w takes the blocks n1 - 1 - w, n1 - 5 - w, ...: the nearest keys, whose bias is least, first
+  int n = w.n1 - 1 - wave;
+  const bool some = n >= w.n0;
+  int entry = 0, entry0 = 0;
+  if (some) {
+    entry0 = table_at(n);
+    entry = table_at(max(n - 4, w.n0));
+  }
+
+  bf16x8 qf[BF ? DP / (8 * GROUPS) : 1];
   float* qs = (float*)smem;
   if constexpr (BF) {
 #pragma unroll
-    for (int x = 0; x < DP / 16; ++x) {                // (the order of the pieces of a key)
-      const int d = E4M3 ? 32 * (x / 2) + 16 * g + 8 * (x % 2) : 16 * x + 8 * g;
+    for (int x = 0; x < DP / (8 * GROUPS); ++x) {      // (the order of the pieces of a key)
+      const int d = E4M3 ? 16 * GROUPS * (x / 2) + 16 * g + 8 * (x % 2) : 8 * GROUPS * x + 8 * g;
       qf[x] = *reinterpret_cast<const bf16x8*>(qrow + d * 2);
     }
   } else {
-    for (int x = tid; x < kRows * (QS / 4); x += 256) {   // (zeros behind D: they are multiplied by zeros)
-      const int qr = x / (QS / 4), d = 4 * (x - qr * (QS / 4)), R = min(t.tile * kRows + qr, M - 1), qi = R / G;
+    for (int x = tid; x < ROWS * (QS / 4); x += 256) {   // (zeros behind D: they are multiplied by zeros)
+      const int qr = x / (QS / 4), d = 4 * (x - qr * (QS / 4)), R = min(t.tile * ROWS + qr, all_rows - 1), qi = R / G;
       f32x4 y = {0.f, 0.f, 0.f, 0.f};
       if (d < D) y = *reinterpret_cast<const f32x4*>((const float*)a.q.ptr + (int64_t)(s.r.first + qi) * a.q.ss + (int64_t)(t.hk * G + R - qi * G) * a.q.sh + d);
       *reinterpret_cast<f32x4*>(qs + qr * QS + d) = y;
@@ -107,9 +156,6 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void cache_stream_kernel(con
     besides = -slope * (float)(p > near ? p - near : near - p);
   }
 
-  // the pages of a block, one for its first 16 keys and one for the others
-  const int32_t* table = c.table + (int64_t)t.b * c.width;
-  auto table_at = [&](int n) { return table[min((n * kKeys + 16 * (lane & 1)) >> c.shift, c.width - 1)]; };
   const char* kbase = (const char*)c.k.ptr + (int64_t)t.hk * c.k.sh * (int)sizeof(S);
   const char* vbase = (const char*)c.v.ptr + (int64_t)t.hk * c.v.sh * (int)sizeof(S);
   const uint32_t k_off = (uint32_t)((r & 15) * c.k.ss * (int)sizeof(S)) + 16 * g;
@@ -133,107 +179,103 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void cache_stream_kernel(con
   auto at = [&](const char* base, const View& v, const Pages& p, int n, int m) {
     return base + ((int64_t)p.p[m] * v.sb + (int64_t)((n * kKeys + 16 * m) & ((1 << c.shift) - 1)) * v.ss) * (int)sizeof(S);
   };
-  u32x4 kr[NJ];
-  uint32_t vr[16][VW];
-  int k_sc = 0, v_sc = 0;                              // bytes of the scales: of the lane's key; of the halves in lanes 0 and 16
+  u32x4 kr[TILES][NJ];
+  uint32_t vr[NS][VW];
+  int k_sc = 0, v_sc = 0;                              // bytes of the scales of the halves, in lanes 0 and 32
   auto load_k = [&](const Pages& p, int n) {
-    const char* x0 = at(kbase, c.k, p, n, 0);
-    const char* x1 = at(kbase, c.k, p, n, 1);
-    const char* x = (r < 16 ? x0 : x1) + k_off;
+    const char* half[2] = {at(kbase, c.k, p, n, 0), at(kbase, c.k, p, n, 1)};
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      if (BF || (2 * j + g) * EPC < D) kr[j] = *reinterpret_cast<const u32x4*>(x + 32 * j);
-      else kr[j] = u32x4{0, 0, 0, 0};
+    for (int y = 0; y < TILES; ++y) {
+      const char* x = (ROWS == 32 ? (r < 16 ? half[0] : half[1]) : half[y]) + k_off;
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        if (BF || (GROUPS * j + g) * EPC < D) kr[y][j] = *reinterpret_cast<const u32x4*>(x + 16 * GROUPS * j);
+        else kr[y][j] = u32x4{0, 0, 0, 0};
+      }
     }
-    if constexpr (E4M3) k_sc = c.k_scale[(int64_t)(r < 16 ? p.p[0] : p.p[1]) * c.Hkv + t.hk];
+    if constexpr (E4M3) k_sc = c.k_scale[(int64_t)(lane < 32 ? p.p[0] : p.p[1]) * c.Hkv + t.hk];
   };
   auto load_v = [&](const Pages& p, int n) {
+    const char* half[2] = {at(vbase, c.v, p, n, 0), at(vbase, c.v, p, n, 1)};
 #pragma unroll
-    for (int m = 0; m < 2; ++m) {
-      const char* x = at(vbase, c.v, p, n, m);
+    for (int v = 0; v < NS; ++v) {
+      const int k0 = M::row(v, 0);
+      const char* y = half[k0 / 16] + k0 % 16 * c.v.ss * (int)sizeof(S) + v_off;
+      uint32_t* to = vr[v];
+      if (!v_lane) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const char* y = x + (8 * (e / 4) + e % 4) * c.v.ss * (int)sizeof(S) + v_off;
-        uint32_t* to = vr[8 * m + e];
-        if (!v_lane) {
+        for (int d = 0; d < VW; ++d) to[d] = 0;
+      } else if constexpr (VB == 2) to[0] = *reinterpret_cast<const uint16_t*>(y);
+      else if constexpr (VB == 4) to[0] = *reinterpret_cast<const uint32_t*>(y);
+      else if constexpr (VB == 8) {
+        const u32x2 z = *reinterpret_cast<const u32x2*>(y);
+        to[0] = z[0]; to[1] = z[1];
+      } else {
 #pragma unroll
-          for (int d = 0; d < VW; ++d) to[d] = 0;
-        } else if constexpr (VB == 2) to[0] = *reinterpret_cast<const uint16_t*>(y);
-        else if constexpr (VB == 4) to[0] = *reinterpret_cast<const uint32_t*>(y);
-        else if constexpr (VB == 8) {
-          const u32x2 z = *reinterpret_cast<const u32x2*>(y);
-          to[0] = z[0]; to[1] = z[1];
-        } else {
-#pragma unroll
-          for (int d = 0; d < VW; d += 4) {
-            const u32x4 z = *reinterpret_cast<const u32x4*>(y + 4 * d);
-            to[d] = z[0]; to[d + 1] = z[1]; to[d + 2] = z[2]; to[d + 3] = z[3];
-          }
+        for (int d = 0; d < VW; d += 4) {
+          const u32x4 z = *reinterpret_cast<const u32x4*>(y + 4 * d);
+          to[d] = z[0]; to[d + 1] = z[1]; to[d + 2] = z[2]; to[d + 3] = z[3];
         }
       }
     }
-    if constexpr (E4M3) v_sc = c.v_scale[(int64_t)(r < 16 ? p.p[0] : p.p[1]) * c.Hkv + t.hk];
+    if constexpr (E4M3) v_sc = c.v_scale[(int64_t)(lane < 32 ? p.p[0] : p.p[1]) * c.Hkv + t.hk];
   };
+  auto scale_of = [&](int bytes, int m) { return E4M3 ? __uint_as_float((uint32_t)__builtin_amdgcn_readlane(bytes, 32 * m) << 23) : 1.f; };
 
-  f32x16 acc[DB];
+  Acc acc[DB];
 #pragma unroll
-  for (int db = 0; db < DB; ++db)
+  for (int d = 0; d < DB; ++d)
 #pragma unroll
-    for (int v = 0; v < 16; ++v) acc[db][v] = 0.f;
+    for (int v = 0; v < NA; ++v) acc[d][v] = 0.f;
   float m_run = kUnset, l_run = 0.f;
   bool bad = false;
 
-  // wavefront w takes the blocks n1 - 1 - w, n1 - 5 - w, ...: the nearest keys, whose bias is least, first
-  int n = w.n1 - 1 - wave;
-  const bool some = n >= w.n0;
   Pages now{{0, 0}, {false, false}};
-  int entry = 0;
   if (some) {
-    now = pages_of(table_at(n));
-    entry = table_at(max(n - 4, w.n0));
+    now = pages_of(entry0);
     load_k(now, n);
     load_v(now, n);
   }
   for (; n >= w.n0; n -= 4) {
     const int key0 = n * kKeys;
-    f32x16 sc;
+    float sc[NS];
 #pragma unroll
-    for (int v = 0; v < 16; ++v) sc[v] = 0.f;
-    const float ks = E4M3 ? __uint_as_float((uint32_t)k_sc << 23) : 1.f;
-    if constexpr (BF) {
+    for (int y = 0; y < TILES; ++y) {
+      Acc z;
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) {
-        if constexpr (E4M3) {
-#pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            const u32x4 f = {bf16_of_e4m3<false>(kr[j][2 * y], ks), bf16_of_e4m3<true>(kr[j][2 * y], ks), bf16_of_e4m3<false>(kr[j][2 * y + 1], ks),
-                             bf16_of_e4m3<true>(kr[j][2 * y + 1], ks)};
-            sc = mfma32(__builtin_bit_cast(bf16x8, f), qf[2 * j + y], sc);
-          }
-        } else {
-          sc = mfma32(__builtin_bit_cast(bf16x8, kr[j]), qf[j], sc);
-        }
-      }
-    } else {
+      for (int v = 0; v < NA; ++v) z[v] = 0.f;
+      const float ks = ROWS == 32 ? (r < 16 ? scale_of(k_sc, 0) : scale_of(k_sc, 1)) : scale_of(k_sc, y);
 #pragma unroll
       for (int j = 0; j < NJ; ++j) {
-        const float* q = qs + r * QS + (2 * j + g) * EPC;
-        if (2 * EPC * j >= D) break;
+        const u32x4 k = kr[y][j];
+        if constexpr (BF && E4M3) {
 #pragma unroll
-        for (int x = 0; x < EPC; x += 4) {
-          const f32x4 qv = *reinterpret_cast<const f32x4*>(q + x);
-          float f[4];
-          if constexpr (E4M3) {
-            const float2 lo = e4m3_pair<false>(kr[j][x / 4]), hi = e4m3_pair<true>(kr[j][x / 4]);
-            f[0] = lo.x * ks; f[1] = lo.y * ks; f[2] = hi.x * ks; f[3] = hi.y * ks;
-          } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) f[e] = __uint_as_float(kr[j][e]);
+          for (int x = 0; x < 2; ++x) {
+            const u32x4 f = {bf16_of_e4m3<false>(k[2 * x], ks), bf16_of_e4m3<true>(k[2 * x], ks), bf16_of_e4m3<false>(k[2 * x + 1], ks), bf16_of_e4m3<true>(k[2 * x + 1], ks)};
+            z = M::mul(__builtin_bit_cast(bf16x8, f), qf[2 * j + x], z);
           }
+        } else if constexpr (BF) {
+          z = M::mul(__builtin_bit_cast(bf16x8, k), qf[j], z);
+        } else if (GROUPS * EPC * j < D) {
+          const float* q = qs + r * QS + (GROUPS * j + g) * EPC;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) sc = mfma_f32(f[e], qv[e], sc);
+          for (int x = 0; x < EPC; x += 4) {
+            const f32x4 qv = *reinterpret_cast<const f32x4*>(q + x);
+            float f[4];
+            if constexpr (E4M3) {
+              const float2 lo = e4m3_pair<false>(k[x / 4]), hi = e4m3_pair<true>(k[x / 4]);
+              f[0] = lo.x * ks; f[1] = lo.y * ks; f[2] = hi.x * ks; f[3] = hi.y * ks;
+            } else {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) f[e] = __uint_as_float(k[e]);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) z = M::mul(f[e], qv[e], z);
+          }
         }
       }
+#pragma unroll
+      for (int v = 0; v < NA; ++v) sc[NA * y + v] = z[v];
     }
     // the keys' registers are free for the next block's
     const Pages next = pages_of(entry);
@@ -245,28 +287,28 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void cache_stream_kernel(con
     }
 
     if constexpr (MOD) {
-      const float x0 = (float)(near - key0 - 4 * g);
+      const float x0 = (float)(near - key0 - M::row(0, g));
 #pragma unroll
-      for (int v = 0; v < 16; ++v) {
+      for (int v = 0; v < NS; ++v) {
         if (cap) sc[v] = BF ? fmaf(-2.f * k1, cap_r(sc[v], c2), k1) : k1 * tanhf(sc[v] * (a.scale / a.cap));
         else sc[v] *= c2;
-        sc[v] = fmaf(-slope2, fabsf(x0 - (float)(8 * (v / 4) + v % 4)), sc[v]);
+        sc[v] = fmaf(-slope2, fabsf(x0 - (float)M::row(v, 0)), sc[v]);
       }
     }
     if (!whole) {
-      const int l0 = see.lo - key0 - 4 * g, h0 = see.hi - key0 - 4 * g;
+      const int l0 = see.lo - key0 - M::row(0, g), h0 = see.hi - key0 - M::row(0, g);
 #pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        const int key = 8 * (v / 4) + v % 4;
-        sc[v] = key >= l0 && key < h0 && now.ok[v / 8] ? sc[v] : -INFINITY;
+      for (int v = 0; v < NS; ++v) {
+        const int key = M::row(v, 0);
+        sc[v] = key >= l0 && key < h0 && now.ok[key / 16] ? sc[v] : -INFINITY;
       }
     }
     // The reference of the exponents is lazy: it moves where a block's sum says that some exponent was large
-    float p[16], sum;
+    float p[NS], sum;
     auto exponentials = [&]() {
       sum = 0.f;
 #pragma unroll
-      for (int v = 0; v < 16; ++v) {
+      for (int v = 0; v < NS; ++v) {
         p[v] = __builtin_amdgcn_exp2f(MOD ? sc[v] - m_run : fmaf(sc[v], c2, -m_run));
         sum += p[v];
       }
@@ -275,15 +317,15 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void cache_stream_kernel(con
     if (__builtin_expect(__any(sum > kSumMost), 0)) {
       float top = -INFINITY;
 #pragma unroll
-      for (int v = 0; v < 16; ++v) top = fmaxf(top, sc[v]);
-      const float m_new = fmaxf(m_run, xhalf_max(MOD ? top : top * c2));
+      for (int v = 0; v < NS; ++v) top = fmaxf(top, sc[v]);
+      const float m_new = fmaxf(m_run, M::max(MOD ? top : top * c2));
       const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
       l_run *= alpha;
       m_run = m_new;
 #pragma unroll
-      for (int db = 0; db < DB; ++db)
+      for (int d = 0; d < DB; ++d)
 #pragma unroll
-        for (int v = 0; v < 16; ++v) acc[db][v] *= alpha;
+        for (int v = 0; v < NA; ++v) acc[d][v] *= alpha;
       exponentials();
     }
     l_run += sum;
@@ -291,20 +333,20 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void cache_stream_kernel(con
     if (!whole) {                                      // nothing of what no row sees; of the rest, what is not finite is added at the end
       bool found = false;
 #pragma unroll
-      for (int x = 0; x < 16; ++x) {
-        const int key = key0 + 8 * (x / 4) + 4 * g + x % 4;
-        const bool in = key >= w.lo && key < w.hi && now.ok[x / 8];
+      for (int v = 0; v < NS; ++v) {
+        const int key = key0 + M::row(v, g);
+        const bool in = key >= w.lo && key < w.hi && now.ok[M::row(v, 0) / 16];
 #pragma unroll
         for (int d = 0; d < VW; ++d) {
-          vr[x][d] = in ? vr[x][d] : 0;
-          found = drop_not_finite<S>(vr[x][d]) || found;
+          vr[v][d] = in ? vr[v][d] : 0;
+          found = drop_not_finite<S>(vr[v][d]) || found;
         }
       }
       bad = bad || __any(found);
     }
     if constexpr (BF) {
 #pragma unroll
-      for (int m = 0; m < 2; ++m) {
+      for (int m = 0; m < NS / 8; ++m) {               // eight keys a lane: the contraction of one matrix instruction
         u32x4 hi, lo;                                  // probabilities as the sum of two bf16: 2^-16 of them is left out
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -312,53 +354,52 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void cache_stream_kernel(con
           hi[e] = pack_bf16(x, y);
           lo[e] = pack_bf16(x - __uint_as_float(hi[e] << 16), y - __uint_as_float(hi[e] & 0xffff0000u));
         }
-        u32x4 f[DB];
-        const float vs = E4M3 ? __uint_as_float((uint32_t)__builtin_amdgcn_readlane(v_sc, 16 * m) << 23) : 1.f;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const uint32_t* x = vr[8 * m + 2 * e];
-          const uint32_t* y = vr[8 * m + 2 * e + 1];
-          if constexpr (E4M3) {
+        for (int d = 0; d < DB; d += 2) {
+          u32x4 f[2];
 #pragma unroll
-            for (int d = 0; d < DB; d += 2) {
-              const uint32_t z = __builtin_amdgcn_perm(y[0], x[0], d ? 0x07030602 : 0x05010400);
-              f[d][e] = bf16_of_e4m3<false>(z, vs);
-              f[d + 1][e] = bf16_of_e4m3<true>(z, vs);
+          for (int e = 0; e < 4; ++e) {                // values of one column by pairs of keys
+            const int v = 8 * m + 2 * e;
+            const float vs = scale_of(v_sc, M::row(v, 0) / 16);
+            if constexpr (E4M3) {
+              const uint32_t z = __builtin_amdgcn_perm(vr[v + 1][d / 4], vr[v][d / 4], d % 4 ? 0x07030602 : 0x05010400);
+              f[0][e] = bf16_of_e4m3<false>(z, vs);
+              f[1][e] = bf16_of_e4m3<true>(z, vs);
+            } else {
+              f[0][e] = __builtin_amdgcn_perm(vr[v + 1][d / 2], vr[v][d / 2], 0x05040100);
+              f[1][e] = __builtin_amdgcn_perm(vr[v + 1][d / 2], vr[v][d / 2], 0x07060302);
             }
-          } else {
-#pragma unroll
-            for (int d = 0; d < DB; ++d) f[d][e] = __builtin_amdgcn_perm(y[d / 2], x[d / 2], d % 2 ? 0x07060302 : 0x05040100);
           }
-        }
 #pragma unroll
-        for (int d = 0; d < DB; ++d) {
-          acc[d] = mfma32(__builtin_bit_cast(bf16x8, f[d]), __builtin_bit_cast(bf16x8, hi), acc[d]);
-          acc[d] = mfma32(__builtin_bit_cast(bf16x8, f[d]), __builtin_bit_cast(bf16x8, lo), acc[d]);
+          for (int x = 0; x < 2; ++x) {
+            acc[d + x] = M::mul(__builtin_bit_cast(bf16x8, f[x]), __builtin_bit_cast(bf16x8, hi), acc[d + x]);
+            acc[d + x] = M::mul(__builtin_bit_cast(bf16x8, f[x]), __builtin_bit_cast(bf16x8, lo), acc[d + x]);
+          }
         }
       }
     } else {
-      const float vs[2] = {E4M3 ? __uint_as_float((uint32_t)__builtin_amdgcn_readlane(v_sc, 0) << 23) : 1.f,
-                           E4M3 ? __uint_as_float((uint32_t)__builtin_amdgcn_readlane(v_sc, 16) << 23) : 1.f};
 #pragma unroll
-      for (int v = 0; v < 16; ++v)
+      for (int v = 0; v < NS; ++v) {
+        const float vs = scale_of(v_sc, M::row(v, 0) / 16);
 #pragma unroll
         for (int d = 0; d < DB; ++d) {
           float f;
           if constexpr (E4M3) {
             const float2 z = (d & 2) ? e4m3_pair<true>(vr[v][d / 4]) : e4m3_pair<false>(vr[v][d / 4]);
-            f = ((d & 1) ? z.y : z.x) * vs[v / 8];
+            f = ((d & 1) ? z.y : z.x) * vs;
           } else {
             f = __uint_as_float(vr[v][d]);
           }
-          acc[d] = mfma_f32(f, p[v], acc[d]);
+          acc[d] = M::mul(f, p[v], acc[d]);
         }
+      }
     }
     if (more) load_v(next, n - 4);
     now = next;
   }
 
   // ---- the four wavefronts' sums, against the highest of their references
-  const float l = xhalf_sum(l_run);
+  const float l = M::sum(l_run);
   if (tid == 0) any_bad = 0;
   if (g == 0) {
     stat_m[wave][r] = m_run;
@@ -375,16 +416,15 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void cache_stream_kernel(con
     if (pass > 0) __syncthreads();
     if (r < live)
 #pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        const int rho = 8 * (v / 4) + 4 * g + v % 4;
-        float* to = fold + (wave * kRows + r) * FS + PW * rho;
+      for (int v = 0; v < NA; ++v) {
+        float* to = fold + (wave * ROWS + r) * FS + PW * M::row(v, g);
 #pragma unroll
         for (int d = 0; d < PW; ++d) to[d] = acc[PW * pass + d][v] * weight;
       }
     __syncthreads();
-    for (int x = tid; x < live * 32; x += 256) {
-      const int y = x >> 5, rho = x & 31, d0 = DB * rho + PW * pass;
-      const int R = t.tile * kRows + y, yi = R / G, yh = t.hk * G + R - yi * G;
+    for (int x = tid; x < live * ROWS; x += 256) {
+      const int y = x / ROWS, rho = x % ROWS, d0 = DB * rho + PW * pass;
+      const int R = t.tile * ROWS + y, yi = R / G, yh = t.hk * G + R - yi * G;
       if (!BF && d0 >= D) continue;
       const float top = fmaxf(fmaxf(stat_m[0][y], stat_m[1][y]), fmaxf(stat_m[2][y], stat_m[3][y]));
       float sum = 0.f, o[PW];
@@ -394,7 +434,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void cache_stream_kernel(con
       for (int k = 0; k < 4; ++k) {
         sum += stat_l[k][y] * __builtin_amdgcn_exp2f(stat_m[k][y] - top);
 #pragma unroll
-        for (int d = 0; d < PW; ++d) o[d] += fold[(k * kRows + y) * FS + PW * rho + d];
+        for (int d = 0; d < PW; ++d) o[d] += fold[(k * ROWS + y) * FS + PW * rho + d];
       }
       if (__builtin_expect(any_bad, 0)) {              // what the blocks at the masks' edges left out, of the keys that this row sees
         const RowSpan ys = row_span(a, s, yi);
@@ -413,7 +453,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void cache_stream_kernel(con
         }
       }
       if (part) {
-        float* to = a.part_o + ((int64_t)t.state * kRows + y) * D + d0;
+        float* to = a.part_o + (a.plan.base + (int64_t)t.state * ROWS + y) * D + d0;
 #pragma unroll
         for (int d = 0; d < PW; ++d) to[d] = o[d];
         continue;
@@ -441,7 +481,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void cache_stream_kernel(con
     float sum = 0.f;
 #pragma unroll
     for (int k = 0; k < 4; ++k) sum += stat_l[k][r] * __builtin_amdgcn_exp2f(stat_m[k][r] - m_all);
-    if (part) a.part_row[(int64_t)t.state * kRows + r] = make_float4(m_all, sum, besides, 0.f);
+    if (part) a.part_row[a.plan.base + (int64_t)t.state * ROWS + r] = make_float4(m_all, sum, besides, 0.f);
     else a.lse[(int64_t)h * a.T + s.r.first + i] = sum != 0.f ? m_all * kScoreLn2 + logf(sum) + besides : -INFINITY;
   }
 }
@@ -456,19 +496,21 @@ __global__ __launch_bounds__(256) void cache_combine_kernel(const CacheAttnArgs 
   for (int64_t row = row0; row < min(row0 + each, rows); ++row) {
     const int t = (int)(row / a.Hq), h = (int)(row - (int64_t)t * a.Hq);
     if (t < first || t >= end) continue;
-    const int4 at = a.info[t];                         // {first state, shares, row tiles, row of the sequence}
-    if (at.y <= 1) {
+    const int4 at = a.info[t];
+    const int shares = at.y & 0xffff, tile_rows = at.y >> 16;
+    if (shares <= 1) {
       row += a.Hq - 1 - h;                             // nor are the token's other heads split
       continue;
     }
-    const int hk = h / G, R = at.w * G + h - hk * G, tile = R / kRows;
-    const int64_t s0 = at.x + (int64_t)(at.z - 1 - tile) * a.c.Hkv + hk, step = (int64_t)at.z * a.c.Hkv;
-    if (at.x < 0 || at.w < 0 || at.z <= tile || s0 + (at.y - 1) * step >= a.plan.states) continue;
+    const int hk = h / G, R = at.w * G + h - hk * G, tile = tile_rows > 0 ? R / tile_rows : 0;
+    // (where starts are no starts, a token may not have been told of: nothing is read outside the states)
+    const int64_t s0 = at.x + ((int64_t)(at.z - 1 - tile) * a.c.Hkv + hk) * tile_rows + (R - tile * tile_rows), step = (int64_t)at.z * a.c.Hkv * tile_rows;
+    if (tile_rows <= 0 || at.x < 0 || at.w < 0 || at.z <= tile || s0 + (shares - 1) * step >= a.state_rows) continue;
     float top = kUnset, sum = 0.f, besides = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int k0 = 0; k0 < at.y; k0 += 256) {           // their weights, against the highest reference so far
+    for (int k0 = 0; k0 < shares; k0 += 256) {           // their weights, against the highest reference so far
       float4 st = make_float4(kUnset, 0.f, 0.f, 0.f);
-      if (k0 + tid < at.y) st = a.part_row[(s0 + (k0 + tid) * step) * kRows + R % kRows];
+      if (k0 + tid < shares) st = a.part_row[s0 + (k0 + tid) * step];
       float m = st.x;
 #pragma unroll
       for (int d = 1; d < 64; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
@@ -487,13 +529,13 @@ __global__ __launch_bounds__(256) void cache_combine_kernel(const CacheAttnArgs 
       top = m;
       sum = sum * old + ((sum_of[0] + sum_of[1]) + (sum_of[2] + sum_of[3]));
       o *= old;
-      const int n = min(at.y - k0, 256);
+      const int n = min(shares - k0, 256);
       if (y < lanes)
         for (int k = y; k < n; k += 4 * lanes) {       // four loads in flight
           f32x4 z[4];
 #pragma unroll
           for (int u = 0; u < 4; ++u)
-            z[u] = *reinterpret_cast<const f32x4*>(a.part_o + ((s0 + (int64_t)(k0 + min(k + u * lanes, n - 1)) * step) * kRows + R % kRows) * D + 4 * x);
+            z[u] = *reinterpret_cast<const f32x4*>(a.part_o + (s0 + (int64_t)(k0 + min(k + u * lanes, n - 1)) * step) * D + 4 * x);
 #pragma unroll
           for (int u = 0; u < 4; ++u)
             if (k + u * lanes < n) o += z[u] * weights[k + u * lanes];
@@ -520,9 +562,10 @@ hipError_t launch_cache_attn(const CacheAttnArgs& a, bool bf16, hipStream_t stre
   if (a.plan.grid <= 0 || a.plan.grid > kScoreGridMost) return hipErrorInvalidValue;
   ProfScope prof("cache_attn", stream);
   const dim3 grid((unsigned)a.plan.grid), block(256);
-  const bool mod = a.cap > 0.f || a.slopes;
+  const bool mod = a.cap > 0.f || a.slopes, few = a.plan.rows == 16;
   auto go = [&](auto plain, auto modified) { hipLaunchKernelGGL(mod ? modified : plain, grid, block, 0, stream, a); };
-#define ST_STREAM(T, S, DP) go(cache_stream_kernel<T, S, DP, false>, cache_stream_kernel<T, S, DP, true>)
+#define ST_STREAM(T, S, DP) (few ? go(cache_stream_kernel<T, S, 16, DP, false>, cache_stream_kernel<T, S, 16, DP, true>) \
+                                 : go(cache_stream_kernel<T, S, 32, DP, false>, cache_stream_kernel<T, S, 32, DP, true>))
   const int D = a.c.D;
   if (bf16 && a.c.dtype == ST_E4M3) D == 128 ? ST_STREAM(uint16_t, uint8_t, 128) : ST_STREAM(uint16_t, uint8_t, 64);
   else if (bf16) D == 128 ? ST_STREAM(uint16_t, uint16_t, 128) : ST_STREAM(uint16_t, uint16_t, 64);

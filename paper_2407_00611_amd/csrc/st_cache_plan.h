@@ -2,8 +2,8 @@
 // sequence to sequence by orders of magnitude; a workgroup finds its piece of the work from them by itself.
 //
 // Sequence b has S_b row tiles, each of which walks about L_b key blocks.  With c key blocks a share, c = sum S_b L_b Hkv / target or the
-// least, sequence b is cut into ceil(L_b / c) shares: at most target + sum S_b Hkv workgroups, and of sequences with several shares
-// at most 2 target, each of which leaves a partial state.
+// least, sequence b is cut into L_b / c shares, rounded: at most target + sum S_b Hkv workgroups, and of sequences with several shares
+// at most 4/3 target (x rounded is at most 4/3 x where it is 2 or more), each of which leaves a partial state.
 #pragma once
 
 #include "st_cache.h"
@@ -42,97 +42,91 @@ __device__ __forceinline__ RowSpan row_span(const CacheAttnArgs& a, const SeqSpa
   return y;
 }
 
+// Sums over the wavefront's lanes, by data parallel primitives: inclusive, in a fixed order
 template <typename T>
-__device__ __forceinline__ T wave_scan(T x) {        // inclusive
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const T y = __shfl_up(x, d);
-    if (lane >= d) x += y;
+__device__ __forceinline__ T from_lanes_before(T x, T none, int how) {
+  const int i = __builtin_bit_cast(int, x), z = __builtin_bit_cast(int, none);
+  int y;
+  switch (how) {
+    case 0: y = __builtin_amdgcn_update_dpp(z, i, 0x111, 0xf, 0xf, false); break;   // row_shr 1, 2, 4, 8
+    case 1: y = __builtin_amdgcn_update_dpp(z, i, 0x112, 0xf, 0xf, false); break;
+    case 2: y = __builtin_amdgcn_update_dpp(z, i, 0x114, 0xf, 0xf, false); break;
+    case 3: y = __builtin_amdgcn_update_dpp(z, i, 0x118, 0xf, 0xf, false); break;
+    case 4: y = __builtin_amdgcn_update_dpp(z, i, 0x142, 0xa, 0xf, false); break;   // lane 15 of a row to the next row: rows 1 and 3
+    default: y = __builtin_amdgcn_update_dpp(z, i, 0x143, 0xc, 0xf, false);         // lane 31 to the upper half
   }
+  return __builtin_bit_cast(T, y);
+}
+template <typename T>
+__device__ __forceinline__ T wave_scan(T x) {
+#pragma unroll
+  for (int d = 0; d < 6; ++d) x += from_lanes_before(x, T(0), d);
   return x;
 }
+__device__ __forceinline__ float wave_last(float x) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63)); }
+__device__ __forceinline__ int wave_last(int x) { return __builtin_amdgcn_readlane(x, 63); }
 
-struct PlanRoom {
-  int64_t sums[8];
-  CacheItem item;
-};
-// 256 threads; room: LDS
+// Every wavefront for itself, a sequence a lane: no barrier, and one look at the lengths is all the memory that a batch of 64 waits for.
+// The span of the sequence found comes with it.
 template <int ROWS, int KEYS>
-__device__ __forceinline__ CacheItem find_item(const CacheAttnArgs& a, PlanRoom* room) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), G = a.Hq / a.c.Hkv;
-  auto work = [&](int b, int& S, int& L) {
+__device__ __forceinline__ CacheItem find_item(const CacheAttnArgs& a, SeqSpan& span) {
+  const int lane = threadIdx.x & 63, G = a.Hq / a.c.Hkv;
+  auto work = [&](int b, SeqSpan& s, int& S, int& L) {
     S = L = 0;
+    s = SeqSpan{SeqRows{0, 0}, 0, 0};
     if (b >= a.c.B) return;
-    const SeqSpan s = seq_span(a, b);
+    s = seq_span(a, b);
     const int M = s.r.n * G;
     if (M <= a.plan.rows_from || M > a.plan.rows_to) return;
     S = (M + ROWS - 1) / ROWS;
     const RowSpan first = row_span(a, s, 0), last = row_span(a, s, s.r.n - 1);
     L = max((last.hi + KEYS - 1) / KEYS - first.lo / KEYS, 0);
   };
+  SeqSpan s0;
   int S0, L0;
-  work(tid, S0, L0);
-  int64_t sum = (int64_t)S0 * L0;
-  for (int b = tid + 256; b < a.c.B; b += 256) {
+  work(lane, s0, S0, L0);
+  // (fp32 with some room above: the same sum in every wavefront, and shares that are never too many)
+  float all = wave_last(wave_scan((float)S0 * (float)L0));
+  for (int b = lane + 64; b - lane < a.c.B; b += 64) {
+    SeqSpan s;
     int S, L;
-    work(b, S, L);
-    sum += (int64_t)S * L;
+    work(b, s, S, L);
+    all += wave_last(wave_scan((float)S * (float)L));
   }
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
-  if (lane == 0) room->sums[wave] = sum;
-  if (tid == 0) room->item.b = -1;
-  __syncthreads();
-  const int64_t all = (room->sums[0] + room->sums[1] + room->sums[2] + room->sums[3]) * a.c.Hkv;
-  const int c = (int)min(max((all + a.plan.target - 1) / a.plan.target, (int64_t)a.plan.least), (int64_t)1 << 30);
-  const int64_t me = blockIdx.x;
-  int64_t items_before = 0, states_before = 0;
-  for (int b0 = 0; b0 < a.c.B; b0 += 256) {
-    if (b0 > 0) work(b0 + tid, S0, L0);
-    const int shares = max((L0 + c - 1) / c, 1);
-    const int64_t n = (int64_t)S0 * shares * a.c.Hkv, m = shares > 1 ? n : 0;
-    int64_t x = wave_scan(n), y = wave_scan(m);
-    __syncthreads();
-    if (lane == 63) room->sums[wave] = x, room->sums[4 + wave] = y;
-    __syncthreads();
-    int64_t nx = 0, ny = 0;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      if (w < wave) x += room->sums[w], y += room->sums[4 + w];
-      nx += room->sums[w];
-      ny += room->sums[4 + w];
-    }
-    x += items_before - n;
-    y += states_before - m;
-    if (me >= x && me < x + n) {
-      const int at = (int)(me - x), rest = at / a.c.Hkv;
-      CacheItem& t = room->item;
-      t.b = b0 + tid;
+  const int c = max((int)fminf(all * (float)a.c.Hkv / (float)a.plan.target * 1.0001f + 1.f, 1e9f), a.plan.least);
+  const int me = blockIdx.x;
+  CacheItem t;
+  t.b = -1;
+  int items_before = 0, states_before = 0;
+  for (int b0 = 0; b0 < a.c.B; b0 += 64) {
+    if (b0 > 0) work(b0 + lane, s0, S0, L0);
+    const int shares = max((int)(((int64_t)L0 + c / 2) / c), 1);
+    // (a launch has at most 2^22 workgroups: what starts that are no starts name beyond that is left out)
+    const int n = (int)min((int64_t)S0 * shares * a.c.Hkv, (int64_t)1 << 24), m = shares > 1 ? n : 0;
+    const int x = wave_scan(n), y = wave_scan(m);
+    const uint64_t mine = __ballot(me - items_before >= x - n && me - items_before < x);
+    if (mine) {
+      const int l = __ffsll((unsigned long long)mine) - 1;
+      auto of = [&](int z) { return __builtin_amdgcn_readlane(z, l); };
+      t.b = b0 + l;
+      const int at = me - items_before - of(x - n), rest = at / a.c.Hkv;
+      t.tiles = of(S0);
+      t.shares = of(shares);
       t.hk = at - rest * a.c.Hkv;
-      t.share = rest / S0;
-      t.tile = S0 - 1 - (rest - t.share * S0);       // later rows see more: first
-      t.shares = shares;
-      t.tiles = S0;
-      // (starts that are no starts may name more rows than there are: what there is no room for is left out)
-      t.first_state = (int)min(y, (int64_t)1 << 30);
-      t.state = (int)min(y + at, (int64_t)1 << 30);
-      if (shares > 1 && t.state >= a.plan.states) t.b = -1;
+      t.share = rest / t.tiles;
+      t.tile = t.tiles - 1 - (rest - t.share * t.tiles);   // later rows see more: first
+      t.first_state = states_before + of(y - m);
+      t.state = t.first_state + at;
+      if (t.shares > 1 && (t.state < 0 || t.state >= a.plan.states)) t.b = -1;
+      span.r.first = of(s0.r.first);
+      span.r.n = of(s0.r.n);
+      span.len = of(s0.len);
+      span.pos = (int64_t)((uint64_t)(uint32_t)of((int)s0.pos) | (uint64_t)(uint32_t)of((int)(s0.pos >> 32)) << 32);
+      return t;
     }
-    __syncthreads();
-    items_before += nx;
-    states_before += ny;
-    if (items_before > me) break;
+    items_before = (int)min((int64_t)items_before + wave_last(x), (int64_t)1 << 30);
+    states_before = (int)min((int64_t)states_before + wave_last(y), (int64_t)1 << 30);
   }
-  CacheItem t = room->item;
-  t.b = __builtin_amdgcn_readfirstlane(t.b);
-  t.hk = __builtin_amdgcn_readfirstlane(t.hk);
-  t.tile = __builtin_amdgcn_readfirstlane(t.tile);
-  t.share = __builtin_amdgcn_readfirstlane(t.share);
-  t.shares = __builtin_amdgcn_readfirstlane(t.shares);
-  t.tiles = __builtin_amdgcn_readfirstlane(t.tiles);
-  t.first_state = __builtin_amdgcn_readfirstlane(t.first_state);
-  t.state = __builtin_amdgcn_readfirstlane(t.state);
   return t;
 }
 
@@ -161,7 +155,7 @@ template <int ROWS>
 __device__ __forceinline__ void tell_rows(const CacheAttnArgs& a, const SeqSpan& s, const CacheItem& t, int G) {
   if (t.share != 0 || t.hk != 0 || !a.info) return;
   const int i0 = (t.tile * ROWS + G - 1) / G, i1 = min((t.tile * ROWS + ROWS + G - 1) / G, s.r.n);   // their first head is in this tile
-  for (int i = i0 + threadIdx.x; i < i1; i += 256) a.info[s.r.first + i] = make_int4(t.first_state, t.shares, t.tiles, i);
+  for (int i = i0 + threadIdx.x; i < i1; i += 256) a.info[s.r.first + i] = make_int4((int)(a.plan.base + (int64_t)t.first_state * ROWS), t.shares | ROWS << 16, t.tiles, i);
 }
 
 }  // namespace st
