@@ -19,7 +19,7 @@ BINDING = os.path.join(PKG, "_binding.so")
 OBJ_DIR = os.path.join(PKG, "_build")
 
 SOURCES = ["st_api.cpp", "st_runtime.cpp", "st_f32.hip", "st_elementwise.hip", "st_fwd_bf16.hip", "st_bwd_bf16.hip", "st_bwd_dkv_fast.hip", "st_bwd_dq_fast.hip", "st_fwd_fast.hip", "st_probe.hip",
-           "st_api_score.cpp", "st_score.hip", "st_score_bf16.hip", "st_score_f32.hip", "st_rope.hip", "st_api_cache.cpp", "st_cache.hip", "st_cache_attn.hip"]
+           "st_api_score.cpp", "st_score.hip", "st_score_bf16.hip", "st_score_f32.hip", "st_rope.hip", "st_api_cache.cpp", "st_cache.hip", "st_cache_attn.hip", "st_cache_prompt.hip"]
 # assembly main loops written out by generator scripts before compiling: (script, output)
 GENERATED = [("gen_bwd_dkv_asm.py", "st_bwd_dkv_asm.inc"), ("gen_bwd_dq_asm.py", "st_bwd_dq_asm.inc"),
              ("gen_fwd_asm.py", "st_fwd_asm.inc"), ("gen_fwd_asm.py 64", "st_fwd64_asm.inc"),

@@ -12,8 +12,12 @@ using st::hip_fail;
 
 namespace {
 
-// A share of a walk is at least so many blocks of 32 keys, two for each of a workgroup's wavefronts; workgroups that shares are made for
-constexpr int kLeastBlocks = 8, kPlaces = 1024;
+// A share of a walk is at least so many blocks of 32 keys, two for each of a workgroup's wavefronts.  Workgroups that shares are made for:
+// tiles of 16 rows wait for memory, and more of them than the chip holds at once even out what the lengths leave (64 ragged sequences 124 us,
+// 140 with 1024); for tiles of 32 rows, which are work, each share has 32 rows of O to join.
+constexpr int kLeastBlocks = 8, kPlacesOfFew = 2048, kPlaces = 512;
+// Rows up to which sixteen wavefronts join the states of each, where they may be sixteen and more
+constexpr int kManyRows = 512;
 // Batches whose sequences all have at most so many rows have one launch for them
 constexpr int kFewRows = 64;
 
@@ -84,17 +88,20 @@ st_status check_rows(const st_cache_rows* r, const st_cache* c) {
 st::CachePlan launch_plan(const st_cache_rows* r, const st_cache* c, int rows, int from, int to, int64_t base) {
   const int64_t G = r->Hq / c->Hkv, some = std::min(c->B, r->T), most_rows = std::min<int64_t>((int64_t)std::min(r->max_rows, r->T) * G, to);
   const int64_t tiles = std::min(r->T * G / rows + some, some * ((most_rows + rows - 1) / rows));
-  const int64_t blocks = ((int64_t)c->width * c->page + st::kCacheKeys - 1) / st::kCacheKeys;
+  const int keys = rows == st::kPromptRows ? st::kPromptKeys : st::kCacheKeys;
+  const int64_t blocks = ((int64_t)c->width * c->page + keys - 1) / keys;
   st::CachePlan p{};
   p.rows = rows;
   p.rows_from = from;
   p.rows_to = to;
   p.least = kLeastBlocks;
-  p.target = kPlaces;
+  p.target = rows == 16 ? kPlacesOfFew : kPlaces;
   const int64_t jobs = tiles * c->Hkv, most = std::max<int64_t>((blocks + p.least / 2) / p.least, 1);
   p.grid = std::min(p.target + jobs, jobs * most);
+  if (rows == 16) p.grid = (p.grid + 8 * c->Hkv - 1) / (8 * c->Hkv) * (8 * c->Hkv);   // (whole rounds of the order in which they take their pieces)
   p.states = most > 1 ? (int32_t)std::min<int64_t>(p.target * 4 / 3 + 1, jobs * most) : 0;
   p.base = base;
+  p.jobs = jobs;
   return p;
 }
 // The launches of a call: sequences of up to 16 rows and those of more have kernels of their own where there may be both
@@ -102,23 +109,25 @@ struct Plans {
   int n;
   st::CachePlan p[2];
   int64_t rows;              // of all states
+  bool many;                 // states of a row
 };
 Plans plans_of(const st_cache_rows* r, const st_cache* c) {
   constexpr int kAll = 0x7fffffff;
   const int64_t most = (int64_t)std::min(r->max_rows, r->T) * (r->Hq / c->Hkv);
+  const int large = r->dtype == ST_BF16 && most > kFewRows ? st::kPromptRows : 32;
   Plans y{};
+  y.n = 1;
   if (most <= 16) {
-    y.n = 1;
     y.p[0] = launch_plan(r, c, 16, 0, kAll, 0);
   } else if (most <= kFewRows || c->B == 1) {
-    y.n = 1;
-    y.p[0] = launch_plan(r, c, 32, 0, kAll, 0);
+    y.p[0] = launch_plan(r, c, large, 0, kAll, 0);
   } else {
     y.n = 2;
-    y.p[0] = launch_plan(r, c, 32, 16, kAll, 0);
-    y.p[1] = launch_plan(r, c, 16, 0, 16, (int64_t)y.p[0].states * 32);
+    y.p[0] = launch_plan(r, c, large, 16, kAll, 0);
+    y.p[1] = launch_plan(r, c, 16, 0, 16, (int64_t)y.p[0].states * large);
   }
   for (int x = 0; x < y.n; ++x) y.rows += (int64_t)y.p[x].states * y.p[x].rows;
+  y.many = y.n == 1 && (int64_t)r->T * r->Hq <= kManyRows && y.p[0].states >= 16 * y.p[0].jobs;
   return y;
 }
 struct Room {
@@ -245,9 +254,10 @@ st_status st_attn_cache(const st_cache_rows* r, const st_cache* c, const int32_t
   a.state_rows = plans.rows;
   for (int x = 0; x < plans.n; ++x) {
     a.plan = plans.p[x];
-    ST_HIP(st::launch_cache_attn(a, r->dtype == ST_BF16, (hipStream_t)hip_stream), "st_attn_cache launch");
+    ST_HIP(a.plan.rows == st::kPromptRows ? st::launch_cache_prompt(a, (hipStream_t)hip_stream) : st::launch_cache_attn(a, r->dtype == ST_BF16, (hipStream_t)hip_stream),
+           "st_attn_cache launch");
   }
-  if (plans.rows > 0) ST_HIP(st::launch_cache_combine(a, r->dtype == ST_BF16, (hipStream_t)hip_stream), "st_attn_cache combine");
+  if (plans.rows > 0) ST_HIP(st::launch_cache_combine(a, r->dtype == ST_BF16, plans.many, (hipStream_t)hip_stream), "st_attn_cache combine");
   return ST_OK;
 }
 

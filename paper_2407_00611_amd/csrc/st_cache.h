@@ -33,13 +33,13 @@ struct ReadArgs {
 
 // Which sequences a launch takes and how it is split (st_cache_plan.h)
 struct CachePlan {
-  int32_t rows;                                      // of a tile: 16 or 32
+  int32_t rows;                                      // of a tile: 16, 32, or 128 (prompts)
   int32_t rows_from, rows_to;                        // packed rows (token, head of a group) of a sequence: rows_from < rows <= rows_to
   int32_t least;                                     // key blocks of a share, at least
   int32_t target;                                    // workgroups that the shares are made for
   int32_t states;                                    // partial states there is room for
   int64_t base;                                      // rows of the states of launches before
-  int64_t grid;
+  int64_t jobs, grid;                                // tiles times KV heads, at most; workgroups
 };
 
 struct CacheAttnArgs {
@@ -63,11 +63,14 @@ struct CacheAttnArgs {
 };
 
 constexpr int kCacheKeys = 32;                       // keys of a block
+constexpr int kPromptRows = 128, kPromptKeys = 64;   // of the kernel for prompts
 
 hipError_t launch_cache_append(const AppendArgs& a, bool bf16, hipStream_t stream);
 hipError_t launch_cache_read(const ReadArgs& a, int out_dtype, hipStream_t stream);
 hipError_t launch_cache_attn(const CacheAttnArgs& a, bool bf16, hipStream_t stream);
-hipError_t launch_cache_combine(const CacheAttnArgs& a, bool bf16, hipStream_t stream);
+hipError_t launch_cache_prompt(const CacheAttnArgs& a, hipStream_t stream);
+// many: there may be 16 states of a row and more, and rows are few
+hipError_t launch_cache_combine(const CacheAttnArgs& a, bool bf16, bool many, hipStream_t stream);
 
 // ---- device side
 

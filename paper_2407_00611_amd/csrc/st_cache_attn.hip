@@ -17,6 +17,7 @@ namespace st {
 namespace {
 
 constexpr int kKeys = kCacheKeys;
+constexpr int kManyWaves = 16;                       // of a row whose states are many
 constexpr float kUnset = -1e30f;                     // reference of a row that has met no key: whatever comes exceeds it
 constexpr float kSumMost = 4096.f;                   // a lane's sum over its keys of a block beyond which a row's reference moves
 
@@ -486,14 +487,17 @@ __global__ __launch_bounds__(256, (stream_waves<T, S, ROWS, DP>())) void cache_s
   }
 }
 
-// Joins the states of rows whose walk was split: a row at a time, eight states side by side at 128 columns.  Rows that are whole cost a look.
-__global__ __launch_bounds__(256) void cache_combine_kernel(const CacheAttnArgs a, int each, int bf16) {
-  __shared__ f32x4 fold[256];
-  __shared__ float weights[256], top_of[4], sum_of[4];
-  const int tid = threadIdx.x, D = a.c.D, G = a.Hq / a.c.Hkv, vecs = D / 4, lanes = 256 / vecs, x = tid % vecs, y = tid / vecs;
+// Joins the states of rows whose walk was split: W wavefronts a row, each with a part of the states, 64 D / 4 lanes' worth of them side by
+// side.  A wavefront of its own for each row (W = 1) where shares are few, of which a wavefront goes through `each` rows one behind the
+// other; rows that are whole cost a look.
+template <int W>
+__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void cache_combine_kernel(const CacheAttnArgs a, int each, int bf16) {
+  constexpr int kAtOnce = 4;
+  __shared__ f32x4 fold[W == 1 ? 1 : W][64];
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), D = a.c.D, G = a.Hq / a.c.Hkv, vecs = D / 4, side = 64 / vecs, x = lane % vecs, y = lane / vecs;
   const int first = max(min(a.starts[0], a.T), 0), end = max(min(a.starts[a.c.B], a.T), 0);
-  const int64_t row0 = (int64_t)blockIdx.x * each, rows = (int64_t)a.T * a.Hq;
-  for (int64_t row = row0; row < min(row0 + each, rows); ++row) {
+  const int64_t rows = (int64_t)a.T * a.Hq, row0 = W == 1 ? ((int64_t)blockIdx.x * 4 + wave) * each : (int64_t)blockIdx.x;
+  for (int64_t row = row0; row < min(row0 + (W == 1 ? each : 1), rows); ++row) {
     const int t = (int)(row / a.Hq), h = (int)(row - (int64_t)t * a.Hq);
     if (t < first || t >= end) continue;
     const int4 at = a.info[t];
@@ -506,53 +510,61 @@ __global__ __launch_bounds__(256) void cache_combine_kernel(const CacheAttnArgs 
     // (where starts are no starts, a token may not have been told of: nothing is read outside the states)
     const int64_t s0 = at.x + ((int64_t)(at.z - 1 - tile) * a.c.Hkv + hk) * tile_rows + (R - tile * tile_rows), step = (int64_t)at.z * a.c.Hkv * tile_rows;
     if (tile_rows <= 0 || at.x < 0 || at.w < 0 || at.z <= tile || s0 + (shares - 1) * step >= a.state_rows) continue;
+    const int mine = wave * side + y, all = (W == 1 ? 1 : W) * side;   // this lane's states: mine, mine + all, ...
+    const int k0 = W == 1 ? y : mine;
+    f32x4 z[kAtOnce];
+    float zm[kAtOnce];
+    auto load = [&](int k) {
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u) {
+        const int64_t from = s0 + min(k + u * all, shares - 1) * step;
+        z[u] = *reinterpret_cast<const f32x4*>(a.part_o + from * D + 4 * x);
+        zm[u] = a.part_row[from].x;
+      }
+    };
+    load(k0);
+    // reference and sum of the whole row
     float top = kUnset, sum = 0.f, besides = 0.f;
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int k0 = 0; k0 < shares; k0 += 256) {           // their weights, against the highest reference so far
+    for (int k = lane; k - lane < shares; k += 64) {
       float4 st = make_float4(kUnset, 0.f, 0.f, 0.f);
-      if (k0 + tid < shares) st = a.part_row[s0 + (k0 + tid) * step];
-      float m = st.x;
-#pragma unroll
-      for (int d = 1; d < 64; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
-      __syncthreads();
-      if ((tid & 63) == 0) top_of[tid >> 6] = m;
-      __syncthreads();
-      m = fmaxf(fmaxf(fmaxf(top_of[0], top_of[1]), fmaxf(top_of[2], top_of[3])), top);
-      const float e = __builtin_amdgcn_exp2f(st.x - m), old = __builtin_amdgcn_exp2f(top - m);
-      weights[tid] = e;
-      float l = st.y * e;
-#pragma unroll
-      for (int d = 1; d < 64; d *= 2) l += __shfl_xor(l, d);
-      if ((tid & 63) == 0) sum_of[tid >> 6] = l;
-      if (tid == 0) besides = st.z;
-      __syncthreads();
+      if (k < shares) st = a.part_row[s0 + k * step];
+      if (k == 0) besides = st.z;
+      const float m = fmaxf(top, st.x);
+      sum = sum * __builtin_amdgcn_exp2f(top - m) + st.y * __builtin_amdgcn_exp2f(st.x - m);
       top = m;
-      sum = sum * old + ((sum_of[0] + sum_of[1]) + (sum_of[2] + sum_of[3]));
-      o *= old;
-      const int n = min(shares - k0, 256);
-      if (y < lanes)
-        for (int k = y; k < n; k += 4 * lanes) {       // four loads in flight
-          f32x4 z[4];
-#pragma unroll
-          for (int u = 0; u < 4; ++u)
-            z[u] = *reinterpret_cast<const f32x4*>(a.part_o + (s0 + (int64_t)(k0 + min(k + u * lanes, n - 1)) * step) * D + 4 * x);
-#pragma unroll
-          for (int u = 0; u < 4; ++u)
-            if (k + u * lanes < n) o += z[u] * weights[k + u * lanes];
-        }
     }
-    fold[tid] = o;
-    __syncthreads();
-    if (y == 0) {
-      for (int k = 1; k < lanes; ++k) o += fold[k * vecs + x];
-      o *= sum != 0.f ? 1.f / sum : 0.f;
-      const int64_t to = row * D + 4 * x;
-      if (a.o) *reinterpret_cast<f32x4*>(a.o + to) = o;
-      if (a.o_lowp && bf16) *reinterpret_cast<u32x2*>((uint16_t*)a.o_lowp + to) = u32x2{pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3])};
-      else if (a.o_lowp) *reinterpret_cast<f32x4*>((float*)a.o_lowp + to) = o;
-      if (x == 0) a.lse[(int64_t)h * a.T + t] = sum != 0.f ? top * kScoreLn2 + logf(sum) + besides : -INFINITY;
+    float m = top;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
+    sum *= __builtin_amdgcn_exp2f(top - m);
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int k = k0; k < shares; k += kAtOnce * all) {
+      if (k > k0) load(k);
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u)
+        if (y < side && k + u * all < shares) o += z[u] * __builtin_amdgcn_exp2f(zm[u] - m);
     }
-    __syncthreads();
+    if constexpr (W > 1) {
+      fold[wave][lane] = o;
+      __syncthreads();
+      if (wave != 0) return;
+      for (int w = 1; w < W; ++w) o += fold[w][lane];
+    }
+    for (int u = 1; u < side; ++u) {                   // the states side by side
+      f32x4 other;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) other[e] = __shfl(o[e], lane + u * vecs);
+      if (y == 0) o += other;
+    }
+    if (y != 0) continue;
+    o *= sum != 0.f ? 1.f / sum : 0.f;
+    const int64_t to = row * D + 4 * x;
+    if (a.o) *reinterpret_cast<f32x4*>(a.o + to) = o;
+    if (a.o_lowp && bf16) *reinterpret_cast<u32x2*>((uint16_t*)a.o_lowp + to) = u32x2{pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3])};
+    else if (a.o_lowp) *reinterpret_cast<f32x4*>((float*)a.o_lowp + to) = o;
+    if (x == 0) a.lse[(int64_t)h * a.T + t] = sum != 0.f ? m * kScoreLn2 + logf(sum) + besides : -INFINITY;
   }
 }
 
@@ -575,13 +587,18 @@ hipError_t launch_cache_attn(const CacheAttnArgs& a, bool bf16, hipStream_t stre
   return hipGetLastError();
 }
 
-hipError_t launch_cache_combine(const CacheAttnArgs& a, bool bf16, hipStream_t stream) {
-  const int64_t rows = (int64_t)a.T * a.Hq, blocks = rows < 4096 ? rows : 4096;
+hipError_t launch_cache_combine(const CacheAttnArgs& a, bool bf16, bool many, hipStream_t stream) {
+  const int64_t rows = (int64_t)a.T * a.Hq;
   if (rows <= 0) return hipSuccess;
-  if (rows > 0x7fffffff * (int64_t)64) return hipErrorInvalidValue;
   ProfScope prof("cache_combine", stream);
-  const int each = (int)((rows + blocks - 1) / blocks);
-  hipLaunchKernelGGL(cache_combine_kernel, dim3((unsigned)((rows + each - 1) / each)), dim3(256), 0, stream, a, each, bf16 ? 1 : 0);
+  if (many) {
+    if (rows > kScoreGridMost) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(cache_combine_kernel<kManyWaves>, dim3((unsigned)rows), dim3(64 * kManyWaves), 0, stream, a, 1, bf16 ? 1 : 0);
+    return hipGetLastError();
+  }
+  const int64_t waves = rows < 16384 ? rows : 16384, each = (rows + waves - 1) / waves, blocks = (rows + 4 * each - 1) / (4 * each);
+  if (each > 0x7fffffff) return hipErrorInvalidValue;
+  hipLaunchKernelGGL(cache_combine_kernel<1>, dim3((unsigned)blocks), dim3(256), 0, stream, a, (int)each, bf16 ? 1 : 0);
   return hipGetLastError();
 }
 

@@ -7,6 +7,7 @@
 #pragma once
 
 #include "st_cache.h"
+#include "st_mfma.h"
 
 namespace st {
 
@@ -94,7 +95,13 @@ __device__ __forceinline__ CacheItem find_item(const CacheAttnArgs& a, SeqSpan& 
     all += wave_last(wave_scan((float)S * (float)L));
   }
   const int c = max((int)fminf(all * (float)a.c.Hkv / (float)a.plan.target * 1.0001f + 1.f, 1e9f), a.plan.least);
-  const int me = blockIdx.x;
+  // Sequences of few rows read every key once: the heads of one run of tokens, whose rows lie side by side, go to the workgroups of one XCD at
+  // about the same time.
+  int me = blockIdx.x;
+  if (ROWS == 16) {
+    const int x = me % kDispatchXcds, y = me / kDispatchXcds, z = y / a.c.Hkv;
+    me = (z * kDispatchXcds + x) * a.c.Hkv + y - z * a.c.Hkv;
+  }
   CacheItem t;
   t.b = -1;
   int items_before = 0, states_before = 0;
