@@ -94,7 +94,7 @@ st::CachePlan launch_plan(const st_cache_rows* r, const st_cache* c, int rows, i
   p.rows = rows;
   p.rows_from = from;
   p.rows_to = to;
-  p.least = kLeastBlocks;
+  p.least = r->dtype == ST_F32 ? kLeastBlocks / 2 : kLeastBlocks;
   p.target = rows == 16 ? kPlacesOfFew : kPlaces;
   const int64_t jobs = tiles * c->Hkv, most = std::max<int64_t>((blocks + p.least / 2) / p.least, 1);
   p.grid = std::min(p.target + jobs, jobs * most);

@@ -31,13 +31,12 @@ __device__ __forceinline__ void sincos_turns(double x, double& s, double& c) {
 }
 __device__ __forceinline__ void sincos_turns(double x, float& s, float& c) { sincospif((float)(2.0 * x), &s, &c); }
 
-// To fp32 so that a second rounding, to fewer bits, gives what one rounding of x would: towards zero, with a one in the last place where
-// anything was cut off.
+// To fp32 so that a second rounding, to fewer bits, gives what one rounding of x would: cut off behind 23 bits, with a one in the last of them
+// where anything was cut off.
 __device__ __forceinline__ float sticky(double x) {
-  const float f = (float)x;
-  if ((double)f == x || f != f) return f;
-  const uint32_t u = __float_as_uint(f) - (fabs((double)f) > fabs(x) ? 1u : 0u);
-  return __uint_as_float(u | 1u);
+  const uint64_t u = __double_as_longlong(x);
+  const uint32_t low = (uint32_t)u;
+  return (float)__longlong_as_double((u & 0xffffffff00000000ull) | (low & 0xe0000000u) | min(low & 0x1fffffffu, 1u) << 29);
 }
 __device__ __forceinline__ float sticky(float x) { return x; }
 
@@ -157,45 +156,7 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, const Piece& p,
       }
     }
   };
-  Vec<V> x[U], z[U];
-  float unit = 1.f;
-  if constexpr (E4M3) {
-    uint8_t* scale = (key ? a.c.k_scale : a.c.v_scale) + (int64_t)page * g.Hkv + h;
-    const int had = begun > 0 ? (int)*scale - 127 : -126;
-    float top = 0.f;
-    for (int row = group; row < n; row += groups) {
-      make(row, x, z);
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          if (at[u].live && is_finite(x[u].x[e])) top = fmaxf(top, fabsf(x[u].x[e]));
-          if (at[u].live && is_finite(z[u].x[e])) top = fmaxf(top, fabsf(z[u].x[e]));
-        }
-    }
-    for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
-    if ((tid & 63) == 0) shared[tid >> 6] = __float_as_int(top);
-    __syncthreads();
-    top = __int_as_float(max(max(shared[0], shared[1]), max(shared[2], shared[3])));
-    const int e = max(had, exponent_for(top));
-    unit = power_of_two(-e);
-    if (e > had && begun > 0) {
-      const int less = e - had;
-      const float by = less < 32 ? power_of_two(-less) : 0.f;
-      for (int row = group; row < begun; row += groups)
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          S* to_row = dst + (int64_t)row * to.ss;
-          load_pairs<V, NEXT>(to_row, at[u], x[u], z[u]);
-#pragma unroll
-          for (int y = 0; y < V; ++y) x[u].x[y] *= by, z[u].x[y] *= by;
-          if (at[u].live) store_pairs<V, NEXT>(to_row, at[u], x[u], z[u]);
-        }
-    }
-    if (tid == 0) *scale = (uint8_t)(e + 127);
-  }
-  for (int row = group; row < n; row += groups) {
-    make(row, x, z);
+  auto store_row = [&](int row, Vec<V> (&x)[U], Vec<V> (&z)[U], float unit) {
     S* to_row = dst + (int64_t)(begun + row) * to.ss;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -208,6 +169,69 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, const Piece& p,
       }
       if (at[u].live) store_pairs<V, NEXT>(to_row, at[u], x[u], z[u]);
     }
+  };
+  if constexpr (!E4M3) {
+    for (int row = group; row < n; row += groups) {
+      Vec<V> x[U], z[U];
+      make(row, x, z);
+      store_row(row, x, z, 1.f);
+    }
+  } else {
+    uint8_t* scale = (key ? a.c.k_scale : a.c.v_scale) + (int64_t)page * g.Hkv + h;
+    const int had = begun > 0 ? (int)*scale - 127 : -126;
+    float top = 0.f;
+    auto highest = [&](const Vec<V> (&x)[U], const Vec<V> (&z)[U]) {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          if (at[u].live && is_finite(x[u].x[e])) top = fmaxf(top, fabsf(x[u].x[e]));
+          if (at[u].live && is_finite(z[u].x[e])) top = fmaxf(top, fabsf(z[u].x[e]));
+        }
+    };
+    // The first rows of a lane stay in registers until the scale is known, the others are made again (pages of up to 64 tokens of 128: none)
+    constexpr int kHeld = 4;
+    Vec<V> x[kHeld][U], z[kHeld][U];
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k)
+      if (group + k * groups < n) {
+        make(group + k * groups, x[k], z[k]);
+        highest(x[k], z[k]);
+      }
+    for (int row = group + kHeld * groups; row < n; row += groups) {
+      Vec<V> y[U], w[U];
+      make(row, y, w);
+      highest(y, w);
+    }
+    for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+    if ((tid & 63) == 0) shared[tid >> 6] = __float_as_int(top);
+    __syncthreads();
+    top = __int_as_float(max(max(shared[0], shared[1]), max(shared[2], shared[3])));
+    const int e = max(had, exponent_for(top));
+    const float unit = power_of_two(-e);
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k)
+      if (group + k * groups < n) store_row(group + k * groups, x[k], z[k], unit);
+    for (int row = group + kHeld * groups; row < n; row += groups) {
+      Vec<V> y[U], w[U];
+      make(row, y, w);
+      store_row(row, y, w, unit);
+    }
+    if (e > had && begun > 0) {
+      const int less = e - had;
+      const float by = less < 32 ? power_of_two(-less) : 0.f;
+      for (int row = group; row < begun; row += groups)
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          S* to_row = dst + (int64_t)row * to.ss;
+          Vec<V> y, w;
+          load_pairs<V, NEXT>(to_row, at[u], y, w);
+#pragma unroll
+          for (int v = 0; v < V; ++v) y.x[v] *= by, w.x[v] *= by;
+          if (at[u].live) store_pairs<V, NEXT>(to_row, at[u], y, w);
+        }
+    }
+    if (tid == 0) *scale = (uint8_t)(e + 127);
   }
 }
 
@@ -223,7 +247,9 @@ __global__ __launch_bounds__(kThreads) void cache_append_kernel(const AppendArgs
   __syncthreads();
   const int y = blockIdx.y;
   if (y < 2 * g.Hkv) {
-    append_rows<T, typename std::conditional<E4M3, double, float>::type, S, V, U, NEXT>(a, p, y >> 1, (y & 1) == 0, lanes, shared);
+    // (four pairs a lane in fp64: with eight the registers leave two wavefronts a SIMD)
+    constexpr int VK = E4M3 && V == 8 ? 4 : V;
+    append_rows<T, typename std::conditional<E4M3, double, float>::type, S, VK, U, NEXT>(a, p, y >> 1, (y & 1) == 0, lanes * (V / VK), shared);
     return;
   }
   // queries: some heads of the piece's tokens, eight tokens at a time, whose angles serve all heads
