@@ -424,7 +424,8 @@ st_status st_cache_append(const st_rope_desc* desc, const st_cache* cache, const
                           const st_tensor* q_out, void* hip_stream);
 
 /* Tokens first[b] .. first[b] + count - 1 of every sequence (first: device int32 [B], NULL: 0) as chunks [B,count,Hkv,D], views in
- * `dtype` (that of the cache; of ST_E4M3 either other); tokens past a sequence's end are zeros.  k_out or v_out may be NULL. */
+ * `dtype` (that of the cache; of ST_E4M3 either other); tokens past a sequence's end are zeros.  k_out or v_out may be NULL.
+ * count <= 2^28, count Hkv D < 2^34. */
 st_status st_cache_read(const st_cache* cache, const int32_t* first, int32_t count, int32_t dtype, const st_tensor* k_out,
                         const st_tensor* v_out, void* hip_stream);
 

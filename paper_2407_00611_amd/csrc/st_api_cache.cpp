@@ -193,7 +193,7 @@ st_status st_cache_read(const st_cache* c, const int32_t* first, int32_t count, 
   if (count < 0) return fail(ST_ERR_INVALID_ARG, "negative size");
   if (reinterpret_cast<uintptr_t>(first) % 4) return fail(ST_ERR_ALIGNMENT, "first: not 4-byte aligned");
   const int64_t n = (int64_t)count * c->Hkv * c->D;
-  if (n / 2048 >= 1 << 23) return fail(ST_ERR_UNSUPPORTED, "2^34 values of a sequence or more");
+  if (count > 1 << 28 || n >= (int64_t)1 << 34) return fail(ST_ERR_UNSUPPORTED, "more than 2^28 tokens or 2^34 values of a sequence");
   if (n == 0 || c->B == 0) return ST_OK;
   if (k_out == nullptr && v_out == nullptr) return fail(ST_ERR_INVALID_ARG, "k_out and v_out: one of them is needed");
   st::ReadArgs a;

@@ -14,7 +14,6 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kMaxPairs = 128;
 constexpr int kTokensMost = 8;                       // tokens whose angles a workgroup holds for the queries
-constexpr int kQueryRows = 512;                      // rows (token, head) of queries for a workgroup, about
 
 // ---- arithmetic of the keys: fp32 as the queries', or fp64
 
@@ -29,7 +28,18 @@ __device__ __forceinline__ void sincos_turns(double x, double& s, double& c) {
   s = k & 2 ? -u : u;
   c = (k + 1) & 2 ? -v : v;
 }
-__device__ __forceinline__ void sincos_turns(double x, float& s, float& c) { sincospif((float)(2.0 * x), &s, &c); }
+// Sine and cosine of p f, f in 64ths of a turn: those of the nearest 64th from a table, and of the rest, at most pi / 64, from series whose next
+// terms are below 1e-12.  The product is rounded to a whole number by an addition to 1.5 2^52, whose last bits are that number's.
+constexpr int kParts = 64;
+__device__ __forceinline__ void sincos_part(double p, double f, const double2* table, double& s, double& c) {
+  constexpr double kWhole = 6755399441055744.0, t = 6.283185307179586477 / kParts;
+  const double w = fma(p, f, kWhole), r = fma(p, f, kWhole - w), z = r * r;
+  const double2 at = table[(uint32_t)__double_as_longlong(w) % kParts];
+  const double ps = r * (t + z * (-t * t * t / 6 + z * (t * t * t * t * t / 120)));
+  const double pc = 1.0 + z * (-t * t / 2 + z * (t * t * t * t / 24 - z * (t * t * t * t * t * t / 720)));
+  s = at.x * pc + at.y * ps;
+  c = at.y * pc - at.x * ps;
+}
 
 // To fp32 so that a second rounding, to fewer bits, gives what one rounding of x would: cut off behind 23 bits, with a one in the last of them
 // where anything was cut off.
@@ -56,8 +66,9 @@ __device__ __forceinline__ int exponent_for(float top) {
 }
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }   // -126 .. 127
 
-__device__ __forceinline__ double place_of_token(const RopeArgs& g, int64_t token, int t, int pair) {
-  if (!g.positions) return (double)token;
+// Position of packed row t for a pair: that of its token, `place`, or from a table
+__device__ __forceinline__ double position_of(const RopeArgs& g, double place, int t, int pair) {
+  if (!g.positions) return place;
   int axis = 0, end = 0;                             // (no index that is known at run time only: the list would be copied to memory)
 #pragma unroll
   for (int y = 0; y + 1 < ST_ROPE_MAX_AXES; ++y) {
@@ -100,7 +111,7 @@ __device__ __forceinline__ bool find_piece(const AppendArgs& a, Piece& p, int* f
 
 // T: of the rows; A: of the arithmetic of keys; S: what the pages hold
 template <typename T, typename A, typename S, int V, int U, bool NEXT>
-__device__ __forceinline__ void append_rows(const AppendArgs& a, const Piece& p, int h, bool key, int lanes, int* shared) {
+__device__ __forceinline__ void append_rows(const AppendArgs& a, const Piece& p, int h, bool key, int lanes, int* shared, double2* parts) {
   constexpr bool E4M3 = std::is_same<S, uint8_t>::value;
   const RopeArgs& g = a.g;
   const int tid = threadIdx.x, chunk = tid & (lanes - 1), group = tid / lanes, groups = kThreads / lanes, half = g.rot / 2;
@@ -118,8 +129,17 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, const Piece& p,
   for (int u = 0; u < U; ++u) {
     at[u] = place_of<V, NEXT>(g, chunk + u * lanes);
 #pragma unroll
-    for (int e = 0; e < V; ++e) f[u][e] = key && at[u].pair + e < half ? g.freq[at[u].pair + e] * kPerTurn : 0.0;
+    for (int e = 0; e < V; ++e) f[u][e] = key && at[u].pair + e < half ? g.freq[at[u].pair + e] * (kPerTurn * (E4M3 ? kParts : 1)) : 0.0;
   }
+  if (E4M3 && key) {
+    if (tid < kParts) {
+      double sn, cs;
+      sincos_turns(tid < kParts / 2 ? tid / (double)kParts : tid / (double)kParts - 1.0, sn, cs);
+      parts[tid] = make_double2(sn, cs);
+    }
+    __syncthreads();
+  }
+  const double place0 = (double)(g.offset + p.lo);
   auto make = [&](int row, Vec<V> (&x)[U], Vec<V> (&z)[U]) {   // of the rows as they are stored, before they are rounded
 #pragma unroll
     for (int u = 0; u < U; ++u) load_pairs<V, NEXT>(src + row * in.ss, at[u], x[u], z[u]);
@@ -145,8 +165,10 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, const Piece& p,
           w *= g.k_weight ? r * (A)wb.x[e] : r;
         }
         if (at[u].pair + e < half) {                   // (others as they are: zero times infinity is NaN)
+          const double place = position_of(g, place0 + (double)row, p.row0 + row, at[u].pair + e);
           A c, s;
-          sincos_turns(fraction(place_of_token(g, g.offset + p.lo + row, p.row0 + row, at[u].pair + e) * f[u][e]), s, c);
+          if constexpr (E4M3) sincos_part(place, f[u][e], parts, s, c);
+          else sincospif((float)(2.0 * fraction(place * f[u][e])), &s, &c);
           const A m = y * c - w * s;
           w = y * s + w * c;
           y = m;
@@ -235,11 +257,11 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, const Piece& p,
   }
 }
 
-// grid (pieces, 2 Hkv + groups of query heads)
+// grid (pieces, 2 Hkv + eights of a page's tokens): keys and values of a head, or all query heads of eight tokens
 template <typename T, typename S, int V, int U, bool NEXT>
-__global__ __launch_bounds__(kThreads) void cache_append_kernel(const AppendArgs a, int lanes, int q_heads) {
+__global__ __launch_bounds__(kThreads, (std::is_same<S, uint8_t>::value ? 4 : 1)) void cache_append_kernel(const AppendArgs a, int lanes) {
   constexpr bool E4M3 = std::is_same<S, uint8_t>::value;
-  __shared__ float2 angles[kTokensMost * kMaxPairs];
+  __shared__ __attribute__((aligned(16))) float2 angles[kTokensMost * kMaxPairs];
   __shared__ int shared[4];
   const RopeArgs& g = a.g;
   Piece p;
@@ -249,104 +271,121 @@ __global__ __launch_bounds__(kThreads) void cache_append_kernel(const AppendArgs
   if (y < 2 * g.Hkv) {
     // (four pairs a lane in fp64: with eight the registers leave two wavefronts a SIMD)
     constexpr int VK = E4M3 && V == 8 ? 4 : V;
-    append_rows<T, typename std::conditional<E4M3, double, float>::type, S, VK, U, NEXT>(a, p, y >> 1, (y & 1) == 0, lanes * (V / VK), shared);
+    append_rows<T, typename std::conditional<E4M3, double, float>::type, S, VK, U, NEXT>(a, p, y >> 1, (y & 1) == 0, lanes * (V / VK), shared, (double2*)angles);
     return;
   }
-  // queries: some heads of the piece's tokens, eight tokens at a time, whose angles serve all heads
-  const int h0 = (y - 2 * g.Hkv) * q_heads, heads = min(q_heads, g.Hq - h0), half = g.rot / 2;
+  const int t0 = (y - 2 * g.Hkv) * kTokensMost, n = min(kTokensMost, p.hi - p.lo - t0), half = g.rot / 2;
+  if (n <= 0) return;
   const int tid = threadIdx.x, chunk = tid & (lanes - 1), group = tid / lanes, groups = kThreads / lanes;
+  // row / heads = row inv_heads / 2^32 while rows x heads stay below 2^32: at most 16384 heads of eight tokens
+  const uint32_t heads = (uint32_t)g.Hq, rows = heads * (uint32_t)n, inv_heads = 0xffffffffu / heads + 1;
   Place<V, NEXT> at[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) at[u] = place_of<V, NEXT>(g, chunk + u * lanes);
-  for (int t0 = 0; t0 < p.hi - p.lo; t0 += kTokensMost) {
-    const int n = min(kTokensMost, p.hi - p.lo - t0);
-    if (t0 > 0) __syncthreads();
-    for (int x = tid; x < n * half; x += kThreads) {
-      const int t = x / half, j = x - t * half;
-      float2 w;
-      sincos_turns(fraction(place_of_token(g, g.offset + p.lo + t0 + t, p.row0 + t0 + t, j) * (g.freq[j] * kPerTurn)), w.y, w.x);
-      angles[x] = w;
+  Vec<V> x[U], z[U], wa[U], wb[U];
+  auto fetch = [&](uint32_t row) {
+    row = min(row, rows - 1);
+    const uint32_t t = heads > 1 ? __umulhi(row, inv_heads) : row;
+    const T* src = (const T*)g.q.ptr + (int64_t)(p.row0 + t0 + (int)t) * g.q.ss + (int64_t)(row - t * heads) * g.q.sh;
+#pragma unroll
+    for (int u = 0; u < U; ++u) load_pairs<V, NEXT>(src, at[u], x[u], z[u]);
+  };
+  fetch(group);
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+    if (g.q_weight) load_pairs<V, NEXT>(g.q_weight, at[u], wa[u], wb[u]);
+  const double place0 = (double)(g.offset + p.lo + t0);
+  for (int e = tid; e < n * half; e += kThreads) {
+    const int t = e / half, j = e - t * half;
+    float2 w;
+    sincospif((float)(2.0 * fraction(position_of(g, place0 + (double)t, p.row0 + t0 + t, j) * (g.freq[j] * kPerTurn))), &w.y, &w.x);
+    angles[e] = w;
+  }
+  __syncthreads();
+  for (uint32_t row = group; row < rows; row += groups) {
+    const uint32_t t = heads > 1 ? __umulhi(row, inv_heads) : row;
+    T* dst = (T*)const_cast<void*>(g.q_out.ptr) + (int64_t)(p.row0 + t0 + (int)t) * g.q_out.ss + (int64_t)(row - t * heads) * g.q_out.sh;
+    Vec<V> ya[U], yb[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) ya[u] = x[u], yb[u] = z[u];
+    if (row + groups < rows) fetch(row + groups);
+    float r = 1.f;
+    if (g.norm) {
+      float sum = 0.f;
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int e = 0; e < V; ++e) sum += at[u].live ? ya[u].x[e] * ya[u].x[e] + yb[u].x[e] * yb[u].x[e] : 0.f;
+      r = rsqrtf(row_sum(sum, lanes) / (float)g.D + g.eps);
     }
-    __syncthreads();
-    for (int row = group; row < n * heads; row += groups) {
-      const int t = row / heads, h = h0 + row - t * heads;
-      const int64_t i = p.row0 + t0 + t;
-      const T* src = (const T*)g.q.ptr + i * g.q.ss + h * g.q.sh;
-      T* dst = (T*)const_cast<void*>(g.q_out.ptr) + i * g.q_out.ss + h * g.q_out.sh;
-      Vec<V> x[U], z[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) load_pairs<V, NEXT>(src, at[u], x[u], z[u]);
-      float r = 1.f;
-      if (g.norm) {
-        float sum = 0.f;
+    for (int u = 0; u < U; ++u) {
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-          for (int e = 0; e < V; ++e) sum += at[u].live ? x[u].x[e] * x[u].x[e] + z[u].x[e] * z[u].x[e] : 0.f;
-        r = rsqrtf(row_sum(sum, lanes) / (float)g.D + g.eps);
+      for (int e = 0; e < V; ++e) {
+        const bool turned = at[u].pair + e < half;
+        const float2 w = turned ? angles[t * half + at[u].pair + e] : make_float2(1.f, 0.f);
+        const float m = g.norm ? ya[u].x[e] * (g.q_weight ? r * wa[u].x[e] : r) : ya[u].x[e];
+        const float o = g.norm ? yb[u].x[e] * (g.q_weight ? r * wb[u].x[e] : r) : yb[u].x[e];
+        ya[u].x[e] = turned ? m * w.x - o * w.y : m;   // (others as they are: zero times infinity is NaN)
+        yb[u].x[e] = turned ? m * w.y + o * w.x : o;
       }
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        Vec<V> wa, wb, ya, yb;
-        if (g.q_weight) load_pairs<V, NEXT>(g.q_weight, at[u], wa, wb);
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          const bool turned = at[u].pair + e < half;
-          const float2 w = turned ? angles[t * half + at[u].pair + e] : make_float2(1.f, 0.f);
-          const float m = g.norm ? x[u].x[e] * (g.q_weight ? r * wa.x[e] : r) : x[u].x[e];
-          const float o = g.norm ? z[u].x[e] * (g.q_weight ? r * wb.x[e] : r) : z[u].x[e];
-          ya.x[e] = turned ? m * w.x - o * w.y : m;
-          yb.x[e] = turned ? m * w.y + o * w.x : o;
-        }
-        if (at[u].live) store_pairs<V, NEXT>(dst, at[u], ya, yb);
-      }
+      if (at[u].live) store_pairs<V, NEXT>(dst, at[u], ya[u], yb[u]);
     }
   }
 }
 
 // ---- chunks
 
-// V neighbouring values of a row a thread; grid (., B, 2: keys and values)
-template <typename S, typename T, int V>
-__global__ __launch_bounds__(kThreads) void cache_read_kernel(const ReadArgs a) {
+// Bound by memory.  A workgroup takes `tokens` neighbouring tokens of a sequence, whose pages it looks up first, and a thread 16 bytes of the
+// chunk at a time, four of them under way; grid (., B, 2: keys and values).  vecs: such pieces of a row, inv: 2^32 / pieces of a token and of a row.
+constexpr int kReadTokens = 64, kReadAtOnce = 4;
+template <typename S, typename T>
+__global__ __launch_bounds__(kThreads) void cache_read_kernel(const ReadArgs a, int tokens, uint32_t vecs, uint32_t inv_token, uint32_t inv_row) {
+  constexpr int V = 16 / (int)sizeof(T);
+  __shared__ int pages[kReadTokens];
   const CacheArgs& c = a.c;
   const View& out = blockIdx.z ? a.v_out : a.k_out;
   if (!out.ptr) return;
   const View& in = blockIdx.z ? c.v : c.k;
-  const int b = blockIdx.y, len = seq_len(c, b), per = c.D / V, heads = c.Hkv;
-  const int64_t first = a.first ? a.first[b] : 0, x = (int64_t)blockIdx.x * kThreads + threadIdx.x, row = x / per;
-  const int d = (int)(x - row * per) * V;
-  const int64_t i = row / heads;
-  const int h = (int)(row - i * heads);
-  if (i >= a.count) return;
-  const int64_t token = first + i;
-  const int page = token >= 0 && token < len ? page_of(c, b, (int)(token >> c.shift)) : -1;
-  float y[V];
-#pragma unroll
-  for (int e = 0; e < V; ++e) y[e] = 0.f;
-  if (page >= 0) {
-    const S* src = (const S*)in.ptr + (int64_t)page * in.sb + (token & ((1 << c.shift) - 1)) * in.ss + (int64_t)h * in.sh + d;
-    if constexpr (std::is_same<S, uint8_t>::value) {
-      const u32x4 w = *reinterpret_cast<const u32x4*>(src);
-      const float s = scale_value((blockIdx.z ? c.v_scale : c.k_scale)[(int64_t)page * heads + h]);
-#pragma unroll
-      for (int e = 0; e < V; e += 4) {
-        const float2 p = e4m3_pair<false>(w[e / 4]), q = e4m3_pair<true>(w[e / 4]);
-        y[e] = p.x * s; y[e + 1] = p.y * s; y[e + 2] = q.x * s; y[e + 3] = q.y * s;
-      }
-    } else {
-      const Vec<V> w = load<V>(src);
-#pragma unroll
-      for (int e = 0; e < V; ++e) y[e] = w.x[e];
-    }
+  const uint8_t* scales = blockIdx.z ? c.v_scale : c.k_scale;
+  const int b = blockIdx.y, tid = threadIdx.x, i0 = blockIdx.x * tokens, n = min(tokens, a.count - i0), mask = (1 << c.shift) - 1;
+  const int64_t first = (a.first ? a.first[b] : 0) + (int64_t)i0;
+  if (tid < n) {
+    const int64_t token = first + tid;
+    pages[tid] = token >= 0 && token < seq_len(c, b) ? page_of(c, b, (int)(token >> c.shift)) : -1;
   }
-  T* dst = (T*)const_cast<void*>(out.ptr) + b * out.sb + i * out.ss + h * out.sh + d;
+  __syncthreads();
+  const uint32_t token_vecs = vecs * (uint32_t)c.Hkv, all = token_vecs * (uint32_t)n;
+  T* dst = (T*)const_cast<void*>(out.ptr) + b * out.sb;
+  for (uint32_t x0 = tid; x0 < all; x0 += kThreads * kReadAtOnce) {
+    Vec<V> y[kReadAtOnce];
+    float unit[kReadAtOnce];
+    int page[kReadAtOnce], i[kReadAtOnce], h[kReadAtOnce], d[kReadAtOnce];
 #pragma unroll
-  for (int e = 0; e < V; e += 8) {
-    Vec<8> w;
+    for (int u = 0; u < kReadAtOnce; ++u) {
+      const uint32_t x = min(x0 + u * kThreads, all - 1), t = tokens == 1 ? 0 : token_vecs > 1 ? __umulhi(x, inv_token) : x, w = x - t * token_vecs;
+      const uint32_t z = vecs > 1 ? __umulhi(w, inv_row) : w;
+      i[u] = (int)t;
+      h[u] = (int)z;
+      d[u] = (int)(w - z * vecs) * V;
+      page[u] = pages[t];
+      unit[u] = 0.f;
 #pragma unroll
-    for (int u = 0; u < 8; ++u) w.x[u] = y[e + u];
-    store<8>(dst + e, w);
+      for (int e = 0; e < V; ++e) y[u].x[e] = 0.f;
+      if (page[u] >= 0) {
+        y[u] = load<V>((const S*)in.ptr + (int64_t)page[u] * in.sb + (int64_t)((int)(first + i[u]) & mask) * in.ss + (int64_t)h[u] * in.sh + d[u]);
+        if constexpr (std::is_same<S, uint8_t>::value) unit[u] = scale_value(scales[(int64_t)page[u] * c.Hkv + h[u]]);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kReadAtOnce; ++u) {
+      if (x0 + u * kThreads >= all) break;
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        if constexpr (std::is_same<S, uint8_t>::value) y[u].x[e] *= unit[u];
+      }
+      store<V>(dst + (int64_t)(i0 + i[u]) * out.ss + (int64_t)h[u] * out.sh + d[u], y[u]);
+    }
   }
 }
 
@@ -356,7 +395,7 @@ hipError_t launch_cache_append(const AppendArgs& a, bool bf16, hipStream_t strea
   const RopeArgs& g = a.g;
   if (g.S <= 0 || a.c.B <= 0) return hipSuccess;
   const int64_t pieces = ((int64_t)g.S >> a.c.shift) + 2 * (int64_t)a.c.B;
-  const int q_heads = std::max(1, kQueryRows >> a.c.shift), y = 2 * g.Hkv + (g.Hq + q_heads - 1) / q_heads;
+  const int y = 2 * g.Hkv + (g.Hq > 0 ? (1 << a.c.shift) / kTokensMost : 0);
   if (pieces > (1 << 23) || y > 65535) return hipErrorInvalidValue;
   const dim3 grid((unsigned)pieces, (unsigned)y), block(kThreads);
   ProfScope prof("cache_append", stream);
@@ -364,7 +403,7 @@ hipError_t launch_cache_append(const AppendArgs& a, bool bf16, hipStream_t strea
     constexpr int V = decltype(v)::value, U = decltype(u)::value;
     constexpr bool NEXT = decltype(next)::value;
     const int lanes = lanes_of(g.D, V);
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, a, lanes, q_heads); };
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, a, lanes); };
     if (a.c.dtype == ST_E4M3) bf16 ? go(cache_append_kernel<uint16_t, uint8_t, V, U, NEXT>) : go(cache_append_kernel<float, uint8_t, V, U, NEXT>);
     else bf16 ? go(cache_append_kernel<uint16_t, uint16_t, V, U, NEXT>) : go(cache_append_kernel<float, float, V, U, NEXT>);
   });
@@ -373,14 +412,19 @@ hipError_t launch_cache_append(const AppendArgs& a, bool bf16, hipStream_t strea
 
 hipError_t launch_cache_read(const ReadArgs& a, int out_dtype, hipStream_t stream) {
   if (a.count <= 0 || a.c.B <= 0) return hipSuccess;
-  const int V = a.c.dtype == ST_E4M3 ? 16 : 8;
-  const int64_t threads = (int64_t)a.count * a.c.Hkv * (a.c.D / V), blocks = (threads + kThreads - 1) / kThreads;
+  const uint32_t vecs = (uint32_t)(a.c.D / (out_dtype == ST_BF16 ? 8 : 4)), token_vecs = vecs * (uint32_t)a.c.Hkv;
+  // eight rounds of a workgroup; fewer where that leaves the chip less than four workgroups a compute unit
+  const int64_t full = std::max<int64_t>(2 * (int64_t)a.count * a.c.B / 1024, 1);
+  const int tokens = (int)std::min<int64_t>(std::min<int64_t>(std::max<int64_t>(2048 / token_vecs, 1), kReadTokens), full);
+  const int64_t blocks = ((int64_t)a.count + tokens - 1) / tokens;
   if (blocks > (1 << 23)) return hipErrorInvalidValue;
+  // x / y = x inv / 2^32 while x y stays below 2^32: the 2048 pieces of several tokens, or those of one token of 16384 heads by those of a row
+  const uint32_t inv_token = 0xffffffffu / token_vecs + 1, inv_row = 0xffffffffu / vecs + 1;
   const dim3 grid((unsigned)blocks, (unsigned)a.c.B, 2), block(kThreads);
   ProfScope prof("cache_read", stream);
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, a); };
-  if (a.c.dtype == ST_E4M3) out_dtype == ST_BF16 ? go(cache_read_kernel<uint8_t, uint16_t, 16>) : go(cache_read_kernel<uint8_t, float, 16>);
-  else out_dtype == ST_BF16 ? go(cache_read_kernel<uint16_t, uint16_t, 8>) : go(cache_read_kernel<float, float, 8>);
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, a, tokens, vecs, inv_token, inv_row); };
+  if (a.c.dtype == ST_E4M3) out_dtype == ST_BF16 ? go(cache_read_kernel<uint8_t, uint16_t>) : go(cache_read_kernel<uint8_t, float>);
+  else out_dtype == ST_BF16 ? go(cache_read_kernel<uint16_t, uint16_t>) : go(cache_read_kernel<float, float>);
   return hipGetLastError();
 }
 
