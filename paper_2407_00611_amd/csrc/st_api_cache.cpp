@@ -16,8 +16,6 @@ namespace {
 // tiles of 16 rows wait for memory, and more of them than the chip holds at once even out what the lengths leave (64 ragged sequences 124 us,
 // 140 with 1024); for tiles of 32 rows, which are work, each share has 32 rows of O to join.
 constexpr int kLeastBlocks = 8, kPlacesOfFew = 2048, kPlaces = 512;
-// Rows up to which sixteen wavefronts join the states of each, where they may be sixteen and more
-constexpr int kManyRows = 512;
 // Batches whose sequences all have at most so many rows have one launch for them
 constexpr int kFewRows = 64;
 
@@ -109,7 +107,7 @@ struct Plans {
   int n;
   st::CachePlan p[2];
   int64_t rows;              // of all states
-  bool many;                 // states of a row
+  int states;                // of a row, on the average
 };
 Plans plans_of(const st_cache_rows* r, const st_cache* c) {
   constexpr int kAll = 0x7fffffff;
@@ -127,7 +125,7 @@ Plans plans_of(const st_cache_rows* r, const st_cache* c) {
     y.p[1] = launch_plan(r, c, 16, 0, 16, (int64_t)y.p[0].states * large);
   }
   for (int x = 0; x < y.n; ++x) y.rows += (int64_t)y.p[x].states * y.p[x].rows;
-  y.many = y.n == 1 && (int64_t)r->T * r->Hq <= kManyRows && y.p[0].states >= 16 * y.p[0].jobs;
+  y.states = y.n == 1 ? (int)(y.p[0].states / y.p[0].jobs) : 1;
   return y;
 }
 struct Room {
@@ -257,7 +255,7 @@ st_status st_attn_cache(const st_cache_rows* r, const st_cache* c, const int32_t
     ST_HIP(a.plan.rows == st::kPromptRows ? st::launch_cache_prompt(a, (hipStream_t)hip_stream) : st::launch_cache_attn(a, r->dtype == ST_BF16, (hipStream_t)hip_stream),
            "st_attn_cache launch");
   }
-  if (plans.rows > 0) ST_HIP(st::launch_cache_combine(a, r->dtype == ST_BF16, plans.many, (hipStream_t)hip_stream), "st_attn_cache combine");
+  if (plans.rows > 0) ST_HIP(st::launch_cache_combine(a, r->dtype == ST_BF16, plans.states, (hipStream_t)hip_stream), "st_attn_cache combine");
   return ST_OK;
 }
 

@@ -69,8 +69,8 @@ hipError_t launch_cache_append(const AppendArgs& a, bool bf16, hipStream_t strea
 hipError_t launch_cache_read(const ReadArgs& a, int out_dtype, hipStream_t stream);
 hipError_t launch_cache_attn(const CacheAttnArgs& a, bool bf16, hipStream_t stream);
 hipError_t launch_cache_prompt(const CacheAttnArgs& a, hipStream_t stream);
-// many: there may be 16 states of a row and more, and rows are few
-hipError_t launch_cache_combine(const CacheAttnArgs& a, bool bf16, bool many, hipStream_t stream);
+// states: so many a row, on the average of what there is room for
+hipError_t launch_cache_combine(const CacheAttnArgs& a, bool bf16, int states, hipStream_t stream);
 
 // ---- device side
 

@@ -17,7 +17,7 @@ namespace st {
 namespace {
 
 constexpr int kKeys = kCacheKeys;
-constexpr int kManyWaves = 16;                       // of a row whose states are many
+constexpr int kManyWaves = 16, kManyRows = 512;      // wavefronts of a row whose states are many; up to so many rows
 constexpr float kUnset = -1e30f;                     // reference of a row that has met no key: whatever comes exceeds it
 constexpr float kSumMost = 4096.f;                   // a lane's sum over its keys of a block beyond which a row's reference moves
 
@@ -487,84 +487,150 @@ __global__ __launch_bounds__(256, (stream_waves<T, S, ROWS, DP>())) void cache_s
   }
 }
 
-// Joins the states of rows whose walk was split: W wavefronts a row, each with a part of the states, 64 D / 4 lanes' worth of them side by
-// side.  A wavefront of its own for each row (W = 1) where shares are few, of which a wavefront goes through `each` rows one behind the
-// other; rows that are whole cost a look.
+// ---- joining the states of rows whose walk was split
+
+// Where the states of a row are: n of them (1: the row is whole), step rows apart
+struct RowStates {
+  int n;
+  int64_t first, step;
+};
+__device__ __forceinline__ RowStates states_of(const CacheAttnArgs& a, int64_t row, int first, int end) {
+  const int t = (int)(row / a.Hq), h = (int)(row - (int64_t)t * a.Hq), G = a.Hq / a.c.Hkv;
+  RowStates y{1, 0, 0};
+  if (t < first || t >= end) return y;
+  const int4 at = a.info[t];
+  const int shares = at.y & 0xffff, tile_rows = at.y >> 16;
+  if (shares <= 1 || tile_rows <= 0) return y;
+  const int hk = h / G, R = at.w * G + h - hk * G, tile = R / tile_rows;
+  y.first = at.x + ((int64_t)(at.z - 1 - tile) * a.c.Hkv + hk) * tile_rows + (R - tile * tile_rows);
+  y.step = (int64_t)at.z * a.c.Hkv * tile_rows;
+  // (where starts are no starts, a token may not have been told of: nothing is read outside the states)
+  if (at.x >= 0 && at.w >= 0 && at.z > tile && y.first + (shares - 1) * y.step < a.state_rows) y.n = shares;
+  return y;
+}
+__device__ __forceinline__ void store_joined(const CacheAttnArgs& a, int64_t row, int x, f32x4 o, float m, float sum, float besides, int bf16) {
+  o *= sum != 0.f ? 1.f / sum : 0.f;
+  const int64_t to = row * a.c.D + 4 * x, t = row / a.Hq;
+  if (a.o) *reinterpret_cast<f32x4*>(a.o + to) = o;
+  if (a.o_lowp && bf16) *reinterpret_cast<u32x2*>((uint16_t*)a.o_lowp + to) = u32x2{pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3])};
+  else if (a.o_lowp) *reinterpret_cast<f32x4*>((float*)a.o_lowp + to) = o;
+  if (x == 0) a.lse[(row - t * a.Hq) * a.T + t] = sum != 0.f ? m * kScoreLn2 + logf(sum) + besides : -INFINITY;
+}
+
+// W wavefronts a row, each with a part of its states, 64 D / 4 lanes' worth of them side by side
 template <int W>
-__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void cache_combine_kernel(const CacheAttnArgs a, int each, int bf16) {
+__device__ __forceinline__ void join_row(const CacheAttnArgs& a, int64_t row, const RowStates& s, f32x4 (*fold)[64], int bf16) {
   constexpr int kAtOnce = 4;
-  __shared__ f32x4 fold[W == 1 ? 1 : W][64];
-  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), D = a.c.D, G = a.Hq / a.c.Hkv, vecs = D / 4, side = 64 / vecs, x = lane % vecs, y = lane / vecs;
+  const int lane = threadIdx.x & 63, wave = W == 1 ? 0 : uniform(threadIdx.x >> 6), D = a.c.D, vecs = D / 4, side = 64 / vecs, x = lane % vecs, y = lane / vecs;
+  const int all = W * side, k0 = wave * side + y;      // this lane's states: k0, k0 + all, ...
+  f32x4 z[kAtOnce];
+  float zm[kAtOnce];
+  auto load = [&](int k) {
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) {
+      const int64_t from = s.first + min(k + u * all, s.n - 1) * s.step;
+      z[u] = *reinterpret_cast<const f32x4*>(a.part_o + from * D + 4 * x);
+      zm[u] = a.part_row[from].x;
+    }
+  };
+  load(k0);
+  // reference and sum of the whole row
+  float top = kUnset, sum = 0.f, besides = 0.f;
+  for (int k = lane; k - lane < s.n; k += 64) {
+    float4 st = make_float4(kUnset, 0.f, 0.f, 0.f);
+    if (k < s.n) st = a.part_row[s.first + k * s.step];
+    if (k == 0) besides = st.z;
+    const float m = fmaxf(top, st.x);
+    sum = sum * __builtin_amdgcn_exp2f(top - m) + st.y * __builtin_amdgcn_exp2f(st.x - m);
+    top = m;
+  }
+  float m = top;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
+  sum *= __builtin_amdgcn_exp2f(top - m);
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int k = k0; k < s.n; k += kAtOnce * all) {
+    if (k > k0) load(k);
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u)
+      if (y < side && k + u * all < s.n) o += z[u] * __builtin_amdgcn_exp2f(zm[u] - m);
+  }
+  if constexpr (W > 1) {
+    fold[wave][lane] = o;
+    __syncthreads();
+    if (wave != 0) return;
+    for (int w = 1; w < W; ++w) o += fold[w][lane];
+  }
+  for (int u = 1; u < side; ++u) {                     // the states side by side
+    f32x4 other;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) other[e] = __shfl(o[e], lane + u * vecs);
+    if (y == 0) o += other;
+  }
+  if (y == 0) store_joined(a, row, x, o, m, sum, besides, bf16);
+}
+
+// Many states of few rows: a workgroup a row
+__global__ __launch_bounds__(64 * kManyWaves) void cache_combine_many_kernel(const CacheAttnArgs a, int bf16) {
+  __shared__ f32x4 fold[kManyWaves][64];
   const int first = max(min(a.starts[0], a.T), 0), end = max(min(a.starts[a.c.B], a.T), 0);
-  const int64_t rows = (int64_t)a.T * a.Hq, row0 = W == 1 ? ((int64_t)blockIdx.x * 4 + wave) * each : (int64_t)blockIdx.x;
-  for (int64_t row = row0; row < min(row0 + (W == 1 ? each : 1), rows); ++row) {
-    const int t = (int)(row / a.Hq), h = (int)(row - (int64_t)t * a.Hq);
-    if (t < first || t >= end) continue;
-    const int4 at = a.info[t];
-    const int shares = at.y & 0xffff, tile_rows = at.y >> 16;
-    if (shares <= 1) {
-      row += a.Hq - 1 - h;                             // nor are the token's other heads split
+  const RowStates s = states_of(a, blockIdx.x, first, end);
+  if (s.n > 1) join_row<kManyWaves>(a, blockIdx.x, s, fold, bf16);
+}
+// Few states of many rows: 64 D / 4 lanes' worth of rows side by side (per: so many, or one where the states may be more), each lane through its
+// row's states, four under way; `rounds` times a wavefront.  Rows with more than kFewStates have the wavefront to themselves, rows that
+// are whole cost a look.
+constexpr int kFewStates = 8;
+__global__ __launch_bounds__(256) void cache_combine_kernel(const CacheAttnArgs a, int rounds, int per, int bf16) {
+  const int lane = threadIdx.x & 63, D = a.c.D, vecs = D / 4, x = lane % vecs, y = lane / vecs;
+  const int first = max(min(a.starts[0], a.T), 0), end = max(min(a.starts[a.c.B], a.T), 0);
+  const int64_t rows = (int64_t)a.T * a.Hq, base = ((int64_t)blockIdx.x * 4 + uniform(threadIdx.x >> 6)) * rounds * per;
+  for (int round = 0; round < rounds; ++round) {
+    const int64_t row0 = base + round * per, row = row0 + y;
+    if (row0 >= rows) break;
+    RowStates s{1, 0, 0};
+    if (y < per && row < rows) s = states_of(a, row, first, end);
+    if (!__any(s.n > 1)) continue;
+    if (per == 1 || __any(s.n > kFewStates)) {
+      for (int u = 0; u < per && row0 + u < rows; ++u) {
+        const RowStates z = states_of(a, row0 + u, first, end);
+        if (z.n > 1) join_row<1>(a, row0 + u, z, nullptr, bf16);
+      }
       continue;
     }
-    const int hk = h / G, R = at.w * G + h - hk * G, tile = tile_rows > 0 ? R / tile_rows : 0;
-    // (where starts are no starts, a token may not have been told of: nothing is read outside the states)
-    const int64_t s0 = at.x + ((int64_t)(at.z - 1 - tile) * a.c.Hkv + hk) * tile_rows + (R - tile * tile_rows), step = (int64_t)at.z * a.c.Hkv * tile_rows;
-    if (tile_rows <= 0 || at.x < 0 || at.w < 0 || at.z <= tile || s0 + (shares - 1) * step >= a.state_rows) continue;
-    const int mine = wave * side + y, all = (W == 1 ? 1 : W) * side;   // this lane's states: mine, mine + all, ...
-    const int k0 = W == 1 ? y : mine;
-    f32x4 z[kAtOnce];
-    float zm[kAtOnce];
-    auto load = [&](int k) {
-#pragma unroll
-      for (int u = 0; u < kAtOnce; ++u) {
-        const int64_t from = s0 + min(k + u * all, shares - 1) * step;
-        z[u] = *reinterpret_cast<const f32x4*>(a.part_o + from * D + 4 * x);
-        zm[u] = a.part_row[from].x;
-      }
-    };
-    load(k0);
-    // reference and sum of the whole row
-    float top = kUnset, sum = 0.f, besides = 0.f;
-    for (int k = lane; k - lane < shares; k += 64) {
-      float4 st = make_float4(kUnset, 0.f, 0.f, 0.f);
-      if (k < shares) st = a.part_row[s0 + k * step];
-      if (k == 0) besides = st.z;
-      const float m = fmaxf(top, st.x);
-      sum = sum * __builtin_amdgcn_exp2f(top - m) + st.y * __builtin_amdgcn_exp2f(st.x - m);
-      top = m;
-    }
-    float m = top;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
-    sum *= __builtin_amdgcn_exp2f(top - m);
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+    if (s.n <= 1) continue;
+    float m = kUnset, sum = 0.f, besides = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int k = k0; k < shares; k += kAtOnce * all) {
-      if (k > k0) load(k);
+    for (int k = 0; k < s.n; k += 4) {
+      f32x4 z[4];
+      float4 st[4];
 #pragma unroll
-      for (int u = 0; u < kAtOnce; ++u)
-        if (y < side && k + u * all < shares) o += z[u] * __builtin_amdgcn_exp2f(zm[u] - m);
-    }
-    if constexpr (W > 1) {
-      fold[wave][lane] = o;
-      __syncthreads();
-      if (wave != 0) return;
-      for (int w = 1; w < W; ++w) o += fold[w][lane];
-    }
-    for (int u = 1; u < side; ++u) {                   // the states side by side
-      f32x4 other;
+      for (int u = 0; u < 4; ++u) {
+        const int64_t from = s.first + min(k + u, s.n - 1) * s.step;
+        if (u == 0 || k + u < s.n) {
+          z[u] = *reinterpret_cast<const f32x4*>(a.part_o + from * D + 4 * x);
+          st[u] = a.part_row[from];
+        } else {
+          z[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+          st[u] = make_float4(kUnset, 0.f, 0.f, 0.f);
+        }
+      }
+      const float top = fmaxf(fmaxf(fmaxf(st[0].x, st[1].x), fmaxf(st[2].x, st[3].x)), m), old = __builtin_amdgcn_exp2f(m - top);
+      o *= old;
+      sum *= old;
+      m = top;
+      besides = st[0].z;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) other[e] = __shfl(o[e], lane + u * vecs);
-      if (y == 0) o += other;
+      for (int u = 0; u < 4; ++u) {
+        if (u > 0 && k + u >= s.n) break;
+        const float w = __builtin_amdgcn_exp2f(st[u].x - m);
+        o += z[u] * w;
+        sum += st[u].y * w;
+      }
     }
-    if (y != 0) continue;
-    o *= sum != 0.f ? 1.f / sum : 0.f;
-    const int64_t to = row * D + 4 * x;
-    if (a.o) *reinterpret_cast<f32x4*>(a.o + to) = o;
-    if (a.o_lowp && bf16) *reinterpret_cast<u32x2*>((uint16_t*)a.o_lowp + to) = u32x2{pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3])};
-    else if (a.o_lowp) *reinterpret_cast<f32x4*>((float*)a.o_lowp + to) = o;
-    if (x == 0) a.lse[(int64_t)h * a.T + t] = sum != 0.f ? m * kScoreLn2 + logf(sum) + besides : -INFINITY;
+    store_joined(a, row, x, o, m, sum, besides, bf16);
   }
 }
 
@@ -587,18 +653,17 @@ hipError_t launch_cache_attn(const CacheAttnArgs& a, bool bf16, hipStream_t stre
   return hipGetLastError();
 }
 
-hipError_t launch_cache_combine(const CacheAttnArgs& a, bool bf16, bool many, hipStream_t stream) {
+hipError_t launch_cache_combine(const CacheAttnArgs& a, bool bf16, int states, hipStream_t stream) {
   const int64_t rows = (int64_t)a.T * a.Hq;
   if (rows <= 0) return hipSuccess;
   ProfScope prof("cache_combine", stream);
-  if (many) {
-    if (rows > kScoreGridMost) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(cache_combine_kernel<kManyWaves>, dim3((unsigned)rows), dim3(64 * kManyWaves), 0, stream, a, 1, bf16 ? 1 : 0);
+  if (states >= 16 && rows <= kManyRows) {
+    hipLaunchKernelGGL(cache_combine_many_kernel, dim3((unsigned)rows), dim3(64 * kManyWaves), 0, stream, a, bf16 ? 1 : 0);
     return hipGetLastError();
   }
-  const int64_t waves = rows < 16384 ? rows : 16384, each = (rows + waves - 1) / waves, blocks = (rows + 4 * each - 1) / (4 * each);
-  if (each > 0x7fffffff) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(cache_combine_kernel<1>, dim3((unsigned)blocks), dim3(256), 0, stream, a, (int)each, bf16 ? 1 : 0);
+  const int64_t per = states >= 4 ? 1 : 64 / (a.c.D / 4), groups = (rows + per - 1) / per, rounds = (groups + 16383) / 16384, blocks = (groups + 4 * rounds - 1) / (4 * rounds);
+  if (rounds > 0x7fffffff) return hipErrorInvalidValue;
+  hipLaunchKernelGGL(cache_combine_kernel, dim3((unsigned)blocks), dim3(256), 0, stream, a, (int)rounds, (int)per, bf16 ? 1 : 0);
   return hipGetLastError();
 }
 
