@@ -517,120 +517,89 @@ __device__ __forceinline__ void store_joined(const CacheAttnArgs& a, int64_t row
   if (x == 0) a.lse[(row - t * a.Hq) * a.T + t] = sum != 0.f ? m * kScoreLn2 + logf(sum) + besides : -INFINITY;
 }
 
-// W wavefronts a row, each with a part of its states, 64 D / 4 lanes' worth of them side by side
-template <int W>
-__device__ __forceinline__ void join_row(const CacheAttnArgs& a, int64_t row, const RowStates& s, f32x4 (*fold)[64], int bf16) {
-  constexpr int kAtOnce = 4;
-  const int lane = threadIdx.x & 63, wave = W == 1 ? 0 : uniform(threadIdx.x >> 6), D = a.c.D, vecs = D / 4, side = 64 / vecs, x = lane % vecs, y = lane / vecs;
-  const int all = W * side, k0 = wave * side + y;      // this lane's states: k0, k0 + all, ...
-  f32x4 z[kAtOnce];
-  float zm[kAtOnce];
-  auto load = [&](int k) {
+// O, not divided by its row sum yet, against the reference m
+struct Joined {
+  float m, sum, besides;
+  f32x4 o;
+};
+__device__ __forceinline__ Joined join(const Joined& a, const Joined& b) {
+  const float m = fmaxf(a.m, b.m), p = __builtin_amdgcn_exp2f(a.m - m), q = __builtin_amdgcn_exp2f(b.m - m);
+  return Joined{m, a.sum * p + b.sum * q, a.besides, a.o * p + b.o * q};
+}
+// states k0, k0 + all, ... of a row, N of them under way
+template <int N>
+__device__ __forceinline__ Joined join_states(const CacheAttnArgs& a, const RowStates& s, int k0, int all, int x) {
+  Joined y{kUnset, 0.f, 0.f, f32x4{0.f, 0.f, 0.f, 0.f}};
+  for (int k = k0; k < s.n; k += N * all) {
+    f32x4 z[N];
+    float4 st[N];
 #pragma unroll
-    for (int u = 0; u < kAtOnce; ++u) {
-      const int64_t from = s.first + min(k + u * all, s.n - 1) * s.step;
-      z[u] = *reinterpret_cast<const f32x4*>(a.part_o + from * D + 4 * x);
-      zm[u] = a.part_row[from].x;
+    for (int u = 0; u < N; ++u) {
+      const int64_t from = s.first + (k + u * all) * s.step;
+      z[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+      st[u] = make_float4(kUnset, 0.f, 0.f, 0.f);
+      if (k + u * all < s.n) {
+        z[u] = *reinterpret_cast<const f32x4*>(a.part_o + from * a.c.D + 4 * x);
+        st[u] = a.part_row[from];
+      }
     }
-  };
-  load(k0);
-  // reference and sum of the whole row
-  float top = kUnset, sum = 0.f, besides = 0.f;
-  for (int k = lane; k - lane < s.n; k += 64) {
-    float4 st = make_float4(kUnset, 0.f, 0.f, 0.f);
-    if (k < s.n) st = a.part_row[s.first + k * s.step];
-    if (k == 0) besides = st.z;
-    const float m = fmaxf(top, st.x);
-    sum = sum * __builtin_amdgcn_exp2f(top - m) + st.y * __builtin_amdgcn_exp2f(st.x - m);
-    top = m;
-  }
-  float m = top;
+    float top = y.m;
 #pragma unroll
-  for (int d = 1; d < 64; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
-  sum *= __builtin_amdgcn_exp2f(top - m);
+    for (int u = 0; u < N; ++u) top = fmaxf(top, st[u].x);
+    const float old = __builtin_amdgcn_exp2f(y.m - top);
+    y.m = top;
+    y.sum *= old;
+    y.o *= old;
+    y.besides = st[0].z;
 #pragma unroll
-  for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int k = k0; k < s.n; k += kAtOnce * all) {
-    if (k > k0) load(k);
-#pragma unroll
-    for (int u = 0; u < kAtOnce; ++u)
-      if (y < side && k + u * all < s.n) o += z[u] * __builtin_amdgcn_exp2f(zm[u] - m);
+    for (int u = 0; u < N; ++u) {
+      const float w = __builtin_amdgcn_exp2f(st[u].x - top);
+      y.sum += st[u].y * w;
+      y.o += z[u] * w;
+    }
   }
-  if constexpr (W > 1) {
-    fold[wave][lane] = o;
-    __syncthreads();
-    if (wave != 0) return;
-    for (int w = 1; w < W; ++w) o += fold[w][lane];
-  }
-  for (int u = 1; u < side; ++u) {                     // the states side by side
-    f32x4 other;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) other[e] = __shfl(o[e], lane + u * vecs);
-    if (y == 0) o += other;
-  }
-  if (y == 0) store_joined(a, row, x, o, m, sum, besides, bf16);
+  return y;
 }
 
-// Many states of few rows: a workgroup a row
+// Many states of few rows: a workgroup a row, 64 D / 4 lanes' worth of its states side by side in each wavefront
 __global__ __launch_bounds__(64 * kManyWaves) void cache_combine_many_kernel(const CacheAttnArgs a, int bf16) {
-  __shared__ f32x4 fold[kManyWaves][64];
+  __shared__ Joined fold[kManyWaves * 64];
+  const int lane = threadIdx.x & 63, vecs = a.c.D / 4, side = 64 / vecs, x = lane % vecs, y = lane / vecs, all = kManyWaves * side;
   const int first = max(min(a.starts[0], a.T), 0), end = max(min(a.starts[a.c.B], a.T), 0);
   const RowStates s = states_of(a, blockIdx.x, first, end);
-  if (s.n > 1) join_row<kManyWaves>(a, blockIdx.x, s, fold, bf16);
+  if (s.n <= 1) return;
+  const int k0 = uniform(threadIdx.x >> 6) * side + y;
+  if (y < side) fold[k0 * vecs + x] = join_states<8>(a, s, k0, all, x);
+  __syncthreads();
+  if (threadIdx.x >= vecs) return;
+  Joined z = fold[x];
+  for (int k = 1; k < min(all, s.n); ++k) z = join(z, fold[k * vecs + x]);
+  store_joined(a, blockIdx.x, x, z.o, z.m, z.sum, z.besides, bf16);
 }
-// Few states of many rows: 64 D / 4 lanes' worth of rows side by side (per: so many, or one where the states may be more), each lane through its
-// row's states, four under way; `rounds` times a wavefront.  Rows with more than kFewStates have the wavefront to themselves, rows that
-// are whole cost a look.
-constexpr int kFewStates = 8;
-__global__ __launch_bounds__(256) void cache_combine_kernel(const CacheAttnArgs a, int rounds, int per, int bf16) {
-  const int lane = threadIdx.x & 63, D = a.c.D, vecs = D / 4, x = lane % vecs, y = lane / vecs;
+// Few states of many rows: 64 D / 4 lanes' worth of rows side by side, each lane through its row's states, four under way; `rounds` times a
+// wavefront.  With alone = 1, for more states, a row at a time and its states side by side.  Rows that are whole cost a look.
+__global__ __launch_bounds__(256) void cache_combine_kernel(const CacheAttnArgs a, int rounds, int alone, int bf16) {
+  const int lane = threadIdx.x & 63, vecs = a.c.D / 4, side = 64 / vecs, per = alone ? 1 : side, x = lane % vecs, y = lane / vecs;
   const int first = max(min(a.starts[0], a.T), 0), end = max(min(a.starts[a.c.B], a.T), 0);
-  const int64_t rows = (int64_t)a.T * a.Hq, base = ((int64_t)blockIdx.x * 4 + uniform(threadIdx.x >> 6)) * rounds * per;
-  for (int round = 0; round < rounds; ++round) {
-    const int64_t row0 = base + round * per, row = row0 + y;
-    if (row0 >= rows) break;
+  const int64_t rows = (int64_t)a.T * a.Hq, base = ((int64_t)blockIdx.x * 4 + uniform(threadIdx.x >> 6)) * rounds * per, stop = min(base + rounds * per, rows);
+  for (int64_t row0 = base; row0 < stop; row0 += per) {
+    const int64_t row = row0 + (alone ? 0 : y);
     RowStates s{1, 0, 0};
-    if (y < per && row < rows) s = states_of(a, row, first, end);
-    if (!__any(s.n > 1)) continue;
-    if (per == 1 || __any(s.n > kFewStates)) {
-      for (int u = 0; u < per && row0 + u < rows; ++u) {
-        const RowStates z = states_of(a, row0 + u, first, end);
-        if (z.n > 1) join_row<1>(a, row0 + u, z, nullptr, bf16);
-      }
+    if (y < side && row < stop) s = states_of(a, row, first, end);
+    if (!__any(s.n > 1)) {                             // nor are the other heads of the last token split
+      row0 = (min(row0 + per, stop) - 1) / a.Hq * a.Hq + a.Hq - per;
       continue;
     }
-    if (s.n <= 1) continue;
-    float m = kUnset, sum = 0.f, besides = 0.f;
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int k = 0; k < s.n; k += 4) {
-      f32x4 z[4];
-      float4 st[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int64_t from = s.first + min(k + u, s.n - 1) * s.step;
-        if (u == 0 || k + u < s.n) {
-          z[u] = *reinterpret_cast<const f32x4*>(a.part_o + from * D + 4 * x);
-          st[u] = a.part_row[from];
-        } else {
-          z[u] = f32x4{0.f, 0.f, 0.f, 0.f};
-          st[u] = make_float4(kUnset, 0.f, 0.f, 0.f);
-        }
+    Joined z = join_states<4>(a, s.n > 1 ? s : RowStates{0, 0, 0}, alone ? y : 0, alone ? side : 1, x);
+    if (alone) {
+      for (int u = 1; u < side; ++u) {
+        const int from = lane + u * vecs;
+        const Joined other{__shfl(z.m, from), __shfl(z.sum, from), 0.f, f32x4{__shfl(z.o[0], from), __shfl(z.o[1], from), __shfl(z.o[2], from), __shfl(z.o[3], from)}};
+        if (y == 0) z = join(z, other);
       }
-      const float top = fmaxf(fmaxf(fmaxf(st[0].x, st[1].x), fmaxf(st[2].x, st[3].x)), m), old = __builtin_amdgcn_exp2f(m - top);
-      o *= old;
-      sum *= old;
-      m = top;
-      besides = st[0].z;
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        if (u > 0 && k + u >= s.n) break;
-        const float w = __builtin_amdgcn_exp2f(st[u].x - m);
-        o += z[u] * w;
-        sum += st[u].y * w;
-      }
+      if (y != 0) continue;
     }
-    store_joined(a, row, x, o, m, sum, besides, bf16);
+    if (s.n > 1) store_joined(a, row, x, z.o, z.m, z.sum, z.besides, bf16);
   }
 }
 
@@ -661,9 +630,10 @@ hipError_t launch_cache_combine(const CacheAttnArgs& a, bool bf16, int states, h
     hipLaunchKernelGGL(cache_combine_many_kernel, dim3((unsigned)rows), dim3(64 * kManyWaves), 0, stream, a, bf16 ? 1 : 0);
     return hipGetLastError();
   }
-  const int64_t per = states >= 4 ? 1 : 64 / (a.c.D / 4), groups = (rows + per - 1) / per, rounds = (groups + 16383) / 16384, blocks = (groups + 4 * rounds - 1) / (4 * rounds);
+  const int alone = states >= 4;
+  const int64_t per = alone ? 1 : 64 / (a.c.D / 4), groups = (rows + per - 1) / per, rounds = (groups + 8191) / 8192, blocks = (groups + 4 * rounds - 1) / (4 * rounds);
   if (rounds > 0x7fffffff) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(cache_combine_kernel, dim3((unsigned)blocks), dim3(256), 0, stream, a, (int)rounds, (int)per, bf16 ? 1 : 0);
+  hipLaunchKernelGGL(cache_combine_kernel, dim3((unsigned)blocks), dim3(256), 0, stream, a, (int)rounds, alone, bf16 ? 1 : 0);
   return hipGetLastError();
 }
 

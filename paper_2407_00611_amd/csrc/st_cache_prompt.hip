@@ -133,11 +133,13 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
   };
   u32x4 raw[E4M3 ? 2 * PASSES : 1];
   constexpr int kPieces = D / 16;                      // of a row in 8 bits; a wavefront takes 64 / kPieces rows, all of one run
+  // in an order in which sixteen lanes' stores to LDS meet no bank twice: four (two) rows apart where the swizzle differs in its last bit
+  const int at_row = lane / kPieces, my_row = wave * (64 / kPieces) + (D == 128 ? (at_row & 1) * 4 + (at_row >> 1) : (at_row & 1) | (at_row >> 1 & 1) << 2 | (at_row >> 2 & 1) << 1 | (at_row >> 3) << 3);
   auto load_raw = [&](int tile, int pages) {
     if constexpr (E4M3) {
 #pragma unroll
       for (int x = 0; x < PASSES; ++x) {
-        const int row = x * (256 / kPieces) + tid / kPieces, run = x * (256 / kPieces / 16) + wave * (64 / kPieces) / 16;
+        const int row = x * (256 / kPieces) + my_row, run = x * (256 / kPieces / 16) + wave * (64 / kPieces) / 16;
         raw[x] = *reinterpret_cast<const u32x4*>(run_base(kb_, c.k, pages, tile, run) + (row & 15) * c.k.ss + (tid % kPieces) * 16);
         raw[PASSES + x] = *reinterpret_cast<const u32x4*>(run_base(vb_, c.v, pages, tile, run) + (row & 15) * c.v.ss + (tid % kPieces) * 16);
       }
@@ -147,7 +149,7 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
     if constexpr (E4M3) {
 #pragma unroll
       for (int x = 0; x < 2 * PASSES; ++x) {
-        const int y = x % PASSES, row = y * (256 / kPieces) + tid / kPieces, run = y * (256 / kPieces / 16) + wave * (64 / kPieces) / 16, chunk = 2 * (tid % kPieces);
+        const int y = x % PASSES, row = y * (256 / kPieces) + my_row, run = y * (256 / kPieces / 16) + wave * (64 / kPieces) / 16, chunk = 2 * (tid % kPieces);
         const float sc = __uint_as_float((uint32_t)__builtin_amdgcn_readlane(scales, run + (x < PASSES ? 0 : 4)) << 23);
         ST_LDS char* to = smem + (2 * stage + (x < PASSES ? 0 : 1)) * kTile;
         auto pair = [&](uint32_t w, bool high) {
