@@ -12,12 +12,17 @@ using st::hip_fail;
 
 namespace {
 
-// A share of a walk is at least so many blocks of 32 keys, two for each of a workgroup's wavefronts.  Workgroups that shares are made for:
-// tiles of 16 rows wait for memory, and more of them than the chip holds at once even out what the lengths leave (64 ragged sequences 124 us,
-// 140 with 1024); for tiles of 32 rows, which are work, each share has 32 rows of O to join.
-constexpr int kLeastBlocks = 8, kPlacesOfFew = 2048, kPlaces = 512;
-// Batches whose sequences all have at most so many rows have one launch for them
-constexpr int kFewRows = 64;
+// A share of a walk is at least so many blocks of keys: two of 32 for each wavefront of a tile of 16 or 32 rows (one in fp32, where a block is
+// four times the work: 3 rows of four sequences 20 us, 23 with two), four of 64 of a prompt's tile (102 rows of 18 sequences 34 us, 46 with
+// eight).
+constexpr int kLeastBlocks = 8, kLeastOfPrompts = 4;
+// Workgroups that shares are made for: tiles of 16 rows wait for memory, and more of them than the chip holds at once even out what the
+// lengths leave (64 ragged sequences 124 us, 140 with 1024); for tiles of 32 and 128 rows, which are work, each share has so many rows of O
+// to join.
+constexpr int kPlacesOfFew = 2048, kPlaces = 512;
+// Sequences of up to so many rows are read again for every 32 of them (16 heads x 24 rows x 2048 tokens as fast either way, 64 rows 30 us and
+// 40); of up to kFewOfShort where there are few tiles, and a step's latency is what counts (246 rows of six sequences 27 us, 31).
+constexpr int kFewRows = 128, kFewOfShort = 256, kShortTiles = 64;
 
 st_status check_cache(const st_cache* c) {
   if (c == nullptr) return fail(ST_ERR_INVALID_ARG, "null cache");
@@ -92,7 +97,7 @@ st::CachePlan launch_plan(const st_cache_rows* r, const st_cache* c, int rows, i
   p.rows = rows;
   p.rows_from = from;
   p.rows_to = to;
-  p.least = r->dtype == ST_F32 ? kLeastBlocks / 2 : kLeastBlocks;
+  p.least = rows == st::kPromptRows ? kLeastOfPrompts : r->dtype == ST_F32 ? kLeastBlocks / 2 : kLeastBlocks;
   p.target = rows == 16 ? kPlacesOfFew : kPlaces;
   const int64_t jobs = tiles * c->Hkv, most = std::max<int64_t>((blocks + p.least / 2) / p.least, 1);
   p.grid = std::min(p.target + jobs, jobs * most);
@@ -112,12 +117,13 @@ struct Plans {
 Plans plans_of(const st_cache_rows* r, const st_cache* c) {
   constexpr int kAll = 0x7fffffff;
   const int64_t most = (int64_t)std::min(r->max_rows, r->T) * (r->Hq / c->Hkv);
-  const int large = r->dtype == ST_BF16 && most > kFewRows ? st::kPromptRows : 32;
+  const bool tall = r->dtype == ST_BF16 && most > kFewRows && (most > kFewOfShort || launch_plan(r, c, st::kPromptRows, 0, kAll, 0).jobs > kShortTiles);
+  const int large = tall ? st::kPromptRows : 32;
   Plans y{};
   y.n = 1;
   if (most <= 16) {
     y.p[0] = launch_plan(r, c, 16, 0, kAll, 0);
-  } else if (most <= kFewRows || c->B == 1) {
+  } else if (most <= kFewRows || c->B == 1 || (most <= kFewOfShort && !tall)) {
     y.p[0] = launch_plan(r, c, large, 0, kAll, 0);
   } else {
     y.n = 2;

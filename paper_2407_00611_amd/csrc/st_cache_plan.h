@@ -26,7 +26,7 @@ __device__ __forceinline__ SeqSpan seq_span(const CacheAttnArgs& a, int b) {
   SeqSpan y;
   y.r = seq_rows(a.starts, b, a.T);
   y.len = seq_len(a.c, b);
-  y.pos = a.q_first ? a.q_first[b] : (int64_t)a.c.lens[b] - y.r.n;
+  y.pos = a.q_first ? min(max(a.q_first[b], -((int64_t)1 << 62)), (int64_t)1 << 62) : (int64_t)a.c.lens[b] - y.r.n;
   y.r.n = min(y.r.n, a.max_rows);
   return y;
 }

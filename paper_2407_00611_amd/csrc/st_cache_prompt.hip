@@ -34,13 +34,19 @@ __device__ __forceinline__ void landed() {
   __syncthreads();
 }
 
-// The tiles of a workgroup's walk in the order it takes them: those that a mask edge crosses first (general; all of them where a page is
-// missing), then the whole ones, each from the last one down.
+// The tiles of a workgroup's walk in the order it takes them: first the general ones, which a mask edge crosses (all of them where a page is
+// missing) or in which a biased row lies, then the whole ones, those before the rows from the nearest one down, those behind them from the
+// nearest one up.  General are [t0, a0), [a1, a2) and [a3, t1), whole [a0, a1) and [a2, a3).
 struct TileWalk {
-  int t0, f0, f1, t1, n_gen;
+  int t0, a0, a1, a2, a3, t1, n_gen;
   __device__ __forceinline__ int tile(int n) const {
-    if (n < n_gen) return n < t1 - f1 ? t1 - 1 - n : f0 - 1 - (n - (t1 - f1));
-    return f1 - 1 - (n - n_gen);
+    if (n < n_gen) {
+      if (n < t1 - a3) return t1 - 1 - n;
+      n -= t1 - a3;
+      return n < a2 - a1 ? a2 - 1 - n : a0 - 1 - (n - (a2 - a1));
+    }
+    n -= n_gen;
+    return n < a1 - a0 ? a1 - 1 - n : a2 + n - (a1 - a0);
   }
 };
 
@@ -86,11 +92,16 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
   }
   if (__any(hole) && lane == 0) missing = 1;
   __syncthreads();
-  const bool plain = !missing && (!BIAS || a.causal);  // (behind a row that sees all tokens a bias falls again)
-  walk.f0 = plain ? min(max((x1.lo + kBN - 1) / kBN, walk.t0), walk.t1) : walk.t1;
-  walk.f1 = plain ? max(min(x0.hi / kBN, walk.t1), walk.f0) : walk.t1;
-  if (!plain) walk.f0 = walk.f1 = walk.t1;
-  walk.n_gen = walk.f0 - walk.t0 + walk.t1 - walk.f1;
+  walk.a0 = min(max((x1.lo + kBN - 1) / kBN, walk.t0), walk.t1);
+  walk.a3 = max(min(x0.hi / kBN, walk.t1), walk.a0);
+  if (missing) walk.a0 = walk.a3 = walk.t1;
+  walk.a1 = walk.a2 = walk.a3;
+  if (BIAS) {                                          // whole: with all rows on one side
+    const int64_t p0 = s.pos + first / G, p1 = s.pos + last / G;
+    walk.a1 = max(min((int)(min(max(p0 + 1, (int64_t)0), (int64_t)s.len) / kBN), walk.a3), walk.a0);
+    walk.a2 = max(min((int)((min(max(p1, (int64_t)0), (int64_t)s.len) + kBN - 1) / kBN), walk.a3), walk.a1);
+  }
+  walk.n_gen = walk.a0 - walk.t0 + walk.a2 - walk.a1 + walk.t1 - walk.a3;
   const int n_all = walk.t1 - walk.t0;
   const int n0 = (int)((int64_t)n_all * t.share / t.shares), n1 = (int)((int64_t)n_all * (t.share + 1) / t.shares);
 
@@ -195,7 +206,7 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
     constexpr bool GEN = decltype(general)::value;
     const int d0 = near - key0 - 4 * g;
     const ScoreTile<CAP, BIAS> f(k, slope2, d0);
-    const float side = f.slope;                        // (whole tiles lie before the row)
+    const float side = d0 > 0 ? f.slope : -f.slope;    // (before the row the bias rises with the key)
     const float off = BIAS && !GEN ? slope2 * fabsf((float)d0) : 0.f;
     const int l0 = see.lo - key0 - 4 * g, h0 = see.hi - key0 - 4 * g;
 #pragma unroll
@@ -282,7 +293,8 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
       Block y[KB];
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) products(y[kb], ktile + 32 * kb * D * 2);
-      const bool dirty = not_finite<D>(reads, ktile + kTile) || not_finite<D>(reads, ktile + kTile + 32 * D * 2);
+      const bool cut = missing || y1.lo > key0 || y0.hi < key0 + kBN;
+      const bool dirty = cut && (not_finite<D>(reads, ktile + kTile) || not_finite<D>(reads, ktile + kTile + 32 * D * 2));
       bad = bad || dirty;
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) {
@@ -318,6 +330,7 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
     // what the general tiles left out: values that are not finite, of the keys that this row sees
     for (int y = n0; y < min(n1, walk.n_gen); ++y) {
       const int key0 = walk.tile(y) * kBN;
+      if (!missing && y1.lo <= key0 && y0.hi >= key0 + kBN) continue;
       for (int key = max(see.lo, key0); key < min(see.hi, key0 + kBN); ++key) {
         const int page = page_of(c, t.b, key >> c.shift);
         if (page < 0) continue;
