@@ -1,0 +1,146 @@
+"""Prompts against a cache of pages, whose rows fill tiles of 128, and batches at the edges between the kernels of st_attn_cache; long caches,
+many shares of one walk, and storage beyond 32-bit offsets.  Bounds in cache_cases.check_attention."""
+import math
+
+import pytest
+import torch
+
+import paper_2407_00611_amd as st
+from cache_cases import Case, check_attention, rows_of
+from oracle import cache as oc
+from test_gpu_cache_attn import _attend
+
+pytestmark = pytest.mark.gpu
+
+PROMPTS = [
+    dict(lens=[90], counts=[90], page=16),                                             # from the first token on
+    dict(lens=[300], counts=[90], page=64, lowp=True),
+    dict(lens=[411, 60, 70, 0], counts=[100, 1, 2, 0], page=32),                       # with single tokens beside it
+    dict(lens=[500, 200], counts=[93, 87], window=50, page=16),
+    dict(lens=[500], counts=[90], window=64, page=256),
+    dict(lens=[300], counts=[90], causal=False, page=128, layout="heads_first"),
+    dict(lens=[300], counts=[90], causal=False, window=100, page=16),
+    dict(lens=[350], counts=[90], cap=15.0, layout="together", page=64),
+    dict(lens=[350], counts=[90], bias=True, page=16, rows="packed"),
+    dict(lens=[350], counts=[90], bias=True, causal=False, page=16),
+    dict(lens=[350], counts=[90], bias=True, cap=20.0, causal=False, q_first=[130], page=32),
+    dict(lens=[350], counts=[90], bias=True, cap=20.0, window=70, rows="heads_first"),
+    dict(lens=[200, 100], counts=[90, 90], q_first=[190, 5], page=16),                 # rows ahead of the tokens, rows among them
+    dict(lens=[200, 100], counts=[90, 90], q_first=[-40, 250], window=120, page=16),   # rows before the first token, rows that have left all behind
+    dict(lens=[3000], counts=[90], page=64),                                           # a walk in several shares
+    dict(lens=[130], counts=[130], Hq=2, Hkv=1, page=16, more_rows=5),                 # 260 rows: two tiles and four rows
+    dict(lens=[300] * 3, counts=[86, 64, 43], max_rows=80, page=16),
+]
+
+
+@pytest.mark.parametrize("case", range(len(PROMPTS)))
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("kind", ["e4m3", "bf16"])
+def test_prompts(kind, D, case):
+    _attend("bf16", kind, seed=100 + case, **{**dict(Hq=6, Hkv=2, D=D), **PROMPTS[case]})
+
+
+@pytest.mark.parametrize("kind", ["e4m3", "bf16"])
+@pytest.mark.parametrize("counts,Hq,Hkv", [([16, 3], 4, 4), ([17, 3], 4, 4), ([16, 17], 1, 1), ([128, 1], 2, 2), ([129, 16, 1], 8, 8), ([256, 2], 4, 4), ([257, 20], 4, 4)])
+def test_between_the_kernels(kind, counts, Hq, Hkv):
+    """Rows of a sequence where another tile begins: 16, 128 and 256 of them and one more."""
+    _attend("bf16", kind, [c + 30 for c in counts], counts, Hq=Hq, Hkv=Hkv, seed=7)
+
+
+@pytest.mark.parametrize("kind", ["e4m3", "bf16"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_prompts_and_pages_that_are_not_there(kind, D):
+    case = Case(9, kind, [400, 300], 16, 2, D)
+    table = case.table.clone()
+    table[0, 3], table[0, 11], table[0, 24], table[1] = -1, 10 ** 9, -2 ** 31, -7
+    _attend("bf16", kind, [400, 300], [100, 100], Hq=6, Hkv=2, D=D, table=table, seed=9)
+    _attend("bf16", kind, [400, 300], [100, 100], Hq=6, Hkv=2, D=D, table=table, seed=9, bias=True, cap=30.0, window=150)
+
+
+@pytest.mark.parametrize("kind", ["e4m3", "bf16"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_what_is_not_finite_in_a_prompt(kind, D):
+    """NaN in the values of one token and in the keys of a later one; an infinity among the values (pages in bf16): rows before them have what
+    they would have without, bit by bit, rows behind have it where it belongs."""
+    L, n = 400, 100
+    case = Case(11, kind, [L], 16, 1, D)
+    q = torch.randn((1, n, 4, D), generator=case.g).bfloat16().cuda()
+    run = lambda: st.st_attn_cache(q, rows_of([n]).cuda(), case.cache(), True, 0.125)
+    o0, l0 = run()
+    at = lambda token: (int(case.table[0, token // 16]), token % 16, 0)
+    bits = {"nan": torch.tensor(math.nan).to(case.v.dtype), "inf": torch.tensor(math.inf).to(case.v.dtype)}
+    case.v[at(L - 60) + (5,)] = bits["nan"]
+    case.k[at(L - 20) + (9,)] = bits["nan"]
+    if kind == "bf16":
+        case.v[at(L - 40) + (7,)] = bits["inf"]
+    o, lse = run()
+    assert torch.equal(o[0, :40], o0[0, :40]) and torch.equal(lse[0, :, :40], l0[0, :, :40])
+    keep = torch.ones(D, dtype=torch.bool, device="cuda")
+    keep[5] = False
+    assert torch.isnan(o[0, 40:, :, 5]).all() and torch.isnan(o[0, 80:]).all() and torch.isnan(lse[0, :, 80:]).all()
+    assert torch.equal(lse[0, :, 40:80], l0[0, :, 40:80])
+    if kind == "bf16":
+        assert (o[0, 60:80, :, 7] == math.inf).all() and torch.isfinite(o[0, 40:60, :, 7]).all()
+        keep[7] = False
+    # the same tile takes another way where its values are looked at: no more than its roundings apart
+    assert float((o[0, 40:80][:, :, keep] - o0[0, 40:80][:, :, keep]).abs().max()) <= 2.0 ** -8 * float(o0.abs().max())
+
+
+@pytest.mark.parametrize("dtype,kind,D", [("bf16", "e4m3", 128), ("bf16", "bf16", 64), ("f32", "f32", 128)])
+def test_many_shares_of_one_walk(dtype, kind, D):
+    """A token against so many keys that its states are joined in several rounds."""
+    _attend(dtype, kind, [100003], [1], Hq=2, Hkv=1, D=D, page=256, seed=3)
+
+
+@pytest.mark.parametrize("counts", [[1] * 70, [2] * 69 + [40]])
+def test_one_long_sequence_among_many_short_ones(counts):
+    _attend("bf16", "e4m3", [40] * 69 + [3000], counts, Hq=2, Hkv=2, D=64, page=64, seed=4)
+
+
+def test_pages_beyond_32_bits():
+    """Storage of 5 GiB, the sequences' pages at its end (and one at its beginning): appended, read and seen."""
+    page, Hkv, D = 64, 8, 128
+    n_pages = 5 * 2 ** 30 // (page * Hkv * D)
+    k, v = (torch.zeros((n_pages, page, Hkv, D), dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn) for _ in range(2))
+    scales = [torch.full((n_pages, Hkv), 120, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    table = torch.tensor([[n_pages - 1, n_pages - 3, n_pages - 2, 0], [n_pages - 9, n_pages - 8, 1, 2]], dtype=torch.int32)
+    g, lens = torch.Generator().manual_seed(1), [200, 70]
+    x, y = (torch.randn((1, 270, Hkv, D), generator=g).bfloat16() for _ in range(2))
+    starts, cache = rows_of([200, 70]).cuda(), st.KVCache(k, v, table.cuda(), torch.tensor(lens, dtype=torch.int32).cuda(), *scales)
+    freq = torch.zeros(0, dtype=torch.float64).cuda()
+    st.st_cache_append(None, x.cuda(), y.cuda(), starts, cache, freq, norm=False)
+    pages = [oc.Pages(torch.zeros((12, page, Hkv, D)), torch.zeros((12, Hkv), dtype=torch.int64)) for _ in range(2)]
+    small = torch.tensor([[11, 9, 10, 0], [3, 4, 1, 2]])                      # the same pages of a cache of twelve
+    for p, rows in zip(pages, (x, y)):
+        p.append(small, lens, [0, 200, 270], rows[0].double())
+    class Held:
+        def held(self, b, lens, table):
+            (hk, there), (hv, _) = (p.held(small, lens, b) for p in pages)
+            return hk, hv, there
+    Held.lens = lens
+    got = st.st_cache_read(cache, None, 200)
+    for i in range(2):
+        for b in range(2):
+            assert torch.equal(got[i][b, :lens[b]].double().cpu(), pages[i].held(small, lens, b)[0])
+    for counts in ([1, 1], [200, 70]):
+        q = torch.randn((1, sum(counts), 16, D), generator=g).bfloat16().cuda()
+        o, lse = st.st_attn_cache(q, rows_of(counts).cuda(), cache, True, 0.09)
+        check_attention(Held(), q[:, :, :], rows_of(counts), o, lse, True, 0.09)
+
+
+def test_strides_as_far_apart_as_they_may_be():
+    """Tokens of a page 2^20 - 16 values apart, pages in one another's gaps."""
+    far, Hkv, D, page = (1 << 20) - 16, 2, 64, 16
+    case = Case(5, "e4m3", [40, 20], page, Hkv, D)
+    n = case.k.shape[0]
+    store = [torch.zeros(far * page, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    wide = [s.view(torch.float8_e4m3fn).as_strided((n, page, Hkv, D), (Hkv * D, far, D, 1)) for s in store]
+    for to, x in zip(wide, (case.k, case.v)):
+        to.copy_(x)
+    cache = case.cache()._replace(k=wide[0], v=wide[1])
+    for counts in ([1, 1], [40, 20]):
+        q = torch.randn((1, sum(counts), 16, D), generator=case.g).bfloat16().cuda()
+        o, lse = st.st_attn_cache(q, rows_of(counts).cuda(), cache, True, 0.125)
+        check_attention(case, q, rows_of(counts), o, lse, True, 0.125)
+    for x, y in zip(st.st_cache_read(cache, None, 40), st.st_cache_read(case.cache(), None, 40)):
+        assert torch.equal(x, y)
