@@ -56,7 +56,13 @@ __device__ __forceinline__ A lanes_sum(A x, int lanes) {
   return x;
 }
 __device__ __forceinline__ float inv_root(float x) { return rsqrtf(x); }
-__device__ __forceinline__ double inv_root(double x) { return 1.0 / sqrt(x); }
+// (the instruction's 2^-26 by two steps of Newton's; zero of an infinity, as of fp32)
+__device__ __forceinline__ double inv_root(double x) {
+  double y = __builtin_amdgcn_rsq(x);
+#pragma unroll
+  for (int k = 0; k < 2; ++k) y = fma(0.5 * y, fma(-x * y, y, 1.0), y);
+  return x == INFINITY ? 0.0 : y;
+}
 
 __device__ __forceinline__ bool is_finite(float x) { return fabsf(x) <= 3.402823466e38f; }
 // The least e, -126 at the least, with top <= 448 2^e = 1.75 2^(e + 8)
@@ -155,39 +161,51 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, const Piece& p,
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      Vec<V> wa, wb;
-      if (g.k_weight) load_pairs<V, NEXT>(g.k_weight, at[u], wa, wb);
+      A y[V], w[V];
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        A y = (A)x[u].x[e], w = (A)z[u].x[e];
-        if (g.norm) {
-          y *= g.k_weight ? r * (A)wa.x[e] : r;
-          w *= g.k_weight ? r * (A)wb.x[e] : r;
+      for (int e = 0; e < V; ++e) y[e] = (A)x[u].x[e], w[e] = (A)z[u].x[e];
+      if (g.norm) {
+        Vec<V> wa, wb;
+        if (g.k_weight) load_pairs<V, NEXT>(g.k_weight, at[u], wa, wb);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          y[e] *= g.k_weight ? r * (A)wa.x[e] : r;
+          w[e] *= g.k_weight ? r * (A)wb.x[e] : r;
         }
-        if (at[u].pair + e < half) {                   // (others as they are: zero times infinity is NaN)
+      }
+      if (at[u].pair < half) {                         // (a lane's pairs turn all or none; those as they are: zero times infinity is NaN)
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
           const double place = position_of(g, place0 + (double)row, p.row0 + row, at[u].pair + e);
           A c, s;
           if constexpr (E4M3) sincos_part(place, f[u][e], parts, s, c);
           else sincospif((float)(2.0 * fraction(place * f[u][e])), &s, &c);
-          const A m = y * c - w * s;
-          w = y * s + w * c;
-          y = m;
+          const A m = y[e] * c - w[e] * s;
+          w[e] = y[e] * s + w[e] * c;
+          y[e] = m;
         }
-        x[u].x[e] = E4M3 ? sticky(y) : (float)y;
-        z[u].x[e] = E4M3 ? sticky(w) : (float)w;
+      }
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        x[u].x[e] = E4M3 ? sticky(y[e]) : (float)y[e];
+        z[u].x[e] = E4M3 ? sticky(w[e]) : (float)w[e];
       }
     }
   };
+  bool all_finite = true;
   auto store_row = [&](int row, Vec<V> (&x)[U], Vec<V> (&z)[U], float unit) {
     S* to_row = dst + (int64_t)(begun + row) * to.ss;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if constexpr (E4M3) {
+        if (__builtin_expect(!all_finite, 0))
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-          x[u].x[e] = is_finite(x[u].x[e]) ? x[u].x[e] * unit : NAN;
-          z[u].x[e] = is_finite(z[u].x[e]) ? z[u].x[e] * unit : NAN;
-        }
+          for (int e = 0; e < V; ++e) {
+            x[u].x[e] = is_finite(x[u].x[e]) ? x[u].x[e] : NAN;
+            z[u].x[e] = is_finite(z[u].x[e]) ? z[u].x[e] : NAN;
+          }
+#pragma unroll
+        for (int e = 0; e < V; ++e) x[u].x[e] *= unit, z[u].x[e] *= unit;
       }
       if (at[u].live) store_pairs<V, NEXT>(to_row, at[u], x[u], z[u]);
     }
@@ -201,16 +219,25 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, const Piece& p,
   } else {
     uint8_t* scale = (key ? a.c.k_scale : a.c.v_scale) + (int64_t)page * g.Hkv + h;
     const int had = begun > 0 ? (int)*scale - 127 : -126;
-    float top = 0.f;
-    auto highest = [&](const Vec<V> (&x)[U], const Vec<V> (&z)[U]) {
+    // the highest magnitude, as the bits of one, which are in order: an infinity or NaN is above all finite ones
+    uint32_t top = 0;
+    auto highest = [&](const Vec<V> (&x)[U], const Vec<V> (&z)[U], uint32_t below) {
 #pragma unroll
       for (int u = 0; u < U; ++u)
+        if (at[u].live)
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-          if (at[u].live && is_finite(x[u].x[e])) top = fmaxf(top, fabsf(x[u].x[e]));
-          if (at[u].live && is_finite(z[u].x[e])) top = fmaxf(top, fabsf(z[u].x[e]));
-        }
+          for (int e = 0; e < V; ++e) {
+            const uint32_t y = __float_as_uint(x[u].x[e]) & 0x7fffffff, w = __float_as_uint(z[u].x[e]) & 0x7fffffff;
+            top = max(top, max(y < below ? y : 0, w < below ? w : 0));
+          }
     };
+    auto of_all = [&]() {
+      for (int d = 1; d < 64; d *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, d));
+      if ((tid & 63) == 0) shared[tid >> 6] = (int)top;
+      __syncthreads();
+      top = max(max((uint32_t)shared[0], (uint32_t)shared[1]), max((uint32_t)shared[2], (uint32_t)shared[3]));
+    };
+    constexpr uint32_t kInfinity = 0x7f800000u;
     // The first rows of a lane stay in registers until the scale is known, the others are made again (pages of up to 64 tokens of 128: none)
     constexpr int kHeld = 4;
     Vec<V> x[kHeld][U], z[kHeld][U];
@@ -218,18 +245,26 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, const Piece& p,
     for (int k = 0; k < kHeld; ++k)
       if (group + k * groups < n) {
         make(group + k * groups, x[k], z[k]);
-        highest(x[k], z[k]);
+        highest(x[k], z[k], 0xffffffffu);
       }
     for (int row = group + kHeld * groups; row < n; row += groups) {
       Vec<V> y[U], w[U];
       make(row, y, w);
-      highest(y, w);
+      highest(y, w, 0xffffffffu);
     }
-    for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
-    if ((tid & 63) == 0) shared[tid >> 6] = __float_as_int(top);
-    __syncthreads();
-    top = __int_as_float(max(max(shared[0], shared[1]), max(shared[2], shared[3])));
-    const int e = max(had, exponent_for(top));
+    of_all();
+    if (__builtin_expect(top >= kInfinity, 0)) {       // the highest of the finite ones
+      all_finite = false;
+      top = 0;
+      for (int row = group; row < n; row += groups) {
+        Vec<V> y[U], w[U];
+        make(row, y, w);
+        highest(y, w, kInfinity);
+      }
+      __syncthreads();
+      of_all();
+    }
+    const int e = max(had, exponent_for(__uint_as_float(top)));
     const float unit = power_of_two(-e);
 #pragma unroll
     for (int k = 0; k < kHeld; ++k)
@@ -292,8 +327,11 @@ __global__ __launch_bounds__(kThreads, (std::is_same<S, uint8_t>::value ? 4 : 1)
   };
   fetch(group);
 #pragma unroll
-  for (int u = 0; u < U; ++u)
+  for (int u = 0; u < U; ++u) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) wa[u].x[e] = wb[u].x[e] = 1.f;
     if (g.q_weight) load_pairs<V, NEXT>(g.q_weight, at[u], wa[u], wb[u]);
+  }
   const double place0 = (double)(g.offset + p.lo + t0);
   for (int e = tid; e < n * half; e += kThreads) {
     const int t = e / half, j = e - t * half;
@@ -320,14 +358,18 @@ __global__ __launch_bounds__(kThreads, (std::is_same<S, uint8_t>::value ? 4 : 1)
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
+      if (g.norm) {
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        const bool turned = at[u].pair + e < half;
-        const float2 w = turned ? angles[t * half + at[u].pair + e] : make_float2(1.f, 0.f);
-        const float m = g.norm ? ya[u].x[e] * (g.q_weight ? r * wa[u].x[e] : r) : ya[u].x[e];
-        const float o = g.norm ? yb[u].x[e] * (g.q_weight ? r * wb[u].x[e] : r) : yb[u].x[e];
-        ya[u].x[e] = turned ? m * w.x - o * w.y : m;   // (others as they are: zero times infinity is NaN)
-        yb[u].x[e] = turned ? m * w.y + o * w.x : o;
+        for (int e = 0; e < V; ++e) ya[u].x[e] *= r * wa[u].x[e], yb[u].x[e] *= r * wb[u].x[e];
+      }
+      if (at[u].pair < half) {                         // (a lane's pairs turn all or none; those as they are: zero times infinity is NaN)
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          const float2 w = angles[t * half + at[u].pair + e];
+          const float m = ya[u].x[e], o = yb[u].x[e];
+          ya[u].x[e] = m * w.x - o * w.y;
+          yb[u].x[e] = m * w.y + o * w.x;
+        }
       }
       if (at[u].live) store_pairs<V, NEXT>(dst, at[u], ya[u], yb[u]);
     }
