@@ -146,9 +146,11 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, const Piece& p,
     __syncthreads();
   }
   const double place0 = (double)(g.offset + p.lo);
-  auto make = [&](int row, Vec<V> (&x)[U], Vec<V> (&z)[U]) {   // of the rows as they are stored, before they are rounded
+  auto load_row = [&](int row, Vec<V> (&x)[U], Vec<V> (&z)[U]) {
 #pragma unroll
     for (int u = 0; u < U; ++u) load_pairs<V, NEXT>(src + row * in.ss, at[u], x[u], z[u]);
+  };
+  auto finish = [&](int row, Vec<V> (&x)[U], Vec<V> (&z)[U]) {   // of rows as they are stored, before they are rounded
     if (!key) return;
     A r = 1;
     if (g.norm) {
@@ -191,6 +193,10 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, const Piece& p,
         z[u].x[e] = E4M3 ? sticky(w[e]) : (float)w[e];
       }
     }
+  };
+  auto make = [&](int row, Vec<V> (&x)[U], Vec<V> (&z)[U]) {
+    load_row(row, x, z);
+    finish(row, x, z);
   };
   bool all_finite = true;
   auto store_row = [&](int row, Vec<V> (&x)[U], Vec<V> (&z)[U], float unit) {
@@ -242,9 +248,11 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, const Piece& p,
     constexpr int kHeld = 4;
     Vec<V> x[kHeld][U], z[kHeld][U];
 #pragma unroll
+    for (int k = 0; k < kHeld; ++k) load_row(min(group + k * groups, n - 1), x[k], z[k]);
+#pragma unroll
     for (int k = 0; k < kHeld; ++k)
       if (group + k * groups < n) {
-        make(group + k * groups, x[k], z[k]);
+        finish(group + k * groups, x[k], z[k]);
         highest(x[k], z[k], 0xffffffffu);
       }
     for (int row = group + kHeld * groups; row < n; row += groups) {
