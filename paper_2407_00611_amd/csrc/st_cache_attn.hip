@@ -160,8 +160,9 @@ __global__ __launch_bounds__(256, (stream_waves<T, S, ROWS, DP>())) void cache_s
   const char* kbase = (const char*)c.k.ptr + (int64_t)t.hk * c.k.sh * (int)sizeof(S);
   const char* vbase = (const char*)c.v.ptr + (int64_t)t.hk * c.v.sh * (int)sizeof(S);
   const uint32_t k_off = (uint32_t)((r & 15) * c.k.ss * (int)sizeof(S)) + 16 * g;
-  const uint32_t v_off = (uint32_t)(4 * g * c.v.ss * (int)sizeof(S)) + r * VB;
-  const bool v_lane = BF || DB * r < D;
+  // columns behind a head's end are those of a matrix row that is not stored: others are read in their place, by eights
+  const uint32_t v_off = (uint32_t)(4 * g * c.v.ss * (int)sizeof(S)) + (BF || DB * r < D ? r * VB : 0);
+  const uint32_t v_up = DB > 8 && DB * r + 8 >= D ? 0 : 8 * sizeof(S);
 
   struct Pages {
     int p[2];
@@ -203,10 +204,7 @@ __global__ __launch_bounds__(256, (stream_waves<T, S, ROWS, DP>())) void cache_s
       const int k0 = M::row(v, 0);
       const char* y = half[k0 / 16] + k0 % 16 * c.v.ss * (int)sizeof(S) + v_off;
       uint32_t* to = vr[v];
-      if (!v_lane) {
-#pragma unroll
-        for (int d = 0; d < VW; ++d) to[d] = 0;
-      } else if constexpr (VB == 2) to[0] = *reinterpret_cast<const uint16_t*>(y);
+      if constexpr (VB == 2) to[0] = *reinterpret_cast<const uint16_t*>(y);
       else if constexpr (VB == 4) to[0] = *reinterpret_cast<const uint32_t*>(y);
       else if constexpr (VB == 8) {
         const u32x2 z = *reinterpret_cast<const u32x2*>(y);
@@ -214,7 +212,8 @@ __global__ __launch_bounds__(256, (stream_waves<T, S, ROWS, DP>())) void cache_s
       } else {
 #pragma unroll
         for (int d = 0; d < VW; d += 4) {
-          const u32x4 z = *reinterpret_cast<const u32x4*>(y + 4 * d);
+          constexpr int kEight = 8 * (int)sizeof(S) / 4;   // words of eight values
+          const u32x4 z = *reinterpret_cast<const u32x4*>(DB > 8 && d >= kEight ? y + v_up + 4 * (d - kEight) : y + 4 * d);
           to[d] = z[0]; to[d + 1] = z[1]; to[d + 2] = z[2]; to[d + 3] = z[3];
         }
       }

@@ -77,6 +77,17 @@ def test_head_sizes_of_fp32(D, kind):
     _attend("f32", kind, [70, 33], [40, 17], D=D, Hq=2, Hkv=1, cap=20.0, bias=True)
 
 
+@pytest.mark.parametrize("D", [136, 200, 248])
+@pytest.mark.parametrize("layout", ["dense", "heads_first", "together"])
+def test_heads_that_end_inside_a_lanes_columns(D, layout):
+    """A lane has 16 columns of a large fp32 head, and the last one's head ends after eight.  What follows are another head's values, or
+    those of a page without tokens, which are NaN; behind the last page, with all its tokens, nothing follows."""
+    seed = next(s for s in range(100) if int(torch.randperm(10, generator=torch.Generator().manual_seed(s))[0]) == 9)
+    for how in ({}, dict(cap=20.0, bias=True, window=30)):
+        case, *_ = _attend("f32", "f32", [48, 21], [5, 1], D=D, Hq=6, Hkv=3, layout=layout, seed=seed, **how)
+        assert int(case.table[0, 0]) == case.k.shape[0] - 1
+
+
 @pytest.mark.parametrize("dtype,kind", PAIRS)
 def test_pages_that_are_not_there(dtype, kind):
     """Entries that name no page: their tokens are not seen.  Whole sequences of them see nothing."""
