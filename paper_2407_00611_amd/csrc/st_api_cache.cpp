@@ -16,9 +16,9 @@ namespace {
 // four times the work: 3 rows of four sequences 20 us, 23 with two), four of 64 of a prompt's tile (102 rows of 18 sequences 34 us, 46 with
 // eight).
 constexpr int kLeastBlocks = 8, kLeastOfPrompts = 4;
-// Workgroups that shares are made for: tiles of 16 rows wait for memory, and more of them than the chip holds at once even out what the
-// lengths leave (64 ragged sequences 124 us, 140 with 1024); for tiles of 32 and 128 rows, which are work, each share has so many rows of O
-// to join.
+// Workgroups that shares are made for: sequences of up to 16 rows wait for memory, and more workgroups than the chip holds at once even out
+// what the lengths leave (64 ragged sequences 124 us, 140 with 1024); those of more rows are work, and each share has so many rows of O to
+// join (fp32, D = 256, 256 rows of two sequences 96 us, 120 with 1024, 168 with 2048).
 constexpr int kPlacesOfFew = 2048, kPlaces = 512;
 // Sequences of up to so many rows are read again for every 32 of them (16 heads x 24 rows x 2048 tokens as fast either way, 64 rows 30 us and
 // 40); of up to kFewOfShort where there are few tiles, and a step's latency is what counts (246 rows of six sequences 27 us, 31).
@@ -98,7 +98,7 @@ st::CachePlan launch_plan(const st_cache_rows* r, const st_cache* c, int rows, i
   p.rows_from = from;
   p.rows_to = to;
   p.least = rows == st::kPromptRows ? kLeastOfPrompts : r->dtype == ST_F32 ? kLeastBlocks / 2 : kLeastBlocks;
-  p.target = rows == 16 ? kPlacesOfFew : kPlaces;
+  p.target = most_rows <= 16 ? kPlacesOfFew : kPlaces;
   const int64_t jobs = tiles * c->Hkv, most = std::max<int64_t>((blocks + p.least / 2) / p.least, 1);
   p.grid = std::min(p.target + jobs, jobs * most);
   if (rows == 16) p.grid = (p.grid + 8 * c->Hkv - 1) / (8 * c->Hkv) * (8 * c->Hkv);   // (whole rounds of the order in which they take their pieces)
@@ -121,7 +121,7 @@ Plans plans_of(const st_cache_rows* r, const st_cache* c) {
   const int large = tall ? st::kPromptRows : 32;
   Plans y{};
   y.n = 1;
-  if (most <= 16) {
+  if (most <= 16 || (r->dtype == ST_F32 && c->D > st::kTallCacheHead)) {
     y.p[0] = launch_plan(r, c, 16, 0, kAll, 0);
   } else if (most <= kFewRows || c->B == 1 || (most <= kFewOfShort && !tall)) {
     y.p[0] = launch_plan(r, c, large, 0, kAll, 0);

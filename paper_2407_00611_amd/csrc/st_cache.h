@@ -63,6 +63,8 @@ struct CacheAttnArgs {
 };
 
 constexpr int kCacheKeys = 32;                       // keys of a block
+constexpr int kTallCacheHead = 128;                  // the largest head with tiles of 32 rows: of larger ones a lane has no room for its part of O,
+                                                     // keys and values (D = 256, fp32: 4 x 20 rows of a group against 2000 tokens 46 us so, 31 in tiles of 16)
 constexpr int kPromptRows = 128, kPromptKeys = 64;   // of the kernel for prompts
 
 hipError_t launch_cache_append(const AppendArgs& a, bool bf16, hipStream_t stream);

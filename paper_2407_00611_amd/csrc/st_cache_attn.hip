@@ -56,21 +56,18 @@ __device__ __forceinline__ uint32_t bf16_of_e4m3(uint32_t x, float scale) {
   return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, HIGH));
 }
 
-// the parts of x (values of S side by side) that are an infinity or NaN become zero; whether there were any
+// The parts of x (values of S side by side) that are an infinity or NaN become zero; which there were.  One more at the lowest place of such
+// a value's exponent (e4m3: of all its bits) reaches its sign.  (The empty statement keeps the compiler from putting the last step off
+// until all words' masks are there, for which there are no registers; of whole words it keeps a bit each by itself.)
 template <typename S>
-__device__ __forceinline__ bool drop_not_finite(uint32_t& x) {
+__device__ __forceinline__ uint32_t drop_not_finite(uint32_t& x) {
   uint32_t mask;
-  if constexpr (sizeof(S) == 1) {
-    mask = (((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7;
-    mask *= 0xffu;
-  } else if constexpr (sizeof(S) == 2) {
-    mask = (((x & 0x7fff7fffu) + 0x00800080u) & 0x80008000u) >> 15;
-    mask *= 0xffffu;
-  } else {
-    mask = (x & 0x7f800000u) == 0x7f800000u ? 0xffffffffu : 0u;
-  }
+  if constexpr (sizeof(S) == 1) mask = ((((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7) * 0xffu;
+  else if constexpr (sizeof(S) == 2) mask = ((((x & 0x7fff7fffu) + 0x00800080u) & 0x80008000u) >> 15) * 0xffffu;
+  else mask = (x & 0x7f800000u) == 0x7f800000u ? 0xffffffffu : 0u;
   x &= ~mask;
-  return mask != 0;
+  if constexpr (sizeof(S) < 4) asm volatile("" : "+v"(x));
+  return mask;
 }
 
 // One value of the pages
@@ -81,7 +78,7 @@ __device__ __forceinline__ float stored(const uint8_t* p, uint8_t scale) { retur
 // wavefronts on a SIMD that the registers leave room for
 template <typename T, typename S, int ROWS, int DP>
 constexpr int stream_waves() {
-  return DP > 128 ? (ROWS == 16 ? 2 : 1) : ROWS == 16 ? (DP <= 64 ? 4 : sizeof(S) == 1 ? 3 : 2) : 2;
+  return DP > 128 ? (sizeof(S) == 1 ? 2 : 1) : ROWS == 16 ? (DP <= 64 ? 4 : sizeof(S) == 1 ? 3 : 2) : 2;
 }
 
 // T: of the rows (bf16: on the bf16 matrix unit, D = DP; fp32: on the fp32 one, D <= DP); S: what the pages hold; MOD: scores may be capped, biased
@@ -96,9 +93,10 @@ __global__ __launch_bounds__(256, (stream_waves<T, S, ROWS, DP>())) void cache_s
   constexpr int EPC = 16 / (int)sizeof(S), NJ = DP / (GROUPS * EPC);           // values of a piece, pieces of a key's row a lane
   constexpr int VB = DB * (int)sizeof(S), VW = VB < 4 ? 1 : VB / 4;            // bytes and words of a lane's columns
   constexpr int PW = DB < 4 ? DB : 4, PASSES = DB / PW, FS = ROWS * PW + 4;    // folding: columns at a time
+  constexpr bool LATE = (int)sizeof(S) * DP > 512;     // no room for keys and values at once: values are loaded as they are needed
   constexpr int QS = DP + 4;
   constexpr int kFold = 4 * ROWS * FS * 4, kQ = BF ? 0 : ROWS * QS * 4;
-  static_assert(NJ >= 1 && VB >= 2 && DB >= 2, "a lane takes part in every product");
+  static_assert(NJ >= 1 && VB >= 2 && DB >= 2 && (ROWS == 16 || DP <= kTallCacheHead), "a lane takes part in every product");
   __shared__ __attribute__((aligned(16))) char smem[kFold > kQ ? kFold : kQ];
   __shared__ float stat_m[4][ROWS], stat_l[4][ROWS];
   __shared__ int any_bad;
@@ -234,7 +232,7 @@ __global__ __launch_bounds__(256, (stream_waves<T, S, ROWS, DP>())) void cache_s
   if (some) {
     now = pages_of(entry0);
     load_k(now, n);
-    load_v(now, n);
+    if (!LATE) load_v(now, n);
   }
   for (; n >= w.n0; n -= 4) {
     const int key0 = n * kKeys;
@@ -281,8 +279,9 @@ __global__ __launch_bounds__(256, (stream_waves<T, S, ROWS, DP>())) void cache_s
     const Pages next = pages_of(entry);
     const bool more = n - 4 >= w.n0;
     const bool whole = key0 >= w.all_lo && key0 + kKeys <= w.all_hi && now.ok[0] && now.ok[1];
+    if (LATE) load_v(now, n);
     if (more) {
-      load_k(next, n - 4);
+      if (!LATE) load_k(next, n - 4);
       entry = table_at(max(n - 8, w.n0));
     }
 
@@ -331,7 +330,7 @@ __global__ __launch_bounds__(256, (stream_waves<T, S, ROWS, DP>())) void cache_s
     l_run += sum;
 
     if (!whole) {                                      // nothing of what no row sees; of the rest, what is not finite is added at the end
-      bool found = false;
+      uint32_t found = 0;
 #pragma unroll
       for (int v = 0; v < NS; ++v) {
         const int key = key0 + M::row(v, g);
@@ -339,10 +338,10 @@ __global__ __launch_bounds__(256, (stream_waves<T, S, ROWS, DP>())) void cache_s
 #pragma unroll
         for (int d = 0; d < VW; ++d) {
           vr[v][d] = in ? vr[v][d] : 0;
-          found = drop_not_finite<S>(vr[v][d]) || found;
+          found |= drop_not_finite<S>(vr[v][d]);
         }
       }
-      bad = bad || __any(found);
+      bad = bad || __any(found != 0);
     }
     if constexpr (BF) {
 #pragma unroll
@@ -394,7 +393,10 @@ __global__ __launch_bounds__(256, (stream_waves<T, S, ROWS, DP>())) void cache_s
         }
       }
     }
-    if (more) load_v(next, n - 4);
+    if (more) {
+      if (LATE) load_k(next, n - 4);
+      else load_v(next, n - 4);
+    }
     now = next;
   }
 
@@ -610,14 +612,16 @@ hipError_t launch_cache_attn(const CacheAttnArgs& a, bool bf16, hipStream_t stre
   const dim3 grid((unsigned)a.plan.grid), block(256);
   const bool mod = a.cap > 0.f || a.slopes, few = a.plan.rows == 16;
   auto go = [&](auto plain, auto modified) { hipLaunchKernelGGL(mod ? modified : plain, grid, block, 0, stream, a); };
-#define ST_STREAM(T, S, DP) (few ? go(cache_stream_kernel<T, S, 16, DP, false>, cache_stream_kernel<T, S, 16, DP, true>) \
-                                 : go(cache_stream_kernel<T, S, 32, DP, false>, cache_stream_kernel<T, S, 32, DP, true>))
+#define ST_STREAM_FEW(T, S, DP) go(cache_stream_kernel<T, S, 16, DP, false>, cache_stream_kernel<T, S, 16, DP, true>)
+#define ST_STREAM(T, S, DP) (few ? ST_STREAM_FEW(T, S, DP) : go(cache_stream_kernel<T, S, 32, DP, false>, cache_stream_kernel<T, S, 32, DP, true>))
   const int D = a.c.D;
+  if (!few && D > kTallCacheHead) return hipErrorInvalidValue;
   if (bf16 && a.c.dtype == ST_E4M3) D == 128 ? ST_STREAM(uint16_t, uint8_t, 128) : ST_STREAM(uint16_t, uint8_t, 64);
   else if (bf16) D == 128 ? ST_STREAM(uint16_t, uint16_t, 128) : ST_STREAM(uint16_t, uint16_t, 64);
-  else if (a.c.dtype == ST_E4M3) D > 128 ? ST_STREAM(float, uint8_t, 256) : D > 64 ? ST_STREAM(float, uint8_t, 128) : ST_STREAM(float, uint8_t, 64);
-  else D > 128 ? ST_STREAM(float, float, 256) : D > 64 ? ST_STREAM(float, float, 128) : ST_STREAM(float, float, 64);
+  else if (a.c.dtype == ST_E4M3) D > kTallCacheHead ? ST_STREAM_FEW(float, uint8_t, 256) : D > 64 ? ST_STREAM(float, uint8_t, 128) : ST_STREAM(float, uint8_t, 64);
+  else D > kTallCacheHead ? ST_STREAM_FEW(float, float, 256) : D > 64 ? ST_STREAM(float, float, 128) : ST_STREAM(float, float, 64);
 #undef ST_STREAM
+#undef ST_STREAM_FEW
   return hipGetLastError();
 }
 
