@@ -402,7 +402,8 @@ st_status st_qk_rope_bwd(const st_rope_desc* desc, const st_tensor* q, const st_
  * Rows of a call are packed: T rows, of which sequence b has the n_b = starts[b + 1] - starts[b] from starts[b] on (device int32
  * [B + 1], rising, in 0 .. T; n_b may be 0).  Row i of sequence b is its token lens[b] - n_b + i.  Rows of no sequence (T may be
  * more than there are, as for a captured call) are left as they were.
- * A page may be in the tables of several sequences (a common beginning), but only one of them may append to it, in one call at a time.
+ * A page may be in the tables of several sequences (a common beginning), but only one of them may append to it, in one call at a time,
+ * and of the pages that a call appends to each stands once in its sequence's table.
  * D: multiples of 8 up to 256 (ST_E4M3: of 16); B <= 65535, T <= 2^25, width page <= 2^30. */
 typedef struct {
   int32_t  dtype, n_pages, page, Hkv, D, B, width;
@@ -416,9 +417,10 @@ typedef struct {
  *               sequences + offset, or come from `positions` int32 [n_axes,1,T].  Hkv and D are the cache's
  *   q, k, v     [1,T,heads,D] views in desc->dtype; q_out as q, which it may be
  * ST_E4M3: the scale of a page and head is 2^e with the least e for which all new values of the page are within 448 2^e, and not
- * below what the rows have that were there before, which are rescaled where it grows.  Keys are normed and rotated in fp64 there, so
- * that each is the nearest stored value to the exact one; values that are not finite are stored as NaN and do not count for the scale.
- * Repeating a call with the same tensors changes nothing. */
+ * below what the rows have that were there before, which are rescaled where it grows; values that are not finite are stored as NaN and
+ * do not count for the scale.  Keys for pages in fewer bits than fp32 are normed and rotated in fp64, so that in ST_E4M3 each is the
+ * nearest stored value to the exact one, in ST_BF16 that of the exact one in fp32; queries, and keys in ST_F32, in fp32.
+ * Repeating a call with the same tensors, q_out not q, changes nothing. */
 st_status st_cache_append(const st_rope_desc* desc, const st_cache* cache, const int32_t* starts, const st_tensor* q, const st_tensor* k,
                           const st_tensor* v, const float* q_weight, const float* k_weight, const double* freq, const int32_t* positions,
                           const st_tensor* q_out, void* hip_stream);
@@ -438,7 +440,9 @@ st_status st_cache_read(const st_cache* cache, const int32_t* first, int32_t cou
  *   o_part fp32 and / or o_lowp in dtype, dense [1,T,Hq,D]; lse_part fp32 [1,Hq,T]: a state that st_attn_merge and st_attn_combine fold
  *   (B = 1, Sq = T).  A row that sees nothing has O = 0, lse = -inf.
  * ST_BF16 with D = 64 or 128 (pages of ST_BF16 or ST_E4M3), ST_F32 with any D (pages of ST_F32 or ST_E4M3).  Scores, softmax and sums
- * are fp32; infinities and NaN reach the rows that see them, and no others.  Results do not depend on the order of the pages. */
+ * are fp32; exp(s - max) meets the values as two bf16 parts (2^-16), in sequences of many rows (more than 128, or 256 where there are
+ * few, of a KV head's query heads) as one (2^-8, as in st_score).  Infinities and NaN reach the rows that see them, and no others.
+ * Results do not depend on the order of the pages. */
 typedef struct {
   int32_t dtype, T, Hq, max_rows, causal, window;
   float   scale, softcap;

@@ -15,7 +15,8 @@ constexpr int kThreads = 256;
 constexpr int kMaxPairs = 128;
 constexpr int kTokensMost = 8;                       // tokens whose angles a workgroup holds for the queries
 
-// ---- arithmetic of the keys: fp32 as the queries', or fp64
+// ---- arithmetic of the keys: fp32 as the queries' for pages in fp32, otherwise fp64, so that a value is rounded as one of the 64-bit
+// definition is (in fp32 one of 30000 bf16 keys fell to the other side; 4000 prompt rows of eight sequences 273 us, 256 with it)
 
 // sine and cosine of x turns, |x| <= 1/2: x is taken to the nearest quarter, |r| <= pi / 4 from there, and both series of r are cut where the
 // next term is below 1e-12
@@ -48,7 +49,6 @@ __device__ __forceinline__ float sticky(double x) {
   const uint32_t low = (uint32_t)u;
   return (float)__longlong_as_double((u & 0xffffffff00000000ull) | (low & 0xe0000000u) | min(low & 0x1fffffffu, 1u) << 29);
 }
-__device__ __forceinline__ float sticky(float x) { return x; }
 
 template <typename A>
 __device__ __forceinline__ A lanes_sum(A x, int lanes) {
@@ -118,7 +118,7 @@ __device__ __forceinline__ bool find_piece(const AppendArgs& a, Piece& p, int* f
 // T: of the rows; A: of the arithmetic of keys; S: what the pages hold
 template <typename T, typename A, typename S, int V, int U, bool NEXT>
 __device__ __forceinline__ void append_rows(const AppendArgs& a, const Piece& p, int h, bool key, int lanes, int* shared, double2* parts) {
-  constexpr bool E4M3 = std::is_same<S, uint8_t>::value;
+  constexpr bool E4M3 = std::is_same<S, uint8_t>::value, F64 = std::is_same<A, double>::value;
   const RopeArgs& g = a.g;
   const int tid = threadIdx.x, chunk = tid & (lanes - 1), group = tid / lanes, groups = kThreads / lanes, half = g.rot / 2;
   if (p.j >= a.c.width) return;
@@ -135,9 +135,9 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, const Piece& p,
   for (int u = 0; u < U; ++u) {
     at[u] = place_of<V, NEXT>(g, chunk + u * lanes);
 #pragma unroll
-    for (int e = 0; e < V; ++e) f[u][e] = key && at[u].pair + e < half ? g.freq[at[u].pair + e] * (kPerTurn * (E4M3 ? kParts : 1)) : 0.0;
+    for (int e = 0; e < V; ++e) f[u][e] = key && at[u].pair + e < half ? g.freq[at[u].pair + e] * (kPerTurn * (F64 ? kParts : 1)) : 0.0;
   }
-  if (E4M3 && key) {
+  if (F64 && key) {
     if (tid < kParts) {
       double sn, cs;
       sincos_turns(tid < kParts / 2 ? tid / (double)kParts : tid / (double)kParts - 1.0, sn, cs);
@@ -180,7 +180,7 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, const Piece& p,
         for (int e = 0; e < V; ++e) {
           const double place = position_of(g, place0 + (double)row, p.row0 + row, at[u].pair + e);
           A c, s;
-          if constexpr (E4M3) sincos_part(place, f[u][e], parts, s, c);
+          if constexpr (F64) sincos_part(place, f[u][e], parts, s, c);
           else sincospif((float)(2.0 * fraction(place * f[u][e])), &s, &c);
           const A m = y[e] * c - w[e] * s;
           w[e] = y[e] * s + w[e] * c;
@@ -189,8 +189,8 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, const Piece& p,
       }
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        x[u].x[e] = E4M3 ? sticky(y[e]) : (float)y[e];
-        z[u].x[e] = E4M3 ? sticky(w[e]) : (float)w[e];
+        if constexpr (E4M3) x[u].x[e] = sticky(y[e]), z[u].x[e] = sticky(w[e]);
+        else x[u].x[e] = (float)y[e], z[u].x[e] = (float)w[e];
       }
     }
   };
@@ -303,7 +303,7 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, const Piece& p,
 // grid (pieces, 2 Hkv + eights of a page's tokens): keys and values of a head, or all query heads of eight tokens
 template <typename T, typename S, int V, int U, bool NEXT>
 __global__ __launch_bounds__(kThreads, (std::is_same<S, uint8_t>::value ? 4 : 1)) void cache_append_kernel(const AppendArgs a, int lanes) {
-  constexpr bool E4M3 = std::is_same<S, uint8_t>::value;
+  constexpr bool F64 = sizeof(S) < 4;
   __shared__ __attribute__((aligned(16))) float2 angles[kTokensMost * kMaxPairs];
   __shared__ int shared[4];
   const RopeArgs& g = a.g;
@@ -313,8 +313,8 @@ __global__ __launch_bounds__(kThreads, (std::is_same<S, uint8_t>::value ? 4 : 1)
   const int y = blockIdx.y;
   if (y < 2 * g.Hkv) {
     // (four pairs a lane in fp64: with eight the registers leave two wavefronts a SIMD)
-    constexpr int VK = E4M3 && V == 8 ? 4 : V;
-    append_rows<T, typename std::conditional<E4M3, double, float>::type, S, VK, U, NEXT>(a, p, y >> 1, (y & 1) == 0, lanes * (V / VK), shared, (double2*)angles);
+    constexpr int VK = F64 && V == 8 ? 4 : V;
+    append_rows<T, typename std::conditional<F64, double, float>::type, S, VK, U, NEXT>(a, p, y >> 1, (y & 1) == 0, lanes * (V / VK), shared, (double2*)angles);
     return;
   }
   const int t0 = (y - 2 * g.Hkv) * kTokensMost, n = min(kTokensMost, p.hi - p.lo - t0), half = g.rot / 2;

@@ -1,8 +1,8 @@
 """Appending to a cache of pages and reading chunks of it (st_cache_append, st_cache_read) against the 64-bit oracle.
 
 What is stored has to be the oracle's, bit by bit, in 8 bits (keys are made in 64 bits there, and two evaluations in 64 bits that differ
-by 2^-50 round to one e4m3 value but for one in 2^-45) and for values, which are copied; keys in the storage type and queries are fp32
-arithmetic rounded once, with the tolerances of st_qk_rope_fwd's tests."""
+by 2^-50 round to one e4m3 value but for one in 2^-45) and for values, which are copied; keys in fp32 and queries are fp32 arithmetic
+rounded once, with the tolerances of st_qk_rope_fwd's tests (keys in bf16, made in 64 bits too, are within them)."""
 import math
 
 import pytest
@@ -124,6 +124,23 @@ APPENDS = [
 @pytest.mark.parametrize("dtype,kind", [("bf16", "e4m3"), ("bf16", "bf16"), ("f32", "e4m3"), ("f32", "f32")])
 def test_appending(dtype, kind, case):
     _append(dtype, kind, seed=case, **APPENDS[case])
+
+
+@pytest.mark.parametrize("pairs,rot", [("halves", 128), ("neighbours", 64)])
+def test_bf16_keys_are_those_of_64_bits(pairs, rot):
+    """Made in 64 bits, to fp32, to bf16: two evaluations in 64 bits that differ by 2^-48 end in one value but for one in 2^-24 (of fp32
+    steps) by 2^-16 (where that step is a tie of bf16); of 2^18 values none differ."""
+    g, T, D, offset = torch.Generator().manual_seed(40), 512, 128, 100000
+    q, k, v = (torch.randn((1, T, 4, D), generator=g).bfloat16().cuda() for _ in range(3))
+    w = (1 + 0.3 * torch.randn(D, generator=g)).cuda()
+    freq = (10000.0 ** (-torch.arange(rot // 2, dtype=torch.float64) / (rot // 2))).cuda()
+    case = Case(41, "bf16", [0], 64, 4, D, more=T // 64)
+    cache = case.cache([T])
+    st.st_cache_append(q, k, v, rows_of([T]).cuda(), cache, freq, offset=offset, pairs=pairs, q_weight=w, k_weight=w)
+    place = (torch.arange(T, dtype=torch.int64) + offset).expand(rot // 2, 1, T).cuda()
+    want = so.rope(k.double(), w.double(), freq, place, pairs, True).float().bfloat16()
+    got, _ = st.st_cache_read(cache, None, T)
+    assert torch.equal(got, want.to(got.device))
 
 
 def test_one_by_one_and_growing():
