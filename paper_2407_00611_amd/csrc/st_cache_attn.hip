@@ -8,6 +8,15 @@
 // Keys and values go from memory to the operand registers: the order of a contraction is free as long as both sides agree, so a lane takes
 // 16-byte pieces of its key's row as they lie, and for the second product the values of D / tile neighbouring columns of the eight (sixteen)
 // keys that its exponentials belong to.
+//
+// Bound by memory where sequences are long: 64 sequences of 400 to 8192 tokens (32/8 heads of 128, pages of 16 in 8 bits, 561 MB) take
+// 119 us, 4.7 TB/s, and 5 for the join; one of 131072 (269 MB) 50 us, 5.3 TB/s, and 7.5 for the join of its 256 shares.  The matrix unit
+// is busy for a tenth of that, so a tile of 16 rows of which four are filled costs nothing.  Short walks are chains of latencies: one
+// token against 700 takes 8 us (lengths and tables, keys, products, fold) and 3.7 for the join, in two launches.
+//
+// A step's keys and values are loaded a step ahead, into registers: a ring in LDS would read and write every byte once more, and what it
+// saves, addresses, is a few instructions for 32 keys.  Probabilities meet the values as two bf16 parts (high and rest): the second product
+// has time to spare, and O keeps 16 bits more than with one.
 #include <type_traits>
 
 #include "st_cache_plan.h"
