@@ -510,12 +510,12 @@ __device__ __forceinline__ RowStates states_of(const CacheAttnArgs& a, int64_t r
   if (t < first || t >= end) return y;
   const int4 at = a.info[t];
   const int shares = at.y & 0xffff, tile_rows = at.y >> 16;
-  if (shares <= 1 || tile_rows <= 0) return y;
+  // (where starts are no starts, a token may not have been told of: nothing is read outside the states, and no number leaves its type)
+  if (shares <= 1 || tile_rows <= 0 || tile_rows > kPromptRows || at.x < 0 || at.z <= 0 || at.z > a.state_rows || at.w < 0 || at.w >= a.T) return y;
   const int hk = h / G, R = at.w * G + h - hk * G, tile = R / tile_rows;
   y.first = at.x + ((int64_t)(at.z - 1 - tile) * a.c.Hkv + hk) * tile_rows + (R - tile * tile_rows);
   y.step = (int64_t)at.z * a.c.Hkv * tile_rows;
-  // (where starts are no starts, a token may not have been told of: nothing is read outside the states)
-  if (at.x >= 0 && at.w >= 0 && at.z > tile && y.first + (shares - 1) * y.step < a.state_rows) y.n = shares;
+  if (tile < at.z && y.first + (shares - 1) * y.step < a.state_rows) y.n = shares;
   return y;
 }
 __device__ __forceinline__ void store_joined(const CacheAttnArgs& a, int64_t row, int x, f32x4 o, float m, float sum, float besides, int bf16) {

@@ -163,6 +163,8 @@ __device__ __forceinline__ void tell_rows(const CacheAttnArgs& a, const SeqSpan&
   if (t.share != 0 || t.hk != 0 || !a.info) return;
   const int i0 = (t.tile * ROWS + G - 1) / G, i1 = min((t.tile * ROWS + ROWS + G - 1) / G, s.r.n);   // their first head is in this tile
   for (int i = i0 + threadIdx.x; i < i1; i += 256) a.info[s.r.first + i] = make_int4((int)(a.plan.base + (int64_t)t.first_state * ROWS), t.shares | ROWS << 16, t.tiles, i);
+  if (t.tile != t.tiles - 1) return;                   // rows that are not computed have no states
+  for (int i = s.r.n + threadIdx.x, n = seq_rows(a.starts, t.b, a.T).n; i < n; i += 256) a.info[s.r.first + i] = make_int4(0, 0, 0, 0);
 }
 
 }  // namespace st

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import paper_2407_00611_amd as st
-from cache_cases import Case, check_attention, rows_of
+from cache_cases import TYPES, Case, check_attention, rows_of
 from oracle import cache as oc
 from test_gpu_cache_attn import _attend
 
@@ -95,6 +95,26 @@ def test_many_shares_of_one_walk(dtype, kind, D):
 @pytest.mark.parametrize("counts", [[1] * 70, [2] * 69 + [40]])
 def test_one_long_sequence_among_many_short_ones(counts):
     _attend("bf16", "e4m3", [40] * 69 + [3000], counts, Hq=2, Hkv=2, D=64, page=64, seed=4)
+
+
+@pytest.mark.parametrize("dtype,kind", [("bf16", "e4m3"), ("f32", "f32")])
+@pytest.mark.parametrize("counts,most", [([5, 3], 2), ([300, 2], 90), ([40, 1], 20)])
+def test_rows_that_are_not_computed_where_walks_are_split(dtype, kind, counts, most):
+    """Whatever the workspace holds, and a call of more rows left in it: rows behind max_rows stay as they are."""
+    case = Case(15, kind, [4000, 2500], 16, 1, 128)
+    T, dt = sum(counts), TYPES[dtype]
+    q = torch.randn((1, T, 4, 128), generator=case.g).to(dt).cuda()
+    starts, cache = rows_of(counts).cuda(), case.cache()
+    ws = torch.empty(st.st_attn_cache_workspace_bytes(q, cache) + st.st_attn_cache_workspace_bytes(q, cache, most) + 512, dtype=torch.uint8, device="cuda")
+    for fill in (None, 0, 1, 127, 255):
+        if fill is None:
+            st.st_attn_cache(q, starts, cache, True, 0.1, workspace=ws)
+        else:
+            ws.fill_(fill)
+        o, lse = torch.full((1, T, 4, 128), 7.0, device="cuda"), torch.full((1, 4, T), 7.0, device="cuda")
+        st.st_attn_cache(q, starts, cache, True, 0.1, max_rows=most, o_part=o, lse_part=lse, workspace=ws)
+        done = check_attention(case, q, rows_of(counts), o, lse, True, 0.1, max_rows=most)
+        assert not done.all() and (o[0, ~done] == 7.0).all() and (lse[0][:, ~done] == 7.0).all(), fill
 
 
 def test_pages_beyond_32_bits():
