@@ -24,6 +24,13 @@ constexpr int kPlacesOfFew = 2048, kPlaces = 512;
 // 40); of up to kFewOfShort where there are few tiles, and a step's latency is what counts (246 rows of six sequences 27 us, 31).
 constexpr int kFewRows = 128, kFewOfShort = 256, kShortTiles = 64;
 
+// Where no walk of bf16 rows has more blocks than this, none is split and no join launched: a step of a workgroup's four wavefronts is 1.1 us,
+// a launch that joins 3 and more.  kWhole blocks for one sequence (400 tokens 9.5 us, 11.1 split; 700 tokens 12.2, 11.3), three times as many where
+// there are a workgroup or two for each compute unit (1200 tokens of 32 sequences, 8 heads 19 us, 26; of 64 ragged ones 26, 28; 2000 tokens of
+// those 46, 44), kWholeOfMany where the last of many have the chip for themselves (32 sequences of 24 heads of 64, 700 tokens 23 us, 25; 980 tokens
+// 32, 30).
+constexpr int kWhole = 16, kWholeOfMany = 24;
+
 st_status check_cache(const st_cache* c) {
   if (c == nullptr) return fail(ST_ERR_INVALID_ARG, "null cache");
   if (c->dtype != ST_F32 && c->dtype != ST_BF16 && c->dtype != ST_E4M3) return fail(ST_ERR_INVALID_ARG, "cache: unknown dtype %d", c->dtype);
@@ -92,14 +99,17 @@ st::CachePlan launch_plan(const st_cache_rows* r, const st_cache* c, int rows, i
   const int64_t G = r->Hq / c->Hkv, some = std::min(c->B, r->T), most_rows = std::min<int64_t>((int64_t)std::min(r->max_rows, r->T) * G, to);
   const int64_t tiles = std::min(r->T * G / rows + some, some * ((most_rows + rows - 1) / rows));
   const int keys = rows == st::kPromptRows ? st::kPromptKeys : st::kCacheKeys;
-  const int64_t blocks = ((int64_t)c->width * c->page + keys - 1) / keys;
+  int64_t blocks = ((int64_t)c->width * c->page + keys - 1) / keys;
+  if (r->causal && r->window > 0) blocks = std::min(blocks, ((int64_t)r->window + std::min(r->max_rows, r->T) - 1 + keys - 1) / keys + 1);
   st::CachePlan p{};
   p.rows = rows;
   p.rows_from = from;
   p.rows_to = to;
   p.least = rows == st::kPromptRows ? kLeastOfPrompts : r->dtype == ST_F32 ? kLeastBlocks / 2 : kLeastBlocks;
   p.target = most_rows <= 16 ? kPlacesOfFew : kPlaces;
-  const int64_t jobs = tiles * c->Hkv, most = std::max<int64_t>((blocks + p.least / 2) / p.least, 1);
+  const int64_t jobs = tiles * c->Hkv;
+  if (r->dtype == ST_BF16 && rows != st::kPromptRows && blocks <= (jobs <= kPlaces ? std::min(kWhole + jobs / 8, 3 * (int64_t)kWhole) : kWholeOfMany)) p.least = 4 * kWhole;
+  const int64_t most = std::max<int64_t>((blocks + p.least / 2) / p.least, 1);
   p.grid = std::min(p.target + jobs, jobs * most);
   if (rows == 16) p.grid = (p.grid + 8 * c->Hkv - 1) / (8 * c->Hkv) * (8 * c->Hkv);   // (whole rounds of the order in which they take their pieces)
   p.states = most > 1 ? (int32_t)std::min<int64_t>(p.target * 4 / 3 + 1, jobs * most) : 0;
