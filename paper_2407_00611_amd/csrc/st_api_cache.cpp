@@ -16,6 +16,9 @@ namespace {
 // four times the work: 3 rows of four sequences 20 us, 23 with two), four of 64 of a prompt's tile (102 rows of 18 sequences 34 us, 46 with
 // eight).
 constexpr int kLeastBlocks = 8, kLeastOfPrompts = 4;
+// bf16 walks of so many blocks and more, of so many tiles and heads, have workgroups enough with shares of twice that (4000 tokens of 16
+// sequences, 8 heads 40 us, 44 with eight blocks; 1500 tokens of 8 ragged ones 15.6, 13.7).
+constexpr int kLongBlocks = 96, kLongJobs = 64;
 // Workgroups that shares are made for: sequences of up to 16 rows wait for memory, and more workgroups than the chip holds at once even out
 // what the lengths leave (64 ragged sequences 124 us, 140 with 1024); those of more rows are work, and each share has so many rows of O to
 // join (fp32, D = 256, 256 rows of two sequences 96 us, 120 with 1024, 168 with 2048).
@@ -109,6 +112,7 @@ st::CachePlan launch_plan(const st_cache_rows* r, const st_cache* c, int rows, i
   p.target = most_rows <= 16 ? kPlacesOfFew : kPlaces;
   const int64_t jobs = tiles * c->Hkv;
   if (r->dtype == ST_BF16 && rows != st::kPromptRows && blocks <= (jobs <= kPlaces ? std::min(kWhole + jobs / 8, 3 * (int64_t)kWhole) : kWholeOfMany)) p.least = 4 * kWhole;
+  else if (r->dtype == ST_BF16 && rows != st::kPromptRows && blocks >= kLongBlocks && jobs >= kLongJobs) p.least = 2 * kLeastBlocks;
   const int64_t most = std::max<int64_t>((blocks + p.least / 2) / p.least, 1);
   p.grid = std::min(p.target + jobs, jobs * most);
   if (rows == 16) p.grid = (p.grid + 8 * c->Hkv - 1) / (8 * c->Hkv) * (8 * c->Hkv);   // (whole rounds of the order in which they take their pieces)
