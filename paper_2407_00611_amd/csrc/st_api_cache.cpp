@@ -114,9 +114,11 @@ st::CachePlan launch_plan(const st_cache_rows* r, const st_cache* c, int rows, i
   if (r->dtype == ST_BF16 && rows != st::kPromptRows && blocks <= (jobs <= kPlaces ? std::min(kWhole + jobs / 8, 3 * (int64_t)kWhole) : kWholeOfMany)) p.least = 4 * kWhole;
   else if (r->dtype == ST_BF16 && rows != st::kPromptRows && blocks >= kLongBlocks && jobs >= kLongJobs) p.least = 2 * kLeastBlocks;
   const int64_t most = std::max<int64_t>((blocks + p.least / 2) / p.least, 1);
+  p.most = (int32_t)most;
   p.grid = std::min(p.target + jobs, jobs * most);
   if (rows == 16) p.grid = (p.grid + 8 * c->Hkv - 1) / (8 * c->Hkv) * (8 * c->Hkv);   // (whole rounds of the order in which they take their pieces)
-  p.states = most > 1 ? (int32_t)std::min<int64_t>(p.target * 4 / 3 + 1, jobs * most) : 0;
+  // (as many as with the shortest shares: a window, which shortens walks, never needs more room than none)
+  p.states = most > 1 ? (int32_t)std::min<int64_t>(p.target * 4 / 3 + 1, jobs * std::max(most, (blocks + kLeastBlocks / 2) / kLeastBlocks)) : 0;
   p.base = base;
   p.jobs = jobs;
   return p;
@@ -145,7 +147,7 @@ Plans plans_of(const st_cache_rows* r, const st_cache* c) {
     y.p[1] = launch_plan(r, c, 16, 0, 16, (int64_t)y.p[0].states * large);
   }
   for (int x = 0; x < y.n; ++x) y.rows += (int64_t)y.p[x].states * y.p[x].rows;
-  y.states = y.n == 1 ? (int)(y.p[0].states / y.p[0].jobs) : 1;
+  y.states = y.n == 1 ? (int)std::min<int64_t>(y.p[0].states / y.p[0].jobs, y.p[0].most) : 1;
   return y;
 }
 struct Room {

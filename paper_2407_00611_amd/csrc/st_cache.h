@@ -38,6 +38,7 @@ struct CachePlan {
   int32_t least;                                     // key blocks of a share, at least
   int32_t target;                                    // workgroups that the shares are made for
   int32_t states;                                    // partial states there is room for
+  int32_t most;                                      // shares of a walk, at most
   int64_t base;                                      // rows of the states of launches before
   int64_t jobs, grid;                                // tiles times KV heads, at most; workgroups
 };

@@ -87,6 +87,20 @@ def test_attention():
     assert lib.st_attn_cache(None, None, None, None, None, None, None, None, None, 0, None) == 1
 
 
+@pytest.mark.parametrize("dtype,Hq,Hkv,B,T", [(1, 32, 8, 1, 1), (1, 32, 8, 8, 8), (1, 32, 8, 16, 80), (1, 24, 24, 64, 64), (1, 8, 2, 64, 700), (0, 8, 2, 16, 16), (0, 8, 8, 3, 400)])
+def test_a_window_needs_no_more_room_than_none(dtype, Hq, Hkv, B, T):
+    """A workspace for rows without a window is enough for every window, and one for a longer table for every shorter one."""
+    need = lambda width, window, causal=1: lib.st_attn_cache_workspace_bytes(C.byref(_rows(dtype=dtype, T=T, Hq=Hq, max_rows=T, window=window, causal=causal)),
+                                                                             C.byref(_cache(dtype=dtype, Hkv=Hkv, B=B, width=width)))
+    last = 0
+    for width in list(range(1, 260, 3)) + [500, 1000, 8192]:
+        most = need(width, 0)
+        assert need(width, 0, 0) == most and need(width, 64, 0) == most
+        assert max(need(width, w) for w in (1, 17, 300, 700, 1000, 1500, 2000, 2950, 3000, 4000, 10 ** 6)) <= most, width
+        assert most >= last, width
+        last = most
+
+
 def test_appending():
     for bad, status in ((dict(dtype=2), 1), (dict(B=2), 1), (dict(B=0), 1), (dict(seg=2, offset2=9), 1), (dict(Hkv=1), 1), (dict(D=64, rot=64, axis_pairs=(C.c_int32 * 4)(32)), 1),
                         (dict(Hq=-1), 1), (dict(dtype=0), 2), (dict(S=-1), 1), (dict(S=(1 << 25) + 1), 2), (dict(rot=130), 1), (dict(rot=64), 1), (dict(pairing=2), 1),
