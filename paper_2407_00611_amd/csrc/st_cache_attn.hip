@@ -351,6 +351,10 @@ __global__ __launch_bounds__(256, (stream_waves<T, S, ROWS, DP>())) void cache_s
         }
       }
       bad = bad || __any(found != 0);
+      if constexpr (E4M3) {                            // the scale of a half without a token that is seen may be anything: what is zero times it is to stay so
+        const bool low = now.ok[0] && key0 < w.hi && key0 + 16 > w.lo, high = now.ok[1] && key0 + 16 < w.hi && key0 + 32 > w.lo;
+        v_sc = (lane < 32 ? low : high) ? v_sc : 127;
+      }
     }
     if constexpr (BF) {
 #pragma unroll
