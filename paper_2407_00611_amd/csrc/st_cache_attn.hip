@@ -28,6 +28,7 @@ namespace {
 constexpr int kKeys = kCacheKeys;
 constexpr int kManyWaves = 16, kManyRows = 512;      // wavefronts of a row whose states are many; up to so many rows
 constexpr float kUnset = -1e30f;                     // reference of a row that has met no key: whatever comes exceeds it
+constexpr int kScan = 4;                             // tokens looked at together for values that are not finite: a part of a page
 constexpr float kSumMost = 4096.f;                   // a lane's sum over its keys of a block beyond which a row's reference moves
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
@@ -78,6 +79,8 @@ __device__ __forceinline__ uint32_t drop_not_finite(uint32_t& x) {
   if constexpr (sizeof(S) < 4) asm volatile("" : "+v"(x));
   return mask;
 }
+
+__device__ __forceinline__ bool is_finite(float x) { return fabsf(x) <= 3.402823466e38f; }
 
 // One value of the pages
 __device__ __forceinline__ float stored(const float* p, uint8_t) { return *p; }
@@ -451,20 +454,33 @@ __global__ __launch_bounds__(256, (stream_waves<T, S, ROWS, DP>())) void cache_s
 #pragma unroll
         for (int d = 0; d < PW; ++d) o[d] += fold[(k * ROWS + y) * FS + PW * rho + d];
       }
-      if (__builtin_expect(any_bad, 0)) {              // what the blocks at the masks' edges left out, of the keys that this row sees
-        const RowSpan ys = row_span(a, s, yi);
-        for (int key = max(ys.lo, w.n0 * kKeys); key < min(ys.hi, w.n1 * kKeys); ++key) {
-          const int page = page_of(c, t.b, key >> c.shift);
-          const int b0 = key / kKeys * kKeys;
-          if (page < 0) continue;
-          const bool inner = b0 >= w.all_lo && b0 + kKeys <= w.all_hi && page_of(c, t.b, b0 >> c.shift) >= 0 && page_of(c, t.b, min((b0 + 16) >> c.shift, c.width - 1)) >= 0;
-          if (inner) continue;
+      // Values that are not finite: the blocks at the masks' edges left them out, and in whole ones an infinity times both parts of a probability,
+      // or times one that fp32 does not hold, is NaN.  Where this row sees any, they are what its columns have.
+      bool odd = any_bad;
 #pragma unroll
-          for (int d = 0; d < PW; ++d) {
-            const float z = stored((const S*)(vbase + ((int64_t)page * c.v.sb + (int64_t)(key & ((1 << c.shift) - 1)) * c.v.ss) * (int)sizeof(S)) + d0 + d,
-                                   E4M3 ? c.v_scale[(int64_t)page * c.Hkv + t.hk] : (uint8_t)127);
-            if (!(fabsf(z) <= 3.402823466e38f)) o[d] += z;
-          }
+      for (int d = 0; d < PW; ++d) odd = odd || !is_finite(o[d]);
+      if (__builtin_expect(odd, 0)) {
+        const RowSpan ys = row_span(a, s, yi);
+        const int k0 = max(ys.lo, w.n0 * kKeys), k1 = min(ys.hi, w.n1 * kKeys);
+        float found[PW];
+#pragma unroll
+        for (int d = 0; d < PW; ++d) found[d] = 0.f;
+        for (int key = k0 & ~(kScan - 1); key < k1; key += kScan) {
+          const int page = page_of(c, t.b, key >> c.shift);
+          if (page < 0) continue;
+          const S* from = (const S*)(vbase + ((int64_t)page * c.v.sb + (int64_t)(key & ((1 << c.shift) - 1)) * c.v.ss) * (int)sizeof(S)) + d0;
+          const uint8_t scale = E4M3 ? c.v_scale[(int64_t)page * c.Hkv + t.hk] : (uint8_t)127;
+#pragma unroll
+          for (int u = 0; u < kScan; ++u)
+#pragma unroll
+            for (int d = 0; d < PW; ++d) {
+              const float z = stored(from + u * c.v.ss + d, scale);
+              found[d] += key + u >= k0 && key + u < k1 && !is_finite(z) ? z : 0.f;
+            }
+        }
+        if (sum == sum) {                              // (a score that is NaN makes all columns so)
+#pragma unroll
+          for (int d = 0; d < PW; ++d) o[d] = found[d] == 0.f ? o[d] : found[d];
         }
       }
       if (part) {

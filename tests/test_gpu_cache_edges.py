@@ -1,7 +1,12 @@
-"""Where a cache's attention can go wrong at the ends of what it takes: scales of pages without a token."""
+"""Where a cache's attention can go wrong at the ends of what it takes: scales of pages without a token, infinities and NaN wherever they
+lie."""
+import math
+
 import pytest
 import torch
 
+import paper_2407_00611_amd as st
+from cache_cases import TYPES, Case, rows_of
 from test_gpu_cache_attn import _attend
 
 pytestmark = pytest.mark.gpu
@@ -28,3 +33,68 @@ def test_scales_of_pages_without_a_token_are_not_used(dtype, D, byte):
     how = dict(Hq=4, Hkv=1, D=D, change=change)
     _attend(dtype, "e4m3", [200, 130], [110, 90], **how)
     _attend(dtype, "e4m3", [5001, 1200], [1, 1], **how)                           # walks in shares
+
+
+# ---- infinities and NaN, wherever the token lies
+
+def _plant(case, token, d, x, b=0):
+    case.v[int(case.table[b, token // case.page]), token % case.page, 0, d] = torch.tensor(x, device="cuda").to(case.v.dtype)
+
+
+WALKS = [(400, 1), (400, 3), (400, 20), (5000, 1), (5000, 7), (20000, 2), (400, 100), (3000, 90)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("L,n", WALKS)
+def test_an_infinity_is_one_wherever_its_token_lies(dtype, L, n):
+    """Early tokens, which all rows see, and one at the edge of what they see: a row has what the definition says in the columns that such a
+    token has, and in the others, bit by bit, what it has without."""
+    D = 64
+    case = Case(21, dtype, [L], 16, 1, D)
+    q = torch.randn((1, n, 4, D), generator=case.g).to(TYPES[dtype]).cuda()
+    print(f"[{dtype}, {n} rows of {L}]", flush=True)
+    run = lambda: st.st_attn_cache(q, rows_of([n]).cuda(), case.cache(), True, 0.125)
+    o0, l0 = run()
+    edge = L - (n + 1) // 2                                                      # seen by the last rows only
+    for token, d, x in ((40, 3, math.inf), (41, 60, -math.inf), (17, 9, math.inf), (300, 9, math.inf), (90, 10, math.inf), (L - n - 1, 10, -math.inf),
+                        (100, 11, math.nan), (101, 11, math.inf), (edge, 12, math.inf), (5, 13, math.inf), (edge, 13, -math.inf)):
+        _plant(case, token, d, x)
+    o, lse = run()
+    assert torch.equal(lse, l0)
+    late = (torch.arange(n, device="cuda") >= edge - (L - n))[:, None].expand(n, 4)
+    assert (o[0, :, :, 3] == math.inf).all() and (o[0, :, :, 60] == -math.inf).all() and (o[0, :, :, 9] == math.inf).all()
+    assert torch.isnan(o[0, :, :, 10]).all() and torch.isnan(o[0, :, :, 11]).all()
+    assert (o[0, :, :, 12][late] == math.inf).all() and torch.isfinite(o[0, :, :, 12][~late]).all()
+    assert torch.isnan(o[0, :, :, 13][late]).all() and (o[0, :, :, 13][~late] == math.inf).all()
+    keep = torch.ones(D, dtype=torch.bool, device="cuda")
+    keep[[3, 60, 9, 10, 11, 12, 13]] = False
+    # (tiles of prompts at the edge take another way: no more than its roundings apart)
+    if n * 4 > 256 and dtype == "bf16":
+        assert float((o[..., keep] - o0[..., keep]).abs().max()) <= 2.0 ** -8 * float(o0[..., keep].abs().max())
+    else:
+        assert torch.equal(o[..., keep], o0[..., keep])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("cap", [0.0, 150.0])
+@pytest.mark.parametrize("L,n", WALKS[:3])
+def test_an_infinity_of_no_weight_to_speak_of(dtype, cap, L, n):
+    """A token whose probability is e^-120 and less, no number of fp32: what is infinite times it is infinite all the same."""
+    D = 64
+    case = Case(22, dtype, [L], 16, 1, D)
+    q = torch.randn((1, n, 4, D), generator=case.g)
+    q[..., 0] = 16.0
+    q = q.to(TYPES[dtype]).cuda()
+    case.k[..., 0] = 0.0
+    tokens = (40, L // 2, L - n - 1, L - n)
+    for x, token in enumerate(tokens):
+        case.k[int(case.table[0, token // 16]), token % 16, 0, 0] = -100.0         # a score of -200, or what the cap leaves of it
+        _plant(case, token, 5 + x, -math.inf if x == 2 else math.inf)
+    print(f"[{dtype}, {n} rows of {L}, cap {cap}]", flush=True)
+    o, lse = st.st_attn_cache(q, rows_of([n]).cuda(), case.cache(), True, 0.125, softcap=cap)
+    assert torch.isfinite(lse).all()
+    for x in range(4):
+        assert (o[0, :, :, 5 + x] == (-math.inf if x == 2 else math.inf)).all(), x
+    keep = torch.ones(D, dtype=torch.bool, device="cuda")
+    keep[5:9] = False
+    assert torch.isfinite(o[..., keep]).all()
