@@ -538,8 +538,19 @@ __device__ __forceinline__ RowStates states_of(const CacheAttnArgs& a, int64_t r
   if (tile < at.z && y.first + (shares - 1) * y.step < a.state_rows) y.n = shares;
   return y;
 }
-__device__ __forceinline__ void store_joined(const CacheAttnArgs& a, int64_t row, int x, f32x4 o, float m, float sum, float besides, int bf16) {
+__device__ __forceinline__ void store_joined(const CacheAttnArgs& a, const RowStates& s, int64_t row, int x, f32x4 o, float m, float sum, float besides, int bf16) {
   o *= sum != 0.f ? 1.f / sum : 0.f;
+  if (__builtin_expect(!(is_finite(o[0]) && is_finite(o[1]) && is_finite(o[2]) && is_finite(o[3])) && sum == sum, 0)) {
+    // an infinity times the weight of a state that counts for nothing is NaN: what is not finite in any state is what the row has
+    f32x4 found = {0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < s.n; ++k) {
+      const f32x4 z = *reinterpret_cast<const f32x4*>(a.part_o + (s.first + k * s.step) * a.c.D + 4 * x);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) found[e] += is_finite(z[e]) ? 0.f : z[e];
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = found[e] == 0.f ? o[e] : found[e];
+  }
   const int64_t to = row * a.c.D + 4 * x, t = row / a.Hq;
   if (a.o) *reinterpret_cast<f32x4*>(a.o + to) = o;
   if (a.o_lowp && bf16) *reinterpret_cast<u32x2*>((uint16_t*)a.o_lowp + to) = u32x2{pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3])};
@@ -604,7 +615,7 @@ __global__ __launch_bounds__(64 * kManyWaves) void cache_combine_many_kernel(con
   if (threadIdx.x >= vecs) return;
   Joined z = fold[x];
   for (int k = 1; k < min(all, s.n); ++k) z = join(z, fold[k * vecs + x]);
-  store_joined(a, blockIdx.x, x, z.o, z.m, z.sum, z.besides, bf16);
+  store_joined(a, s, blockIdx.x, x, z.o, z.m, z.sum, z.besides, bf16);
 }
 // Few states of many rows: 64 D / 4 lanes' worth of rows side by side, each lane through its row's states, four under way; `rounds` times a
 // wavefront.  With alone = 1, for more states, a row at a time and its states side by side.  Rows that are whole cost a look.
@@ -629,7 +640,7 @@ __global__ __launch_bounds__(256) void cache_combine_kernel(const CacheAttnArgs 
       }
       if (y != 0) continue;
     }
-    if (s.n > 1) store_joined(a, row, x, z.o, z.m, z.sum, z.besides, bf16);
+    if (s.n > 1) store_joined(a, s, row, x, z.o, z.m, z.sum, z.besides, bf16);
   }
 }
 
