@@ -20,6 +20,7 @@ constexpr int kRows = kPromptRows, kBN = kPromptKeys;
 constexpr float kUnset = -1e30f;                     // reference of a row that has met no key: whatever comes exceeds it
 constexpr float kSumMost = 4096.f;                   // a lane's sum over sixteen keys beyond which a row's reference moves
 
+__device__ __forceinline__ bool is_finite(float x) { return fabsf(x) <= 3.402823466e38f; }
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 // Whether 32 rows of an LDS tile hold an infinity or NaN: their products with zeros are NaN then
@@ -330,29 +331,58 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
 
   // ---- O = acc / l, lse = m ln 2 + ln l; or the state of a share
   const float l = xhalf_sum(l_run);
-  if (R >= all_rows) return;
-  if (__builtin_expect(bad, 0)) {
-    // what the general tiles left out: values that are not finite, of the keys that this row sees
-    for (int y = n0; y < min(n1, walk.n_gen); ++y) {
-      const int key0 = walk.tile(y) * kBN;
-      if (!missing && y1.lo <= key0 && y0.hi >= key0 + kBN) continue;
-      for (int key = max(see.lo, key0); key < min(see.hi, key0 + kBN); ++key) {
-        const int page = page_of(c, t.b, key >> c.shift);
-        if (page < 0) continue;
-        const S* row_at = (const S*)(vb_ + ((int64_t)page * c.v.sb + (int64_t)(key & ((1 << c.shift) - 1)) * c.v.ss) * (int)sizeof(S));
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) bad = bad || !is_finite(acc[db][v]);
+  if (__builtin_expect(__any(bad), 0)) {
+    // Values that are not finite: general tiles left them out, and in whole ones an infinity times a probability that bf16 does not hold is
+    // NaN.  What of them a row sees is what its columns have.  A lane looks at a key of the tile, then all at the columns of those that have any.
+    uint32_t had[DB];                                  // columns that met one, a bit each
+#pragma unroll
+    for (int db = 0; db < DB; ++db) had[db] = 0;
+    for (int y = n0; y < n1; ++y) {
+      const int key0 = walk.tile(y) * kBN, mine = key0 + lane;
+      auto row_of = [&](int key, int page) {
+        return (const S*)(vb_ + ((int64_t)page * c.v.sb + (int64_t)(key & ((1 << c.shift) - 1)) * c.v.ss) * (int)sizeof(S));
+      };
+      auto value = [&](S x, float scale) {
+        if constexpr (E4M3) return e4m3_pair<false>(x).x * scale;
+        else return __uint_as_float((uint32_t)x << 16);
+      };
+      const int page = mine < y1.hi ? page_of(c, t.b, mine >> c.shift) : -1;
+      float scale = 1.f;
+      uint32_t some = 0;
+      if (page >= 0) {
+        const uint32_t byte = E4M3 ? c.v_scale[(int64_t)page * c.Hkv + t.hk] : 127, more = E4M3 ? e4m3_beyond(byte) : 0x00800080u;
+        const uint32_t bits = E4M3 ? 0x7f7f7f7fu : 0x7fff7fffu;
+        scale = scale_value((uint8_t)byte);
+        const S* from = row_of(mine, page);
+        for (int d = 0; d < D; d += 16 / (int)sizeof(S)) {
+          const u32x4 z = *reinterpret_cast<const u32x4*>(from + d);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) some |= ((z[e] & bits) + more) & ~bits;
+        }
+      }
+      for (uint64_t left = __ballot(some != 0); left; left &= left - 1) {
+        const int at = __ffsll((unsigned long long)left) - 1, key = key0 + at;
+        const S* from = row_of(key, __builtin_amdgcn_readlane(page, at));
+        const float sc = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(scale), at));
+        if (key < see.lo || key >= see.hi || l != l) continue;      // (a score that is NaN makes all columns so)
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
           for (int v = 0; v < 16; ++v) {
-            const int d = 32 * db + 8 * (v / 4) + 4 * g + v % 4;
-            float z;
-            if constexpr (E4M3) z = e4m3_pair<false>(row_at[d]).x;
-            else z = __uint_as_float((uint32_t)row_at[d] << 16);
-            if (!(fabsf(z) <= 3.402823466e38f)) acc[db][v] += z;
+            const float z = value(from[32 * db + 8 * (v / 4) + 4 * g + v % 4], sc);
+            const uint32_t lost = is_finite(z) ? 0 : 1u << v;
+            acc[db][v] = lost ? (had[db] & lost ? acc[db][v] : 0.f) + z : acc[db][v];
+            had[db] |= lost;
+            if (v % 4 == 3) asm volatile("" ::: "memory");         // (four at a time: masks of more have no registers)
           }
       }
     }
   }
+  if (R >= all_rows) return;
   const bool part = t.shares > 1;
   const float inv = part ? 1.f : l != 0.f ? 1.f / l : 0.f;
   const int64_t state = a.plan.base + (int64_t)t.state * kRows + wave * 32 + r;

@@ -22,6 +22,10 @@ __device__ __forceinline__ uint32_t e4m3_of(float a, float b, float c, float d) 
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, y, true);
 }
 
+// Times 2^(scale - 127) a code is beyond fp32, and bf16, from 2^(255 - scale) on: what to add to codes without their sign so that those, and
+// NaN, reach the sign's place
+__device__ __forceinline__ uint32_t e4m3_beyond(uint32_t scale) { return (0x80u - (uint32_t)min(0x7f, 8 * (262 - (int)scale))) * 0x01010101u; }
+
 // V neighbouring values from their codes, and back
 template <int V>
 __device__ __forceinline__ Vec<V> load(const uint8_t* p) {

@@ -77,7 +77,7 @@ def test_an_infinity_is_one_wherever_its_token_lies(dtype, L, n):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("cap", [0.0, 150.0])
-@pytest.mark.parametrize("L,n", WALKS[:6])
+@pytest.mark.parametrize("L,n", WALKS)
 def test_an_infinity_of_no_weight_to_speak_of(dtype, cap, L, n):
     """A token whose probability is e^-120 and less, no number of fp32: what is infinite times it is infinite all the same."""
     D = 64
