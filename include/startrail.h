@@ -394,8 +394,9 @@ st_status st_qk_rope_bwd(const st_rope_desc* desc, const st_tensor* q, const st_
  *   k, v           [n_pages, page, Hkv, D] views (stride_b of a page, stride_s of a token, below 2^20, stride_h of a head), rows
  *                  16-byte aligned
  *   k_scale, v_scale  ST_E4M3 only: device bytes [n_pages, Hkv]; a stored value stands for its e4m3 value times 2^(scale - 127)
- *                  (1 <= scale <= 254; of pages that hold no token anything).  Whole powers of two: every value is exact in bf16, and a page whose scale grows keeps its
- *                  rows but for what falls below the least e4m3 value
+ *                  (1 <= scale <= 254; of pages that hold no token anything), an infinity where fp32 does not hold that.  Whole powers
+ *                  of two: every value is exact in bf16, and a page whose scale grows keeps its rows but for what falls below the
+ *                  least e4m3 value
  *   table          device int32 [B, width].  An entry that is no page (negative, or >= n_pages: a page that a window has left behind)
  *                  holds nothing: its tokens are not stored, not seen, and read as zeros
  *   lens           device int32 [B]: tokens of every sequence, those that a call appends among them; at most width page of them

@@ -67,12 +67,12 @@ __device__ __forceinline__ uint32_t bf16_of_e4m3(uint32_t x, float scale) {
 }
 
 // The parts of x (values of S side by side) that are an infinity or NaN become zero; which there were.  One more at the lowest place of such
-// a value's exponent (e4m3: of all its bits) reaches its sign.  (The empty statement keeps the compiler from putting the last step off
+// a value's exponent reaches its sign (e4m3, with a scale that makes infinities: e4m3_beyond).  (The empty statement keeps the compiler from putting the last step off
 // until all words' masks are there, for which there are no registers; of whole words it keeps a bit each by itself.)
 template <typename S>
-__device__ __forceinline__ uint32_t drop_not_finite(uint32_t& x) {
+__device__ __forceinline__ uint32_t drop_not_finite(uint32_t& x, uint32_t beyond) {
   uint32_t mask;
-  if constexpr (sizeof(S) == 1) mask = ((((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7) * 0xffu;
+  if constexpr (sizeof(S) == 1) mask = ((((x & 0x7f7f7f7fu) + beyond) & 0x80808080u) >> 7) * 0xffu;
   else if constexpr (sizeof(S) == 2) mask = ((((x & 0x7fff7fffu) + 0x00800080u) & 0x80008000u) >> 15) * 0xffffu;
   else mask = (x & 0x7f800000u) == 0x7f800000u ? 0xffffffffu : 0u;
   x &= ~mask;
@@ -342,7 +342,13 @@ __global__ __launch_bounds__(256, (stream_waves<T, S, ROWS, DP>())) void cache_s
     l_run += sum;
 
     if (!whole) {                                      // nothing of what no row sees; of the rest, what is not finite is added at the end
-      uint32_t found = 0;
+      uint32_t found = 0, beyond[2] = {0, 0};
+      if constexpr (E4M3) {                            // the scale of a half without a token that is seen may be anything: what is zero times it is to stay so
+        const bool low = now.ok[0] && key0 < w.hi && key0 + 16 > w.lo, high = now.ok[1] && key0 + 16 < w.hi && key0 + 32 > w.lo;
+        v_sc = (lane < 32 ? low : high) ? v_sc : 127;
+        beyond[0] = e4m3_beyond(__builtin_amdgcn_readlane(v_sc, 0));
+        beyond[1] = e4m3_beyond(__builtin_amdgcn_readlane(v_sc, 32));
+      }
 #pragma unroll
       for (int v = 0; v < NS; ++v) {
         const int key = key0 + M::row(v, g);
@@ -350,14 +356,10 @@ __global__ __launch_bounds__(256, (stream_waves<T, S, ROWS, DP>())) void cache_s
 #pragma unroll
         for (int d = 0; d < VW; ++d) {
           vr[v][d] = in ? vr[v][d] : 0;
-          found |= drop_not_finite<S>(vr[v][d]);
+          found |= drop_not_finite<S>(vr[v][d], beyond[M::row(v, 0) / 16]);
         }
       }
       bad = bad || __any(found != 0);
-      if constexpr (E4M3) {                            // the scale of a half without a token that is seen may be anything: what is zero times it is to stay so
-        const bool low = now.ok[0] && key0 < w.hi && key0 + 16 > w.lo, high = now.ok[1] && key0 + 16 < w.hi && key0 + 32 > w.lo;
-        v_sc = (lane < 32 ? low : high) ? v_sc : 127;
-      }
     }
     if constexpr (BF) {
 #pragma unroll

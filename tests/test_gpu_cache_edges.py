@@ -1,5 +1,5 @@
 """Where a cache's attention can go wrong at the ends of what it takes: scales of pages without a token, infinities and NaN wherever they
-lie."""
+lie, values beyond fp32."""
 import math
 
 import pytest
@@ -98,3 +98,30 @@ def test_an_infinity_of_no_weight_to_speak_of(dtype, cap, L, n):
     keep = torch.ones(D, dtype=torch.bool, device="cuda")
     keep[5:9] = False
     assert torch.isfinite(o[..., keep]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("L,n", WALKS)
+def test_values_beyond_fp32_reach_those_who_see_them(dtype, L, n):
+    """e4m3 values times a scale so high that fp32 does not hold the product, which is an infinity then: of a token that the last rows see, and
+    of one that all see."""
+    D = 64
+    case = Case(23, "e4m3", [L], 16, 1, D)
+    q = torch.randn((1, n, 4, D), generator=case.g).to(TYPES[dtype]).cuda()
+    edge = L - (n + 1) // 2
+    late = (torch.arange(n, device="cuda") >= edge - (L - n))[:, None].expand(n, 4)
+    run = lambda: st.st_attn_cache(q, rows_of([n]).cuda(), case.cache(), True, 0.125)
+    for byte, code in ((247, 256.0), (250, 32.0), (250, 448.0), (254, 2.0)):
+        print(f"[{dtype}, {n} rows of {L}, {code} times 2^{byte - 127}]", flush=True)
+        for page in {int(case.table[0, edge // 16]), int(case.table[0, 2])}:
+            case.v[page] = 0
+            case.scales[1][page] = byte
+        _plant(case, edge, 12, code)
+        _plant(case, 40, 3, -code)
+        _plant(case, 41, 4, 2.0 ** -9)
+        o, lse = run()
+        assert torch.isfinite(lse).all()
+        assert (o[0, :, :, 3] == -math.inf).all() and torch.isfinite(o[0, :, :, 4]).all()
+        assert (o[0, :, :, 12][late] == math.inf).all() and torch.isfinite(o[0, :, :, 12][~late]).all()
+        k, v = st.st_cache_read(case.cache(), None, L)
+        assert v[0, 40, 0, 3] == -math.inf and v[0, edge, 0, 12] == math.inf and torch.isfinite(v[0, 41]).all()
