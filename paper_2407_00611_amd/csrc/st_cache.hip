@@ -75,7 +75,7 @@ __device__ __forceinline__ int exponent_for(float top) {
   const uint32_t u = __float_as_uint(top);
   return max((int)(u >> 23) - 127 - 8 + ((u & 0x7fffff) > 0x600000 ? 1 : 0), -126);
 }
-__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }   // -126 .. 127
+__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float(e > -127 ? (uint32_t)(e + 127) << 23 : 0x00400000u); }   // -127 .. 127
 
 // Position of packed row t for a pair: that of its token, `place`, or from a table
 __device__ __forceinline__ double position_of(const RopeArgs& g, double place, int t, int pair) {
@@ -229,7 +229,7 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, const Piece& p,
     }
   } else {
     uint8_t* scale = (key ? a.c.k_scale : a.c.v_scale) + (int64_t)page * g.Hkv + h;
-    const int had = begun > 0 ? (int)*scale - 127 : -126;
+    const int had = begun > 0 ? min(max((int)*scale - 127, -126), 127) : -126;
     // the highest magnitude, as the bits of one, which are in order: an infinity or NaN is above all finite ones
     uint32_t top = 0;
     auto highest = [&](const Vec<V> (&x)[U], const Vec<V> (&z)[U], uint32_t below) {

@@ -1,5 +1,5 @@
-"""Where a cache's attention can go wrong at the ends of what it takes: scales of pages without a token, infinities and NaN wherever they
-lie, values beyond fp32."""
+"""Where a cache's attention and appending can go wrong at the ends of what they take: scales of pages without a token, infinities and NaN
+wherever they lie, values beyond fp32, pages of the highest scales."""
 import math
 
 import pytest
@@ -125,3 +125,26 @@ def test_values_beyond_fp32_reach_those_who_see_them(dtype, L, n):
         assert (o[0, :, :, 12][late] == math.inf).all() and torch.isfinite(o[0, :, :, 12][~late]).all()
         k, v = st.st_cache_read(case.cache(), None, L)
         assert v[0, 40, 0, 3] == -math.inf and v[0, edge, 0, 12] == math.inf and torch.isfinite(v[0, 41]).all()
+
+
+# ---- appending
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("byte", [254, 253, 200, 1])
+def test_appending_to_a_page_of_any_scale(dtype, byte):
+    """A program's own page, begun with a scale at the ends of what there are: new rows are stored in it."""
+    case = Case(24, "e4m3", [3], 16, 1, 64)
+    for i, pages in enumerate((case.k, case.v)):
+        case.scales[i].fill_(byte)
+        case.oracle[i].e.fill_(byte - 127)
+    k, v = (torch.randn((1, 5, 1, 64), generator=case.g).to(TYPES[dtype]).cuda() for _ in range(2))
+    k[0, 0], v[0, 2], k[0, 1, 0, :9], v[0, 4, 0, 5:20] = 1e38, -3e37, 2e36, 1.5e38
+    starts, lens = rows_of([5]), [8]
+    st.st_cache_append(None, k, v, starts.cuda(), case.cache(lens), torch.zeros(0, dtype=torch.float64).cuda(), norm=False)
+    for i, x in enumerate((k, v)):
+        case.oracle[i].append(case.table, lens, starts, x[0].double().cpu())
+        page = int(case.table[0, 0])
+        assert int(case.scales[i][page, 0]) - 127 == int(case.oracle[i].e[page, 0])
+        got = (case.k, case.v)[i][page, :8].double().cpu()
+        assert torch.equal(got, case.oracle[i].x[page, :8])
+        assert (got[3:] != 0).any()
