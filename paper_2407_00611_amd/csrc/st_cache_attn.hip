@@ -27,7 +27,6 @@ namespace {
 
 constexpr int kKeys = kCacheKeys;
 constexpr int kManyWaves = 16, kManyRows = 512;      // wavefronts of a row whose states are many; up to so many rows
-constexpr float kUnset = -1e30f;                     // reference of a row that has met no key: whatever comes exceeds it
 constexpr int kScan = 4;                             // tokens looked at together for values that are not finite: a part of a page
 constexpr float kSumMost = 4096.f;                   // a lane's sum over its keys of a block beyond which a row's reference moves
 

@@ -11,6 +11,9 @@
 
 namespace st {
 
+// Reference of the exponents of a row that has met no key: the lowest number, so that whatever fp32 holds of a score counts
+constexpr float kUnset = -3.402823466e38f;
+
 struct CacheItem {
   int b, hk, tile, share;    // b < 0: none
   int shares, tiles;         // of the sequence

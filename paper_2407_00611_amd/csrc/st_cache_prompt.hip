@@ -17,7 +17,6 @@ namespace st {
 namespace {
 
 constexpr int kRows = kPromptRows, kBN = kPromptKeys;
-constexpr float kUnset = -1e30f;                     // reference of a row that has met no key: whatever comes exceeds it
 constexpr float kSumMost = 4096.f;                   // a lane's sum over sixteen keys beyond which a row's reference moves
 
 __device__ __forceinline__ bool is_finite(float x) { return fabsf(x) <= 3.402823466e38f; }

@@ -1,5 +1,5 @@
 """Where a cache's attention and appending can go wrong at the ends of what they take: scales of pages without a token, infinities and NaN
-wherever they lie, values beyond fp32, pages of the highest scales."""
+wherever they lie, values beyond fp32, pages of the highest scales, scores near the ends of fp32."""
 import math
 
 import pytest
@@ -148,3 +148,32 @@ def test_appending_to_a_page_of_any_scale(dtype, byte):
         got = (case.k, case.v)[i][page, :8].double().cpu()
         assert torch.equal(got, case.oracle[i].x[page, :8])
         assert (got[3:] != 0).any()
+
+
+# ---- scores near the ends of fp32
+
+@pytest.mark.parametrize("dtype,kind", [("bf16", "bf16"), ("bf16", "e4m3"), ("f32", "f32"), ("f32", "e4m3")])
+@pytest.mark.parametrize("L,n", WALKS + [(1, 1), (33, 2)])
+def test_scores_near_the_ends_of_fp32(dtype, kind, L, n):
+    """A row whose scores are all far below zero still has a softmax: of all tokens alike, the mean of the values."""
+    D, Hq = 64, 4
+    case = Case(26, kind, [L], 16, 1, D)
+    q = torch.zeros((1, n, Hq, D))
+    q[..., 0] = torch.tensor([1.0, -1.0, 2.0 ** 10, 0.0])[None, None]
+    q = q.mul(2.0 ** 60).to(TYPES[dtype]).cuda()
+    case.k[..., 0] = torch.tensor(-256.0, device="cuda").to(case.k.dtype)
+    if kind == "e4m3":
+        case.scales[0].fill_(127 + 40)
+    else:
+        case.k[..., 0] = torch.tensor(-2.0 ** 48, device="cuda").to(case.k.dtype)
+    o, lse = st.st_attn_cache(q, rows_of([n]).cuda(), case.cache(), True, 1.0)
+    s = torch.tensor([-1.0, 1.0, -2.0 ** 10, 0.0]).double() * 2.0 ** 108
+    _, v, _ = case.held(0)
+    v = v[:, 0]
+    for i in range(n):
+        seen = v[:L - n + i + 1]
+        mean, mass = seen.mean(0), seen.abs().mean(0)
+        bound = mass * (2.0 ** -8 if dtype == "bf16" else 2.0 ** -20) + 1e-30
+        for h in range(Hq):
+            assert ((o[0, i, h].double().cpu() - mean).abs() <= bound).all(), (i, h)
+            assert abs(float(lse[0, h, i]) - float(s[h] + math.log(len(seen)))) <= 2.0 ** -20 * abs(float(s[h])) + 1e-5
