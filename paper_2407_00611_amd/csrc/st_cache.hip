@@ -24,24 +24,24 @@ constexpr int kTokensMost = 8;                       // tokens whose angles a wo
 // definition is (in fp32 one of 30000 bf16 keys fell to the other side; 4000 prompt rows of eight sequences 273 us, 256 with it)
 
 // sine and cosine of x turns, |x| <= 1/2: x is taken to the nearest quarter, |r| <= pi / 4 from there, and both series of r are cut where the
-// next term is below 1e-12
+// next term is below 1e-16
 __device__ __forceinline__ void sincos_turns(double x, double& s, double& c) {
   const double n = rint(4.0 * x), r = (x - 0.25 * n) * 6.283185307179586477, z = r * r;
-  const double ps = r * (1.0 + z * (-1.0 / 6 + z * (1.0 / 120 + z * (-1.0 / 5040 + z * (1.0 / 362880 + z * (-1.0 / 39916800 + z * (1.0 / 6227020800.0)))))));
-  const double pc = 1.0 + z * (-0.5 + z * (1.0 / 24 + z * (-1.0 / 720 + z * (1.0 / 40320 + z * (-1.0 / 3628800 + z * (1.0 / 479001600.0))))));
+  const double ps = r * (1.0 + z * (-1.0 / 6 + z * (1.0 / 120 + z * (-1.0 / 5040 + z * (1.0 / 362880 + z * (-1.0 / 39916800 + z * (1.0 / 6227020800.0 - z / 1307674368000.0)))))));
+  const double pc = 1.0 + z * (-0.5 + z * (1.0 / 24 + z * (-1.0 / 720 + z * (1.0 / 40320 + z * (-1.0 / 3628800 + z * (1.0 / 479001600.0 + z * (-1.0 / 87178291200.0 + z / 20922789888000.0)))))));
   const int k = (int)n & 3;
   const double u = k & 1 ? pc : ps, v = k & 1 ? ps : pc;
   s = k & 2 ? -u : u;
   c = (k + 1) & 2 ? -v : v;
 }
 // Sine and cosine of p f, f in 64ths of a turn: those of the nearest 64th from a table, and of the rest, at most pi / 64, from series whose next
-// terms are below 1e-12.  The product is rounded to a whole number by an addition to 1.5 2^52, whose last bits are that number's.
+// terms are below 1e-15.  The angle itself is off by 2^-52 of p f at most: f and its unit are rounded.  The product is rounded to a whole number by an addition to 1.5 2^52, whose last bits are that number's.
 constexpr int kParts = 64;
 __device__ __forceinline__ void sincos_part(double p, double f, const double2* table, double& s, double& c) {
   constexpr double kWhole = 6755399441055744.0, t = 6.283185307179586477 / kParts;
   const double w = fma(p, f, kWhole), r = fma(p, f, kWhole - w), z = r * r;
   const double2 at = table[(uint32_t)__double_as_longlong(w) % kParts];
-  const double ps = r * (t + z * (-t * t * t / 6 + z * (t * t * t * t * t / 120)));
+  const double ps = r * (t + z * (-t * t * t / 6 + z * (t * t * t * t * t / 120 - z * (t * t * t * t * t * t * t / 5040))));
   const double pc = 1.0 + z * (-t * t / 2 + z * (t * t * t * t / 24 - z * (t * t * t * t * t * t / 720)));
   s = at.x * pc + at.y * ps;
   c = at.y * pc - at.x * ps;

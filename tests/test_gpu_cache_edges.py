@@ -1,7 +1,9 @@
 """Where a cache's attention and appending can go wrong at the ends of what they take: scales of pages without a token, infinities and NaN
-wherever they lie, values beyond fp32, pages of the highest scales, scores near the ends of fp32."""
+wherever they lie, values beyond fp32, pages of the highest scales, keys beside a tie, scores near the
+ends of fp32."""
 import math
 
+import numpy as np
 import pytest
 import torch
 
@@ -148,6 +150,40 @@ def test_appending_to_a_page_of_any_scale(dtype, byte):
         got = (case.k, case.v)[i][page, :8].double().cpu()
         assert torch.equal(got, case.oracle[i].x[page, :8])
         assert (got[3:] != 0).any()
+
+
+def test_keys_beside_a_tie():
+    """Rotated keys that are 2^-43 of themselves above or below the middle of two e4m3 values, at every place of a page and for every 64th
+    of a turn: angles, sines and cosines made in 64 bits decide them rightly, those that are 2^-41 off do not."""
+    n, rng = 256, np.random.default_rng(1)
+    freq = 1.0
+    a = np.zeros((n, 2)), np.zeros((n, 2))
+    for place in range(n):
+        sn, cs = math.sin(place * freq), math.cos(place * freq)
+        if abs(sn) < 0.3:                                                        # (little to choose b by)
+            continue
+        x = rng.uniform(0.3, 0.9, 1 << 18).astype(np.float32).astype(np.float64)
+        tie = 1.0625
+        b = ((x * cs - tie) / sn).astype(np.float32).astype(np.float64)
+        off = ((x.astype(np.longdouble) * np.longdouble(cs) - b.astype(np.longdouble) * np.longdouble(sn)) - np.longdouble(tie)).astype(np.float64)
+        for side in range(2):
+            good = np.where(off > 0, off, np.inf) if side == 0 else np.where(off < 0, -off, np.inf)
+            good = np.where(good < 2.0 ** -43, np.inf, good)
+            i = int(good.argmin())
+            assert good[i] < 2.0 ** -38
+            a[0][place, side], a[1][place, side] = x[i], b[i]
+    k = torch.zeros((1, n, 2, 32))
+    k[0, :, :, 0], k[0, :, :, 1] = torch.tensor(a[0]), torch.tensor(a[1])
+    k[0, :, :, 2] = 448.0                                                        # (the scale is 1)
+    k = k.cuda()
+    case = Case(25, "e4m3", [0], 256, 2, 32, more=1)
+    st.st_cache_append(None, k, k, rows_of([n]).cuda(), case.cache([n]), torch.tensor([freq], dtype=torch.float64).cuda(), norm=False, pairs="neighbours")
+    page = int(case.table[0, 0])
+    assert (case.scales[0][page] == 127).all()
+    got = case.k[page, :, :, 0].float().cpu()
+    for place in range(n):
+        if a[0][place, 0]:
+            assert got[place].tolist() == [1.125, 1.0], place
 
 
 # ---- scores near the ends of fp32
