@@ -441,8 +441,9 @@ st_status st_cache_read(const st_cache* cache, const int32_t* first, int32_t cou
  *   o_part fp32 and / or o_lowp in dtype, dense [1,T,Hq,D]; lse_part fp32 [1,Hq,T]: a state that st_attn_merge and st_attn_combine fold
  *   (B = 1, Sq = T).  A row that sees nothing has O = 0, lse = -inf.
  * ST_BF16 with D = 64 or 128 (pages of ST_BF16 or ST_E4M3), ST_F32 with any D (pages of ST_F32 or ST_E4M3).  Scores, softmax and sums
- * are fp32; exp(s - max) meets the values as two bf16 parts (2^-16), in sequences of many rows (more than 128, or 256 where there are
- * few, of a KV head's query heads) as one (2^-8, as in st_score).  Infinities and NaN reach the rows that see them, and no others.
+ * are fp32; of bf16 rows exp(s - max) meets the values as two bf16 parts (2^-16), whatever else is in the call, in sequences of up to 128
+ * rows of a KV head's query heads (n_b Hq / Hkv), and in all of a call with min(max_rows, T) Hq / Hkv <= 256 and few tiles of 128 rows (64, KV heads
+ * counted); as one (2^-8, as in st_score) in longer ones.  Infinities and NaN reach the rows that see them, and no others.
  * Results do not depend on the order of the pages. */
 typedef struct {
   int32_t dtype, T, Hq, max_rows, causal, window;

@@ -26,6 +26,9 @@ constexpr int kPlacesOfFew = 2048, kPlaces = 512;
 // Sequences of up to so many rows are read again for every 32 of them (16 heads x 24 rows x 2048 tokens as fast either way, 64 rows 30 us and
 // 40); of up to kFewOfShort where there are few tiles, and a step's latency is what counts (246 rows of six sequences 27 us, 31).
 constexpr int kFewRows = 128, kFewOfShort = 256, kShortTiles = 64;
+// Beside sequences of more, those of up to so many rows are taken in tiles of 16, and only those behind in a prompt's tiles, with probabilities
+// in two parts up to 128 rows (six of 20 rows beside two prompts 101 us, 136 in a prompt's tile; fifteen of 32 beside one 135, 195; of 64 200, 170).
+constexpr int kFewBesides = 32;
 
 // Where no walk of bf16 rows has more blocks than this, none is split and no join launched: a step of a workgroup's four wavefronts is 1.1 us,
 // a launch that joins 3 and more.  kWhole blocks for one sequence (400 tokens 9.5 us, 11.1 split; 700 tokens 12.2, 11.3), three times as many where
@@ -109,7 +112,7 @@ st::CachePlan launch_plan(const st_cache_rows* r, const st_cache* c, int rows, i
   p.rows_from = from;
   p.rows_to = to;
   p.least = rows == st::kPromptRows ? kLeastOfPrompts : r->dtype == ST_F32 ? kLeastBlocks / 2 : kLeastBlocks;
-  p.target = most_rows <= 16 ? kPlacesOfFew : kPlaces;
+  p.target = most_rows <= 16 || (r->dtype == ST_BF16 && rows == 16) ? kPlacesOfFew : kPlaces;
   const int64_t jobs = tiles * c->Hkv;
   if (r->dtype == ST_BF16 && rows != st::kPromptRows && blocks <= (jobs <= kPlaces ? std::min(kWhole + jobs / 8, 3 * (int64_t)kWhole) : kWholeOfMany)) p.least = 4 * kWhole;
   else if (r->dtype == ST_BF16 && rows != st::kPromptRows && blocks >= kLongBlocks && jobs >= kLongJobs) p.least = 2 * kLeastBlocks;
@@ -123,7 +126,7 @@ st::CachePlan launch_plan(const st_cache_rows* r, const st_cache* c, int rows, i
   p.jobs = jobs;
   return p;
 }
-// The launches of a call: sequences of up to 16 rows and those of more have kernels of their own where there may be both
+// The launches of a call: sequences of few rows and those of more have kernels of their own where there may be both
 struct Plans {
   int n;
   st::CachePlan p[2];
@@ -134,7 +137,7 @@ Plans plans_of(const st_cache_rows* r, const st_cache* c) {
   constexpr int kAll = 0x7fffffff;
   const int64_t most = (int64_t)std::min(r->max_rows, r->T) * (r->Hq / c->Hkv);
   const bool tall = r->dtype == ST_BF16 && most > kFewRows && (most > kFewOfShort || launch_plan(r, c, st::kPromptRows, 0, kAll, 0).jobs > kShortTiles);
-  const int large = tall ? st::kPromptRows : 32;
+  const int large = tall ? st::kPromptRows : 32, few = tall ? kFewBesides : 16;
   Plans y{};
   y.n = 1;
   if (most <= 16 || (r->dtype == ST_F32 && c->D > st::kTallCacheHead)) {
@@ -143,8 +146,8 @@ Plans plans_of(const st_cache_rows* r, const st_cache* c) {
     y.p[0] = launch_plan(r, c, large, 0, kAll, 0);
   } else {
     y.n = 2;
-    y.p[0] = launch_plan(r, c, large, 16, kAll, 0);
-    y.p[1] = launch_plan(r, c, 16, 0, 16, (int64_t)y.p[0].states * large);
+    y.p[0] = launch_plan(r, c, large, few, kAll, 0);
+    y.p[1] = launch_plan(r, c, 16, 0, few, (int64_t)y.p[0].states * large);
   }
   for (int x = 0; x < y.n; ++x) y.rows += (int64_t)y.p[x].states * y.p[x].rows;
   y.states = y.n == 1 ? (int)std::min<int64_t>(y.p[0].states / y.p[0].jobs, y.p[0].most) : 1;

@@ -16,7 +16,7 @@
 //
 // A step's keys and values are loaded a step ahead, into registers: a ring in LDS would read and write every byte once more, and what it
 // saves, addresses, is a few instructions for 32 keys.  Probabilities meet the values as two bf16 parts (high and rest): the second product
-// has time to spare, and O keeps 16 bits more than with one.
+// has time to spare, and of O 2^-16 is lost, 2^-8 with one part.
 #include <type_traits>
 
 #include "st_cache_plan.h"

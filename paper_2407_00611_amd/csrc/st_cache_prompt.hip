@@ -2,7 +2,8 @@
 //
 //   S^T = K Q^T and O^T += V^T P^T, as st_score_bf16.hip: a lane has one row of its wavefront's 32.
 // Pages in bf16 come to LDS by direct loads; those in 8 bits through registers, where they become bf16 by a power of two, exactly, once for
-// the workgroup's 128 rows.  Probabilities are rounded to bf16 for the second product, 2^-8 relative at most.
+// the workgroup's 128 rows.  Probabilities are rounded to bf16 for the second product, 2^-8 relative at most (as in st_score_bf16.hip: a second
+// part is half of all matrix instructions more); those of sequences whose rows fit one tile meet it in two parts, 2^-16, as everywhere else.
 //
 // Bound by the matrix and the vector unit in turn: 2048 rows against 18432 tokens in 8 bits (32/8 heads of 128, 584 GFLOP) take 625 to 675 us
 // on one card, 865 to 935 TFLOP/s; of all cycles the matrix units are busy 41 %, exponentials, sums and conversions take about as many, and
@@ -56,7 +57,7 @@ struct TileWalk {
 };
 
 template <typename S, int D, bool CAP, bool BIAS>
-__global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArgs a) {
+__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cache_prompt_kernel(const CacheAttnArgs a) {
   constexpr bool E4M3 = std::is_same<S, uint8_t>::value;
   constexpr int KB = kBN / 32, KS = D / 16, DB = D / 32;
   constexpr int kTile = kBN * D * 2;
@@ -99,7 +100,9 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
   __syncthreads();
   walk.a0 = min(max((x1.lo + kBN - 1) / kBN, walk.t0), walk.t1);
   walk.a3 = max(min(x0.hi / kBN, walk.t1), walk.a0);
-  if (missing) walk.a0 = walk.a3 = walk.t1;
+  // Rows that fit one tile have probabilities in two parts, as those of other kernels, whatever batch their sequence is in, and general tiles
+  const bool fine = all_rows <= kRows;
+  if (missing || fine) walk.a0 = walk.a3 = walk.t1;
   walk.a1 = walk.a2 = walk.a3;
   if (BIAS) {                                          // whole: with all rows on one side
     const int64_t p0 = s.pos + first / G, p1 = s.pos + last / G;
@@ -207,7 +210,7 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
     for (int ks = 0; ks < KS; ++ks) y.sc = mfma32(reads.frag(ktile, 0, ks), qf[ks], y.sc);
   };
   // seen: the keys' runs of 16 that have a page (general tiles)
-  auto softmax = [&](auto general, Block& y, int key0, int seen) {
+  auto softmax = [&](auto general, Block& y, int key0, int seen, u32x4* rest = nullptr) {
     constexpr bool GEN = decltype(general)::value;
     const int d0 = near - key0 - 4 * g;
     const ScoreTile<CAP, BIAS> f(k, slope2, d0);
@@ -250,15 +253,21 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
 #pragma unroll
     for (int m = 0; m < 2; ++m)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) y.pf[m][e] = pack_bf16(p[8 * m + 2 * e], p[8 * m + 2 * e + 1]);
+      for (int e = 0; e < 4; ++e) {
+        const float a0 = p[8 * m + 2 * e], a1 = p[8 * m + 2 * e + 1];
+        y.pf[m][e] = pack_bf16(a0, a1);
+        if (rest) rest[m][e] = pack_bf16(a0 - __uint_as_float(y.pf[m][e] << 16), a1 - __uint_as_float(y.pf[m][e] & 0xffff0000u));
+      }
   };
-  auto contract = [&](auto scrub, const Block& y, uint32_t vtile) {
+  auto contract = [&](auto scrub, const u32x4* pf, uint32_t vtile, const u32x4* rest = nullptr) {
 #pragma unroll
     for (int m = 0; m < 2; ++m)
 #pragma unroll
       for (int db = 0; db < DB; ++db) {
-        const bf16x8 vf = reads.frag_tr(vtile, 16 * m, db);
-        acc[db] = mfma32(decltype(scrub)::value ? finite_bf16(vf) : vf, __builtin_bit_cast(bf16x8, y.pf[m]), acc[db]);
+        bf16x8 vf = reads.frag_tr(vtile, 16 * m, db);
+        if (decltype(scrub)::value) vf = finite_bf16(vf);
+        acc[db] = mfma32(vf, __builtin_bit_cast(bf16x8, pf[m]), acc[db]);
+        if (rest) acc[db] = mfma32(vf, __builtin_bit_cast(bf16x8, rest[m]), acc[db]);
       }
   };
 
@@ -290,6 +299,27 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
     pages_next = pages_then;
     buf ^= 1;
   };
+  for (; fine && n < n1; ++n) {                        // a block at a time: registers for the second parts
+    fetch();
+    const int key0 = walk.tile(n) * kBN;
+    const uint32_t ktile = smem_addr + buf * 2 * kTile;
+#pragma unroll 1
+    for (int kb = 0; kb < KB; ++kb) {
+      const int at = key0 + 32 * kb;
+      if (first + wave * 32 > last || y0.lo >= at + 32 || y1.hi <= at) continue;      // no rows, or none that sees any of the block
+      const uint32_t vblock = ktile + kTile + 32 * kb * D * 2;
+      const int seen = (__builtin_amdgcn_readlane(pages, 2 * kb) >= 0 ? 1 : 0) | (__builtin_amdgcn_readlane(pages, 2 * kb + 1) >= 0 ? 2 : 0);
+      const bool dirty = (seen != 3 || y1.lo > at || y0.hi < at + 32) && not_finite<D>(reads, vblock);
+      bad = bad || dirty;
+      Block y;
+      u32x4 rest[2];
+      products(y, ktile + 32 * kb * D * 2);
+      softmax(std::true_type(), y, at, seen, rest);
+      if (__builtin_expect(dirty, 0)) contract(std::true_type(), y.pf, vblock, rest);
+      else contract(std::false_type(), y.pf, vblock, rest);
+    }
+    arrived();
+  }
   for (; n < min(n1, walk.n_gen); ++n) {
     fetch();
     const int key0 = walk.tile(n) * kBN;
@@ -306,8 +336,8 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
         const uint32_t vblock = ktile + kTile + 32 * kb * D * 2;
         const int seen = (__builtin_amdgcn_readlane(pages, 2 * kb) >= 0 ? 1 : 0) | (__builtin_amdgcn_readlane(pages, 2 * kb + 1) >= 0 ? 2 : 0);
         softmax(std::true_type(), y[kb], key0 + 32 * kb, seen);
-        if (__builtin_expect(dirty, 0)) contract(std::true_type(), y[kb], vblock);
-        else contract(std::false_type(), y[kb], vblock);
+        if (__builtin_expect(dirty, 0)) contract(std::true_type(), y[kb].pf, vblock);
+        else contract(std::false_type(), y[kb].pf, vblock);
       }
     }
     arrived();
@@ -323,7 +353,7 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
       softmax(std::false_type(), y[kb], key0 + 32 * kb, 3);
-      contract(std::false_type(), y[kb], ktile + kTile + 32 * kb * D * 2);
+      contract(std::false_type(), y[kb].pf, ktile + kTile + 32 * kb * D * 2);
     }
     arrived();
   }

@@ -1,6 +1,6 @@
 """Where a cache's attention and appending can go wrong at the ends of what they take: scales of pages without a token, infinities and NaN
 wherever they lie, values beyond fp32, pages of the highest scales, keys beside a tie, scores near the
-ends of fp32."""
+ends of fp32, probabilities in two parts whatever the batch."""
 import math
 
 import numpy as np
@@ -8,7 +8,7 @@ import pytest
 import torch
 
 import paper_2407_00611_amd as st
-from cache_cases import TYPES, Case, rows_of
+from cache_cases import TYPES, Case, check_attention, rows_of
 from test_gpu_cache_attn import _attend
 
 pytestmark = pytest.mark.gpu
@@ -213,3 +213,35 @@ def test_scores_near_the_ends_of_fp32(dtype, kind, L, n):
         for h in range(Hq):
             assert ((o[0, i, h].double().cpu() - mean).abs() <= bound).all(), (i, h)
             assert abs(float(lse[0, h, i]) - float(s[h] + math.log(len(seen)))) <= 2.0 ** -20 * abs(float(s[h])) + 1e-5
+
+
+# ---- the precision of the probabilities
+
+def _two_parts(dtype, kind, lens, counts, held, Hq=4, Hkv=1, D=64, T=None, max_rows=None, seed=31):
+    """Sequences `held` to the bound of probabilities in two parts, fp32 O."""
+    case = Case(seed, kind, lens, 16, Hkv, D)
+    T = sum(counts) if T is None else T
+    q = torch.randn((1, T, Hq, D), generator=case.g).to(TYPES[dtype]).cuda()
+    starts = rows_of(counts)
+    print(f"[{dtype} from {kind}, {lens} by {counts}, {Hq}/{Hkv} D{D}, T {T}, max_rows {max_rows}]", flush=True)
+    o, lse = st.st_attn_cache(q, starts.cuda(), case.cache(), True, 1 / math.sqrt(D), max_rows=max_rows)
+    check_attention(case, q, starts, o, lse, True, 1 / math.sqrt(D), max_rows=max_rows, two_parts=held)
+
+
+@pytest.mark.parametrize("kind", ["e4m3", "bf16"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("counts,Hq,Hkv", [([1, 1], 8, 2), ([1], 4, 4), ([5, 3], 4, 1), ([20, 7], 4, 1), ([32, 16], 4, 1), ([64, 3], 4, 1)])
+def test_probabilities_in_two_parts(kind, D, counts, Hq, Hkv):
+    for lens in ([90] * len(counts), [1700, 64][:len(counts)]):
+        _two_parts("bf16", kind, lens, counts, range(len(counts)), Hq, Hkv, D, max_rows=max(counts))
+
+
+@pytest.mark.parametrize("kind", ["e4m3", "bf16"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("counts,Hq,Hkv,held", [([5, 200, 20, 1], 4, 1, [0, 2, 3]), ([32, 33, 70], 4, 1, [0]), ([1] * 9, 32, 1, range(9)),
+                                                ([8, 100, 1], 16, 1, [0, 2]), ([128, 129], 1, 1, [0]), ([60, 128, 300], 2, 2, [0]),
+                                                ([20], 4, 1, [0]), ([1], 32, 1, [0])])
+def test_precision_does_not_depend_on_the_batch(kind, D, counts, Hq, Hkv, held):
+    """Up to 128 rows of a group: two parts, beside prompts, and with max_rows left at what the call could have."""
+    for more in (0, 400):
+        _two_parts("bf16", kind, [c + 150 for c in counts], counts, held, Hq, Hkv, D, T=sum(counts) + more)
