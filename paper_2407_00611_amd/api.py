@@ -1037,7 +1037,8 @@ def st_attn_cache(q, starts, cache: KVCache, causal: bool, scale: float, max_row
                   workspace=None, stream=None):
     """(O, lse) of packed rows q [1,T,Hq,D] against the cache: sequence b has rows starts[b] .. starts[b + 1] - 1 (int32 [B + 1]), at
     positions from q_first[b] on (int64 [B], counted from the cache's first token; None: its last tokens).  A row sees the tokens up
-    to its position (causal), the last `window` of them (0: all).  No sequence has more than max_rows rows (None: T).  O [1,T,Hq,D] is
+    to its position (causal), the last `window` of them (0: all).  No sequence has more than max_rows rows (None: T), and the call is planned
+    for as many, as for tokens up to the table's width: give it where it is known (1 for single tokens).  O [1,T,Hq,D] is
     the fp32 state, or with lowp=True alone in the dtype of q; both are written where o_part and o_lowp are given (the fp32 one is
     returned); lse fp32 [1,Hq,T].  Rows of no sequence are left as they were."""
     done = _short(_binding.cache_attn, stream, *cache, q, starts, causal, scale, max_rows, window, softcap, slopes, q_first, o_part, lse_part, o_lowp, lowp,

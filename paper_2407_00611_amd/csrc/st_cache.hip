@@ -6,7 +6,7 @@
 //
 // Appending: a workgroup has the new rows of a page and head, keys or values, whose scale it needs before it stores any; up to four rows a lane
 // stay in registers meanwhile, so that everything is read once.  Queries are a workgroup's of eight tokens, whose angles all heads share.
-// Prompts of 11000 tokens (32/8 heads of 128 in 8 bits) take 61 us for 248 MB, 4.1 TB/s: memory, and the vector unit over half of the time (22 of
+// Prompts of 11000 tokens (32/8 heads of 128 in 8 bits) take 61 us for 248 MB, 4.0 TB/s: memory, and the vector unit over half of the time (22 of
 // 40 million cycles), for keys in fp64 above all.  One token each of 16 sequences: 7.5 us, a launch and its chain of latencies.
 #include <algorithm>
 
@@ -21,7 +21,7 @@ constexpr int kMaxPairs = 128;
 constexpr int kTokensMost = 8;                       // tokens whose angles a workgroup holds for the queries
 
 // ---- arithmetic of the keys: fp32 as the queries' for pages in fp32, otherwise fp64, so that a value is rounded as one of the 64-bit
-// definition is (in fp32 one of 30000 bf16 keys fell to the other side; 4000 prompt rows of eight sequences 273 us, 256 with it)
+// definition is (in fp32 one of 30000 bf16 keys fell to the other side; the prompts above to bf16 pages: 70 us for 270 MB)
 
 // sine and cosine of x turns, |x| <= 1/2: x is taken to the nearest quarter, |r| <= pi / 4 from there, and both series of r are cut where the
 // next term is below 1e-16

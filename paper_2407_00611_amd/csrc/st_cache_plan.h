@@ -70,7 +70,8 @@ __device__ __forceinline__ T wave_scan(T x) {
 __device__ __forceinline__ float wave_last(float x) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63)); }
 __device__ __forceinline__ int wave_last(int x) { return __builtin_amdgcn_readlane(x, 63); }
 
-// Every wavefront for itself, a sequence a lane: no barrier, and one look at the lengths is all the memory that a batch of 64 waits for.
+// Every wavefront for itself, a sequence a lane: no barrier, and one look at the lengths is all the memory that a batch of 64 waits for.  Larger
+// batches cost every workgroup two rounds for each 64 sequences (the same 560 MB in 64 sequences 123.5 us, 256 144, 512 171, 4096 2.1 ms).
 // The span of the sequence found comes with it.
 template <int ROWS, int KEYS>
 __device__ __forceinline__ CacheItem find_item(const CacheAttnArgs& a, SeqSpan& span) {

@@ -5,8 +5,8 @@
 // the workgroup's 128 rows.  Probabilities are rounded to bf16 for the second product, 2^-8 relative at most (as in st_score_bf16.hip: a second
 // part is half of all matrix instructions more); those of sequences whose rows fit one tile meet it in two parts, 2^-16, as everywhere else.
 //
-// Bound by the matrix and the vector unit in turn: 2048 rows against 18432 tokens in 8 bits (32/8 heads of 128, 584 GFLOP) take 625 to 675 us
-// on one card, 865 to 935 TFLOP/s; of all cycles the matrix units are busy 41 %, exponentials, sums and conversions take about as many, and
+// Bound by the matrix and the vector unit in turn: 2048 rows against 18432 tokens in 8 bits (32/8 heads of 128, 584 GFLOP) take 620 to 685 us
+// as cards differ, 850 to 940 TFLOP/s; of all cycles the matrix units are busy 41 %, exponentials, sums and conversions take about as many, and
 // two wavefronts on a SIMD, which is what 128 accumulators and operands leave room for, overlap little of both.  Raised priority around the
 // products won 1 % here and lost 2 % of mixed batches; conversions spread over the products' loop lost more than they hid.
 #include <type_traits>
