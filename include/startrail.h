@@ -419,8 +419,9 @@ typedef struct {
  *   q, k, v     [1,T,heads,D] views in desc->dtype; q_out as q, which it may be
  * ST_E4M3: the scale of a page and head is 2^e with the least e for which all new values of the page are within 448 2^e, and not
  * below what the rows have that were there before, which are rescaled where it grows; values that are not finite are stored as NaN and
- * do not count for the scale.  Keys for pages in fewer bits than fp32 are normed and rotated in fp64, so that in ST_E4M3 each is the
- * nearest stored value to the exact one, in ST_BF16 that of the exact one in fp32; queries, and keys in ST_F32, in fp32.
+ * do not count for the scale.  Keys for pages in fewer bits than fp32 are normed and rotated in fp64 (angles to 2^-52 of themselves), so that
+ * in ST_E4M3 each is the nearest stored value to the exact one, in ST_BF16 that of the exact one in fp32, but where the exact one is as
+ * close to the middle of two; queries, and keys in ST_F32, in fp32.
  * Repeating a call with the same tensors, q_out not q, changes nothing. */
 st_status st_cache_append(const st_rope_desc* desc, const st_cache* cache, const int32_t* starts, const st_tensor* q, const st_tensor* k,
                           const st_tensor* v, const float* q_weight, const float* k_weight, const double* freq, const int32_t* positions,
